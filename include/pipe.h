@@ -556,6 +556,105 @@ int pipe_timing_read(double* total_ms, int* launches);
 int pipe_mfma_probe(int iters, int operands, double* tops_out, void* stream);
 int pipe_hbm_probe(int64_t bytes, double* gbps_out, void* stream);
 
+/* ---- Attention over a 4-bit key/value cache and over packed prompts ----
+ *
+ * What a generating transformer needs next to its expanded layers: pages for the keys and values of
+ * every request, the tokens' places in them, the cache itself in 4 bits, and the two attentions.
+ *
+ * Types of activations: fp32 (what the layers above emit), fp16 or bf16.  Heads: Hq query heads share
+ * Hkv key/value heads, Hq a multiple of Hkv; query head h reads key/value head h / (Hq/Hkv).
+ * head_dim D: 64 or 128.  q, k and v are [tokens][heads][D] with strides in elements for tokens and heads
+ * (slices of one projection's output need no copy; strides >= 0); D is dense.  Any alignment that the type has is
+ * served; 16-byte aligned addresses and strides are read with wider loads.  Outputs are 16-byte aligned.
+ *
+ * The cache is n_pages pages of pipe_cache_page_bytes(Hkv, D, P) bytes, 16-byte aligned; P tokens a page, P = 16,
+ * 32, 64, 128 or 256, n_pages * P < 2^31.  A page holds one block of P * (D + 8) bytes per head:
+ *   [0, P*D/2)            codes of K, D/2 bytes a token; value 2i in the low half of byte i, 2i+1 in the high one
+ *   [P*D/2, P*D)          codes of V, likewise
+ *   [P*D, P*D + 4P)       one word a token: scale s of K in bf16 (low half), offset m of K in bf16 (high half)
+ *   [P*D + 4P, P*(D+8))   the words of V
+ * A code c (0..15) stands for s*c + m.  Slot p*P + i is token i of page p.  Memory that was never written may hold
+ * anything: no call lets the contents of a slot beyond a request's length reach a result.
+ *
+ * Request b's tokens lie at the pages table_dev[b][0], table_dev[b][1], ...  ([B][table_width], each entry P tokens).
+ * Entries and slots outside the cache (the planner writes -1 where pages ran out) are never followed: a token whose slot
+ * is outside is not written, reads as zeros and is left out of the attention.
+ *
+ * All calls are asynchronous on `stream`, allocate nothing but library scratch, and may be captured into a graph
+ * (pipe_cache_attention after pipe_prepare_cache_attention on that stream).                                        */
+enum { PIPE_F32 = 0, PIPE_F16 = 1, PIPE_BF16 = 2 };
+
+/* Bytes of one page; 0 if the cache has no such page (Hkv < 1, D not 64 or 128, P not one of the above). */
+int64_t pipe_cache_page_bytes(int Hkv, int D, int P);
+
+/* Tables of the next step, on the device: request b has cached_dev[b] tokens in its pages and brings fresh_dev[b] more.
+ *   Pages are taken from free_dev[n_free] in order, from free_dev[used_dev[0]] on: requests ascending, within a request
+ *   its pages ascending; a partly filled last page is filled up first.  New pages enter table_dev (in and out); other
+ *   entries are not touched.  Outputs:
+ *     lengths_dev [B]      cached + fresh
+ *     starts_dev  [B+1]    first fresh token of each request in the packed order, and their total
+ *     slots_dev, positions_dev [T]   per fresh token its slot and its position in the request; -1 from the total on,
+ *                          so that a captured graph can serve steps of up to T tokens; a slot is -1 too where the
+ *                          token's page is missing
+ *     counts_dev [3]       pages used so far (the next call's used_dev; at most n_free); pages that are missing
+ *                          because the free list or the table's width ended; tokens cut off because they exceed T
+ *                          (they count as not brought: lengths, starts and pages leave them out)
+ *   counts_dev and used_dev must not overlap (several workgroups read the one and write the other).  Negative
+ *   entries of cached_dev and fresh_dev count as 0.  The outcome does not depend on the launch.  B <= 4096.
+ * Errors: PIPE_EINVAL (NULL, P), PIPE_ESHAPE (B outside 1..4096, T < 0, table_width < 1, n_free < 0).              */
+int pipe_cache_plan(const int32_t* cached_dev, const int32_t* fresh_dev, int B, int P, const int32_t* free_dev,
+                    int n_free, const int32_t* used_dev, int32_t* table_dev, int table_width, int T,
+                    int32_t* lengths_dev, int32_t* starts_dev, int32_t* slots_dev, int32_t* positions_dev,
+                    int32_t* counts_dev, void* stream);
+
+/* Writes the keys and values of T tokens to their slots.  A row (one token's one head) of values x becomes, in fp32
+ * with one rounding per operation, m = the bf16 value next to min(x) below or equal, s = the bf16 value next to
+ * (max(x) - m) / 15 above or equal (0 if under 2^-126), r = 1 / s, c = clamp(rint((x - m) * r), 0, 15), rint to even
+ * (c = 0 where s = 0).  So every value is within s/2 of its code's (within 2^-122 where s = 0).  A row that holds a NaN or an infinity, or whose
+ * range exceeds bf16's, has s = m = NaN: all of it reads as NaN.  Two tokens of a call must not have the same slot.  */
+int pipe_cache_write(const void* k_dev, const void* v_dev, int type, int T, int Hkv, int D, int64_t k_token_stride,
+                     int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int32_t* slots_dev,
+                     void* cache_dev, int n_pages, int P, void* stream);
+
+/* The values s*c + m of T slots (rounded once to `type`), dense [T][Hkv][D] each: for a prefix that a prompt attends to,
+ * for moving requests, for checks.                                                                                 */
+int pipe_cache_read(const void* cache_dev, int n_pages, int P, const int32_t* slots_dev, int T, int Hkv, int D,
+                    int type, void* k_dev, void* v_dev, void* stream);
+
+/* Attention of T fresh tokens over the cache, their own keys and values included (written before).  Request b's tokens
+ * are starts_dev[b] .. starts_dev[b+1]-1 of q (ascending, at most T), the last of them is the last of its
+ * lengths_dev[b] cached tokens: with n tokens, the i-th sees cached tokens 0 .. length - n + i.
+ *   out [T][Hq][D] dense, of q's type: softmax(scale * q K^T) V; zeros for a token that sees nothing (length 0, or more
+ *   queries than cached tokens) and for rows of q that belong to no request.
+ *   max_length: about the longest length, a hint for splitting the work (any value gives the same result up to rounding);
+ *   0: table_width * P.
+ * Scores, maxima, sums and outputs are fp32.  The codes meet q in fp16 products summed in fp32: q of 16 bits as it is
+ * (bf16 with a power of two per row that brings its largest value to 2^12 or so: values under 2^-26 of it are rounded), fp32 as
+ * the sum of two fp16 values; the weights of the softmax times V's scales likewise: one fp16 value with 11 significant
+ * bits for 16-bit outputs, two for fp32.
+ * Errors: PIPE_EINVAL (NULL, type, P, scale not finite), PIPE_ESHAPE (T < 0, B < 1, heads, D, table_width < 1, cache too large),
+ * PIPE_ENOTREADY (scratch would have to grow during a capture).                                                   */
+int pipe_cache_attention(const void* q_dev, int type, int T, int Hq, int Hkv, int D, int64_t q_token_stride,
+                         int64_t q_head_stride, const int32_t* starts_dev, const int32_t* lengths_dev, int B,
+                         const void* cache_dev, int n_pages, int P, const int32_t* table_dev, int table_width,
+                         float scale, int max_length, void* out_dev, void* stream);
+/* Scratch of pipe_cache_attention on this stream for up to these sizes.                                            */
+int pipe_prepare_cache_attention(int T, int Hq, int Hkv, int D, int B, int max_length, void* stream);
+
+/* Attention over packed sequences: sequence b has queries q_starts_dev[b] .. q_starts_dev[b+1]-1 and keys
+ * k_starts_dev[b] .. k_starts_dev[b+1]-1 (NULL: q_starts_dev; ascending, at most Tq and Tk).  causal: with n queries and
+ * m keys, query i sees keys 0 .. m - n + i (aligned at the end: new tokens behind a prefix); otherwise all m.
+ *   out [Tq][Hq][D] dense, of the same type as q, k and v; zeros for a query that sees nothing and for rows of q that
+ *   belong to no sequence.
+ * Scores, maxima, sums and outputs are fp32; for 16-bit types the softmax weights are rounded to that type for the
+ * product with V.
+ * Errors: PIPE_EINVAL (NULL, type, scale not finite), PIPE_ESHAPE (Tq or Tk < 0, B < 1, heads, D, strides).       */
+int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_dev, int type, int Tq, int Tk, int Hq,
+                          int Hkv, int D, int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride,
+                          int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                          const int32_t* q_starts_dev, const int32_t* k_starts_dev, int B, int causal, float scale,
+                          void* out_dev, void* stream);
+
 const char* pipe_strerror(int code);
 /* Text of the last HIP error seen by this thread ("" if none). */
 const char* pipe_last_device_error(void);

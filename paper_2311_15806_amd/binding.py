@@ -90,6 +90,15 @@ def _load():
     lib.pipe_hbm_probe.argtypes = [C.c_int64, C.POINTER(C.c_double), vp]
     lib.pipe_timing_enable.argtypes = [ci]
     lib.pipe_timing_read.argtypes = [C.POINTER(C.c_double), pi]
+    i64 = C.c_int64
+    lib.pipe_cache_page_bytes.argtypes = [ci, ci, ci]
+    lib.pipe_cache_page_bytes.restype = i64
+    lib.pipe_cache_plan.argtypes = [vp, vp, ci, ci, vp, ci, vp, vp, ci, ci, vp, vp, vp, vp, vp, vp]
+    lib.pipe_cache_write.argtypes = [vp, vp, ci, ci, ci, ci, i64, i64, i64, i64, vp, vp, ci, ci, vp]
+    lib.pipe_cache_read.argtypes = [vp, ci, ci, vp, ci, ci, ci, ci, vp, vp, vp]
+    lib.pipe_cache_attention.argtypes = [vp, ci, ci, ci, ci, ci, i64, i64, vp, vp, ci, vp, ci, ci, vp, ci, cf, ci, vp, vp]
+    lib.pipe_prepare_cache_attention.argtypes = [ci, ci, ci, ci, ci, ci, vp]
+    lib.pipe_prompt_attention.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, i64, i64, i64, i64, i64, i64, vp, vp, ci, ci, cf, vp, vp]
     lib.pipe_strerror.argtypes = [ci]
     lib.pipe_strerror.restype = C.c_char_p
     lib.pipe_last_device_error.restype = C.c_char_p
@@ -717,3 +726,129 @@ def pipe_hbm_probe(nbytes: int = 1 << 31) -> float:
     t = C.c_double()
     _check(_lib.pipe_hbm_probe(int(nbytes), C.byref(t), _stream()), "pipe_hbm_probe")
     return t.value
+
+
+# ---------------------------------------------------------------- attention over a 4-bit cache and over packed prompts
+
+PIPE_F32 = 0
+PIPE_F16 = 1
+PIPE_BF16 = 2
+_TYPES = {torch.float32: PIPE_F32, torch.float16: PIPE_F16, torch.bfloat16: PIPE_BF16}
+
+
+def _type(dtype: torch.dtype) -> int:
+    t = _TYPES.get(dtype)
+    if t is None:
+        raise ValueError("expected float32, float16 or bfloat16, got %s" % dtype)
+    return t
+
+
+def _heads(t: torch.Tensor, name: str):
+    """(address, token stride, head stride) of [tokens, heads, head_dim] with a dense last axis."""
+    if not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError("%s must be a device tensor [tokens, heads, head_dim] with a dense last axis" % name)
+    return t.data_ptr(), t.stride(0), t.stride(1)
+
+
+def _cache_pages(cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int) -> int:
+    if cache.dim() != 2 or cache.shape[1] != pipe_cache_page_bytes(kv_heads, head_dim, page_size):
+        raise ValueError("the cache must be uint8 [pages, pipe_cache_page_bytes(kv_heads, head_dim, page_size)]")
+    return cache.shape[0]
+
+
+def pipe_cache_page_bytes(kv_heads: int, head_dim: int, page_size: int) -> int:
+    """Bytes of one page of a 4-bit cache: torch.empty(pages, this, dtype=torch.uint8) is a cache."""
+    n = _lib.pipe_cache_page_bytes(int(kv_heads), int(head_dim), int(page_size))
+    if n == 0:
+        raise ValueError("kv_heads >= 1, head_dim 64 or 128, page_size 16, 32, 64, 128 or 256")
+    return n
+
+
+def pipe_cache_plan(cached: torch.Tensor, fresh: torch.Tensor, page_size: int, free: torch.Tensor, used: torch.Tensor,
+                    table: torch.Tensor, tokens: int):
+    """Tables of the next step (all int32): request b holds cached[b] tokens and brings fresh[b]; new pages come from free[used[0]:]
+    and enter table [B, width] in place.  Returns (lengths [B], starts [B+1], slots [tokens], positions [tokens], counts [3]);
+    counts -- pages used, pages missing, tokens cut off -- is the next step's `used`."""
+    B, i32 = cached.shape[0], torch.int32
+    if cached.dim() != 1 or fresh.shape != cached.shape or table.dim() != 2 or table.shape[0] != B or free.dim() != 1 or used.numel() < 1:
+        raise ValueError("cached and fresh are [B], table is [B, width], free is [pages], used holds a number")
+    if tokens < 0:
+        raise ValueError("tokens must not be negative")
+    lengths, starts, slots, positions, counts = cached.new_empty(2 * B + 4 + 2 * tokens).split([B, B + 1, tokens, tokens, 3])
+    _check(_lib.pipe_cache_plan(_ptr(cached, i32), _ptr(fresh, i32), B, int(page_size), _ptr(free, i32), free.shape[0], _ptr(used, i32),
+                                _ptr(table, i32), table.shape[1], int(tokens), lengths.data_ptr(), starts.data_ptr(), slots.data_ptr(),
+                                positions.data_ptr(), counts.data_ptr(), _stream()), "pipe_cache_plan")
+    return lengths, starts, slots, positions, counts
+
+
+def pipe_cache_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor, page_size: int) -> None:
+    """Keys and values [T, kv_heads, head_dim] in 4 bits to slots [T] (int32; a slot outside the cache is skipped)."""
+    kp, kt, kh = _heads(k, "k")
+    vp, vt, vh = _heads(v, "v")
+    T, H, D = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype or tuple(slots.shape) != (T,):
+        raise ValueError("k and v must have one shape and type, slots one entry a token")
+    _check(_lib.pipe_cache_write(kp, vp, _type(k.dtype), T, H, D, kt, kh, vt, vh, _ptr(slots, torch.int32), _ptr(cache, torch.uint8),
+                                 _cache_pages(cache, page_size, H, D), int(page_size), _stream()), "pipe_cache_write")
+
+
+def pipe_cache_read(slots: torch.Tensor, cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int,
+                    dtype: torch.dtype = torch.float32):
+    """(k, v) [T, kv_heads, head_dim]: the values that the codes at slots [T] stand for (zeros for a slot outside the cache)."""
+    T = slots.shape[0]
+    k = torch.empty((T, kv_heads, head_dim), dtype=dtype, device=cache.device)
+    v = torch.empty_like(k)
+    _check(_lib.pipe_cache_read(_ptr(cache, torch.uint8), _cache_pages(cache, page_size, kv_heads, head_dim), int(page_size),
+                                _ptr(slots, torch.int32), T, int(kv_heads), int(head_dim), _type(dtype), k.data_ptr(), v.data_ptr(),
+                                _stream()), "pipe_cache_read")
+    return k, v
+
+
+def pipe_cache_attention(q: torch.Tensor, starts: torch.Tensor, lengths: torch.Tensor, cache: torch.Tensor, table: torch.Tensor,
+                         page_size: int, kv_heads: int, scale: Optional[float] = None, max_length: int = 0,
+                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the fresh tokens q [T, heads, head_dim] over the cache: request b's queries are starts[b] .. starts[b+1]-1, the last
+    of them the last of its lengths[b] cached tokens.  scale: None = head_dim ** -0.5; max_length: about the longest length (a hint)."""
+    qp, qt, qh = _heads(q, "q")
+    T, H, D = q.shape
+    B = lengths.shape[0]
+    if tuple(starts.shape) != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("starts is [B + 1], lengths [B], table [B, width]")
+    y = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
+    if y.shape != q.shape or y.dtype != q.dtype:
+        raise ValueError("output has the wrong shape or type")
+    i32 = torch.int32
+    _check(_lib.pipe_cache_attention(qp, _type(q.dtype), T, H, int(kv_heads), D, qt, qh, _ptr(starts, i32), _ptr(lengths, i32), B,
+                                     _ptr(cache, torch.uint8), _cache_pages(cache, page_size, kv_heads, D), int(page_size),
+                                     _ptr(table, i32), table.shape[1], D ** -0.5 if scale is None else float(scale), int(max_length),
+                                     _ptr(y), _stream()), "pipe_cache_attention")
+    return y
+
+
+def pipe_prepare_cache_attention(tokens: int, heads: int, kv_heads: int, head_dim: int, requests: int, max_length: int) -> None:
+    """What pipe_cache_attention of these sizes on the current stream would allocate on first use."""
+    _check(_lib.pipe_prepare_cache_attention(int(tokens), int(heads), int(kv_heads), int(head_dim), int(requests), int(max_length),
+                                             _stream()), "pipe_prepare_cache_attention")
+
+
+def pipe_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor,
+                          starts_k: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention over packed sequences: q [Tq, heads, head_dim], k and v [Tk, kv_heads, head_dim]; sequence b is starts[b] ..
+    starts[b+1]-1 of q and starts_k (None: starts) of k and v.  causal: aligned at the end.  scale: None = head_dim ** -0.5."""
+    qp, qt, qh = _heads(q, "q")
+    kp, kt, kh = _heads(k, "k")
+    vp, vt, vh = _heads(v, "v")
+    T, H, D = q.shape
+    if k.shape != v.shape or k.shape[2] != D or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("k and v must have one shape, and q's head_dim and type")
+    if starts.dim() != 1 or starts.shape[0] < 2 or (starts_k is not None and starts_k.shape != starts.shape):
+        raise ValueError("starts and starts_k are [sequences + 1]")
+    y = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
+    if y.shape != q.shape or y.dtype != q.dtype:
+        raise ValueError("output has the wrong shape or type")
+    i32 = torch.int32
+    _check(_lib.pipe_prompt_attention(qp, kp, vp, _type(q.dtype), T, k.shape[0], H, k.shape[1], D, qt, qh, kt, kh, vt, vh,
+                                      _ptr(starts, i32), _ptr(starts_k, i32), starts.shape[0] - 1, 1 if causal else 0,
+                                      D ** -0.5 if scale is None else float(scale), _ptr(y), _stream()), "pipe_prompt_attention")
+    return y

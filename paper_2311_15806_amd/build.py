@@ -27,6 +27,9 @@ SOURCES = [
     ("pipe_probe.hip", []),
     ("pipe_diag.hip", ["-ffp-contract=off"]),
     ("pipe_depthwise.hip", ["-ffp-contract=off"] + PRELOAD),
+    ("pipe_cache.hip", PRELOAD),
+    ("pipe_cache_attn.hip", []),
+    ("pipe_prompt_attn.hip", []),
 ]
 
 COMMON = [

@@ -11,6 +11,7 @@
 #include <string>
 #include <utility>
 
+#include "pipe_attention.h"
 #include "pipe_internal.h"
 
 // ------------------------------------------------------------------ errors
@@ -2360,4 +2361,122 @@ extern "C" int pipe_prepare_chain(const pipe_chain_layer* layers, int L, int N, 
     if (rc == PIPE_OK && (T >= N || (H == 1 && W == 1)))
       rc = chain_forward_grid(layers, L, fake_x, std::min(T, N), H, W, 1.f, split, M, nullptr, fake_y, stream, streamed);
   return rc;
+}
+
+// ------------------------------------------------------------------ 4-bit cache and attention
+static bool known_type(int type) { return type == PIPE_F32 || type == PIPE_F16 || type == PIPE_BF16; }
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// heads and head_dim of the attention calls
+static bool heads_ok(int Hq, int Hkv, int D) { return Hkv >= 1 && Hq >= Hkv && Hq <= 65535 && Hq % Hkv == 0 && (D == 64 || D == 128); }
+
+// (rows of a kernel's grid stay below 2^31)
+static bool rows_ok(int T, int H) { return T >= 0 && (int64_t)T * H <= 0x7fffffff; }
+
+static int cache_view(const void* cache_dev, int n_pages, int P, int Hkv, int D, CacheView* c) {
+  const int shift = pipe_page_shift(P);
+  if (!cache_dev || shift < 0 || !aligned16(cache_dev)) return PIPE_EINVAL;
+  if (n_pages < 1 || ((int64_t)n_pages << shift) > 0x7fffffff || !heads_ok(Hkv, Hkv, D)) return PIPE_ESHAPE;
+  *c = CacheView{(uint8_t*)const_cast<void*>(cache_dev), n_pages, shift, Hkv};
+  return PIPE_OK;
+}
+
+extern "C" int64_t pipe_cache_page_bytes(int Hkv, int D, int P) {
+  if (pipe_page_shift(P) < 0 || !heads_ok(Hkv, Hkv, D)) return 0;
+  return (int64_t)Hkv * P * (D + 8);
+}
+
+extern "C" int pipe_cache_plan(const int32_t* cached_dev, const int32_t* fresh_dev, int B, int P, const int32_t* free_dev,
+                               int n_free, const int32_t* used_dev, int32_t* table_dev, int table_width, int T,
+                               int32_t* lengths_dev, int32_t* starts_dev, int32_t* slots_dev, int32_t* positions_dev,
+                               int32_t* counts_dev, void* stream) {
+  const int shift = pipe_page_shift(P);
+  if (!cached_dev || !fresh_dev || !used_dev || !table_dev || !lengths_dev || !starts_dev || !counts_dev || shift < 0) return PIPE_EINVAL;
+  if (B < 1 || B > PIPE_PLAN_MAX_B || T < 0 || table_width < 1 || n_free < 0) return PIPE_ESHAPE;
+  if ((n_free > 0 && !free_dev) || (T > 0 && (!slots_dev || !positions_dev))) return PIPE_EINVAL;
+  const uintptr_t u = reinterpret_cast<uintptr_t>(used_dev), n = reinterpret_cast<uintptr_t>(counts_dev);
+  if (u + sizeof(int32_t) > n && u < n + 3 * sizeof(int32_t)) return PIPE_EINVAL;
+  return launch_cache_plan(cached_dev, fresh_dev, B, shift, free_dev, n_free, used_dev, table_dev, table_width, T, lengths_dev,
+                           starts_dev, slots_dev, positions_dev, counts_dev, (hipStream_t)stream);
+}
+
+extern "C" int pipe_cache_write(const void* k_dev, const void* v_dev, int type, int T, int Hkv, int D, int64_t k_token_stride,
+                                int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int32_t* slots_dev,
+                                void* cache_dev, int n_pages, int P, void* stream) {
+  if (!known_type(type)) return PIPE_EINVAL;
+  CacheView c;
+  const int rc = cache_view(cache_dev, n_pages, P, Hkv, D, &c);
+  if (rc) return rc;
+  if (!rows_ok(T, Hkv) || k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0) return PIPE_ESHAPE;
+  if (T == 0) return PIPE_OK;
+  if (!k_dev || !v_dev || !slots_dev) return PIPE_EINVAL;
+  return launch_cache_write(k_dev, v_dev, type, T, D, {k_token_stride, k_head_stride}, {v_token_stride, v_head_stride}, slots_dev, c,
+                            (hipStream_t)stream);
+}
+
+extern "C" int pipe_cache_read(const void* cache_dev, int n_pages, int P, const int32_t* slots_dev, int T, int Hkv, int D,
+                               int type, void* k_dev, void* v_dev, void* stream) {
+  if (!known_type(type)) return PIPE_EINVAL;
+  CacheView c;
+  const int rc = cache_view(cache_dev, n_pages, P, Hkv, D, &c);
+  if (rc) return rc;
+  if (!rows_ok(T, Hkv)) return PIPE_ESHAPE;
+  if (T == 0) return PIPE_OK;
+  if (!k_dev || !v_dev || !slots_dev || !aligned16(k_dev) || !aligned16(v_dev)) return PIPE_EINVAL;
+  return launch_cache_read(c, slots_dev, T, D, type, k_dev, v_dev, (hipStream_t)stream);
+}
+
+extern "C" int pipe_cache_attention(const void* q_dev, int type, int T, int Hq, int Hkv, int D, int64_t q_token_stride,
+                                    int64_t q_head_stride, const int32_t* starts_dev, const int32_t* lengths_dev, int B,
+                                    const void* cache_dev, int n_pages, int P, const int32_t* table_dev, int table_width,
+                                    float scale, int max_length, void* out_dev, void* stream) {
+  if (!known_type(type) || !std::isfinite(scale)) return PIPE_EINVAL;
+  CacheView c;
+  const int rc = cache_view(cache_dev, n_pages, P, Hkv, D, &c);
+  if (rc) return rc;
+  if (!heads_ok(Hq, Hkv, D) || !rows_ok(T, Hq) || B < 1 || table_width < 1 || max_length < 0 || q_token_stride < 0 || q_head_stride < 0)
+    return PIPE_ESHAPE;
+  if (T == 0) return PIPE_OK;
+  if (!q_dev || !starts_dev || !lengths_dev || !table_dev || !out_dev || !aligned16(out_dev)) return PIPE_EINVAL;
+  try {
+    CallScope scope(stream);
+    CacheAttnArgs a{};
+    a.q = q_dev; a.qs = {q_token_stride, q_head_stride};
+    a.starts = starts_dev; a.lengths = lengths_dev; a.table = table_dev; a.cache = c;
+    a.type = type; a.T = T; a.Hq = Hq; a.D = D; a.B = B; a.width = table_width; a.max_length = max_length;
+    a.scale = scale; a.out = out_dev;
+    return launch_cache_attention(a, (hipStream_t)stream);
+  } catch (const std::bad_alloc&) {
+    return PIPE_ENOMEM;
+  }
+}
+
+extern "C" int pipe_prepare_cache_attention(int T, int Hq, int Hkv, int D, int B, int max_length, void* stream) {
+  if (T < 1 || max_length < 1) return PIPE_EINVAL;
+  DryScope dry;
+  // addresses that are never dereferenced: nothing is launched in a dry run
+  const int32_t* fake = reinterpret_cast<const int32_t*>(uintptr_t(256));
+  return pipe_cache_attention(fake, PIPE_F32, T, Hq, Hkv, D, (int64_t)Hq * D, D, fake, fake, B, fake, 1, 16, fake, 1, 1.f, max_length,
+                              reinterpret_cast<void*>(uintptr_t(512)), stream);
+}
+
+extern "C" int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_dev, int type, int Tq, int Tk, int Hq,
+                                     int Hkv, int D, int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride,
+                                     int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                                     const int32_t* q_starts_dev, const int32_t* k_starts_dev, int B, int causal, float scale,
+                                     void* out_dev, void* stream) {
+  if (!known_type(type) || !std::isfinite(scale) || (causal != 0 && causal != 1)) return PIPE_EINVAL;
+  if (!heads_ok(Hq, Hkv, D) || !rows_ok(Tq, Hq) || !rows_ok(Tk, Hkv) || B < 1 || q_token_stride < 0 || q_head_stride < 0 ||
+      k_token_stride < 0 || k_head_stride < 0 || v_token_stride < 0 || v_head_stride < 0)
+    return PIPE_ESHAPE;
+  if (k_starts_dev == nullptr && Tk != Tq) return PIPE_ESHAPE;
+  if (Tq == 0) return PIPE_OK;
+  if (!q_dev || !q_starts_dev || !out_dev || !aligned16(out_dev) || (Tk > 0 && (!k_dev || !v_dev))) return PIPE_EINVAL;
+  PromptAttnArgs a{};
+  a.q = q_dev; a.k = k_dev; a.v = v_dev;
+  a.qs = {q_token_stride, q_head_stride}; a.ks = {k_token_stride, k_head_stride}; a.vs = {v_token_stride, v_head_stride};
+  a.q_starts = q_starts_dev; a.k_starts = k_starts_dev ? k_starts_dev : q_starts_dev;
+  a.type = type; a.Tq = Tq; a.Tk = Tk; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.B = B; a.causal = causal; a.scale = scale;
+  a.out = out_dev;
+  return launch_prompt_attention(a, (hipStream_t)stream);
 }

@@ -1,0 +1,62 @@
+// Shared by the cache and attention kernels (pipe_cache.hip, pipe_cache_attn.hip, pipe_prompt_attn.hip).
+#pragma once
+#include "pipe_internal.h"
+
+// The layout of a cache page is stated in pipe.h; a block is one head's part of one page.
+constexpr int PIPE_PLAN_MAX_B = 4096;
+
+struct CacheView {
+  uint8_t* base;
+  int n_pages, shift, Hkv;   // P = 1 << shift
+};
+
+// page sizes that exist, as the power of two; -1 otherwise
+static inline int pipe_page_shift(int P) {
+  for (int s = 4; s <= 8; ++s)
+    if (P == 1 << s) return s;
+  return -1;
+}
+
+struct HeadStrides {
+  int64_t token, head;   // in elements
+};
+
+int launch_cache_plan(const int32_t* cached, const int32_t* fresh, int B, int shift, const int32_t* free_list, int n_free,
+                      const int32_t* used, int32_t* table, int width, int T, int32_t* lengths, int32_t* starts,
+                      int32_t* slots, int32_t* positions, int32_t* counts, hipStream_t st);
+int launch_cache_write(const void* k, const void* v, int type, int T, int D, HeadStrides ks, HeadStrides vs,
+                       const int32_t* slots, CacheView c, hipStream_t st);
+int launch_cache_read(CacheView c, const int32_t* slots, int T, int D, int type, void* k, void* v, hipStream_t st);
+
+struct CacheAttnArgs {
+  const void* q;
+  HeadStrides qs;
+  const int32_t *starts, *lengths, *table;
+  CacheView cache;
+  int type, T, Hq, D, B, width, max_length;
+  float scale;
+  void* out;
+};
+int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st);
+
+struct PromptAttnArgs {
+  const void *q, *k, *v;
+  HeadStrides qs, ks, vs;
+  const int32_t *q_starts, *k_starts;
+  int type, Tq, Tk, Hq, Hkv, D, B, causal;
+  float scale;
+  void* out;
+};
+int launch_prompt_attention(const PromptAttnArgs& a, hipStream_t st);
+
+#if defined(__HIPCC__)
+using bf16 = __bf16;
+using f16 = _Float16;
+__device__ __forceinline__ float to_f(float x) { return x; }
+__device__ __forceinline__ float to_f(f16 x) { return (float)x; }
+__device__ __forceinline__ float to_f(bf16 x) { return (float)x; }
+template <typename T>
+__device__ __forceinline__ T from_f(float x) { return (T)x; }
+__device__ __forceinline__ float word_scale(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float word_offset(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+#endif
