@@ -20,6 +20,12 @@ static inline int pipe_page_shift(int P) {
 struct HeadStrides {
   int64_t token, head;   // in elements
 };
+static inline int type_size(int type) { return type == PIPE_F32 ? 4 : 2; }
+// whether every row of 8 values is 16-byte aligned
+static inline bool rows_wide(const void* p, HeadStrides s, int type) {
+  const int n = 16 / type_size(type);
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && s.token % n == 0 && s.head % n == 0;
+}
 
 int launch_cache_plan(const int32_t* cached, const int32_t* fresh, int B, int shift, const int32_t* free_list, int n_free,
                       const int32_t* used, int32_t* table, int width, int T, int32_t* lengths, int32_t* starts,
@@ -57,6 +63,32 @@ __device__ __forceinline__ float to_f(f16 x) { return (float)x; }
 __device__ __forceinline__ float to_f(bf16 x) { return (float)x; }
 template <typename T>
 __device__ __forceinline__ T from_f(float x) { return (T)x; }
+// 8 values from p; WIDE: p is 16-byte aligned
+template <typename T>
+struct Vec8 { T v[8]; };
+template <typename T, bool WIDE>
+__device__ __forceinline__ void load8(const T* p, float* x) {
+  if constexpr (WIDE) {
+    Vec8<T> r;
+    uint4 w[sizeof(T) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+    __builtin_memcpy(&r, w, sizeof r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = to_f(r.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = to_f(p[i]);
+  }
+}
+// N values to p, which is aligned to their size (a power of two up to 32 bytes)
+template <typename T, int N>
+__device__ __forceinline__ void store_row(T* p, const float* x) {
+  struct alignas(N * sizeof(T) < 16 ? N * sizeof(T) : 16) Row { T v[N]; } r;
+#pragma unroll
+  for (int i = 0; i < N; ++i) r.v[i] = from_f<T>(x[i]);
+  *reinterpret_cast<Row*>(p) = r;
+}
 __device__ __forceinline__ float word_scale(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float word_offset(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 #endif

@@ -145,26 +145,6 @@ __global__ __launch_bounds__(PLAN_NT) void cache_plan_kernel(
 // ------------------------------------------------------------------ rows into the cache and back
 // A row (one token's one head) of D values is D/8 lanes of 8 values; a lane's codes are one 32-bit word of the page, so that a
 // row's words are one store of D/2 contiguous bytes.  Bound by the bytes: D values in, D/2 + 4 bytes out.
-template <typename T>
-struct Vec8 { T v[8]; };
-
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load8(const T* p, float* x) {
-  if constexpr (WIDE) {
-    Vec8<T> r;
-    constexpr int N = sizeof(T) * 8 / 16;
-    uint4 w[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
-    __builtin_memcpy(&r, w, sizeof r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f(r.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_f(p[i]);
-  }
-}
-
 // minimum / maximum over the LANES (8 or 16) lanes of a row
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
@@ -273,17 +253,11 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, const int3
   }
 }
 
-template <typename T>
-bool wide_ok(const void* p, HeadStrides s) {
-  const int n = 16 / (int)sizeof(T);
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && s.token % n == 0 && s.head % n == 0;
-}
-
 template <typename T, int D>
-int write_typed(const void* k, const void* v, int T_, HeadStrides ks, HeadStrides vs, const int32_t* slots, CacheView c, hipStream_t st) {
+int write_typed(const void* k, const void* v, int T_, HeadStrides ks, HeadStrides vs, const int32_t* slots, CacheView c, bool wide, hipStream_t st) {
   const int rows = T_ * c.Hkv;
   const dim3 grid((unsigned)(((int64_t)rows * (D / 8) + 255) / 256));
-  if (wide_ok<T>(k, ks) && wide_ok<T>(v, vs))
+  if (wide)
     PIPE_KLAUNCH((cache_write_kernel<T, D, true>), grid, dim3(256), 0, st, (const T*)k, (const T*)v, rows, c.Hkv, ks, vs, slots, c);
   else
     PIPE_KLAUNCH((cache_write_kernel<T, D, false>), grid, dim3(256), 0, st, (const T*)k, (const T*)v, rows, c.Hkv, ks, vs, slots, c);
@@ -314,9 +288,10 @@ int launch_cache_plan(const int32_t* cached, const int32_t* fresh, int B, int sh
 
 int launch_cache_write(const void* k, const void* v, int type, int T, int D, HeadStrides ks, HeadStrides vs,
                        const int32_t* slots, CacheView c, hipStream_t st) {
-  if (type == PIPE_F32) return D == 64 ? write_typed<float, 64>(k, v, T, ks, vs, slots, c, st) : write_typed<float, 128>(k, v, T, ks, vs, slots, c, st);
-  if (type == PIPE_F16) return D == 64 ? write_typed<f16, 64>(k, v, T, ks, vs, slots, c, st) : write_typed<f16, 128>(k, v, T, ks, vs, slots, c, st);
-  return D == 64 ? write_typed<bf16, 64>(k, v, T, ks, vs, slots, c, st) : write_typed<bf16, 128>(k, v, T, ks, vs, slots, c, st);
+  const bool wide = rows_wide(k, ks, type) && rows_wide(v, vs, type);
+  if (type == PIPE_F32) return D == 64 ? write_typed<float, 64>(k, v, T, ks, vs, slots, c, wide, st) : write_typed<float, 128>(k, v, T, ks, vs, slots, c, wide, st);
+  if (type == PIPE_F16) return D == 64 ? write_typed<f16, 64>(k, v, T, ks, vs, slots, c, wide, st) : write_typed<f16, 128>(k, v, T, ks, vs, slots, c, wide, st);
+  return D == 64 ? write_typed<bf16, 64>(k, v, T, ks, vs, slots, c, wide, st) : write_typed<bf16, 128>(k, v, T, ks, vs, slots, c, wide, st);
 }
 
 int launch_cache_read(CacheView c, const int32_t* slots, int T, int D, int type, void* k, void* v, hipStream_t st) {

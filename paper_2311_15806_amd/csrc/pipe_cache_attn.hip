@@ -1,86 +1,455 @@
 // Attention of fresh tokens over the 4-bit cache.
+//
+// For one key/value head of one request, the rows are its fresh tokens' query heads (row = token * G + head in the group), 16 of
+// them a workgroup's tile; a wave walks 64 cached tokens at a time:
+//   T[t][r] = s_t * (sum_d c_td q_rd) + m_t * (sum_d q_rd)          one MFMA tile per 16 tokens, codes as the A operand
+//   P[t][r] = exp2(rs_r * (T - ref_r))                               ref_r: a row's running reference
+//   O[d][r] += sum_t c'_td * (P * s'_t)                              codes of V as the A operand, P as the B operand
+//   M[r]   += sum_t P * m'_t,  L[r] += sum_t P
+// with T's accumulator layout (lane = row, 4 tokens in a lane's registers) being exactly the B operand's of the second product, once
+// the tokens of a step of 32 are taken in the order 4*kg..+3 of one 16-block, then of the next: no shuffle between the products.
+//
+// Codes become fp16 without arithmetic: the bits of a code at the bottom of a half are the denormal c * 2^-24, four bits up
+// 16 c * 2^-24, which MFMA multiplies exactly; 5 instructions make 8 operand values.  The factors 2^24 and 1/16 sit in q and in the
+// output's scale.  fp32 takes the codes as c - 8 in ordinary halves and q and P in two terms: 11 instructions.
+// What the offset takes out of a sum again is kept small: V's part is sum P' (c - 8) + P (m + 8 s), since m is about -8 s.
+//
+// Bound by the bytes of the codes as long as a tile holds all rows of the head: see the figures at the launch rules.
+#include <algorithm>
+
 #include "pipe_attention.h"
 
 namespace {
 
-// One wave per query row: 64 cached tokens at a time, a lane per token for the scores, a lane per D/64 values for the output.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void cache_attn_kernel(CacheAttnArgs a) {
-  __shared__ float sq[D], sp[64], sps[64];
-  __shared__ int srow[64];
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  const int kvh = h / (a.Hq / a.cache.Hkv);
-  const int shift = a.cache.shift, P = 1 << shift;
-  // the request of this token: the last one that starts at or before it
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr int WAVES = 4, ROWS = 16, STEP = 64;      // tokens of a wave's step
+constexpr int CHUNK_UNIT = WAVES * STEP;            // a split's tokens are a multiple of this: every wave gets whole steps
+constexpr int SPLIT_TILES = 1024;
+constexpr float REF_SLACK = 6.f;                    // log2: a row's reference rises only when a score exceeds it by this
+constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE fits fp16
+
+struct Kernel {
+  CacheAttnArgs a;
+  int G, n_split, chunk;
+  bool wide;        // 16-byte loads of q
+  float* part_o;    // [Hkv][T * G rows][split][D]
+  float* part_ml;   // [Hkv][T * G rows][split][2]: log2 of the reference weight, sum of weights
+};
+
+struct Tile {
+  int b, row0, n_rows, start;   // rows row0 .. row0 + n_rows - 1 of request b, whose tokens start at `start`
+  int first_seen;               // cached tokens that the request's first fresh token sees (may be negative)
+  int end;                      // cached tokens that any row of the tile sees
+  int n_split, chunk;           // splits that have tokens (at least one), and theirs
+};
+
+// Tile `id` of the launch: request b (B: the rows behind the last request, which see nothing) owns the ids from
+// floor(start_b * G / 16) + b on.
+__device__ __forceinline__ Tile find_tile(const Kernel& k, int id) {
+  const CacheAttnArgs& a = k.a;
+  const int lane = threadIdx.x & 63;
+  auto start_of = [&](int b) { return b > 0 ? min(max(a.starts[b], 0), a.T) : 0; };
   int b = -1;
-  for (int i0 = 0; i0 < a.B; i0 += 64) {
-    const unsigned long long m = __ballot(i0 + lane < a.B && a.starts[min(i0 + lane, a.B)] <= t);
-    b += __popcll(m);
+  for (int i0 = 0; i0 <= a.B; i0 += 64) {
+    const int i = i0 + lane;
+    const bool le = i <= a.B && (int)(((int64_t)start_of(min(i, a.B)) * k.G) / ROWS) + i <= id;
+    const int n = __popcll(__ballot(le));
+    b += n;
+    if (n < 64) break;
   }
-  const bool mine = b >= 0 && t < a.starts[a.B];
-  int seen = 0;
-  if (mine) seen = min(a.lengths[b], (int)min((int64_t)a.width << shift, (int64_t)0x7fffffff)) ;
-  const int full = mine ? a.lengths[b] : 0;
-  if (mine) seen = min(seen, full - (a.starts[b + 1] - t) + 1);
-  float qsum = 0;
-  for (int i = lane; i < D; i += 64) sq[i] = to_f(((const T*)a.q)[(int64_t)t * a.qs.token + (int64_t)h * a.qs.head + i]);
-  __syncthreads();
-  for (int i = 0; i < D; ++i) qsum += sq[i];
-  float top = -INFINITY, sum = 0, o[D / 64] = {}, om = 0;
-  const int64_t bytes = (int64_t)P * (D + 8);
-  for (int t0 = 0; t0 < seen; t0 += 64) {
-    const int tok = t0 + lane;
-    float S = -INFINITY, vs = 0, vm = 0;
-    int page = -1;
-    const uint8_t* blk = nullptr;
-    if (tok < seen) page = a.table[(int64_t)b * a.width + (tok >> shift)];
-    const int off = tok & (P - 1);
-    if (page >= 0 && page < a.cache.n_pages) {
-      blk = a.cache.base + ((int64_t)page * a.cache.Hkv + kvh) * bytes;
-      const uint32_t kw = *(const uint32_t*)(blk + P * D + 4 * off), vw = *(const uint32_t*)(blk + P * D + 4 * P + 4 * off);
-      float dot = 0;
-      for (int w = 0; w < D / 8; ++w) {
-        const uint32_t x = ((const uint32_t*)(blk + off * (D / 2)))[w];
-        for (int i = 0; i < 8; ++i) dot = fmaf(sq[8 * w + i], (float)((x >> (4 * i)) & 15u), dot);
-      }
-      S = (word_scale(kw) * dot + word_offset(kw) * qsum) * a.scale;
-      vs = word_scale(vw);
-      vm = word_offset(vw);
-    }
-    float mx = S;
-    for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-    const float ntop = fmaxf(top, mx);
-    const float ref = ntop == -INFINITY ? 0.f : ntop, f = expf(top - ref);
-    top = ntop;
-    const float p = blk ? expf(S - ref) : 0.f;
-    sum = sum * f + p;
-    om = om * f + (blk ? p * vm : 0.f);
-    for (int i = 0; i < D / 64; ++i) o[i] *= f;
-    sps[lane] = blk ? p * vs : 0.f;
-    srow[lane] = blk ? page : -1;
-    __syncthreads();
-    for (int j = 0; j < 64; ++j) {
-      if (srow[j] < 0) continue;
-      const uint8_t* vb = a.cache.base + ((int64_t)srow[j] * a.cache.Hkv + kvh) * bytes + P * D / 2 + ((t0 + j) & (P - 1)) * (D / 2);
-      for (int i = 0; i < D / 64; ++i) {
-        const int d = lane + 64 * i;
-        o[i] = fmaf(sps[j], (float)((vb[d >> 1] >> (4 * (d & 1))) & 15), o[i]);
-      }
-    }
-    __syncthreads();
-  }
-  for (int d = 32; d; d >>= 1) { sum += __shfl_xor(sum, d); om += __shfl_xor(om, d); }
-  const bool none = top == -INFINITY && sum == 0.f;
-  for (int i = 0; i < D / 64; ++i)
-    ((T*)a.out)[((int64_t)t * a.Hq + h) * D + lane + 64 * i] = from_f<T>(none ? 0.f : (o[i] + om) / sum);
+  b = __builtin_amdgcn_readfirstlane(b);
+  Tile t;
+  t.b = b;
+  t.start = start_of(b);
+  const int n = (b < a.B ? start_of(b + 1) : a.T) - t.start;
+  t.row0 = (id - ((int)(((int64_t)t.start * k.G) / ROWS) + b)) * ROWS;
+  t.n_rows = t.row0 < 0 ? 0 : min(ROWS, max(0, n * k.G - t.row0));
+  const int length = b < a.B ? max(0, a.lengths[b]) : 0;
+  t.first_seen = length - n + 1;
+  const int last_row = t.row0 + max(t.n_rows, 1) - 1;
+  const int64_t table = (int64_t)a.width << a.cache.shift;
+  t.end = (int)min((int64_t)max(0, t.first_seen + last_row / k.G), min(table, (int64_t)0x7ffff000));
+  // (a request longer than the hint gets longer splits)
+  const int per = (int)(((int64_t)t.end + k.n_split - 1) / k.n_split);
+  t.chunk = max(k.chunk, (per + CHUNK_UNIT - 1) / CHUNK_UNIT * CHUNK_UNIT);
+  t.n_split = max(1, (t.end + t.chunk - 1) / t.chunk);
+  return t;
 }
 
-template <typename T>
-int run(const CacheAttnArgs& a, hipStream_t st) {
-  const dim3 grid(a.T, a.Hq);
-  if (a.D == 64) PIPE_KLAUNCH((cache_attn_kernel<T, 64>), grid, dim3(64), 0, st, a);
-  else PIPE_KLAUNCH((cache_attn_kernel<T, 128>), grid, dim3(64), 0, st, a);
+// the parts of row r of a tile, of the head of this workgroup
+__device__ __forceinline__ int64_t part_row(const Kernel& k, const Tile& t, int r) {
+  return ((int64_t)blockIdx.y * k.a.T * k.G + (int64_t)t.start * k.G + t.row0 + r) * k.n_split;
+}
+
+// 8 codes of a word -> 4 registers of two fp16 values, nibbles (0,4) (1,5) (2,6) (3,7)
+template <bool CENTRED>
+__device__ __forceinline__ void expand(uint32_t x, uint32_t* o) {
+  if constexpr (CENTRED) {
+    auto half = [](uint32_t w) {   // nibble at bit 4: 64 + c, less 72
+      const h2 v = __builtin_bit_cast(h2, (w & 0x00f000f0u) | 0x54005400u) - (h2){(_Float16)72.f, (_Float16)72.f};
+      return __builtin_bit_cast(uint32_t, v);
+    };
+    o[0] = half(x << 4); o[1] = half(x); o[2] = half(x >> 4); o[3] = half(x >> 8);
+  } else {
+    const uint32_t y = x >> 8;
+    o[0] = x & 0x000f000fu; o[1] = x & 0x00f000f0u; o[2] = y & 0x000f000fu; o[3] = y & 0x00f000f0u;
+  }
+}
+
+// Two values rounded to fp16, and what is left of them rounded likewise.  The first rounding is done once: the single and the packed
+// conversion break ties differently, and a rest taken from the other's result is off by a unit.
+__device__ __forceinline__ uint32_t half_pair(float x, float y) {
+  uint32_t u = __builtin_bit_cast(uint32_t, (h2){(_Float16)x, (_Float16)y});
+  asm volatile("" : "+v"(u));
+  return u;
+}
+__device__ __forceinline__ uint32_t half_rest(float x, float y, uint32_t u) {
+  const h2 v = __builtin_bit_cast(h2, u);
+  return __builtin_bit_cast(uint32_t, (h2){(_Float16)(x - (float)v[0]), (_Float16)(y - (float)v[1])});
+}
+
+__device__ __forceinline__ float max_over_kg(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float sum_over_kg(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// What a wave loads for 64 tokens: 16-block j in [j]
+template <int D>
+struct Loaded {
+  static constexpr int KS = D / 32;
+  uint32_t k[4][KS];       // lane (token l16, kg): KS words from kg * KS on
+  uint32_t v[4][4];        // lane (l16, kg): token 4 kg + i, D/16 codes from l16 * D/16 on
+  u4 kw[4], vw[4];         // words of tokens 4 kg .. + 3
+  uint32_t there;          // 16-blocks whose page exists
+};
+
+template <typename T, int D>
+struct Walk {
+  static constexpr bool FINE = sizeof(T) == 4;     // fp32: centred codes, two terms
+  static constexpr int KS = D / 32, MT = D / 16, NT = FINE ? 2 : 1;
+  const Kernel& kr;
+  const CacheAttnArgs& a;
+  const Tile& t;
+  int l16, kg, kvh;
+
+  __device__ __forceinline__ void load(Loaded<D>& x, const int32_t* pages, int tok0) const {
+    const int shift = a.cache.shift, P = 1 << shift;
+    x.there = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int tok = tok0 + 16 * j;
+      int page = __builtin_amdgcn_readfirstlane(pages[j]);
+      const bool there = page >= 0 && page < a.cache.n_pages;
+      x.there |= there ? 1u << j : 0u;
+      page = there ? page : 0;
+      const uint8_t* blk = a.cache.base + ((int64_t)page * a.cache.Hkv + kvh) * ((int64_t)P * (D + 8));
+      const int off = tok & (P - 1);
+      const uint8_t* kp = blk + off * (D / 2) + l16 * (D / 2) + kg * (KS * 4);
+      if constexpr (KS == 4) {
+        const u4 w = *reinterpret_cast<const u4*>(kp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.k[j][i] = w[i];
+      } else {
+        const uint2 w = *reinterpret_cast<const uint2*>(kp);
+        x.k[j][0] = w.x; x.k[j][1] = w.y;
+      }
+      const uint8_t* vp = blk + P * (D / 2) + off * (D / 2) + kg * (2 * D) + l16 * (D / 32);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (D == 128) x.v[j][i] = *reinterpret_cast<const uint32_t*>(vp + i * (D / 2));
+        else x.v[j][i] = *reinterpret_cast<const uint16_t*>(vp + i * (D / 2));
+      }
+      const uint8_t* wp = blk + P * D + off * 4 + kg * 16;
+      x.kw[j] = *reinterpret_cast<const u4*>(wp);
+      x.vw[j] = *reinterpret_cast<const u4*>(wp + 4 * P);
+    }
+  }
+
+  // pages of the four 16-blocks from tok0 on; -1 beyond `end`
+  __device__ __forceinline__ void pages_of(int32_t* pages, int tok0, int end) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int tok = __builtin_amdgcn_readfirstlane(tok0 + 16 * j);
+      pages[j] = tok < end ? a.table[(int64_t)t.b * a.width + (tok >> a.cache.shift)] : -1;
+    }
+  }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel kr) {
+  using W = Walk<T, D>;
+  constexpr int KS = W::KS, MT = W::MT, NT = W::NT;
+  constexpr bool FINE = W::FINE;
+  __shared__ float s_o[WAVES][ROWS][D + 4];
+  __shared__ float s_ref[WAVES][ROWS], s_sum[WAVES][ROWS];
+  const CacheAttnArgs& a = kr.a;
+  const Tile t = find_tile(kr, blockIdx.x);
+  const int split = blockIdx.z;
+  if (t.n_rows == 0 || split >= t.n_split) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const W w{kr, a, t, lane & 15, lane >> 4, (int)blockIdx.y};
+  const int l16 = w.l16, kg = w.kg;
+
+  // q: row l16, the values that meet the words kg * KS .. of a token
+  const int row = t.row0 + l16;
+  const bool real = l16 < t.n_rows;
+  const int token = real ? row / kr.G : 0, head = real ? row % kr.G : 0;
+  const int seen = real ? t.first_seen + token : 0;      // cached tokens this row sees
+  const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)(w.kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
+  float qv[KS * 8], qmax = 0, qsum = 0;
+#pragma unroll
+  for (int i = 0; i < KS * 8; i += 8) {
+    if (kr.wide) load8<T, true>(qp + i, qv + i);
+    else load8<T, false>(qp + i, qv + i);
+  }
+#pragma unroll
+  for (int i = 0; i < KS * 8; ++i) {
+    qv[i] = real ? qv[i] : 0.f;
+    qmax = fmaxf(qmax, fabsf(qv[i]));
+  }
+  qmax = max_over_kg(qmax);
+  // a power of two that brings the row's largest value to 2^14 .. 2^15, and with it the sign of the scale
+  const int qe = qmax > 0.f && qmax < INFINITY ? max(-80, min(100, 14 - ((int)(__float_as_uint(qmax) >> 23) - 127))) : 0;
+  const float sgn = a.scale < 0.f ? -1.f : 1.f;
+  h8 q[NT][KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    u4 hi, lo;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {                // nibbles n and n + 4 are a register of the operand
+      float x = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n], qe), y = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n + 4], qe);
+      qsum += x + y;
+      if (!FINE && (n & 1)) { x *= 0.0625f; y *= 0.0625f; }
+      hi[n] = half_pair(x, y);
+      lo[n] = half_rest(x, y, hi[n]);
+    }
+    q[0][s] = __builtin_bit_cast(h8, hi);
+    if constexpr (FINE) q[1][s] = __builtin_bit_cast(h8, lo);
+  }
+  qsum = sum_over_kg(qsum);
+  // scores in units of q * 2^qe (and of 2^-24 for denormal codes); rs turns them into log2 of a weight
+  const float unit = FINE ? 1.f : 0x1p-24f;
+  qsum *= unit;
+  const float rs = a.scale == 0.f ? 1.f : ldexpf(fabsf(a.scale) * 1.44269504f, -qe) * (1.f / unit);
+
+  f4 o[MT], ones = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < MT; ++i) o[i] = (f4){0.f, 0.f, 0.f, 0.f};
+  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f;
+  float sigma = 0x1p-100f, psc = P_SCALE * 0x1p100f;   // P' = P * s' * psc, psc = P_SCALE / sigma, s' < 2 sigma
+
+  const int end = (int)min((int64_t)t.end, (int64_t)(split + 1) * t.chunk);
+  int tok = split * t.chunk + wave * STEP;
+  const int full = max(0, t.first_seen + t.row0 / kr.G);   // tokens that every row sees
+  Loaded<D> x;
+  int32_t pages[4];
+  w.pages_of(pages, tok, end);
+  if (tok < end) w.load(x, pages, tok);
+  w.pages_of(pages, tok + CHUNK_UNIT, end);
+  for (; tok < end; tok += CHUNK_UNIT) {
+    const Loaded<D> c = x;
+    if (tok + CHUNK_UNIT < end) {
+      w.load(x, pages, tok + CHUNK_UNIT);
+      w.pages_of(pages, tok + 2 * CHUNK_UNIT, end);
+    }
+    // scores
+    float s[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        uint32_t e[4];
+        expand<FINE>(c.k[j][i], e);
+        const h8 op = __builtin_bit_cast(h8, (u4){e[0], e[1], e[2], e[3]});
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[n][i], acc, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float sc = word_scale(c.kw[j][i]);
+        const float m = FINE ? fmaf(8.f, sc, word_offset(c.kw[j][i])) : word_offset(c.kw[j][i]);
+        s[j][i] = fmaf(sc, acc[i], m * qsum);
+      }
+    }
+    float vs[4][4], vm[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        vs[j][i] = word_scale(c.vw[j][i]);
+        vm[j][i] = fmaf(8.f, vs[j][i], word_offset(c.vw[j][i]));
+      }
+    if (tok + STEP > full || tok + STEP > end || c.there != 15u) {      // some row does not see some token
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool vis = tok + 16 * j + 4 * kg + i < min(seen, end) && ((c.there >> j) & 1u);
+          s[j][i] = vis ? s[j][i] : -INFINITY;
+          vs[j][i] = vis ? vs[j][i] : 0.f;
+          vm[j][i] = vis ? vm[j][i] : 0.f;
+        }
+    }
+    float smax = s[0][0], vmax = fabsf(vs[0][0]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        smax = fmaxf(smax, s[j][i]);
+        vmax = fmaxf(vmax, fabsf(vs[j][i]));
+      }
+    if (__any(smax > lift || vmax > 2.f * sigma)) {
+      const float nr = fmaxf(ref, max_over_kg(smax));
+      const float vm_all = max_over_kg(vmax);
+      const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(vm_all) & 0x7f800000u));
+      const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr));
+      sum *= f;
+      osum *= f;
+      const float fo = f * (sigma / nsigma);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) o[i] *= fo;
+      ones *= fo;
+      ref = nr;
+      nref = nr == -INFINITY ? 0.f : -nr * rs;
+      lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
+      sigma = nsigma;
+      psc = P_SCALE / nsigma;
+    }
+    // weights
+    u4 p[NT][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        float y[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(s[j][i + h], rs, nref));
+          sum += e;
+          osum = fmaf(e, vm[j][i + h], osum);
+          y[h] = e * (vs[j][i + h] * psc);
+        }
+        const uint32_t u = half_pair(y[0], y[1]);
+        p[0][j >> 1][(j & 1) * 2 + (i >> 1)] = u;
+        if constexpr (FINE) p[1][j >> 1][(j & 1) * 2 + (i >> 1)] = half_rest(y[0], y[1], u);
+      }
+    // outputs
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      constexpr int NH = D / 64;       // halves of a V word: 4 codes each
+      uint32_t e[NH][4][4];            // [half][pair of tokens][nibble]
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {    // tokens (0,1) (2,3) of block 2g, then of 2g + 1
+        const uint32_t x0 = c.v[2 * g + (u >> 1)][2 * (u & 1)], x1 = c.v[2 * g + (u >> 1)][2 * (u & 1) + 1];
+        expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x05040100u), e[0][u]);
+        if constexpr (NH == 2) expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x07060302u), e[1][u]);
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int hf = i >> 2, nb = i & 3;
+          const h8 op = __builtin_bit_cast(h8, (u4){e[hf][0][nb], e[hf][1][nb], e[hf][2][nb], e[hf][3][nb]});
+          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, __builtin_bit_cast(h8, p[n][g]), o[i], 0, 0, 0);
+        }
+      }
+      if constexpr (!FINE) {
+        const h8 one = {1, 1, 1, 1, 1, 1, 1, 1};
+        ones = __builtin_amdgcn_mfma_f32_16x16x32_f16(one, __builtin_bit_cast(h8, p[0][g]), ones, 0, 0, 0);
+      }
+    }
+  }
+
+  // a wave's outputs as they are, O[d][row] at d = MT * (4 kg + j) + i, over the reference weight
+  sum = sum_over_kg(sum);
+  osum = sum_over_kg(osum);
+  const float back = sigma * (1.f / P_SCALE);
+  const float lref = ref == -INFINITY ? -INFINITY : ref * rs;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      float v = o[i][j];
+      if constexpr (!FINE) v = fmaf(v, (i & 1) ? 0x1p20f : 0x1p24f, -8.f * ones[j]);
+      s_o[wave][l16][MT * (4 * kg + j) + i] = fmaf(v, back, osum);
+    }
+  if (kg == 0) { s_ref[wave][l16] = lref; s_sum[wave][l16] = sum; }
+  __syncthreads();
+  // the waves' parts together: a thread has D/16 values of a row
+  const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * MT;
+  if (r >= t.n_rows) return;
+  float top = s_ref[0][r];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_ref[i][r]);
+  float y[MT] = {}, all = 0.f;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    const float f = s_ref[i][r] == -INFINITY && s_sum[i][r] == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_ref[i][r] - top);
+    if (f == 0.f) continue;       // (a wave that saw nothing holds no weight)
+    all = fmaf(f, s_sum[i][r], all);
+#pragma unroll
+    for (int d = 0; d < MT; ++d) y[d] = fmaf(f, s_o[i][r][d0 + d], y[d]);
+  }
+  if (t.n_split == 1) {
+    const float inv = top == -INFINITY && all == 0.f ? 0.f : 1.f / all;
+    const int rr = t.row0 + r;
+    T* out = (T*)a.out + ((int64_t)(t.start + rr / kr.G) * a.Hq + w.kvh * kr.G + rr % kr.G) * D + d0;
+#pragma unroll
+    for (int d = 0; d < MT; ++d) y[d] = inv == 0.f ? 0.f : y[d] * inv;
+    store_row<T, MT>(out, y);
+  } else {
+    const int64_t at = part_row(kr, t, r) + split;
+    store_row<float, MT>(kr.part_o + at * D + d0, y);
+    if (d0 == 0) { kr.part_ml[at * 2] = top; kr.part_ml[at * 2 + 1] = all; }
+  }
+}
+
+// The splits' parts of a tile together, in their order.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cache_attn_join_kernel(const Kernel kr) {
+  constexpr int MT = D / 16;
+  const CacheAttnArgs& a = kr.a;
+  const Tile t = find_tile(kr, blockIdx.x);
+  const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * MT;
+  if (r >= t.n_rows || t.n_split == 1) return;
+  const int64_t at = part_row(kr, t, r);
+  float top = -INFINITY;
+  for (int s = 0; s < t.n_split; ++s) top = fmaxf(top, kr.part_ml[(at + s) * 2]);
+  float y[MT] = {}, all = 0.f;
+  for (int s = 0; s < t.n_split; ++s) {
+    const int64_t i = at + s;
+    const float lref = kr.part_ml[i * 2], sum = kr.part_ml[i * 2 + 1];
+    if (lref == -INFINITY && sum == 0.f) continue;
+    const float f = __builtin_amdgcn_exp2f(lref - top);
+    all = fmaf(f, sum, all);
+#pragma unroll
+    for (int d = 0; d < MT; ++d) y[d] = fmaf(f, kr.part_o[i * D + d0 + d], y[d]);
+  }
+  const float inv = top == -INFINITY && all == 0.f ? 0.f : 1.f / all;
+  const int rr = t.row0 + r;
+  T* out = (T*)a.out + ((int64_t)(t.start + rr / kr.G) * a.Hq + (int64_t)blockIdx.y * kr.G + rr % kr.G) * D + d0;
+#pragma unroll
+  for (int d = 0; d < MT; ++d) y[d] = inv == 0.f ? 0.f : y[d] * inv;
+  store_row<T, MT>(out, y);
+}
+
+template <typename T, int D>
+int run(Kernel& k, int tiles, hipStream_t st) {
+  PIPE_KLAUNCH((cache_attn_kernel<T, D>), dim3(tiles, k.a.cache.Hkv, k.n_split), dim3(WAVES * 64), 0, st, k);
   PIPE_HIP(hipGetLastError());
+  if (k.n_split > 1) {
+    PIPE_KLAUNCH((cache_attn_join_kernel<T, D>), dim3(tiles, k.a.cache.Hkv), dim3(256), 0, st, k);
+    PIPE_HIP(hipGetLastError());
+  }
   return PIPE_OK;
 }
 
@@ -88,5 +457,25 @@ int run(const CacheAttnArgs& a, hipStream_t st) {
 
 int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   if (a.T == 0) return PIPE_OK;
-  return a.type == PIPE_F32 ? run<float>(a, st) : a.type == PIPE_F16 ? run<f16>(a, st) : run<bf16>(a, st);
+  Kernel k{};
+  k.a = a;
+  k.G = a.Hq / a.cache.Hkv;
+  k.wide = rows_wide(a.q, a.qs, a.type);
+  const int64_t rows = (int64_t)a.T * k.G, tiles = rows / ROWS + a.B + 1;
+  if (tiles > 0x3fffff) return PIPE_ESHAPE;
+  const int64_t longest = std::min<int64_t>(a.max_length > 0 ? a.max_length : (int64_t)a.width << a.cache.shift, 1 << 30);
+  // Splits: as many as bring the launch to SPLIT_TILES workgroups, each with 256 tokens at least.
+  const int64_t base = (rows + ROWS - 1) / ROWS * a.cache.Hkv;
+  k.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(SPLIT_TILES / base, (longest + CHUNK_UNIT - 1) / CHUNK_UNIT));
+  k.chunk = (int)round_up64((longest + k.n_split - 1) / k.n_split, CHUNK_UNIT);
+  if (k.n_split > 1) {
+    // (T * Hq * n_split <= ROWS * SPLIT_TILES: one size serves every call)
+    const size_t parts = (size_t)ROWS * SPLIT_TILES;
+    k.part_o = (float*)pipe_ws_get(WS_ATTN, parts * (128 + 2) * sizeof(float));
+    if (!k.part_o) return pipe_ws_error();
+    k.part_ml = k.part_o + parts * 128;
+  }
+  if (a.type == PIPE_F32) return a.D == 64 ? run<float, 64>(k, (int)tiles, st) : run<float, 128>(k, (int)tiles, st);
+  if (a.type == PIPE_F16) return a.D == 64 ? run<f16, 64>(k, (int)tiles, st) : run<f16, 128>(k, (int)tiles, st);
+  return a.D == 64 ? run<bf16, 64>(k, (int)tiles, st) : run<bf16, 128>(k, (int)tiles, st);
 }

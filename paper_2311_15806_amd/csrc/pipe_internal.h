@@ -283,7 +283,7 @@ bool pipe_capturing();
   do {                                                      \
     if (!pipe_dry_run()) hipLaunchKernelGGL(__VA_ARGS__);   \
   } while (0)
-enum { WS_QX = 0, WS_ROWSUM, WS_SCAL, WS_Y1, WS_H, WS_QH, WS_ROWSUM_H, WS_RESID, WS_ENERGY, WS_MISC, WS_Q8X, WS_CHAIN, WS_DIAG, WS_DIAG_CODES, WS_DIAG_DENSE, WS_RES, WS_RES_Q, WS_CSUM, WS_ABIAS, WS_SLOTS };
+enum { WS_QX = 0, WS_ROWSUM, WS_SCAL, WS_Y1, WS_H, WS_QH, WS_ROWSUM_H, WS_RESID, WS_ENERGY, WS_MISC, WS_Q8X, WS_CHAIN, WS_DIAG, WS_DIAG_CODES, WS_DIAG_DENSE, WS_RES, WS_RES_Q, WS_CSUM, WS_ABIAS, WS_ATTN, WS_SLOTS };
 
 // A maximum as the bit patterns of its parts (device): max_parts(n) words for the reduction of an n-element input, and n = 0
 // for a slot that a contraction kernel's epilogue raised.
