@@ -9,13 +9,16 @@
 // with T's accumulator layout (lane = row, 4 tokens in a lane's registers) being exactly the B operand's of the second product, once
 // the tokens of a step of 32 are taken in the order 4*kg..+3 of one 16-block, then of the next: no shuffle between the products.
 //
-// Codes become fp16 without arithmetic: the bits of a code at the bottom of a half are the denormal c * 2^-24, four bits up
-// 16 c * 2^-24, which MFMA multiplies exactly; 5 instructions make 8 operand values.  The factors 2^24 and 1/16 sit in q and in the
-// output's scale.  fp32 takes the codes as c - 8 in ordinary halves and q and P in two terms: 11 instructions.
-// What the offset takes out of a sum again is kept small: V's part is sum P' (c - 8) + P (m + 8 s), since m is about -8 s.
+// Codes become fp16 without conversions: four bits at bit 4 of a half under the exponent of 64 are 64 + c; 7 instructions make
+// 8 operand values.  The 64 is taken out of the sums again: from the scores by the accumulator's start, -64 sum q, from the
+// outputs with one more product whose A operand is all ones, O = sum P' (64 + c) - 72 sum P'.  (Without the exponent the bits are
+// the denormal c * 2^-24, two instructions less, but the sums then lose what lies 10 bits deeper: 2.5 times the error.)
+// fp32 takes the codes as c - 8, subtracted in fp16 (exact), and q and P in two terms.
+// The offsets' part of the output is P (m + 8 s), with m about -8 s: no large sums that cancel.
 //
 // Bound by the bytes of the codes as long as a tile holds all rows of the head: see the figures at the launch rules.
 #include <algorithm>
+#include <type_traits>
 
 #include "pipe_attention.h"
 
@@ -25,6 +28,8 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+typedef __attribute__((address_space(4))) int32_t ConstInt;   // memory that the kernel does not write
 
 constexpr int WAVES = 4, ROWS = 16, STEP = 64;      // tokens of a wave's step
 constexpr int CHUNK_UNIT = WAVES * STEP;            // a split's tokens are a multiple of this: every wave gets whole steps
@@ -85,19 +90,24 @@ __device__ __forceinline__ int64_t part_row(const Kernel& k, const Tile& t, int 
   return ((int64_t)blockIdx.y * k.a.T * k.G + (int64_t)t.start * k.G + t.row0 + r) * k.n_split;
 }
 
+// what a part counts, beside the largest reference: nothing if it saw nothing (and NaN if it saw nothing but NaN)
+__device__ __forceinline__ float part_weight(float lref, float sum, float top) {
+  return lref == -INFINITY ? sum : __builtin_amdgcn_exp2f(lref - top);
+}
+
 // 8 codes of a word -> 4 registers of two fp16 values, nibbles (0,4) (1,5) (2,6) (3,7)
+struct Bits {
+  uint32_t mask, c64;   // in registers: with both as literals a code would take an `and` and an `or`, with neither one and_or
+  __device__ __forceinline__ Bits() : mask(0x00f000f0u), c64(0x54005400u) { asm("" : "+v"(mask), "+v"(c64)); }
+};
 template <bool CENTRED>
-__device__ __forceinline__ void expand(uint32_t x, uint32_t* o) {
-  if constexpr (CENTRED) {
-    auto half = [](uint32_t w) {   // nibble at bit 4: 64 + c, less 72
-      const h2 v = __builtin_bit_cast(h2, (w & 0x00f000f0u) | 0x54005400u) - (h2){(_Float16)72.f, (_Float16)72.f};
-      return __builtin_bit_cast(uint32_t, v);
-    };
-    o[0] = half(x << 4); o[1] = half(x); o[2] = half(x >> 4); o[3] = half(x >> 8);
-  } else {
-    const uint32_t y = x >> 8;
-    o[0] = x & 0x000f000fu; o[1] = x & 0x00f000f0u; o[2] = y & 0x000f000fu; o[3] = y & 0x00f000f0u;
-  }
+__device__ __forceinline__ void expand(uint32_t x, const Bits& bits, uint32_t* o) {
+  auto half = [&](uint32_t w) {   // nibble at bit 4: 64 + c, or less 72
+    const uint32_t u = (w & bits.mask) | bits.c64;
+    if constexpr (!CENTRED) return u;
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, u) - (h2){(_Float16)72.f, (_Float16)72.f});
+  };
+  o[0] = half(x << 4); o[1] = half(x); o[2] = half(x >> 4); o[3] = half(x >> 8);
 }
 
 // Two values rounded to fp16, and what is left of them rounded likewise.  The first rounding is done once: the single and the packed
@@ -121,73 +131,114 @@ __device__ __forceinline__ float sum_over_kg(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// What a wave loads for 64 tokens: 16-block j in [j]
-template <int D>
-struct Loaded {
-  static constexpr int KS = D / 32;
-  uint32_t k[4][KS];       // lane (token l16, kg): KS words from kg * KS on
-  uint32_t v[4][4];        // lane (l16, kg): token 4 kg + i, D/16 codes from l16 * D/16 on
-  u4 kw[4], vw[4];         // words of tokens 4 kg .. + 3
-  uint32_t there;          // 16-blocks whose page exists
+// A wave's 64 tokens.  NB page lookups serve them: 1 where a page holds 64 tokens or more, else one for every 16-block.
+template <int NB>
+struct Places {
+  const uint8_t* blk[NB];   // the head's block of the page (any page where there is none)
+  uint32_t off[NB];         // first token in it
+  uint32_t there;           // lookups whose page exists
 };
+// The codes and words of the 64 tokens, as a lane (l16, kg) holds them.
+template <int D>
+struct Tokens {
+  uint32_t k[4][D / 32];    // [16-block]: of token l16 the D/32 words from kg * D/32 on
+  uint32_t v[4][4];         // [16-block]: of token 4 kg + i the D/16 codes from l16 * D/16 on
+  uint32_t kw, vw;          // the words of token 4 kg + l16 % 4 of 16-block l16 / 4
+  uint32_t there;           // lookups whose page exists
+};
+// what lane 4 j + i of a row of 16 lanes holds: the word of this lane's i-th token of 16-block j (folded into the operation that uses it)
+template <int LANE>
+__device__ __forceinline__ float from_lane(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x150 + LANE, 0xf, 0xf, true));
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f) {      // f(0) .. f(N - 1), with constants
+  if constexpr (N > 1) each<N - 1>(f);
+  f(std::integral_constant<int, N - 1>{});
+}
 
-template <typename T, int D>
+template <int D, int NB>
 struct Walk {
-  static constexpr bool FINE = sizeof(T) == 4;     // fp32: centred codes, two terms
-  static constexpr int KS = D / 32, MT = D / 16, NT = FINE ? 2 : 1;
-  const Kernel& kr;
   const CacheAttnArgs& a;
   const Tile& t;
-  int l16, kg, kvh;
+  int kvh;
+  uint32_t at_k, at_v, at_w;   // a lane's place in a 16-block of codes of K, of V, and of words
 
-  __device__ __forceinline__ void load(Loaded<D>& x, const int32_t* pages, int tok0) const {
-    const int shift = a.cache.shift, P = 1 << shift;
+  __device__ __forceinline__ Walk(const CacheAttnArgs& a_, const Tile& t_, int kvh_, int l16, int kg) : a(a_), t(t_), kvh(kvh_) {
+    at_k = l16 * (D / 2) + kg * (D / 8);
+    at_v = kg * (2 * D) + l16 * (D / 32);
+    at_w = ((NB == 1 ? (l16 >> 2) * 16 : 0) + kg * 4 + (l16 & 3)) * 4;
+  }
+  // page entries of the tokens from tok on; -1 from `end` on
+  __device__ __forceinline__ void pages_of(int32_t* pages, int tok, int end) const {
+    // (scalar loads: among the vector loads, the wait for an entry would be one for all codes in flight)
+    const ConstInt* row = (const ConstInt*)(uintptr_t)(a.table + (int64_t)t.b * a.width);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int at = __builtin_amdgcn_readfirstlane(tok + 16 * j);
+      pages[j] = at < end ? row[at >> a.cache.shift] : -1;
+    }
+  }
+  __device__ __forceinline__ void find(Places<NB>& x, const int32_t* pages, int tok) const {
+    const uint32_t P = 1u << a.cache.shift;
+    const uint64_t block = (uint64_t)P * (D + 8), stride = block * (uint32_t)a.cache.Hkv;
+    const uint8_t* head = a.cache.base + block * (uint32_t)kvh;
     x.there = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int tok = tok0 + 16 * j;
-      int page = __builtin_amdgcn_readfirstlane(pages[j]);
-      const bool there = page >= 0 && page < a.cache.n_pages;
+    for (int j = 0; j < NB; ++j) {
+      const uint32_t page = (uint32_t)__builtin_amdgcn_readfirstlane(pages[j]);
+      const bool there = page < (uint32_t)a.cache.n_pages;
       x.there |= there ? 1u << j : 0u;
-      page = there ? page : 0;
-      const uint8_t* blk = a.cache.base + ((int64_t)page * a.cache.Hkv + kvh) * ((int64_t)P * (D + 8));
-      const int off = tok & (P - 1);
-      const uint8_t* kp = blk + off * (D / 2) + l16 * (D / 2) + kg * (KS * 4);
-      if constexpr (KS == 4) {
-        const u4 w = *reinterpret_cast<const u4*>(kp);
+      x.blk[j] = head + stride * (there ? page : 0u);
+      x.off[j] = (uint32_t)(tok + 16 * j) & (P - 1);
+    }
+  }
+  __device__ __forceinline__ void load(Tokens<D>& x, const Places<NB>& p) const {
+    const uint32_t P = 1u << a.cache.shift;
+    constexpr int INNER = NB == 1 ? 16 : 0;
+    x.there = p.there;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int n = NB == 1 ? 0 : j;
+      const uint8_t* kp = p.blk[n] + p.off[n] * (D / 2) + j * INNER * (D / 2);
+      if constexpr (D == 128) {
+        const u4 w = *reinterpret_cast<const u4*>(kp + at_k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x.k[j][i] = w[i];
       } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(kp);
+        const uint2 w = *reinterpret_cast<const uint2*>(kp + at_k);
         x.k[j][0] = w.x; x.k[j][1] = w.y;
       }
-      const uint8_t* vp = blk + P * (D / 2) + off * (D / 2) + kg * (2 * D) + l16 * (D / 32);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (D == 128) x.v[j][i] = *reinterpret_cast<const uint32_t*>(vp + i * (D / 2));
-        else x.v[j][i] = *reinterpret_cast<const uint16_t*>(vp + i * (D / 2));
-      }
-      const uint8_t* wp = blk + P * D + off * 4 + kg * 16;
-      x.kw[j] = *reinterpret_cast<const u4*>(wp);
-      x.vw[j] = *reinterpret_cast<const u4*>(wp + 4 * P);
     }
-  }
-
-  // pages of the four 16-blocks from tok0 on; -1 beyond `end`
-  __device__ __forceinline__ void pages_of(int32_t* pages, int tok0, int end) const {
+    const uint8_t* wp;
+    if constexpr (NB == 1) {
+      wp = p.blk[0] + P * D + p.off[0] * 4;
+    } else {
+      const uint8_t* q[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[j] = p.blk[j] + P * D + p.off[j] * 4;
+      const int j = (threadIdx.x & 15) >> 2;
+      wp = j < 2 ? (j == 0 ? q[0] : q[1]) : (j == 2 ? q[2] : q[3]);
+    }
+    x.kw = *reinterpret_cast<const uint32_t*>(wp + at_w);
+    x.vw = *reinterpret_cast<const uint32_t*>(wp + 4 * P + at_w);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int tok = __builtin_amdgcn_readfirstlane(tok0 + 16 * j);
-      pages[j] = tok < end ? a.table[(int64_t)t.b * a.width + (tok >> a.cache.shift)] : -1;
+      const int n = NB == 1 ? 0 : j;
+      const uint8_t* vp = p.blk[n] + P * (D / 2) + p.off[n] * (D / 2) + j * INNER * (D / 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (D == 128) x.v[j][i] = *reinterpret_cast<const uint32_t*>(vp + i * (D / 2) + at_v);
+        else x.v[j][i] = *reinterpret_cast<const uint16_t*>(vp + i * (D / 2) + at_v);
+      }
     }
   }
 };
 
-template <typename T, int D>
+template <typename T, int D, int NB>
 __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel kr) {
-  using W = Walk<T, D>;
-  constexpr int KS = W::KS, MT = W::MT, NT = W::NT;
-  constexpr bool FINE = W::FINE;
+  constexpr bool FINE = sizeof(T) == 4;                // fp32: centred codes, two terms
+  constexpr int KS = D / 32, MT = D / 16, NT = FINE ? 2 : 1;
   __shared__ float s_o[WAVES][ROWS][D + 4];
   __shared__ float s_ref[WAVES][ROWS], s_sum[WAVES][ROWS];
   const CacheAttnArgs& a = kr.a;
@@ -195,8 +246,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   const int split = blockIdx.z;
   if (t.n_rows == 0 || split >= t.n_split) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const W w{kr, a, t, lane & 15, lane >> 4, (int)blockIdx.y};
-  const int l16 = w.l16, kg = w.kg;
+  const int l16 = lane & 15, kg = lane >> 4;
+  const Walk<D, NB> w(a, t, blockIdx.y, l16, kg);
+  const Bits bits;
 
   // q: row l16, the values that meet the words kg * KS .. of a token
   const int row = t.row0 + l16;
@@ -205,10 +257,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   const int seen = real ? t.first_seen + token : 0;      // cached tokens this row sees
   const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)(w.kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
   float qv[KS * 8], qmax = 0, qsum = 0;
+  if (kr.wide) {
 #pragma unroll
-  for (int i = 0; i < KS * 8; i += 8) {
-    if (kr.wide) load8<T, true>(qp + i, qv + i);
-    else load8<T, false>(qp + i, qv + i);
+    for (int i = 0; i < KS * 8; i += 8) load8<T, true>(qp + i, qv + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < KS * 8; i += 8) load8<T, false>(qp + i, qv + i);
   }
 #pragma unroll
   for (int i = 0; i < KS * 8; ++i) {
@@ -225,9 +279,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
     u4 hi, lo;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {                // nibbles n and n + 4 are a register of the operand
-      float x = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n], qe), y = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n + 4], qe);
+      const float x = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n], qe), y = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n + 4], qe);
       qsum += x + y;
-      if (!FINE && (n & 1)) { x *= 0.0625f; y *= 0.0625f; }
       hi[n] = half_pair(x, y);
       lo[n] = half_rest(x, y, hi[n]);
     }
@@ -235,113 +288,130 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
     if constexpr (FINE) q[1][s] = __builtin_bit_cast(h8, lo);
   }
   qsum = sum_over_kg(qsum);
-  // scores in units of q * 2^qe (and of 2^-24 for denormal codes); rs turns them into log2 of a weight
-  const float unit = FINE ? 1.f : 0x1p-24f;
-  qsum *= unit;
-  const float rs = a.scale == 0.f ? 1.f : ldexpf(fabsf(a.scale) * 1.44269504f, -qe) * (1.f / unit);
+  // scores in units of q * 2^qe; rs turns them into log2 of a weight
+  const float rs = a.scale == 0.f ? 1.f : ldexpf(fabsf(a.scale) * 1.44269504f, -qe);
+  const float acc0 = FINE ? 0.f : -64.f * qsum;
 
   f4 o[MT], ones = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < MT; ++i) o[i] = (f4){0.f, 0.f, 0.f, 0.f};
-  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f;
-  float sigma = 0x1p-100f, psc = P_SCALE * 0x1p100f;   // P' = P * s' * psc, psc = P_SCALE / sigma, s' < 2 sigma
+  // weights are exp2(rs * T + nref), nref = -rs * ref + log2(P_SCALE / sigma) with sigma a power of two, all scales of V under 2 sigma
+  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = 0x1p-100f;
 
   const int end = (int)min((int64_t)t.end, (int64_t)(split + 1) * t.chunk);
-  int tok = split * t.chunk + wave * STEP;
   const int full = max(0, t.first_seen + t.row0 / kr.G);   // tokens that every row sees
-  Loaded<D> x;
-  int32_t pages[4];
+  int tok = split * t.chunk + wave * STEP, steps = 0;
+  int32_t pages[NB];
+  Tokens<D> even, odd;
+  auto fetch = [&](Tokens<D>& x, int from) {
+    Places<NB> at;
+    w.find(at, pages, from);
+    w.load(x, at);
+  };
   w.pages_of(pages, tok, end);
-  if (tok < end) w.load(x, pages, tok);
+  if (tok < end) fetch(even, tok);
   w.pages_of(pages, tok + CHUNK_UNIT, end);
-  for (; tok < end; tok += CHUNK_UNIT) {
-    const Loaded<D> c = x;
-    if (tok + CHUNK_UNIT < end) {
-      w.load(x, pages, tok + CHUNK_UNIT);
-      w.pages_of(pages, tok + 2 * CHUNK_UNIT, end);
-    }
+  // one step on `c`, while the next one's loads fly to `n`
+  auto step = [&](const Tokens<D>& c, Tokens<D>& n) {
+    // (behind the end they read page 0, which the caches hold: behind a branch, the wait for this step's would wait for all)
+    fetch(n, tok + CHUNK_UNIT);
+    w.pages_of(pages, tok + 2 * CHUNK_UNIT, end);
     // scores
     float s[4][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      f4 acc = {0.f, 0.f, 0.f, 0.f};
+    const float ks = word_scale(c.kw), km = FINE ? fmaf(8.f, ks, word_offset(c.kw)) : word_offset(c.kw);
+    each<4>([&](auto J) {
+      constexpr int j = J;
+      f4 acc = {acc0, acc0, acc0, acc0};
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
         uint32_t e[4];
-        expand<FINE>(c.k[j][i], e);
+        expand<FINE>(c.k[j][i], bits, e);
         const h8 op = __builtin_bit_cast(h8, (u4){e[0], e[1], e[2], e[3]});
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[n][i], acc, 0, 0, 0);
+        for (int m = 0; m < NT; ++m) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[m][i], acc, 0, 0, 0);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float sc = word_scale(c.kw[j][i]);
-        const float m = FINE ? fmaf(8.f, sc, word_offset(c.kw[j][i])) : word_offset(c.kw[j][i]);
-        s[j][i] = fmaf(sc, acc[i], m * qsum);
-      }
-    }
-    float vs[4][4], vm[4][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        vs[j][i] = word_scale(c.vw[j][i]);
-        vm[j][i] = fmaf(8.f, vs[j][i], word_offset(c.vw[j][i]));
-      }
-    if (tok + STEP > full || tok + STEP > end || c.there != 15u) {      // some row does not see some token
+      each<4>([&](auto I) {
+        constexpr int i = I;
+        s[j][i] = fmaf(from_lane<4 * j + i>(ks), acc[i], from_lane<4 * j + i>(km) * qsum);
+      });
+    });
+    float vs = word_scale(c.vw), vm = fmaf(8.f, vs, word_offset(c.vw));
+    uint32_t vis = 0xffffu;                                             // tokens that this row sees, bit 4 j + i
+    const bool some = tok + STEP > full || tok + STEP > end || c.there != (1u << NB) - 1;      // some row does not see some token
+    if (some) {
+      const int lim = min(seen, end) - tok - 4 * kg;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const bool vis = tok + 16 * j + 4 * kg + i < min(seen, end) && ((c.there >> j) & 1u);
-          s[j][i] = vis ? s[j][i] : -INFINITY;
-          vs[j][i] = vis ? vs[j][i] : 0.f;
-          vm[j][i] = vis ? vm[j][i] : 0.f;
+          const bool yes = 16 * j + i < lim && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
+          s[j][i] = yes ? s[j][i] : -INFINITY;
+          vis &= yes ? ~0u : ~(1u << (4 * j + i));
         }
+      // words that nobody sees may hold anything
+      const bool live = tok + 16 * (l16 >> 2) + 4 * kg + (l16 & 3) < end && ((c.there >> (NB == 1 ? 0 : l16 >> 2)) & 1u);
+      vs = live ? vs : 0.f;
+      vm = live ? vm : 0.f;
     }
-    float smax = s[0][0], vmax = fabsf(vs[0][0]);
+    float smax = s[0][0];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        smax = fmaxf(smax, s[j][i]);
-        vmax = fmaxf(vmax, fabsf(vs[j][i]));
-      }
-    if (__any(smax > lift || vmax > 2.f * sigma)) {
+      for (int i = 0; i < 4; ++i) smax = fmaxf(smax, s[j][i]);
+    if (__any(smax > lift || fabsf(vs) > 2.f * sigma)) {
       const float nr = fmaxf(ref, max_over_kg(smax));
-      const float vm_all = max_over_kg(vmax);
-      const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(vm_all) & 0x7f800000u));
-      const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr));
+      float top = fabsf(vs);                                             // over all 64 tokens
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+      const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(top) & 0x7f800000u));
+      const float f = (ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr))) * (sigma / nsigma);
       sum *= f;
       osum *= f;
-      const float fo = f * (sigma / nsigma);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) o[i] *= fo;
-      ones *= fo;
+      for (int i = 0; i < MT; ++i) o[i] *= f;
+      ones *= f;
       ref = nr;
-      nref = nr == -INFINITY ? 0.f : -nr * rs;
-      lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
       sigma = nsigma;
-      psc = P_SCALE / nsigma;
+      nref = (nr == -INFINITY ? 0.f : -nr * rs) + __builtin_amdgcn_logf(P_SCALE / nsigma);
+      lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
     }
     // weights
     u4 p[NT][2];
+    auto weights = [&](auto SOME) {
+      each<4>([&](auto J) {
+        each<2>([&](auto H) {
+          constexpr int j = J, i = 2 * H;
+          float y[2];
+          each<2>([&](auto U) {
+            constexpr int u = U, lane_of = 4 * j + i + u;
+            const float e = __builtin_amdgcn_exp2f(fmaf(s[j][i + u], rs, nref));
+            sum += e;
+            if constexpr (SOME) {
+              const bool yes = (vis >> lane_of) & 1u;
+              const float m = from_lane<lane_of>(vm), g = from_lane<lane_of>(vs);
+              osum = fmaf(e, yes ? m : 0.f, osum);
+              y[u] = e * (yes ? g : 0.f);
+            } else {
+              osum = fmaf(from_lane<lane_of>(vm), e, osum);
+              y[u] = from_lane<lane_of>(vs) * e;
+            }
+          });
+          const uint32_t u = half_pair(y[0], y[1]);
+          p[0][j >> 1][(j & 1) * 2 + (i >> 1)] = u;
+          if constexpr (FINE) p[1][j >> 1][(j & 1) * 2 + (i >> 1)] = half_rest(y[0], y[1], u);
+        });
+      });
+    };
+    if (some) weights(std::true_type{});
+    else weights(std::false_type{});
+    if constexpr (!FINE) {
+      // the 72s of the sums so far come out now and then: over thousands of tokens of equal weight they would cost fp32 its last digits
+      if ((++steps & 3) == 0) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        float y[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(s[j][i + h], rs, nref));
-          sum += e;
-          osum = fmaf(e, vm[j][i + h], osum);
-          y[h] = e * (vs[j][i + h] * psc);
-        }
-        const uint32_t u = half_pair(y[0], y[1]);
-        p[0][j >> 1][(j & 1) * 2 + (i >> 1)] = u;
-        if constexpr (FINE) p[1][j >> 1][(j & 1) * 2 + (i >> 1)] = half_rest(y[0], y[1], u);
+        for (int i = 0; i < MT; ++i) o[i] = o[i] - 72.f * ones;
+        ones = (f4){0.f, 0.f, 0.f, 0.f};
       }
+    }
     // outputs
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -350,16 +420,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
 #pragma unroll
       for (int u = 0; u < 4; ++u) {    // tokens (0,1) (2,3) of block 2g, then of 2g + 1
         const uint32_t x0 = c.v[2 * g + (u >> 1)][2 * (u & 1)], x1 = c.v[2 * g + (u >> 1)][2 * (u & 1) + 1];
-        expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x05040100u), e[0][u]);
-        if constexpr (NH == 2) expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x07060302u), e[1][u]);
+        expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x05040100u), bits, e[0][u]);
+        if constexpr (NH == 2) expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x07060302u), bits, e[1][u]);
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
+      for (int m = 0; m < NT; ++m) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           const int hf = i >> 2, nb = i & 3;
           const h8 op = __builtin_bit_cast(h8, (u4){e[hf][0][nb], e[hf][1][nb], e[hf][2][nb], e[hf][3][nb]});
-          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, __builtin_bit_cast(h8, p[n][g]), o[i], 0, 0, 0);
+          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, __builtin_bit_cast(h8, p[m][g]), o[i], 0, 0, 0);
         }
       }
       if constexpr (!FINE) {
@@ -367,20 +437,25 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
         ones = __builtin_amdgcn_mfma_f32_16x16x32_f16(one, __builtin_bit_cast(h8, p[0][g]), ones, 0, 0, 0);
       }
     }
+    tok += CHUNK_UNIT;
+  };
+  while (tok < end) {
+    step(even, odd);
+    if (tok >= end) break;
+    step(odd, even);
   }
 
   // a wave's outputs as they are, O[d][row] at d = MT * (4 kg + j) + i, over the reference weight
   sum = sum_over_kg(sum);
   osum = sum_over_kg(osum);
-  const float back = sigma * (1.f / P_SCALE);
-  const float lref = ref == -INFINITY ? -INFINITY : ref * rs;
+  const float lref = ref == -INFINITY ? -INFINITY : -nref;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      float v = o[i][j];
-      if constexpr (!FINE) v = fmaf(v, (i & 1) ? 0x1p20f : 0x1p24f, -8.f * ones[j]);
-      s_o[wave][l16][MT * (4 * kg + j) + i] = fmaf(v, back, osum);
+      float y = o[i][j] + osum;
+      if constexpr (!FINE) y = fmaf(-72.f, ones[j], y);
+      s_o[wave][l16][MT * (4 * kg + j) + i] = y;
     }
   if (kg == 0) { s_ref[wave][l16] = lref; s_sum[wave][l16] = sum; }
   __syncthreads();
@@ -393,8 +468,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   float y[MT] = {}, all = 0.f;
 #pragma unroll
   for (int i = 0; i < WAVES; ++i) {
-    const float f = s_ref[i][r] == -INFINITY && s_sum[i][r] == 0.f ? 0.f : __builtin_amdgcn_exp2f(s_ref[i][r] - top);
-    if (f == 0.f) continue;       // (a wave that saw nothing holds no weight)
+    const float f = part_weight(s_ref[i][r], s_sum[i][r], top);
     all = fmaf(f, s_sum[i][r], all);
 #pragma unroll
     for (int d = 0; d < MT; ++d) y[d] = fmaf(f, s_o[i][r][d0 + d], y[d]);
@@ -428,8 +502,7 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const Kernel kr) {
   for (int s = 0; s < t.n_split; ++s) {
     const int64_t i = at + s;
     const float lref = kr.part_ml[i * 2], sum = kr.part_ml[i * 2 + 1];
-    if (lref == -INFINITY && sum == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(lref - top);
+    const float f = part_weight(lref, sum, top);
     all = fmaf(f, sum, all);
 #pragma unroll
     for (int d = 0; d < MT; ++d) y[d] = fmaf(f, kr.part_o[i * D + d0 + d], y[d]);
@@ -444,7 +517,9 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const Kernel kr) {
 
 template <typename T, int D>
 int run(Kernel& k, int tiles, hipStream_t st) {
-  PIPE_KLAUNCH((cache_attn_kernel<T, D>), dim3(tiles, k.a.cache.Hkv, k.n_split), dim3(WAVES * 64), 0, st, k);
+  const dim3 grid(tiles, k.a.cache.Hkv, k.n_split);
+  if (k.a.cache.shift >= 6) PIPE_KLAUNCH((cache_attn_kernel<T, D, 1>), grid, dim3(WAVES * 64), 0, st, k);
+  else PIPE_KLAUNCH((cache_attn_kernel<T, D, 4>), grid, dim3(WAVES * 64), 0, st, k);
   PIPE_HIP(hipGetLastError());
   if (k.n_split > 1) {
     PIPE_KLAUNCH((cache_attn_join_kernel<T, D>), dim3(tiles, k.a.cache.Hkv), dim3(256), 0, st, k);
@@ -465,7 +540,7 @@ int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   if (tiles > 0x3fffff) return PIPE_ESHAPE;
   const int64_t longest = std::min<int64_t>(a.max_length > 0 ? a.max_length : (int64_t)a.width << a.cache.shift, 1 << 30);
   // Splits: as many as bring the launch to SPLIT_TILES workgroups, each with 256 tokens at least.
-  const int64_t base = (rows + ROWS - 1) / ROWS * a.cache.Hkv;
+  const int64_t base = std::max<int64_t>((rows + ROWS - 1) / ROWS, std::min(a.B, a.T)) * a.cache.Hkv;
   k.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(SPLIT_TILES / base, (longest + CHUNK_UNIT - 1) / CHUNK_UNIT));
   k.chunk = (int)round_up64((longest + k.n_split - 1) / k.n_split, CHUNK_UNIT);
   if (k.n_split > 1) {
