@@ -1,13 +1,13 @@
 // Attention of fresh tokens over the 4-bit cache.
 //
 // For one key/value head of one request, the rows are its fresh tokens' query heads (row = token * G + head in the group), 16 of
-// them a workgroup's tile; a wave walks 64 cached tokens at a time:
+// them a workgroup's tile; a wave walks 32 cached tokens at a time:
 //   T[t][r] = s_t * (sum_d c_td q_rd) + m_t * (sum_d q_rd)          one MFMA tile per 16 tokens, codes as the A operand
 //   P[t][r] = exp2(rs_r * (T - ref_r))                               ref_r: a row's running reference
 //   O[d][r] += sum_t c'_td * (P * s'_t)                              codes of V as the A operand, P as the B operand
 //   M[r]   += sum_t P * m'_t,  L[r] += sum_t P
 // with T's accumulator layout (lane = row, 4 tokens in a lane's registers) being exactly the B operand's of the second product, once
-// the tokens of a step of 32 are taken in the order 4*kg..+3 of one 16-block, then of the next: no shuffle between the products.
+// the tokens of a step are taken in the order 4*kg..+3 of one 16-block, then of the next: no shuffle between the products.
 //
 // Codes become fp16 without conversions: four bits at bit 4 of a half under the exponent of 64 are 64 + c; 7 instructions make
 // 8 operand values.  The 64 is taken out of the sums again: from the scores by the accumulator's start, -64 sum q, from the
@@ -29,11 +29,15 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
+#define GLOBAL __attribute__((address_space(1)))
+typedef const GLOBAL uint8_t* GlobalBytes;
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(4))) int32_t ConstInt;   // memory that the kernel does not write
 
-constexpr int WAVES = 4, ROWS = 16, STEP = 64;      // tokens of a wave's step
+constexpr int WAVES = 4, ROWS = 16, STEP = 32;      // tokens of a wave's step
+constexpr int AHEAD = 2;                            // steps whose loads are in flight while one is worked on
 constexpr int CHUNK_UNIT = WAVES * STEP;            // a split's tokens are a multiple of this: every wave gets whole steps
-constexpr int SPLIT_TILES = 1024;
+constexpr int SPLIT_TILES = 768;
 constexpr float REF_SLACK = 6.f;                    // log2: a row's reference rises only when a score exceeds it by this
 constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE fits fp16
 
@@ -131,19 +135,19 @@ __device__ __forceinline__ float sum_over_kg(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// A wave's 64 tokens.  NB page lookups serve them: 1 where a page holds 64 tokens or more, else one for every 16-block.
+// A step's tokens.  NB page lookups serve them: 1 where a page holds 32 tokens or more, else one for every 16-block.
 template <int NB>
 struct Places {
   const uint8_t* blk[NB];   // the head's block of the page (any page where there is none)
   uint32_t off[NB];         // first token in it
   uint32_t there;           // lookups whose page exists
 };
-// The codes and words of the 64 tokens, as a lane (l16, kg) holds them.
+// The codes and words of a step's tokens, as a lane (l16, kg) holds them.
 template <int D>
 struct Tokens {
-  uint32_t k[4][D / 32];    // [16-block]: of token l16 the D/32 words from kg * D/32 on
-  uint32_t v[4][4];         // [16-block]: of token 4 kg + i the D/16 codes from l16 * D/16 on
-  uint32_t kw, vw;          // the words of token 4 kg + l16 % 4 of 16-block l16 / 4
+  uint32_t k[2][D / 32];    // [16-block]: of token l16 the D/32 words from kg * D/32 on
+  uint32_t v[2][4];         // [16-block]: of token 4 kg + i the D/16 codes from l16 * D/16 on
+  uint32_t w;               // the word of token 4 kg + l16 % 4 of 16-block l16 / 4 % 2: of K in lanes l16 < 8, of V in the others
   uint32_t there;           // lookups whose page exists
 };
 // what lane 4 j + i of a row of 16 lanes holds: the word of this lane's i-th token of 16-block j (folded into the operation that uses it)
@@ -167,7 +171,7 @@ struct Walk {
   __device__ __forceinline__ Walk(const CacheAttnArgs& a_, const Tile& t_, int kvh_, int l16, int kg) : a(a_), t(t_), kvh(kvh_) {
     at_k = l16 * (D / 2) + kg * (D / 8);
     at_v = kg * (2 * D) + l16 * (D / 32);
-    at_w = ((NB == 1 ? (l16 >> 2) * 16 : 0) + kg * 4 + (l16 & 3)) * 4;
+    at_w = ((NB == 1 ? (l16 >> 2 & 1) * 16 : 0) + kg * 4 + (l16 & 3)) * 4 + (l16 >> 3) * (4u << a_.cache.shift);
   }
   // page entries of the tokens from tok on; -1 from `end` on
   __device__ __forceinline__ void pages_of(int32_t* pages, int tok, int end) const {
@@ -193,43 +197,45 @@ struct Walk {
       x.off[j] = (uint32_t)(tok + 16 * j) & (P - 1);
     }
   }
+  // kept whole in scalar registers: a load then needs one register of offset, not two of address that it has to add up first
+  __device__ __forceinline__ static GlobalBytes base(const uint8_t* p) {
+    GlobalBytes g = (GlobalBytes)(uintptr_t)p;
+    asm("" : "+s"(g));
+    return g;
+  }
   __device__ __forceinline__ void load(Tokens<D>& x, const Places<NB>& p) const {
     const uint32_t P = 1u << a.cache.shift;
+    uint32_t at_k = this->at_k, at_v = this->at_v, at_w = this->at_w;
+    asm("" : "+v"(at_k), "+v"(at_v), "+v"(at_w));   // (32 bits here, not widened ahead of the loop)
     constexpr int INNER = NB == 1 ? 16 : 0;
     x.there = p.there;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 2; ++j) {
       const int n = NB == 1 ? 0 : j;
-      const uint8_t* kp = p.blk[n] + p.off[n] * (D / 2) + j * INNER * (D / 2);
+      const GlobalBytes kp = base(p.blk[n] + p.off[n] * (D / 2)) + j * INNER * (D / 2);
       if constexpr (D == 128) {
-        const u4 w = *reinterpret_cast<const u4*>(kp + at_k);
+        const u4 w = *(const GLOBAL u4*)(kp + at_k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x.k[j][i] = w[i];
       } else {
-        const uint2 w = *reinterpret_cast<const uint2*>(kp + at_k);
+        const u2 w = *(const GLOBAL u2*)(kp + at_k);
         x.k[j][0] = w.x; x.k[j][1] = w.y;
       }
     }
-    const uint8_t* wp;
-    if constexpr (NB == 1) {
-      wp = p.blk[0] + P * D + p.off[0] * 4;
-    } else {
-      const uint8_t* q[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) q[j] = p.blk[j] + P * D + p.off[j] * 4;
-      const int j = (threadIdx.x & 15) >> 2;
-      wp = j < 2 ? (j == 0 ? q[0] : q[1]) : (j == 2 ? q[2] : q[3]);
+    GlobalBytes wp = base(p.blk[0] + P * D + p.off[0] * 4);
+    if constexpr (NB == 2) {
+      const GlobalBytes wq = base(p.blk[1] + P * D + p.off[1] * 4);
+      wp = (threadIdx.x & 4) ? wq : wp;
     }
-    x.kw = *reinterpret_cast<const uint32_t*>(wp + at_w);
-    x.vw = *reinterpret_cast<const uint32_t*>(wp + 4 * P + at_w);
+    x.w = *(const GLOBAL uint32_t*)(wp + at_w);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 2; ++j) {
       const int n = NB == 1 ? 0 : j;
-      const uint8_t* vp = p.blk[n] + P * (D / 2) + p.off[n] * (D / 2) + j * INNER * (D / 2);
+      const GlobalBytes vp = base(p.blk[n] + P * (D / 2) + p.off[n] * (D / 2)) + j * INNER * (D / 2);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (D == 128) x.v[j][i] = *reinterpret_cast<const uint32_t*>(vp + i * (D / 2) + at_v);
-        else x.v[j][i] = *reinterpret_cast<const uint16_t*>(vp + i * (D / 2) + at_v);
+        if constexpr (D == 128) x.v[j][i] = *(const GLOBAL uint32_t*)(vp + i * (D / 2) + at_v);
+        else x.v[j][i] = *(const GLOBAL uint16_t*)(vp + i * (D / 2) + at_v);
       }
     }
   }
@@ -302,24 +308,29 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   const int full = max(0, t.first_seen + t.row0 / kr.G);   // tokens that every row sees
   int tok = split * t.chunk + wave * STEP, steps = 0;
   int32_t pages[NB];
-  Tokens<D> even, odd;
+  Tokens<D> r0, r1, r2;      // AHEAD + 1 of them, in turn
   auto fetch = [&](Tokens<D>& x, int from) {
     Places<NB> at;
     w.find(at, pages, from);
     w.load(x, at);
   };
   w.pages_of(pages, tok, end);
-  if (tok < end) fetch(even, tok);
-  w.pages_of(pages, tok + CHUNK_UNIT, end);
-  // one step on `c`, while the next one's loads fly to `n`
+  if (tok < end) {
+    fetch(r0, tok);
+    w.pages_of(pages, tok + CHUNK_UNIT, end);
+    fetch(r1, tok + CHUNK_UNIT);
+    w.pages_of(pages, tok + AHEAD * CHUNK_UNIT, end);
+  }
+  // one step on `c`, while the next ones' loads fly, AHEAD steps on to `n`
   auto step = [&](const Tokens<D>& c, Tokens<D>& n) {
     // (behind the end they read page 0, which the caches hold: behind a branch, the wait for this step's would wait for all)
-    fetch(n, tok + CHUNK_UNIT);
-    w.pages_of(pages, tok + 2 * CHUNK_UNIT, end);
+    fetch(n, tok + AHEAD * CHUNK_UNIT);
+    w.pages_of(pages, tok + (AHEAD + 1) * CHUNK_UNIT, end);
     // scores
-    float s[4][4];
-    const float ks = word_scale(c.kw), km = FINE ? fmaf(8.f, ks, word_offset(c.kw)) : word_offset(c.kw);
-    each<4>([&](auto J) {
+    float s[2][4];
+    float ws = word_scale(c.w), wo = word_offset(c.w), wm = fmaf(8.f, ws, wo);      // scale, offset, and the offset of c - 8
+    const float ko = FINE ? wm : wo;
+    each<2>([&](auto J) {
       constexpr int j = J;
       f4 acc = {acc0, acc0, acc0, acc0};
 #pragma unroll
@@ -332,16 +343,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
       }
       each<4>([&](auto I) {
         constexpr int i = I;
-        s[j][i] = fmaf(from_lane<4 * j + i>(ks), acc[i], from_lane<4 * j + i>(km) * qsum);
+        s[j][i] = fmaf(from_lane<4 * j + i>(ws), acc[i], from_lane<4 * j + i>(ko) * qsum);
       });
     });
-    float vs = word_scale(c.vw), vm = fmaf(8.f, vs, word_offset(c.vw));
-    uint32_t vis = 0xffffu;                                             // tokens that this row sees, bit 4 j + i
+    uint32_t vis = 0xffu;                                             // tokens that this row sees, bit 4 j + i
     const bool some = tok + STEP > full || tok + STEP > end || c.there != (1u << NB) - 1;      // some row does not see some token
     if (some) {
       const int lim = min(seen, end) - tok - 4 * kg;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const bool yes = 16 * j + i < lim && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
@@ -349,18 +359,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
           vis &= yes ? ~0u : ~(1u << (4 * j + i));
         }
       // words that nobody sees may hold anything
-      const bool live = tok + 16 * (l16 >> 2) + 4 * kg + (l16 & 3) < end && ((c.there >> (NB == 1 ? 0 : l16 >> 2)) & 1u);
-      vs = live ? vs : 0.f;
-      vm = live ? vm : 0.f;
+      const int j = l16 >> 2 & 1;
+      const bool live = tok + 16 * j + 4 * kg + (l16 & 3) < end && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
+      ws = live ? ws : 0.f;
+      wm = live ? wm : 0.f;
     }
     float smax = s[0][0];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) smax = fmaxf(smax, s[j][i]);
-    if (__any(smax > lift || fabsf(vs) > 2.f * sigma)) {
+    const float vs = l16 < 8 ? 0.f : fabsf(ws);
+    if (__any(smax > lift || vs > 2.f * sigma)) {
       const float nr = fmaxf(ref, max_over_kg(smax));
-      float top = fabsf(vs);                                             // over all 64 tokens
+      float top = vs;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
       const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(top) & 0x7f800000u));
@@ -376,29 +388,29 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
       lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
     }
     // weights
-    u4 p[NT][2];
+    u4 p[NT];
     auto weights = [&](auto SOME) {
-      each<4>([&](auto J) {
+      each<2>([&](auto J) {
         each<2>([&](auto H) {
           constexpr int j = J, i = 2 * H;
           float y[2];
           each<2>([&](auto U) {
-            constexpr int u = U, lane_of = 4 * j + i + u;
+            constexpr int u = U, bit = 4 * j + i + u, lane_of = 8 + bit;
             const float e = __builtin_amdgcn_exp2f(fmaf(s[j][i + u], rs, nref));
             sum += e;
             if constexpr (SOME) {
-              const bool yes = (vis >> lane_of) & 1u;
-              const float m = from_lane<lane_of>(vm), g = from_lane<lane_of>(vs);
+              const bool yes = (vis >> bit) & 1u;
+              const float m = from_lane<lane_of>(wm), g = from_lane<lane_of>(ws);
               osum = fmaf(e, yes ? m : 0.f, osum);
               y[u] = e * (yes ? g : 0.f);
             } else {
-              osum = fmaf(from_lane<lane_of>(vm), e, osum);
-              y[u] = from_lane<lane_of>(vs) * e;
+              osum = fmaf(from_lane<lane_of>(wm), e, osum);
+              y[u] = from_lane<lane_of>(ws) * e;
             }
           });
           const uint32_t u = half_pair(y[0], y[1]);
-          p[0][j >> 1][(j & 1) * 2 + (i >> 1)] = u;
-          if constexpr (FINE) p[1][j >> 1][(j & 1) * 2 + (i >> 1)] = half_rest(y[0], y[1], u);
+          p[0][j * 2 + (i >> 1)] = u;
+          if constexpr (FINE) p[1][j * 2 + (i >> 1)] = half_rest(y[0], y[1], u);
         });
       });
     };
@@ -406,43 +418,42 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
     else weights(std::false_type{});
     if constexpr (!FINE) {
       // the 72s of the sums so far come out now and then: over thousands of tokens of equal weight they would cost fp32 its last digits
-      if ((++steps & 3) == 0) {
+      if ((++steps & 7) == 0) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) o[i] = o[i] - 72.f * ones;
         ones = (f4){0.f, 0.f, 0.f, 0.f};
       }
     }
     // outputs
+    constexpr int NH = D / 64;       // halves of a V word: 4 codes each
+    uint32_t e[NH][4][4];            // [half][pair of tokens][nibble]
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      constexpr int NH = D / 64;       // halves of a V word: 4 codes each
-      uint32_t e[NH][4][4];            // [half][pair of tokens][nibble]
+    for (int u = 0; u < 4; ++u) {    // tokens (0,1) (2,3) of one block, then of the other
+      const uint32_t x0 = c.v[u >> 1][2 * (u & 1)], x1 = c.v[u >> 1][2 * (u & 1) + 1];
+      expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x05040100u), bits, e[0][u]);
+      if constexpr (NH == 2) expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x07060302u), bits, e[1][u]);
+    }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {    // tokens (0,1) (2,3) of block 2g, then of 2g + 1
-        const uint32_t x0 = c.v[2 * g + (u >> 1)][2 * (u & 1)], x1 = c.v[2 * g + (u >> 1)][2 * (u & 1) + 1];
-        expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x05040100u), bits, e[0][u]);
-        if constexpr (NH == 2) expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x07060302u), bits, e[1][u]);
+    for (int m = 0; m < NT; ++m) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int hf = i >> 2, nb = i & 3;
+        const h8 op = __builtin_bit_cast(h8, (u4){e[hf][0][nb], e[hf][1][nb], e[hf][2][nb], e[hf][3][nb]});
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, __builtin_bit_cast(h8, p[m]), o[i], 0, 0, 0);
       }
-#pragma unroll
-      for (int m = 0; m < NT; ++m) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const int hf = i >> 2, nb = i & 3;
-          const h8 op = __builtin_bit_cast(h8, (u4){e[hf][0][nb], e[hf][1][nb], e[hf][2][nb], e[hf][3][nb]});
-          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, __builtin_bit_cast(h8, p[m][g]), o[i], 0, 0, 0);
-        }
-      }
-      if constexpr (!FINE) {
-        const h8 one = {1, 1, 1, 1, 1, 1, 1, 1};
-        ones = __builtin_amdgcn_mfma_f32_16x16x32_f16(one, __builtin_bit_cast(h8, p[0][g]), ones, 0, 0, 0);
-      }
+    }
+    if constexpr (!FINE) {
+      const h8 one = {1, 1, 1, 1, 1, 1, 1, 1};
+      ones = __builtin_amdgcn_mfma_f32_16x16x32_f16(one, __builtin_bit_cast(h8, p[0]), ones, 0, 0, 0);
     }
     tok += CHUNK_UNIT;
   };
   while (tok < end) {
-    step(even, odd);
+    step(r0, r2);
     if (tok >= end) break;
-    step(odd, even);
+    step(r1, r0);
+    if (tok >= end) break;
+    step(r2, r1);
   }
 
   // a wave's outputs as they are, O[d][row] at d = MT * (4 kg + j) + i, over the reference weight
@@ -518,8 +529,8 @@ __global__ __launch_bounds__(256) void cache_attn_join_kernel(const Kernel kr) {
 template <typename T, int D>
 int run(Kernel& k, int tiles, hipStream_t st) {
   const dim3 grid(tiles, k.a.cache.Hkv, k.n_split);
-  if (k.a.cache.shift >= 6) PIPE_KLAUNCH((cache_attn_kernel<T, D, 1>), grid, dim3(WAVES * 64), 0, st, k);
-  else PIPE_KLAUNCH((cache_attn_kernel<T, D, 4>), grid, dim3(WAVES * 64), 0, st, k);
+  if (k.a.cache.shift >= 5) PIPE_KLAUNCH((cache_attn_kernel<T, D, 1>), grid, dim3(WAVES * 64), 0, st, k);
+  else PIPE_KLAUNCH((cache_attn_kernel<T, D, 2>), grid, dim3(WAVES * 64), 0, st, k);
   PIPE_HIP(hipGetLastError());
   if (k.n_split > 1) {
     PIPE_KLAUNCH((cache_attn_join_kernel<T, D>), dim3(tiles, k.a.cache.Hkv), dim3(256), 0, st, k);
