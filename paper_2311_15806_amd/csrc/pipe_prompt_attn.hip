@@ -1,4 +1,6 @@
 // Attention over packed sequences.
+#include <type_traits>
+
 #include "pipe_attention.h"
 
 namespace {
@@ -53,6 +55,295 @@ __global__ __launch_bounds__(64) void prompt_attn_kernel(PromptAttnArgs a) {
     ((T*)a.out)[((int64_t)t * a.Hq + h) * D + lane + 64 * i] = from_f<T>(none ? 0.f : o[i] / sum);
 }
 
+// ------------------------------------------------------------------ 16-bit types
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+constexpr int WAVES = 4, WROWS = 32, QROWS = WAVES * WROWS, KEYS = 64;
+constexpr float REF_SLACK = 8.f;   // log2: a row's reference rises only when a score exceeds it by this
+
+__device__ __forceinline__ f16v mfma(u4 x, u4 y, f16v c, f16) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, x), __builtin_bit_cast(h8, y), c, 0, 0, 0);
+}
+__device__ __forceinline__ f16v mfma(u4 x, u4 y, f16v c, bf16) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), c, 0, 0, 0);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pack(float x, float y) {
+  struct { T a, b; } v = {(T)x, (T)y};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+struct Kernel {
+  PromptAttnArgs a;
+  int G, n_tiles;
+};
+
+struct Tile {
+  int row0, n_rows, start;    // rows row0 .. of a sequence whose queries start at `start`; row = query * G + head in the group
+  int k0, nk;                 // its keys
+  int first_seen;             // keys that its first query sees (causal; may be negative)
+};
+
+// Tile `id` of the launch: sequence b (B: the rows behind the last one, which see nothing) owns the ids from
+// floor(start_b * G / QROWS) + b on.
+__device__ __forceinline__ Tile find_tile(const Kernel& k, int id) {
+  const PromptAttnArgs& a = k.a;
+  const int lane = threadIdx.x & 63;
+  auto start_of = [&](int b) { return b > 0 ? min(max(a.q_starts[b], 0), a.Tq) : 0; };
+  int b = -1;
+  for (int i0 = 0; i0 <= a.B; i0 += 64) {
+    const int i = i0 + lane;
+    const bool le = i <= a.B && (int)(((int64_t)start_of(min(i, a.B)) * k.G) / QROWS) + i <= id;
+    const int n = __popcll(__ballot(le));
+    b += n;
+    if (n < 64) break;
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  Tile t;
+  t.start = start_of(b);
+  const int n = (b < a.B ? start_of(b + 1) : a.Tq) - t.start;
+  t.row0 = (id - ((int)(((int64_t)t.start * k.G) / QROWS) + b)) * QROWS;
+  t.n_rows = t.row0 < 0 ? 0 : min(QROWS, max(0, n * k.G - t.row0));
+  t.k0 = b < a.B ? min(max(a.k_starts[b], 0), a.Tk) : 0;
+  t.nk = b < a.B ? max(0, min(a.k_starts[b + 1], a.Tk) - t.k0) : 0;
+  t.first_seen = t.nk - n + 1;
+  return t;
+}
+
+// Where chunk c (8 values) of key row r lies in its LDS row, as a chunk: the rows that one read of 16 lanes touches (16 rows' same chunk of K;
+// 4 rows' 4 chunks of V) then lie in different banks.
+template <int D>
+__device__ __forceinline__ int swizzle(int r, int c) {
+  if constexpr (D == 128) return c ^ (((r & 3) << 2) | ((r >> 2) & 3));
+  return c ^ (((r & 2) << 1) | ((r >> 2) & 3));
+}
+
+template <typename T, int D, bool WIDE>
+__global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel kr) {
+  constexpr int CH = D / 8, KS = D / 16, DB = D / 32;    // chunks of a row, steps of the score product, blocks of the output's
+  constexpr int LOADS = KEYS * CH / 256;                 // 16-byte loads a lane makes of a tile of K (and of V)
+  // one array per slot: the compiler tells loads into one from reads of another by the array
+  __shared__ alignas(1024) u4 k_a[KEYS * CH], k_b[KEYS * CH], v_a[KEYS * CH], v_b[KEYS * CH];
+  const PromptAttnArgs& a = kr.a;
+  // (long tiles first: the last queries see most)
+  const int id = blockIdx.x, kvh = id % a.Hkv;
+  const Tile t = find_tile(kr, kr.n_tiles - 1 - id / a.Hkv);
+  if (t.n_rows == 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, h = lane >> 5;
+
+  // ---- this lane's row
+  const int lrow = wave * WROWS + n;
+  const bool real = lrow < t.n_rows;
+  const int row = t.row0 + (real ? lrow : 0);
+  const int token = row / kr.G, head = kvh * kr.G + row % kr.G;
+  const int seen = !real ? 0 : a.causal ? max(0, min(t.nk, t.first_seen + token)) : t.nk;
+  const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)head * a.qs.head + 8 * h;
+  u4 q[KS];
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = real && a.scale != 0.f ? ~0u : 0u;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    if constexpr (WIDE) {
+      q[s] = *reinterpret_cast<const u4*>(qp + 16 * s);
+    } else {
+      T v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = qp[16 * s + i];
+      __builtin_memcpy(&q[s], v, 16);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[s][i] = (q[s][i] ^ flip) & keep;
+  const float rs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
+
+  // ---- keys: how many any row of the workgroup / of the wave sees, and how many every row of the wave sees
+  auto seen_by = [&](int r) { return a.causal ? max(0, min(t.nk, t.first_seen + (t.row0 + r) / kr.G)) : t.nk; };
+  const int end = seen_by(t.n_rows - 1);
+  const int wave_rows = min(WROWS, t.n_rows - wave * WROWS);
+  const int wend = wave_rows > 0 ? seen_by(wave * WROWS + wave_rows - 1) : 0;
+  const int wfull = wave_rows > 0 ? seen_by(wave * WROWS) : 0;
+
+  // ---- loads of a tile: LDS in the order of the lanes, so that a lane picks what belongs at its place
+  auto fetch = [&](const void* src, const HeadStrides& st, u4* dst, int key0) {
+    const T* base = (const T*)src + (int64_t)(t.k0 + key0) * st.token + (int64_t)kvh * st.head;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int at = (i * WAVES + wave) * 64 + lane, r = at / CH, c = swizzle<D>(r, at % CH);
+      const int rr = min(r, t.nk - 1 - key0);              // (rows behind the last key: the last key again, which nobody sees there)
+      if constexpr (WIDE) {
+        const uint32_t off = (uint32_t)rr * (uint32_t)st.token * (uint32_t)sizeof(T) + c * 16;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((const char*)base + off),
+                                         (__attribute__((address_space(3))) void*)(dst + (i * WAVES + wave) * 64), 16, 0, 0);
+      } else {
+        T v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = base[(int64_t)rr * st.token + c * 8 + e];
+        u4 w;
+        __builtin_memcpy(&w, v, 16);
+        dst[at] = w;
+      }
+    }
+  };
+
+  f16v o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  constexpr float P_LOG = sizeof(T) == 2 && std::is_same_v<T, f16> ? 7.f : 0.f;    // fp16: weights up to 2^15, so that small ones keep their digits
+  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f;
+
+  // Places in a tile, in bytes: of K the chunk h of row n -- chunk 2 j + h of row 32 b + n is j and b further, by an exclusive or and an
+  // addition --, of V the piece that this lane brings to a transposed read: of every 16 lanes, lane i brings 4 columns from 4 (i % 4) on
+  // of row i / 4, and gets column i of the 4 rows.
+  const int vr = 4 * h + ((lane >> 2) & 3), vc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
+  int k_at = (n * CH + swizzle<D>(n, h)) * 16, v_at = (vr * CH + swizzle<D>(vr, vc)) * 16 + (lane & 1) * 8;
+  auto step = [&](const u4* ks, const u4* vs, u4* kn, u4* vn, int key0) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // this tile is there, and the other slot free
+    if (key0 + KEYS < end) {
+      fetch(a.k, a.ks, kn, key0 + KEYS);
+      fetch(a.v, a.vs, vn, key0 + KEYS);
+    }
+    if (key0 >= wend) return;
+    asm volatile("" : "+v"(k_at), "+v"(v_at));        // (the places are made here, not kept in 40 registers)
+    // scores, keys in the rows: lane (row n, h) holds keys 32 b + 8 (i / 4) + 4 h + i % 4
+    f16v s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        s[b] = mfma(*reinterpret_cast<const u4*>(reinterpret_cast<const char*>(ks) + (k_at ^ (j << 5)) + b * 32 * CH * 16), q[j], s[b], T());
+      }
+    }
+    const bool some = key0 + KEYS > wfull;            // some row does not see some key
+    if (some) {
+      const int lim = seen - key0 - 4 * h;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 32 * b + 8 * (i >> 2) + (i & 3) < lim ? s[b][i] : -INFINITY;
+    }
+    float smax = s[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) smax = fmaxf(smax, s[b][i]);
+    if (__any(smax > lift)) {
+      const float nr = fmaxf(ref, fmaxf(smax, __shfl_xor(smax, 32)));
+      const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr));
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] *= f;
+      ref = nr;
+      nref = P_LOG - (nr == -INFINITY ? 0.f : nr * rs);
+      lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
+    }
+    u4 p[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[b][i], rs, nref)), e1 = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], rs, nref));
+        sum += e0 + e1;
+        p[b][i >> 3][(i >> 1) & 3] = pack<T>(e0, e1);
+      }
+    // V's operand: its column d = 32 e + n, keys 16 g + 8 u + 4 h + 0..3, read transposed
+    auto column = [&](int g, int u, int e) {
+      const char* at = reinterpret_cast<const char*>(vs) + (v_at ^ (e << 6) ^ (u << 5)) + (16 * g + 8 * u) * CH * 16;
+      return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)at));
+    };
+    if (some) {
+      // A row that does not see a key gives it the weight 0, and 0 times an infinity or a NaN would still reach it.
+      uint32_t big = 0;
+#pragma unroll 1
+      for (int g = 0; g < KEYS / 16; ++g)
+#pragma unroll
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const u2 w = column(g, u, e);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const uint32_t x = w[i] & 0x7fff7fffu;
+              big = max(big, max(x & 0xffffu, x >> 16));
+            }
+          }
+      constexpr uint32_t INF_BITS = std::is_same_v<T, f16> ? 0x7c00u : 0x7f80u;
+      if (__any(big >= INF_BITS)) {
+        // ... so such a tile is summed key by key, each row over the keys that it sees
+#pragma unroll 1
+        for (int k = 0; k < KEYS; ++k) {
+          uint32_t w = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w = (k & 31) / 8 * 2 + ((k & 31) % 4) / 2 + 8 * (k >> 5) == i ? p[i >> 3][(i >> 2) & 1][i & 3] : w;
+          w = __shfl(w, n + 32 * ((k >> 2) & 1));
+          const uint16_t bits = (uint16_t)((k & 1) ? w >> 16 : w);
+          const float pk = to_f(__builtin_bit_cast(T, bits));
+          const bool yes = key0 + k < seen;
+          const T* row_at = reinterpret_cast<const T*>(vs) + k * D;
+#pragma unroll
+          for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int d = 32 * e + 8 * (i >> 2) + 4 * h + (i & 3);
+              const float v = to_f(row_at[swizzle<D>(k, d >> 3) * 8 + (d & 7)]);
+              o[e][i] = yes ? fmaf(pk, v, o[e][i]) : o[e][i];
+            }
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < KEYS / 16; ++g)
+#pragma unroll
+      for (int e = 0; e < DB; ++e) {
+        const u2 x = column(g, 0, e), y = column(g, 1, e);
+        o[e] = mfma((u4){x[0], x[1], y[0], y[1]}, p[g >> 1][g & 1], o[e], T());
+      }
+  };
+
+  if (end > 0) {
+    fetch(a.k, a.ks, k_a, 0);
+    fetch(a.v, a.vs, v_a, 0);
+  }
+  for (int key0 = 0; key0 < end; key0 += 2 * KEYS) {
+    step(k_a, v_a, k_b, v_b, key0);
+    if (key0 + KEYS >= end) break;
+    step(k_b, v_b, k_a, v_a, key0 + KEYS);
+  }
+
+  sum += __shfl_xor(sum, 32);
+  const float inv = ref == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+  if (wave_rows <= 0) return;
+  // 4 values of this lane's columns 8 g + 4 h and 4 of lane ^ 32's make 16 bytes: even groups go to the lower lanes, odd ones to the upper
+  T* out = (T*)a.out + ((int64_t)(t.start + token) * a.Hq + head) * D;
+#pragma unroll
+  for (int e = 0; e < DB; ++e)
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+      u4 w;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        auto value = [&](int j) { return inv == 0.f ? 0.f : o[e][j] * inv; };
+        const uint32_t x = pack<T>(value(4 * g + 2 * i), value(4 * g + 2 * i + 1));
+        const uint32_t y = pack<T>(value(4 * g + 4 + 2 * i), value(4 * g + 4 + 2 * i + 1));
+        const auto z = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+        w[i] = z[0];
+        w[2 + i] = z[1];
+      }
+      if (real) *reinterpret_cast<u4*>(out + 32 * e + 8 * (g + h)) = w;
+    }
+}
+
 template <typename T>
 int run(const PromptAttnArgs& a, hipStream_t st) {
   const dim3 grid(a.Tq, a.Hq);
@@ -62,9 +353,30 @@ int run(const PromptAttnArgs& a, hipStream_t st) {
   return PIPE_OK;
 }
 
+template <typename T, int D>
+int run_mfma(const Kernel& k, hipStream_t st) {
+  const PromptAttnArgs& a = k.a;
+  // (a tile's rows are reached from its first by 32-bit offsets)
+  const bool wide = rows_wide(a.q, a.qs, a.type) && rows_wide(a.k, a.ks, a.type) && rows_wide(a.v, a.vs, a.type) &&
+                    a.ks.token < (1 << 24) && a.vs.token < (1 << 24);
+  const dim3 grid((unsigned)(k.n_tiles * a.Hkv));
+  if (wide) PIPE_KLAUNCH((prompt_mfma_kernel<T, D, true>), grid, dim3(WAVES * 64), 0, st, k);
+  else PIPE_KLAUNCH((prompt_mfma_kernel<T, D, false>), grid, dim3(WAVES * 64), 0, st, k);
+  PIPE_HIP(hipGetLastError());
+  return PIPE_OK;
+}
+
 }  // namespace
 
 int launch_prompt_attention(const PromptAttnArgs& a, hipStream_t st) {
   if (a.Tq == 0) return PIPE_OK;
-  return a.type == PIPE_F32 ? run<float>(a, st) : a.type == PIPE_F16 ? run<f16>(a, st) : run<bf16>(a, st);
+  if (a.type == PIPE_F32) return run<float>(a, st);
+  Kernel k{};
+  k.a = a;
+  k.G = a.Hq / a.Hkv;
+  const int64_t tiles = (int64_t)a.Tq * k.G / QROWS + a.B + 1;
+  if (tiles * a.Hkv > 0xffffff) return PIPE_ESHAPE;
+  k.n_tiles = (int)tiles;
+  if (a.type == PIPE_F16) return a.D == 64 ? run_mfma<f16, 64>(k, st) : run_mfma<f16, 128>(k, st);
+  return a.D == 64 ? run_mfma<bf16, 64>(k, st) : run_mfma<bf16, 128>(k, st);
 }
