@@ -5,61 +5,12 @@
 
 namespace {
 
-// One wave per query row: 64 keys at a time, a lane per key for the scores, a lane per D/64 values for the output.
-template <typename T, int D>
-__global__ __launch_bounds__(64) void prompt_attn_kernel(PromptAttnArgs a) {
-  __shared__ float sq[D], sp[64];
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
-  const int kvh = h / (a.Hq / a.Hkv);
-  int b = -1;
-  for (int i0 = 0; i0 < a.B; i0 += 64)
-    b += __popcll(__ballot(i0 + lane < a.B && a.q_starts[min(i0 + lane, a.B)] <= t));
-  const bool mine = b >= 0 && t < a.q_starts[a.B];
-  int k0 = 0, seen = 0;
-  if (mine) {
-    k0 = max(0, min(a.k_starts[b], a.Tk));
-    seen = min(a.k_starts[b + 1], a.Tk) - k0;
-    if (a.causal) seen = min(seen, seen - (a.q_starts[b + 1] - t) + 1);
-  }
-  for (int i = lane; i < D; i += 64) sq[i] = to_f(((const T*)a.q)[(int64_t)t * a.qs.token + (int64_t)h * a.qs.head + i]);
-  __syncthreads();
-  float top = -INFINITY, sum = 0, o[D / 64] = {};
-  for (int t0 = 0; t0 < seen; t0 += 64) {
-    const int n = min(64, seen - t0);
-    float S = -INFINITY;
-    if (lane < n) {
-      const T* kp = (const T*)a.k + (int64_t)(k0 + t0 + lane) * a.ks.token + (int64_t)kvh * a.ks.head;
-      float dot = 0;
-      for (int i = 0; i < D; ++i) dot = fmaf(sq[i], to_f(kp[i]), dot);
-      S = dot * a.scale;
-    }
-    float mx = S;
-    for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-    const float ntop = fmaxf(top, mx);
-    const float ref = ntop == -INFINITY ? 0.f : ntop, f = expf(top - ref);
-    top = ntop;
-    const float p = expf(S - ref);
-    sum = sum * f + p;
-    for (int i = 0; i < D / 64; ++i) o[i] *= f;
-    sp[lane] = p;
-    __syncthreads();
-    for (int j = 0; j < n; ++j) {
-      const T* vp = (const T*)a.v + (int64_t)(k0 + t0 + j) * a.vs.token + (int64_t)kvh * a.vs.head;
-      for (int i = 0; i < D / 64; ++i) o[i] = fmaf(sp[j], to_f(vp[lane + 64 * i]), o[i]);
-    }
-    __syncthreads();
-  }
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  const bool none = top == -INFINITY && sum == 0.f;
-  for (int i = 0; i < D / 64; ++i)
-    ((T*)a.out)[((int64_t)t * a.Hq + h) * D + lane + 64 * i] = from_f<T>(none ? 0.f : o[i] / sum);
-}
-
 // ------------------------------------------------------------------ 16-bit types
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
+typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 
@@ -81,6 +32,7 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {
 struct Kernel {
   PromptAttnArgs a;
   int G, n_tiles;
+  bool wide;       // 16-byte loads of q, k and v
 };
 
 struct Tile {
@@ -115,6 +67,32 @@ __device__ __forceinline__ Tile find_tile(const Kernel& k, int id) {
   return t;
 }
 
+// A lane's row, and what its wave and its workgroup see.
+template <typename T>
+struct Row {
+  bool real;
+  const T* q;
+  T* out;
+  int seen;                   // keys this row sees
+  int end;                    // keys any row of the workgroup sees
+  int wave_end, wave_full;    // keys any row of the wave sees, and keys that all of them see
+  __device__ __forceinline__ Row(const Kernel& k, const Tile& t, int wave, int n, int kvh) {
+    const PromptAttnArgs& a = k.a;
+    const int lrow = wave * WROWS + n;
+    real = lrow < t.n_rows;
+    const int row = t.row0 + (real ? lrow : 0);
+    const int token = row / k.G, head = kvh * k.G + row % k.G;
+    auto seen_by = [&](int query) { return a.causal ? max(0, min(t.nk, t.first_seen + query)) : t.nk; };
+    seen = real ? seen_by(token) : 0;
+    q = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)head * a.qs.head;
+    out = (T*)a.out + ((int64_t)(t.start + token) * a.Hq + head) * a.D;
+    end = seen_by((t.row0 + t.n_rows - 1) / k.G);
+    const int rows = min(WROWS, t.n_rows - wave * WROWS);
+    wave_end = rows > 0 ? seen_by((t.row0 + wave * WROWS + rows - 1) / k.G) : 0;
+    wave_full = rows > 0 ? seen_by((t.row0 + wave * WROWS) / k.G) : 0;
+  }
+};
+
 // Where chunk c (8 values) of key row r lies in its LDS row, as a chunk: the rows that one read of 16 lanes touches (16 rows' same chunk of K;
 // 4 rows' 4 chunks of V) then lie in different banks.
 template <int D>
@@ -137,15 +115,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
 
-  // ---- this lane's row
-  const int lrow = wave * WROWS + n;
-  const bool real = lrow < t.n_rows;
-  const int row = t.row0 + (real ? lrow : 0);
-  const int token = row / kr.G, head = kvh * kr.G + row % kr.G;
-  const int seen = !real ? 0 : a.causal ? max(0, min(t.nk, t.first_seen + token)) : t.nk;
-  const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)head * a.qs.head + 8 * h;
+  const Row<T> w(kr, t, wave, n, kvh);
+  const T* qp = w.q + 8 * h;
   u4 q[KS];
-  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = real && a.scale != 0.f ? ~0u : 0u;
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = w.real && a.scale != 0.f ? ~0u : 0u;
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     if constexpr (WIDE) {
@@ -163,13 +136,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
     for (int i = 0; i < 4; ++i) q[s][i] = (q[s][i] ^ flip) & keep;
   const float rs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
 
-  // ---- keys: how many any row of the workgroup / of the wave sees, and how many every row of the wave sees
-  auto seen_by = [&](int r) { return a.causal ? max(0, min(t.nk, t.first_seen + (t.row0 + r) / kr.G)) : t.nk; };
-  const int end = seen_by(t.n_rows - 1);
-  const int wave_rows = min(WROWS, t.n_rows - wave * WROWS);
-  const int wend = wave_rows > 0 ? seen_by(wave * WROWS + wave_rows - 1) : 0;
-  const int wfull = wave_rows > 0 ? seen_by(wave * WROWS) : 0;
-
   // ---- loads of a tile: LDS in the order of the lanes, so that a lane picks what belongs at its place
   auto fetch = [&](const void* src, const HeadStrides& st, u4* dst, int key0) {
     const T* base = (const T*)src + (int64_t)(t.k0 + key0) * st.token + (int64_t)kvh * st.head;
@@ -185,9 +151,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         T v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = base[(int64_t)rr * st.token + c * 8 + e];
-        u4 w;
-        __builtin_memcpy(&w, v, 16);
-        dst[at] = w;
+        u4 x;
+        __builtin_memcpy(&x, v, 16);
+        dst[at] = x;
       }
     }
   };
@@ -207,11 +173,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   int k_at = (n * CH + swizzle<D>(n, h)) * 16, v_at = (vr * CH + swizzle<D>(vr, vc)) * 16 + (lane & 1) * 8;
   auto step = [&](const u4* ks, const u4* vs, u4* kn, u4* vn, int key0) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // this tile is there, and the other slot free
-    if (key0 + KEYS < end) {
+    if (key0 + KEYS < w.end) {
       fetch(a.k, a.ks, kn, key0 + KEYS);
       fetch(a.v, a.vs, vn, key0 + KEYS);
     }
-    if (key0 >= wend) return;
+    if (key0 >= w.wave_end) return;
     asm volatile("" : "+v"(k_at), "+v"(v_at));        // (the places are made here, not kept in 40 registers)
     // scores, keys in the rows: lane (row n, h) holds keys 32 b + 8 (i / 4) + 4 h + i % 4
     f16v s[2];
@@ -224,9 +190,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         s[b] = mfma(*reinterpret_cast<const u4*>(reinterpret_cast<const char*>(ks) + (k_at ^ (j << 5)) + b * 32 * CH * 16), q[j], s[b], T());
       }
     }
-    const bool some = key0 + KEYS > wfull;            // some row does not see some key
+    const bool some = key0 + KEYS > w.wave_full;            // some row does not see some key
     if (some) {
-      const int lim = seen - key0 - 4 * h;
+      const int lim = w.seen - key0 - 4 * h;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -270,10 +236,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         for (int e = 0; e < DB; ++e)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const u2 w = column(g, u, e);
+            const u2 y = column(g, u, e);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const uint32_t x = w[i] & 0x7fff7fffu;
+              const uint32_t x = y[i] & 0x7fff7fffu;
               big = max(big, max(x & 0xffffu, x >> 16));
             }
           }
@@ -282,13 +248,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         // ... so such a tile is summed key by key, each row over the keys that it sees
 #pragma unroll 1
         for (int k = 0; k < KEYS; ++k) {
-          uint32_t w = 0;
+          uint32_t pw = 0;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) w = (k & 31) / 8 * 2 + ((k & 31) % 4) / 2 + 8 * (k >> 5) == i ? p[i >> 3][(i >> 2) & 1][i & 3] : w;
-          w = __shfl(w, n + 32 * ((k >> 2) & 1));
-          const uint16_t bits = (uint16_t)((k & 1) ? w >> 16 : w);
+          for (int i = 0; i < 16; ++i) pw = (k & 31) / 8 * 2 + ((k & 31) % 4) / 2 + 8 * (k >> 5) == i ? p[i >> 3][(i >> 2) & 1][i & 3] : pw;
+          pw = __shfl(pw, n + 32 * ((k >> 2) & 1));
+          const uint16_t bits = (uint16_t)((k & 1) ? pw >> 16 : pw);
           const float pk = to_f(__builtin_bit_cast(T, bits));
-          const bool yes = key0 + k < seen;
+          const bool yes = key0 + k < w.seen;
           const T* row_at = reinterpret_cast<const T*>(vs) + k * D;
 #pragma unroll
           for (int e = 0; e < DB; ++e)
@@ -311,56 +277,215 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       }
   };
 
-  if (end > 0) {
+  if (w.end > 0) {
     fetch(a.k, a.ks, k_a, 0);
     fetch(a.v, a.vs, v_a, 0);
   }
-  for (int key0 = 0; key0 < end; key0 += 2 * KEYS) {
+  for (int key0 = 0; key0 < w.end; key0 += 2 * KEYS) {
     step(k_a, v_a, k_b, v_b, key0);
-    if (key0 + KEYS >= end) break;
+    if (key0 + KEYS >= w.end) break;
     step(k_b, v_b, k_a, v_a, key0 + KEYS);
   }
 
   sum += __shfl_xor(sum, 32);
   const float inv = ref == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
-  if (wave_rows <= 0) return;
   // 4 values of this lane's columns 8 g + 4 h and 4 of lane ^ 32's make 16 bytes: even groups go to the lower lanes, odd ones to the upper
-  T* out = (T*)a.out + ((int64_t)(t.start + token) * a.Hq + head) * D;
 #pragma unroll
   for (int e = 0; e < DB; ++e)
 #pragma unroll
     for (int g = 0; g < 4; g += 2) {
-      u4 w;
+      u4 y;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         auto value = [&](int j) { return inv == 0.f ? 0.f : o[e][j] * inv; };
         const uint32_t x = pack<T>(value(4 * g + 2 * i), value(4 * g + 2 * i + 1));
-        const uint32_t y = pack<T>(value(4 * g + 4 + 2 * i), value(4 * g + 4 + 2 * i + 1));
-        const auto z = __builtin_amdgcn_permlane32_swap(x, y, false, false);
-        w[i] = z[0];
-        w[2 + i] = z[1];
+        const uint32_t x2 = pack<T>(value(4 * g + 4 + 2 * i), value(4 * g + 4 + 2 * i + 1));
+        const auto z = __builtin_amdgcn_permlane32_swap(x, x2, false, false);
+        y[i] = z[0];
+        y[2 + i] = z[1];
       }
-      if (real) *reinterpret_cast<u4*>(out + 32 * e + 8 * (g + h)) = w;
+      if (w.real) *reinterpret_cast<u4*>(w.out + 32 * e + 8 * (g + h)) = y;
     }
 }
 
-template <typename T>
-int run(const PromptAttnArgs& a, hipStream_t st) {
-  const dim3 grid(a.Tq, a.Hq);
-  if (a.D == 64) PIPE_KLAUNCH((prompt_attn_kernel<T, 64>), grid, dim3(64), 0, st, a);
-  else PIPE_KLAUNCH((prompt_attn_kernel<T, 128>), grid, dim3(64), 0, st, a);
+// ------------------------------------------------------------------ fp32
+// The same on the fp32 matrix instruction, 32 x 32 with two values of the summed axis: a lane's four values of K (a 16-byte read) meet four
+// of q, in any order that both keep; a lane's weight of key i meets V's row of that key.  Tiles of 32 keys; matrix instructions take 64 cycles
+// each, so that everything else hides behind them.
+template <int D>
+__device__ __forceinline__ int swizzle32(int r, int c) { return c ^ (r & 15); }     // (16 rows' same chunk in different banks)
+
+template <int D, bool WIDE>
+__global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel kr) {
+  constexpr int CH = D / 4, KS = D / 8, DB = D / 32, KEYS32 = 32;
+  constexpr int LOADS = KEYS32 * CH / 256;
+  __shared__ alignas(1024) f4 k_a[KEYS32 * CH], k_b[KEYS32 * CH], v_a[KEYS32 * CH], v_b[KEYS32 * CH];
+  const PromptAttnArgs& a = kr.a;
+  const int id = blockIdx.x, kvh = id % a.Hkv;
+  const Tile t = find_tile(kr, kr.n_tiles - 1 - id / a.Hkv);
+  if (t.n_rows == 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  const Row<float> w(kr, t, wave, n, kvh);
+  const float* qp = w.q + 4 * h;
+  f4 q[KS];
+  const float sgn = a.scale < 0.f ? -1.f : 1.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    if constexpr (WIDE) {
+      q[s] = *reinterpret_cast<const f4*>(qp + 8 * s);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[s][i] = qp[8 * s + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[s][i] = w.real && a.scale != 0.f ? sgn * q[s][i] : 0.f;
+  }
+  const float rs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
+
+  auto fetch = [&](const void* src, const HeadStrides& st, f4* dst, int key0) {
+    const float* base = (const float*)src + (int64_t)(t.k0 + key0) * st.token + (int64_t)kvh * st.head;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int at = (i * WAVES + wave) * 64 + lane, r = at / CH, c = swizzle32<D>(r, at % CH);
+      const int rr = min(r, t.nk - 1 - key0);
+      if constexpr (WIDE) {
+        const uint32_t off = (uint32_t)rr * (uint32_t)st.token * 4u + c * 16;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((const char*)base + off),
+                                         (__attribute__((address_space(3))) void*)(dst + (i * WAVES + wave) * 64), 16, 0, 0);
+      } else {
+        f4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = base[(int64_t)rr * st.token + c * 4 + e];
+        dst[at] = v;
+      }
+    }
+  };
+
+  f16v o[DB];
+#pragma unroll
+  for (int d = 0; d < DB; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f;
+  int k_at = (n * CH + swizzle32<D>(n, h)) * 16, v_at = 4 * h * CH * 16 + ((n >> 2) ^ (4 * h)) * 16 + (n & 3) * 4;   // places in a tile, in bytes: chunk h of K's row n, value n of V's row 4 h
+
+  auto step = [&](const f4* ks, const f4* vs, f4* kn, f4* vn, int key0) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // this tile is there, and the other slot free
+    if (key0 + KEYS32 < w.end) {
+      fetch(a.k, a.ks, kn, key0 + KEYS32);
+      fetch(a.v, a.vs, vn, key0 + KEYS32);
+    }
+    if (key0 >= w.wave_end) return;
+    asm volatile("" : "+v"(k_at), "+v"(v_at));
+    f16v s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      const f4 kv = *reinterpret_cast<const f4*>(reinterpret_cast<const char*>(ks) + (k_at ^ (j << 5)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[i], q[j][i], s, 0, 0, 0);
+    }
+    const bool some = key0 + KEYS32 > w.wave_full;
+    if (some) {
+      const int lim = w.seen - key0 - 4 * h;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < lim ? s[i] : -INFINITY;
+    }
+    float smax = s[0];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) smax = fmaxf(smax, s[i]);
+    if (__any(smax > lift)) {
+      const float nr = fmaxf(ref, fmaxf(smax, __shfl_xor(smax, 32)));
+      const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr));
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] *= f;
+      ref = nr;
+      nref = nr == -INFINITY ? 0.f : -nr * rs;
+      lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], rs, nref));
+      sum += s[i];
+    }
+    // value n of block e of the row of key 8 (i / 4) + 4 h + i % 4
+    auto value = [&](int i, int e) {
+      const int r = 8 * (i >> 2) + (i & 3);                                // the row of h = 0; the one 4 further differs by an exclusive or of 4
+      return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(vs) + (v_at ^ (((8 * e) ^ (r & 15)) << 4)) + r * CH * 16);
+    };
+    if (some) {
+      // (a weight of 0 times an infinity or a NaN: see the 16-bit kernel)
+      bool bad = false;
+#pragma unroll 1
+      for (int r = h; r < KEYS32; r += 2)
+#pragma unroll
+        for (int e = 0; e < DB; ++e) bad |= !(fabsf(reinterpret_cast<const float*>(vs)[r * D + 32 * e + n]) < INFINITY);
+      if (__any(bad)) {
+#pragma unroll 1
+        for (int k = 0; k < KEYS32; ++k) {
+          float p = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p = k / 8 * 4 + k % 4 == i ? s[i] : p;
+          p = __shfl(p, n + 32 * ((k >> 2) & 1));
+          const bool yes = key0 + k < w.seen;
+          const float* row_at = reinterpret_cast<const float*>(vs) + k * D;
+#pragma unroll
+          for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int d = 32 * e + 8 * (i >> 2) + 4 * h + (i & 3);
+              const float v = row_at[swizzle32<D>(k, d >> 2) * 4 + (d & 3)];
+              o[e][i] = yes ? fmaf(p, v, o[e][i]) : o[e][i];
+            }
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int e = 0; e < DB; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(i, e), s[i], o[e], 0, 0, 0);
+  };
+
+  if (w.end > 0) {
+    fetch(a.k, a.ks, k_a, 0);
+    fetch(a.v, a.vs, v_a, 0);
+  }
+  for (int key0 = 0; key0 < w.end; key0 += 2 * KEYS32) {
+    step(k_a, v_a, k_b, v_b, key0);
+    if (key0 + KEYS32 >= w.end) break;
+    step(k_b, v_b, k_a, v_a, key0 + KEYS32);
+  }
+  sum += __shfl_xor(sum, 32);
+  const float inv = ref == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+  if (!w.real) return;
+#pragma unroll
+  for (int e = 0; e < DB; ++e)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      f4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = inv == 0.f ? 0.f : o[e][4 * g + i] * inv;
+      *reinterpret_cast<f4*>(w.out + 32 * e + 8 * g + 4 * h) = y;
+    }
+}
+
+template <int D>
+int run_f32(const Kernel& k, hipStream_t st) {
+  const dim3 grid((unsigned)(k.n_tiles * k.a.Hkv));
+  if (k.wide) PIPE_KLAUNCH((prompt_f32_kernel<D, true>), grid, dim3(WAVES * 64), 0, st, k);
+  else PIPE_KLAUNCH((prompt_f32_kernel<D, false>), grid, dim3(WAVES * 64), 0, st, k);
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
 }
 
 template <typename T, int D>
 int run_mfma(const Kernel& k, hipStream_t st) {
-  const PromptAttnArgs& a = k.a;
-  // (a tile's rows are reached from its first by 32-bit offsets)
-  const bool wide = rows_wide(a.q, a.qs, a.type) && rows_wide(a.k, a.ks, a.type) && rows_wide(a.v, a.vs, a.type) &&
-                    a.ks.token < (1 << 24) && a.vs.token < (1 << 24);
-  const dim3 grid((unsigned)(k.n_tiles * a.Hkv));
-  if (wide) PIPE_KLAUNCH((prompt_mfma_kernel<T, D, true>), grid, dim3(WAVES * 64), 0, st, k);
+  const dim3 grid((unsigned)(k.n_tiles * k.a.Hkv));
+  if (k.wide) PIPE_KLAUNCH((prompt_mfma_kernel<T, D, true>), grid, dim3(WAVES * 64), 0, st, k);
   else PIPE_KLAUNCH((prompt_mfma_kernel<T, D, false>), grid, dim3(WAVES * 64), 0, st, k);
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
@@ -370,13 +495,16 @@ int run_mfma(const Kernel& k, hipStream_t st) {
 
 int launch_prompt_attention(const PromptAttnArgs& a, hipStream_t st) {
   if (a.Tq == 0) return PIPE_OK;
-  if (a.type == PIPE_F32) return run<float>(a, st);
   Kernel k{};
   k.a = a;
   k.G = a.Hq / a.Hkv;
   const int64_t tiles = (int64_t)a.Tq * k.G / QROWS + a.B + 1;
   if (tiles * a.Hkv > 0xffffff) return PIPE_ESHAPE;
   k.n_tiles = (int)tiles;
+  // (a tile's rows are reached from its first by 32-bit offsets)
+  k.wide = rows_wide(a.q, a.qs, a.type) && rows_wide(a.k, a.ks, a.type) && rows_wide(a.v, a.vs, a.type) && a.ks.token < (1 << 24) &&
+           a.vs.token < (1 << 24);
+  if (a.type == PIPE_F32) return a.D == 64 ? run_f32<64>(k, st) : run_f32<128>(k, st);
   if (a.type == PIPE_F16) return a.D == 64 ? run_mfma<f16, 64>(k, st) : run_mfma<f16, 128>(k, st);
   return a.D == 64 ? run_mfma<bf16, 64>(k, st) : run_mfma<bf16, 128>(k, st);
 }
