@@ -36,62 +36,115 @@ typedef __attribute__((address_space(4))) int32_t ConstInt;   // memory that the
 
 constexpr int WAVES = 4, ROWS = 16, STEP = 32;      // tokens of a wave's step
 constexpr int AHEAD = 2;                            // steps whose loads are in flight while one is worked on
-constexpr int CHUNK_UNIT = WAVES * STEP;            // a split's tokens are a multiple of this: every wave gets whole steps
-constexpr int SPLIT_TILES = 768;
+constexpr int UNIT = WAVES * STEP;                  // tokens of a workgroup's step: one step of every wave
+constexpr int SHARES_128 = 512, SHARES_64 = 768;    // workgroups of a launch: as many as the chip holds at once (2 a unit at head_dim 128, 3 at 64)
 constexpr float REF_SLACK = 6.f;                    // log2: a row's reference rises only when a score exceeds it by this
 constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE fits fp16
 
 struct Kernel {
   CacheAttnArgs a;
-  int G, n_split, chunk;
+  int G, n_share;   // workgroups of a key/value head
   bool wide;        // 16-byte loads of q
-  float* part_o;    // [Hkv][T * G rows][split][D]
-  float* part_ml;   // [Hkv][T * G rows][split][2]: log2 of the reference weight, sum of weights
+  float* part_o;    // [Hkv][n_share][2][16][D]
+  float* part_ml;   // [Hkv][n_share][2][16][2]: log2 of the reference weight, sum of weights
 };
+
+// The work of a key/value head is the tiles of all requests one after the other, a tile of request b counting the steps of UNIT tokens that
+// its cache has; every workgroup takes an equal share of the steps, wherever it begins and ends.  So requests of any lengths keep all
+// workgroups busy to the end, and one long request is split.  Of a tile that several shares hold, each writes its part -- of its first tile
+// to place 0, of its last to place 1 -- and the join sums them in their order.
+struct Request {
+  int b, start, n;              // its fresh tokens (b = B: the rows behind the last request, which see nothing)
+  int length;
+  uint32_t tiles, steps;        // ... each of so many steps
+};
+__device__ __forceinline__ Request request(const Kernel& k, int b) {
+  const CacheAttnArgs& a = k.a;
+  auto start_of = [&](int i) { return i > 0 ? min(max(a.starts[i], 0), a.T) : 0; };
+  Request r;
+  r.b = b;
+  r.start = start_of(b);
+  r.n = max(0, (b < a.B ? start_of(b + 1) : a.T) - r.start);
+  r.length = b < a.B ? (int)min((int64_t)max(0, a.lengths[b]), min((int64_t)a.width << a.cache.shift, (int64_t)0x7ffff000)) : 0;
+  r.tiles = ((uint32_t)r.n * (uint32_t)k.G + ROWS - 1) / ROWS;
+  r.steps = max(1u, ((uint32_t)r.length + UNIT - 1) / UNIT);
+  return r;
+}
+struct Place {
+  uint64_t total;               // steps of the head
+  uint64_t at;                  // the place looked for ...
+  int b;                        // ... lies in request b,
+  uint64_t step;                // ... this many of its steps on
+};
+__device__ __forceinline__ uint64_t share_begin(uint64_t total, uint32_t n_share, uint32_t share) { return total * share / n_share; }
+
+// The first place of a share (or the last one, LAST).  By the whole workgroup: every thread sums up to 17 requests, and the one whose sum
+// holds the place walks them again.
+template <bool LAST>
+__device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
+  __shared__ uint64_t s_sum[4], s_step;
+  __shared__ int s_b;
+  const int B1 = k.a.B + 1, per = (B1 + 255) / 256, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int b0 = min(B1, (int)threadIdx.x * per), b1 = min(B1, b0 + per);
+  uint64_t mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Request r = request(k, b);
+    mine += (uint64_t)r.tiles * r.steps;
+  }
+  uint64_t inc = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint64_t o = __shfl_up(inc, d);
+    if (lane >= d) inc += o;
+  }
+  if (lane == 63) s_sum[wave] = inc;
+  if (threadIdx.x == 0) s_b = 0;
+  __syncthreads();
+  uint64_t before = inc - mine;
+  Place p;
+  p.total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    before += w < wave ? s_sum[w] : 0;
+    p.total += s_sum[w];
+  }
+  p.at = LAST ? share_begin(p.total, k.n_share, share + 1) - 1 : share_begin(p.total, k.n_share, share);
+  if (before <= p.at && p.at < before + mine) {
+    for (int b = b0; b < b1; ++b) {
+      const Request r = request(k, b);
+      const uint64_t c = (uint64_t)r.tiles * r.steps;
+      if (p.at < before + c) {
+        s_b = b;
+        s_step = p.at - before;
+        break;
+      }
+      before += c;
+    }
+  }
+  __syncthreads();
+  p.b = __builtin_amdgcn_readfirstlane(s_b);
+  p.step = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s_step >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)s_step);
+  return p;
+}
 
 struct Tile {
   int b, row0, n_rows, start;   // rows row0 .. row0 + n_rows - 1 of request b, whose tokens start at `start`
   int first_seen;               // cached tokens that the request's first fresh token sees (may be negative)
   int end;                      // cached tokens that any row of the tile sees
-  int n_split, chunk;           // splits that have tokens (at least one), and theirs
+  __device__ __forceinline__ Tile(const Kernel& k, const Request& r, uint32_t i) : b(r.b), start(r.start) {
+    row0 = (int)(i * ROWS);
+    n_rows = min(ROWS, r.n * k.G - row0);
+    // (the table's width cuts a length short, not the places of the queries)
+    const int length = r.b < k.a.B ? max(0, k.a.lengths[r.b]) : 0;
+    first_seen = length - r.n + 1;
+    end = min(r.length, max(0, first_seen + (row0 + n_rows - 1) / k.G));
+  }
 };
 
-// Tile `id` of the launch: request b (B: the rows behind the last request, which see nothing) owns the ids from
-// floor(start_b * G / 16) + b on.
-__device__ __forceinline__ Tile find_tile(const Kernel& k, int id) {
-  const CacheAttnArgs& a = k.a;
-  const int lane = threadIdx.x & 63;
-  auto start_of = [&](int b) { return b > 0 ? min(max(a.starts[b], 0), a.T) : 0; };
-  int b = -1;
-  for (int i0 = 0; i0 <= a.B; i0 += 64) {
-    const int i = i0 + lane;
-    const bool le = i <= a.B && (int)(((int64_t)start_of(min(i, a.B)) * k.G) / ROWS) + i <= id;
-    const int n = __popcll(__ballot(le));
-    b += n;
-    if (n < 64) break;
-  }
-  b = __builtin_amdgcn_readfirstlane(b);
-  Tile t;
-  t.b = b;
-  t.start = start_of(b);
-  const int n = (b < a.B ? start_of(b + 1) : a.T) - t.start;
-  t.row0 = (id - ((int)(((int64_t)t.start * k.G) / ROWS) + b)) * ROWS;
-  t.n_rows = t.row0 < 0 ? 0 : min(ROWS, max(0, n * k.G - t.row0));
-  const int length = b < a.B ? max(0, a.lengths[b]) : 0;
-  t.first_seen = length - n + 1;
-  const int last_row = t.row0 + max(t.n_rows, 1) - 1;
-  const int64_t table = (int64_t)a.width << a.cache.shift;
-  t.end = (int)min((int64_t)max(0, t.first_seen + last_row / k.G), min(table, (int64_t)0x7ffff000));
-  // (a request longer than the hint gets longer splits)
-  const int per = (int)(((int64_t)t.end + k.n_split - 1) / k.n_split);
-  t.chunk = max(k.chunk, (per + CHUNK_UNIT - 1) / CHUNK_UNIT * CHUNK_UNIT);
-  t.n_split = max(1, (t.end + t.chunk - 1) / t.chunk);
-  return t;
-}
-
-// the parts of row r of a tile, of the head of this workgroup
-__device__ __forceinline__ int64_t part_row(const Kernel& k, const Tile& t, int r) {
-  return ((int64_t)blockIdx.y * k.a.T * k.G + (int64_t)t.start * k.G + t.row0 + r) * k.n_split;
+template <typename T, int D>
+__device__ __forceinline__ T* out_row(const Kernel& k, const Tile& t, int kvh, int r) {
+  const int row = t.row0 + r;
+  return (T*)k.a.out + ((int64_t)(t.start + row / k.G) * k.a.Hq + (int64_t)kvh * k.G + row % k.G) * D;
 }
 
 // what a part counts, beside the largest reference: nothing if it saw nothing (and NaN if it saw nothing but NaN)
@@ -164,11 +217,10 @@ __device__ __forceinline__ void each(F&& f) {      // f(0) .. f(N - 1), with con
 template <int D, int NB>
 struct Walk {
   const CacheAttnArgs& a;
-  const Tile& t;
-  int kvh;
+  int b, kvh;
   uint32_t at_k, at_v, at_w;   // a lane's place in a 16-block of codes of K, of V, and of words
 
-  __device__ __forceinline__ Walk(const CacheAttnArgs& a_, const Tile& t_, int kvh_, int l16, int kg) : a(a_), t(t_), kvh(kvh_) {
+  __device__ __forceinline__ Walk(const CacheAttnArgs& a_, int b_, int kvh_, int l16, int kg) : a(a_), b(b_), kvh(kvh_) {
     at_k = l16 * (D / 2) + kg * (D / 8);
     at_v = kg * (2 * D) + l16 * (D / 32);
     at_w = ((NB == 1 ? (l16 >> 2 & 1) * 16 : 0) + kg * 4 + (l16 & 3)) * 4 + (l16 >> 3) * (4u << a_.cache.shift);
@@ -176,7 +228,7 @@ struct Walk {
   // page entries of the tokens from tok on; -1 from `end` on
   __device__ __forceinline__ void pages_of(int32_t* pages, int tok, int end) const {
     // (scalar loads: among the vector loads, the wait for an entry would be one for all codes in flight)
-    const ConstInt* row = (const ConstInt*)(uintptr_t)(a.table + (int64_t)t.b * a.width);
+    const ConstInt* row = (const ConstInt*)(uintptr_t)(a.table + (int64_t)b * a.width);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       const int at = __builtin_amdgcn_readfirstlane(tok + 16 * j);
@@ -248,20 +300,28 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   __shared__ float s_o[WAVES][ROWS][D + 4];
   __shared__ float s_ref[WAVES][ROWS], s_sum[WAVES][ROWS];
   const CacheAttnArgs& a = kr.a;
-  const Tile t = find_tile(kr, blockIdx.x);
-  const int split = blockIdx.z;
-  if (t.n_rows == 0 || split >= t.n_split) return;
+  const uint32_t share = blockIdx.x / a.cache.Hkv;
+  const int kvh = blockIdx.x % a.cache.Hkv;
+  const Place first = locate<false>(kr, share);
+  uint64_t left = share_begin(first.total, kr.n_share, share + 1) - first.at;
+  if (left == 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
-  const Walk<D, NB> w(a, t, blockIdx.y, l16, kg);
   const Bits bits;
+  Request rq = request(kr, first.b);
+  uint32_t tile = (uint32_t)(first.step / rq.steps), step0 = (uint32_t)(first.step % rq.steps);
+
+  for (int place = 0;; place = 1) {        // one tile's part after the other
+  const Tile t(kr, rq, tile);
+  const uint32_t n_steps = (uint32_t)min((uint64_t)(rq.steps - step0), left);
+  const Walk<D, NB> w(a, t.b, kvh, l16, kg);
 
   // q: row l16, the values that meet the words kg * KS .. of a token
   const int row = t.row0 + l16;
   const bool real = l16 < t.n_rows;
   const int token = real ? row / kr.G : 0, head = real ? row % kr.G : 0;
   const int seen = real ? t.first_seen + token : 0;      // cached tokens this row sees
-  const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)(w.kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
+  const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)(kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
   float qv[KS * 8], qmax = 0, qsum = 0;
   if (kr.wide) {
 #pragma unroll
@@ -269,6 +329,24 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   } else {
 #pragma unroll
     for (int i = 0; i < KS * 8; i += 8) load8<T, false>(qp + i, qv + i);
+  }
+  // the first steps' loads fly while q is made ready
+  const int end = (int)min((int64_t)t.end, (int64_t)(step0 + n_steps) * UNIT);
+  const int full = max(0, t.first_seen + t.row0 / kr.G);   // tokens that every row sees
+  int tok = (int)step0 * UNIT + wave * STEP, steps = 0;
+  int32_t pages[NB];
+  Tokens<D> r0, r1, r2;      // AHEAD + 1 of them, in turn
+  auto fetch = [&](Tokens<D>& x, int from) {
+    Places<NB> at;
+    w.find(at, pages, from);
+    w.load(x, at);
+  };
+  w.pages_of(pages, tok, end);
+  if (tok < end) {
+    fetch(r0, tok);
+    w.pages_of(pages, tok + UNIT, end);
+    fetch(r1, tok + UNIT);
+    w.pages_of(pages, tok + AHEAD * UNIT, end);
   }
 #pragma unroll
   for (int i = 0; i < KS * 8; ++i) {
@@ -304,28 +382,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   // weights are exp2(rs * T + nref), nref = -rs * ref + log2(P_SCALE / sigma) with sigma a power of two, all scales of V under 2 sigma
   float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = 0x1p-100f;
 
-  const int end = (int)min((int64_t)t.end, (int64_t)(split + 1) * t.chunk);
-  const int full = max(0, t.first_seen + t.row0 / kr.G);   // tokens that every row sees
-  int tok = split * t.chunk + wave * STEP, steps = 0;
-  int32_t pages[NB];
-  Tokens<D> r0, r1, r2;      // AHEAD + 1 of them, in turn
-  auto fetch = [&](Tokens<D>& x, int from) {
-    Places<NB> at;
-    w.find(at, pages, from);
-    w.load(x, at);
-  };
-  w.pages_of(pages, tok, end);
-  if (tok < end) {
-    fetch(r0, tok);
-    w.pages_of(pages, tok + CHUNK_UNIT, end);
-    fetch(r1, tok + CHUNK_UNIT);
-    w.pages_of(pages, tok + AHEAD * CHUNK_UNIT, end);
-  }
   // one step on `c`, while the next ones' loads fly, AHEAD steps on to `n`
   auto step = [&](const Tokens<D>& c, Tokens<D>& n) {
     // (behind the end they read page 0, which the caches hold: behind a branch, the wait for this step's would wait for all)
-    fetch(n, tok + AHEAD * CHUNK_UNIT);
-    w.pages_of(pages, tok + (AHEAD + 1) * CHUNK_UNIT, end);
+    fetch(n, tok + AHEAD * UNIT);
+    w.pages_of(pages, tok + (AHEAD + 1) * UNIT, end);
     // scores
     float s[2][4];
     float ws = word_scale(c.w), wo = word_offset(c.w), wm = fmaf(8.f, ws, wo);      // scale, offset, and the offset of c - 8
@@ -446,7 +507,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
       const h8 one = {1, 1, 1, 1, 1, 1, 1, 1};
       ones = __builtin_amdgcn_mfma_f32_16x16x32_f16(one, __builtin_bit_cast(h8, p[0]), ones, 0, 0, 0);
     }
-    tok += CHUNK_UNIT;
+    tok += UNIT;
   };
   while (tok < end) {
     step(r0, r2);
@@ -472,68 +533,125 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   __syncthreads();
   // the waves' parts together: a thread has D/16 values of a row
   const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * MT;
-  if (r >= t.n_rows) return;
-  float top = s_ref[0][r];
+  if (r < t.n_rows) {
+    float top = s_ref[0][r];
 #pragma unroll
-  for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_ref[i][r]);
-  float y[MT] = {}, all = 0.f;
+    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_ref[i][r]);
+    float y[MT] = {}, all = 0.f;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) {
-    const float f = part_weight(s_ref[i][r], s_sum[i][r], top);
-    all = fmaf(f, s_sum[i][r], all);
+    for (int i = 0; i < WAVES; ++i) {
+      const float f = part_weight(s_ref[i][r], s_sum[i][r], top);
+      all = fmaf(f, s_sum[i][r], all);
 #pragma unroll
-    for (int d = 0; d < MT; ++d) y[d] = fmaf(f, s_o[i][r][d0 + d], y[d]);
+      for (int d = 0; d < MT; ++d) y[d] = fmaf(f, s_o[i][r][d0 + d], y[d]);
+    }
+    if (n_steps == rq.steps) {
+      const float inv = top == -INFINITY && all == 0.f ? 0.f : 1.f / all;
+#pragma unroll
+      for (int d = 0; d < MT; ++d) y[d] = inv == 0.f ? 0.f : y[d] * inv;
+      store_row<T, MT>(out_row<T, D>(kr, t, kvh, r) + d0, y);
+    } else {
+      const int64_t at = (((int64_t)kvh * kr.n_share + share) * 2 + place) * ROWS + r;
+      store_row<float, MT>(kr.part_o + at * D + d0, y);
+      if (d0 == 0) { kr.part_ml[at * 2] = top; kr.part_ml[at * 2 + 1] = all; }
+    }
   }
-  if (t.n_split == 1) {
-    const float inv = top == -INFINITY && all == 0.f ? 0.f : 1.f / all;
-    const int rr = t.row0 + r;
-    T* out = (T*)a.out + ((int64_t)(t.start + rr / kr.G) * a.Hq + w.kvh * kr.G + rr % kr.G) * D + d0;
-#pragma unroll
-    for (int d = 0; d < MT; ++d) y[d] = inv == 0.f ? 0.f : y[d] * inv;
-    store_row<T, MT>(out, y);
-  } else {
-    const int64_t at = part_row(kr, t, r) + split;
-    store_row<float, MT>(kr.part_o + at * D + d0, y);
-    if (d0 == 0) { kr.part_ml[at * 2] = top; kr.part_ml[at * 2 + 1] = all; }
+  left -= n_steps;
+  if (left == 0) break;
+  __syncthreads();                         // (the next part's outputs come to the same places)
+  step0 = 0;
+  if (++tile >= rq.tiles) {
+    tile = 0;
+    do rq = request(kr, rq.b + 1);         // (steps are left: there is a request)
+    while (rq.tiles == 0);
+  }
   }
 }
 
-// The splits' parts of a tile together, in their order.
+// The parts of a tile that several shares hold together, in the shares' order, by the workgroup of the first of them.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_attn_join_kernel(const Kernel kr) {
   constexpr int MT = D / 16;
-  const CacheAttnArgs& a = kr.a;
-  const Tile t = find_tile(kr, blockIdx.x);
-  const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * MT;
-  if (r >= t.n_rows || t.n_split == 1) return;
-  const int64_t at = part_row(kr, t, r);
-  float top = -INFINITY;
-  for (int s = 0; s < t.n_split; ++s) top = fmaxf(top, kr.part_ml[(at + s) * 2]);
-  float y[MT] = {}, all = 0.f;
-  for (int s = 0; s < t.n_split; ++s) {
-    const int64_t i = at + s;
-    const float lref = kr.part_ml[i * 2], sum = kr.part_ml[i * 2 + 1];
-    const float f = part_weight(lref, sum, top);
-    all = fmaf(f, sum, all);
+  __shared__ float s_y[16][16][MT + 1];
+  __shared__ float s_ref[16], s_sum[16];
+  const uint32_t share = blockIdx.x / kr.a.cache.Hkv;
+  const int kvh = blockIdx.x % kr.a.cache.Hkv;
+  const Place last = locate<true>(kr, share);
+  const uint64_t begin = share_begin(last.total, kr.n_share, share);
+  if (last.total == 0 || last.at + 1 == begin) return;                      // an empty share
+  const Request rq = request(kr, last.b);
+  const Tile t(kr, rq, (uint32_t)(last.step / rq.steps));
+  const uint64_t t0 = last.at - last.step % rq.steps, t1 = t0 + rq.steps;   // the tile's steps
+  if (t1 == last.at + 1 || t0 < begin) return;                              // it ends here, or began in an earlier share
+  const uint32_t n_part = (uint32_t)((t1 * kr.n_share - 1) / last.total) - share + 1;      // (empty shares among them)
+  // 16 threads have a row; where there are fewer rows than 16, the parts are dealt to several such groups
+  const int rows = t.n_rows > 8 ? 16 : t.n_rows > 4 ? 8 : t.n_rows > 2 ? 4 : t.n_rows, groups = 16 / rows;
+  const int slot = threadIdx.x >> 4, r = slot % rows, g = slot / rows, dl = threadIdx.x & 15;
+  float top = -INFINITY, all = 0.f, y[MT] = {};
+  if (r < t.n_rows && g < groups) {
+    constexpr int AT_ONCE = 4;
+    for (uint32_t p0 = g; p0 < n_part; p0 += AT_ONCE * groups) {
+      float lref[AT_ONCE], sum[AT_ONCE], x[AT_ONCE][MT];
 #pragma unroll
-    for (int d = 0; d < MT; ++d) y[d] = fmaf(f, kr.part_o[i * D + d0 + d], y[d]);
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const uint32_t p = min(p0 + u * groups, n_part - 1);
+        const uint64_t b0 = share_begin(last.total, kr.n_share, share + p);
+        const bool there = p0 + u * groups < n_part && b0 < share_begin(last.total, kr.n_share, share + p + 1);
+        const int64_t at = (((int64_t)kvh * kr.n_share + share + p) * 2 + (b0 < t0 ? 1 : 0)) * ROWS + r;
+        lref[u] = there ? kr.part_ml[at * 2] : -INFINITY;
+        sum[u] = there ? kr.part_ml[at * 2 + 1] : 0.f;
+#pragma unroll
+        for (int d = 0; d < MT; d += 4) {
+          const f4 v = there ? *reinterpret_cast<const f4*>(kr.part_o + at * D + dl * MT + d) : (f4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[u][d + i] = v[i];
+        }
+      }
+      float high = top;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) high = fmaxf(high, lref[u]);
+      const float f0 = part_weight(top, all, high);
+      all *= f0;
+#pragma unroll
+      for (int d = 0; d < MT; ++d) y[d] *= f0;
+      top = high;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const float f = part_weight(lref[u], sum[u], high);
+        all = fmaf(f, sum[u], all);
+#pragma unroll
+        for (int d = 0; d < MT; ++d) y[d] = fmaf(f, x[u][d], y[d]);
+      }
+    }
   }
-  const float inv = top == -INFINITY && all == 0.f ? 0.f : 1.f / all;
-  const int rr = t.row0 + r;
-  T* out = (T*)a.out + ((int64_t)(t.start + rr / kr.G) * a.Hq + (int64_t)blockIdx.y * kr.G + rr % kr.G) * D + d0;
 #pragma unroll
-  for (int d = 0; d < MT; ++d) y[d] = inv == 0.f ? 0.f : y[d] * inv;
-  store_row<T, MT>(out, y);
+  for (int d = 0; d < MT; ++d) s_y[slot][dl][d] = y[d];
+  if (dl == 0) { s_ref[slot] = top; s_sum[slot] = all; }
+  __syncthreads();
+  if (g != 0 || r >= t.n_rows) return;
+  float high = top;
+  for (int i = 1; i < groups; ++i) high = fmaxf(high, s_ref[i * rows + r]);
+  float sum = 0.f, z[MT] = {};
+  for (int i = 0; i < groups; ++i) {
+    const float f = part_weight(s_ref[i * rows + r], s_sum[i * rows + r], high);
+    sum = fmaf(f, s_sum[i * rows + r], sum);
+#pragma unroll
+    for (int d = 0; d < MT; ++d) z[d] = fmaf(f, s_y[i * rows + r][dl][d], z[d]);
+  }
+  const float inv = high == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int d = 0; d < MT; ++d) z[d] = inv == 0.f ? 0.f : z[d] * inv;
+  store_row<T, MT>(out_row<T, D>(kr, t, kvh, r) + dl * MT, z);
 }
 
 template <typename T, int D>
-int run(Kernel& k, int tiles, hipStream_t st) {
-  const dim3 grid(tiles, k.a.cache.Hkv, k.n_split);
+int run(const Kernel& k, hipStream_t st) {
+  const dim3 grid((unsigned)k.n_share * (unsigned)k.a.cache.Hkv);
   if (k.a.cache.shift >= 5) PIPE_KLAUNCH((cache_attn_kernel<T, D, 1>), grid, dim3(WAVES * 64), 0, st, k);
   else PIPE_KLAUNCH((cache_attn_kernel<T, D, 2>), grid, dim3(WAVES * 64), 0, st, k);
   PIPE_HIP(hipGetLastError());
-  if (k.n_split > 1) {
-    PIPE_KLAUNCH((cache_attn_join_kernel<T, D>), dim3(tiles, k.a.cache.Hkv), dim3(256), 0, st, k);
+  if (k.n_share > 1) {
+    PIPE_KLAUNCH((cache_attn_join_kernel<T, D>), grid, dim3(256), 0, st, k);
     PIPE_HIP(hipGetLastError());
   }
   return PIPE_OK;
@@ -547,21 +665,18 @@ int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   k.a = a;
   k.G = a.Hq / a.cache.Hkv;
   k.wide = rows_wide(a.q, a.qs, a.type);
-  const int64_t rows = (int64_t)a.T * k.G, tiles = rows / ROWS + a.B + 1;
-  if (tiles > 0x3fffff) return PIPE_ESHAPE;
-  const int64_t longest = std::min<int64_t>(a.max_length > 0 ? a.max_length : (int64_t)a.width << a.cache.shift, 1 << 30);
-  // Splits: as many as bring the launch to SPLIT_TILES workgroups, each with 256 tokens at least.
-  const int64_t base = std::max<int64_t>((rows + ROWS - 1) / ROWS, std::min(a.B, a.T)) * a.cache.Hkv;
-  k.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(SPLIT_TILES / base, (longest + CHUNK_UNIT - 1) / CHUNK_UNIT));
-  k.chunk = (int)round_up64((longest + k.n_split - 1) / k.n_split, CHUNK_UNIT);
-  if (k.n_split > 1) {
-    // (T * Hq * n_split <= ROWS * SPLIT_TILES: one size serves every call)
-    const size_t parts = (size_t)ROWS * SPLIT_TILES;
+  // No more shares than there are steps, as far as the longest request is known.
+  const int64_t longest = a.max_length > 0 ? a.max_length : (int64_t)a.width << a.cache.shift;
+  const int64_t tiles = std::max<int64_t>(((int64_t)a.T * k.G + ROWS - 1) / ROWS, std::min(a.B, a.T));
+  const int64_t most = (a.D == 64 ? SHARES_64 : SHARES_128) / a.cache.Hkv;
+  k.n_share = (int)std::max<int64_t>(1, std::min(most, tiles * ((longest + UNIT - 1) / UNIT)));
+  if (k.n_share > 1) {
+    const size_t parts = (size_t)SHARES_64 * 2 * ROWS;       // one size serves every call
     k.part_o = (float*)pipe_ws_get(WS_ATTN, parts * (128 + 2) * sizeof(float));
     if (!k.part_o) return pipe_ws_error();
     k.part_ml = k.part_o + parts * 128;
   }
-  if (a.type == PIPE_F32) return a.D == 64 ? run<float, 64>(k, (int)tiles, st) : run<float, 128>(k, (int)tiles, st);
-  if (a.type == PIPE_F16) return a.D == 64 ? run<f16, 64>(k, (int)tiles, st) : run<f16, 128>(k, (int)tiles, st);
-  return a.D == 64 ? run<bf16, 64>(k, (int)tiles, st) : run<bf16, 128>(k, (int)tiles, st);
+  if (a.type == PIPE_F32) return a.D == 64 ? run<float, 64>(k, st) : run<float, 128>(k, st);
+  if (a.type == PIPE_F16) return a.D == 64 ? run<f16, 64>(k, st) : run<f16, 128>(k, st);
+  return a.D == 64 ? run<bf16, 64>(k, st) : run<bf16, 128>(k, st);
 }
