@@ -52,6 +52,7 @@ extern "C" const char* pipe_strerror(int code) {
 struct WsSet {
   PipeWorkspace slot[WS_SLOTS];
   bool words_cleared = false;  // the control words (WS_SCAL) were set to zero
+  bool zeroed[WS_SLOTS] = {};  // pipe_ws_zeroed has cleared the slot's first words
   bool slots_dirty = false;    // the members' max|h| or range slots hold a value no kernel will clear
 };
 static std::mutex g_ws_mu;
@@ -123,6 +124,18 @@ void* pipe_ws_get(int slot, size_t bytes) {
   w.ptr = fresh;
   w.bytes = want;
   return w.ptr;
+}
+
+void* pipe_ws_zeroed(int slot, size_t bytes, size_t zero, int* rc) {
+  void* p = pipe_ws_get(slot, bytes);
+  *rc = p ? PIPE_OK : pipe_ws_error();
+  if (!p || t_ws->zeroed[slot]) return p;
+  // (once: on the null stream, and waited for, since the caller's stream may not be ordered behind it)
+  if (pipe_capturing()) *rc = PIPE_ENOTREADY;
+  else if (!pipe_hip_ok(hipMemset(p, 0, zero), "hipMemset(workspace)") || !pipe_hip_ok(hipStreamSynchronize(nullptr), "hipStreamSynchronize")) *rc = PIPE_EDEVICE;
+  if (*rc) return nullptr;
+  t_ws->zeroed[slot] = true;
+  return p;
 }
 
 static int g_kernel_choice = 0;

@@ -38,6 +38,8 @@ constexpr int WAVES = 4, ROWS = 16, STEP = 32;      // tokens of a wave's step
 constexpr int AHEAD = 2;                            // steps whose loads are in flight while one is worked on
 constexpr int UNIT = WAVES * STEP;                  // tokens of a workgroup's step: one step of every wave
 constexpr int SHARES_128 = 512, SHARES_64 = 768;    // workgroups of a launch: as many as the chip holds at once (2 a unit at head_dim 128, 3 at 64)
+constexpr size_t ATTN_COUNTS = 4096;                // bytes of the counts of parts
+static_assert(SHARES_64 * sizeof(uint32_t) <= ATTN_COUNTS && SHARES_128 <= SHARES_64);
 constexpr float REF_SLACK = 6.f;                    // log2: a row's reference rises only when a score exceeds it by this
 constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE fits fp16
 
@@ -45,14 +47,15 @@ struct Kernel {
   CacheAttnArgs a;
   int G, n_share;   // workgroups of a key/value head
   bool wide;        // 16-byte loads of q
-  float* part_o;    // [Hkv][n_share][2][16][D]
-  float* part_ml;   // [Hkv][n_share][2][16][2]: log2 of the reference weight, sum of weights
+  uint64_t* part_o;     // [Hkv][n_share][2][16 rows][D/32][16]: pairs of outputs
+  uint64_t* part_ml;    // [Hkv][n_share][2][16 rows]: log2 of the reference weight, sum of weights
+  uint32_t* arrived;    // [Hkv][n_share]: parts written of the tile that begins in the share; zero between calls
 };
 
 // The work of a key/value head is the tiles of all requests one after the other, a tile of request b counting the steps of UNIT tokens that
 // its cache has; every workgroup takes an equal share of the steps, wherever it begins and ends.  So requests of any lengths keep all
 // workgroups busy to the end, and one long request is split.  Of a tile that several shares hold, each writes its part -- of its first tile
-// to place 0, of its last to place 1 -- and the join sums them in their order.
+// to place 0, of its last to place 1 -- and whoever comes last sums them, in the shares' order.
 struct Request {
   int b, start, n;              // its fresh tokens (b = B: the rows behind the last request, which see nothing)
   int length;
@@ -78,9 +81,8 @@ struct Place {
 };
 __device__ __forceinline__ uint64_t share_begin(uint64_t total, uint32_t n_share, uint32_t share) { return total * share / n_share; }
 
-// The first place of a share (or the last one, LAST).  By the whole workgroup: every thread sums up to 17 requests, and the one whose sum
+// The first place of a share.  By the whole workgroup: every thread sums up to 17 requests, and the one whose sum
 // holds the place walks them again.
-template <bool LAST>
 __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
   __shared__ uint64_t s_sum[4], s_step;
   __shared__ int s_b;
@@ -108,7 +110,7 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
     before += w < wave ? s_sum[w] : 0;
     p.total += s_sum[w];
   }
-  p.at = LAST ? share_begin(p.total, k.n_share, share + 1) - 1 : share_begin(p.total, k.n_share, share);
+  p.at = share_begin(p.total, k.n_share, share);
   if (before <= p.at && p.at < before + mine) {
     for (int b = b0; b < b1; ++b) {
       const Request r = request(k, b);
@@ -293,17 +295,97 @@ struct Walk {
   }
 };
 
+// Two floats to and from memory at the scope of the device: the workgroups of a tile sit behind different L2 caches.
+__device__ __forceinline__ void put_pair(uint64_t* p, float x, float y) {
+  __hip_atomic_store(p, ((uint64_t)__float_as_uint(y) << 32) | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_pair(const uint64_t* p) {
+  const uint64_t v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// The parts of a tile together, in the shares' order: the tile's steps begin at t0, in share p0; n_part shares from there on (empty ones among
+// them).  scratch: 16 * 16 * (D/16 + 1) + 32 floats of LDS.
+template <typename T, int D>
+__device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, uint64_t total, uint64_t t0, uint32_t p0, uint32_t n_part, float* scratch) {
+  constexpr int MT = D / 16;
+  float (*s_y)[16][MT + 1] = reinterpret_cast<float (*)[16][MT + 1]>(scratch);
+  float* s_ref = scratch + 16 * 16 * (MT + 1);
+  float* s_sum = s_ref + 16;
+  // 16 threads have a row; where there are fewer rows than 16, the parts are dealt to several such groups
+  const int rows = t.n_rows > 8 ? 16 : t.n_rows > 4 ? 8 : t.n_rows > 2 ? 4 : t.n_rows, groups = 16 / rows;
+  const int slot = threadIdx.x >> 4, r = slot % rows, g = slot / rows, dl = threadIdx.x & 15;
+  float top = -INFINITY, all = 0.f, y[MT] = {};
+  if (r < t.n_rows) {
+    constexpr int AT_ONCE = 4;
+    for (uint32_t q = g; q < n_part; q += AT_ONCE * groups) {
+      float lref[AT_ONCE], sum[AT_ONCE], x[AT_ONCE][MT];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const uint32_t p = min(q + u * groups, n_part - 1) + p0;
+        const uint64_t b0 = share_begin(total, kr.n_share, p);
+        const bool there = q + u * groups < n_part && b0 < share_begin(total, kr.n_share, p + 1);
+        const int64_t at = (((int64_t)kvh * kr.n_share + p) * 2 + (b0 < t0 ? 1 : 0)) * ROWS + r;
+        const float2 m = there ? get_pair(kr.part_ml + at) : make_float2(-INFINITY, 0.f);
+        lref[u] = m.x;
+        sum[u] = m.y;
+#pragma unroll
+        for (int d = 0; d < MT / 2; ++d) {
+          const float2 v = there ? get_pair(kr.part_o + (at * (MT / 2) + d) * 16 + dl) : make_float2(0.f, 0.f);
+          x[u][2 * d] = v.x;
+          x[u][2 * d + 1] = v.y;
+        }
+      }
+      float high = top;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) high = fmaxf(high, lref[u]);
+      const float f0 = part_weight(top, all, high);
+      all *= f0;
+#pragma unroll
+      for (int d = 0; d < MT; ++d) y[d] *= f0;
+      top = high;
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const float f = part_weight(lref[u], sum[u], high);
+        all = fmaf(f, sum[u], all);
+#pragma unroll
+        for (int d = 0; d < MT; ++d) y[d] = fmaf(f, x[u][d], y[d]);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 0; d < MT; ++d) s_y[slot][dl][d] = y[d];
+  if (dl == 0) { s_ref[slot] = top; s_sum[slot] = all; }
+  __syncthreads();
+  if (g == 0 && r < t.n_rows) {
+    float high = top;
+    for (int i = 1; i < groups; ++i) high = fmaxf(high, s_ref[i * rows + r]);
+    float sum = 0.f, z[MT] = {};
+    for (int i = 0; i < groups; ++i) {
+      const float f = part_weight(s_ref[i * rows + r], s_sum[i * rows + r], high);
+      sum = fmaf(f, s_sum[i * rows + r], sum);
+#pragma unroll
+      for (int d = 0; d < MT; ++d) z[d] = fmaf(f, s_y[i * rows + r][dl][d], z[d]);
+    }
+    const float inv = high == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int d = 0; d < MT; ++d) z[d] = inv == 0.f ? 0.f : z[d] * inv;
+    store_row<T, MT>(out_row<T, D>(kr, t, kvh, r) + dl * MT, z);
+  }
+}
+
 template <typename T, int D, int NB>
 __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel kr) {
   constexpr bool FINE = sizeof(T) == 4;                // fp32: centred codes, two terms
   constexpr int KS = D / 32, MT = D / 16, NT = FINE ? 2 : 1;
   __shared__ float s_o[WAVES][ROWS][D + 4];
   __shared__ float s_ref[WAVES][ROWS], s_sum[WAVES][ROWS];
+  __shared__ bool s_last;
   const CacheAttnArgs& a = kr.a;
   const uint32_t share = blockIdx.x / a.cache.Hkv;
   const int kvh = blockIdx.x % a.cache.Hkv;
-  const Place first = locate<false>(kr, share);
-  uint64_t left = share_begin(first.total, kr.n_share, share + 1) - first.at;
+  const Place first = locate(kr, share);
+  uint64_t pos = first.at, left = share_begin(first.total, kr.n_share, share + 1) - pos;
   if (left == 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
@@ -552,10 +634,27 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
       store_row<T, MT>(out_row<T, D>(kr, t, kvh, r) + d0, y);
     } else {
       const int64_t at = (((int64_t)kvh * kr.n_share + share) * 2 + place) * ROWS + r;
-      store_row<float, MT>(kr.part_o + at * D + d0, y);
-      if (d0 == 0) { kr.part_ml[at * 2] = top; kr.part_ml[at * 2 + 1] = all; }
+#pragma unroll
+      for (int d = 0; d < MT / 2; ++d) put_pair(kr.part_o + (at * (MT / 2) + d) * 16 + (threadIdx.x & 15), y[2 * d], y[2 * d + 1]);
+      if (d0 == 0) put_pair(kr.part_ml + at, top, all);
     }
   }
+  if (n_steps != rq.steps) {
+    // Every wave's stores have reached the device's scope before the count says so.
+    const uint64_t t0 = pos - step0, t1 = t0 + rq.steps;
+    const uint32_t p0 = (uint32_t)(((t0 + 1) * kr.n_share - 1) / first.total), p1 = (uint32_t)((t1 * kr.n_share - 1) / first.total);
+    __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
+    __syncthreads();
+    // (parts: the shares from p0 to p1; where there are fewer steps than shares, as many as the tile has steps)
+    uint32_t* count = kr.arrived + kvh * kr.n_share + p0;
+    if (threadIdx.x == 0) s_last = atomicAdd(count, 1u) == (first.total < kr.n_share ? rq.steps : p1 - p0 + 1) - 1;
+    __syncthreads();
+    if (s_last) {
+      join<T, D>(kr, t, kvh, first.total, t0, p0, p1 - p0 + 1, &s_o[0][0][0]);
+      if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  pos += n_steps;
   left -= n_steps;
   if (left == 0) break;
   __syncthreads();                         // (the next part's outputs come to the same places)
@@ -568,92 +667,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   }
 }
 
-// The parts of a tile that several shares hold together, in the shares' order, by the workgroup of the first of them.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void cache_attn_join_kernel(const Kernel kr) {
-  constexpr int MT = D / 16;
-  __shared__ float s_y[16][16][MT + 1];
-  __shared__ float s_ref[16], s_sum[16];
-  const uint32_t share = blockIdx.x / kr.a.cache.Hkv;
-  const int kvh = blockIdx.x % kr.a.cache.Hkv;
-  const Place last = locate<true>(kr, share);
-  const uint64_t begin = share_begin(last.total, kr.n_share, share);
-  if (last.total == 0 || last.at + 1 == begin) return;                      // an empty share
-  const Request rq = request(kr, last.b);
-  const Tile t(kr, rq, (uint32_t)(last.step / rq.steps));
-  const uint64_t t0 = last.at - last.step % rq.steps, t1 = t0 + rq.steps;   // the tile's steps
-  if (t1 == last.at + 1 || t0 < begin) return;                              // it ends here, or began in an earlier share
-  const uint32_t n_part = (uint32_t)((t1 * kr.n_share - 1) / last.total) - share + 1;      // (empty shares among them)
-  // 16 threads have a row; where there are fewer rows than 16, the parts are dealt to several such groups
-  const int rows = t.n_rows > 8 ? 16 : t.n_rows > 4 ? 8 : t.n_rows > 2 ? 4 : t.n_rows, groups = 16 / rows;
-  const int slot = threadIdx.x >> 4, r = slot % rows, g = slot / rows, dl = threadIdx.x & 15;
-  float top = -INFINITY, all = 0.f, y[MT] = {};
-  if (r < t.n_rows && g < groups) {
-    constexpr int AT_ONCE = 4;
-    for (uint32_t p0 = g; p0 < n_part; p0 += AT_ONCE * groups) {
-      float lref[AT_ONCE], sum[AT_ONCE], x[AT_ONCE][MT];
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        const uint32_t p = min(p0 + u * groups, n_part - 1);
-        const uint64_t b0 = share_begin(last.total, kr.n_share, share + p);
-        const bool there = p0 + u * groups < n_part && b0 < share_begin(last.total, kr.n_share, share + p + 1);
-        const int64_t at = (((int64_t)kvh * kr.n_share + share + p) * 2 + (b0 < t0 ? 1 : 0)) * ROWS + r;
-        lref[u] = there ? kr.part_ml[at * 2] : -INFINITY;
-        sum[u] = there ? kr.part_ml[at * 2 + 1] : 0.f;
-#pragma unroll
-        for (int d = 0; d < MT; d += 4) {
-          const f4 v = there ? *reinterpret_cast<const f4*>(kr.part_o + at * D + dl * MT + d) : (f4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[u][d + i] = v[i];
-        }
-      }
-      float high = top;
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) high = fmaxf(high, lref[u]);
-      const float f0 = part_weight(top, all, high);
-      all *= f0;
-#pragma unroll
-      for (int d = 0; d < MT; ++d) y[d] *= f0;
-      top = high;
-#pragma unroll
-      for (int u = 0; u < AT_ONCE; ++u) {
-        const float f = part_weight(lref[u], sum[u], high);
-        all = fmaf(f, sum[u], all);
-#pragma unroll
-        for (int d = 0; d < MT; ++d) y[d] = fmaf(f, x[u][d], y[d]);
-      }
-    }
-  }
-#pragma unroll
-  for (int d = 0; d < MT; ++d) s_y[slot][dl][d] = y[d];
-  if (dl == 0) { s_ref[slot] = top; s_sum[slot] = all; }
-  __syncthreads();
-  if (g != 0 || r >= t.n_rows) return;
-  float high = top;
-  for (int i = 1; i < groups; ++i) high = fmaxf(high, s_ref[i * rows + r]);
-  float sum = 0.f, z[MT] = {};
-  for (int i = 0; i < groups; ++i) {
-    const float f = part_weight(s_ref[i * rows + r], s_sum[i * rows + r], high);
-    sum = fmaf(f, s_sum[i * rows + r], sum);
-#pragma unroll
-    for (int d = 0; d < MT; ++d) z[d] = fmaf(f, s_y[i * rows + r][dl][d], z[d]);
-  }
-  const float inv = high == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int d = 0; d < MT; ++d) z[d] = inv == 0.f ? 0.f : z[d] * inv;
-  store_row<T, MT>(out_row<T, D>(kr, t, kvh, r) + dl * MT, z);
-}
-
 template <typename T, int D>
 int run(const Kernel& k, hipStream_t st) {
   const dim3 grid((unsigned)k.n_share * (unsigned)k.a.cache.Hkv);
   if (k.a.cache.shift >= 5) PIPE_KLAUNCH((cache_attn_kernel<T, D, 1>), grid, dim3(WAVES * 64), 0, st, k);
   else PIPE_KLAUNCH((cache_attn_kernel<T, D, 2>), grid, dim3(WAVES * 64), 0, st, k);
   PIPE_HIP(hipGetLastError());
-  if (k.n_share > 1) {
-    PIPE_KLAUNCH((cache_attn_join_kernel<T, D>), grid, dim3(256), 0, st, k);
-    PIPE_HIP(hipGetLastError());
-  }
   return PIPE_OK;
 }
 
@@ -672,9 +691,12 @@ int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   k.n_share = (int)std::max<int64_t>(1, std::min(most, tiles * ((longest + UNIT - 1) / UNIT)));
   if (k.n_share > 1) {
     const size_t parts = (size_t)SHARES_64 * 2 * ROWS;       // one size serves every call
-    k.part_o = (float*)pipe_ws_get(WS_ATTN, parts * (128 + 2) * sizeof(float));
-    if (!k.part_o) return pipe_ws_error();
-    k.part_ml = k.part_o + parts * 128;
+    int rc = PIPE_OK;
+    uint8_t* ws = (uint8_t*)pipe_ws_zeroed(WS_ATTN, ATTN_COUNTS + parts * (128 + 2) * sizeof(float), ATTN_COUNTS, &rc);
+    if (!ws) return rc;
+    k.arrived = (uint32_t*)ws;
+    k.part_ml = (uint64_t*)(ws + ATTN_COUNTS);
+    k.part_o = k.part_ml + parts;
   }
   if (a.type == PIPE_F32) return a.D == 64 ? run<float, 64>(k, st) : run<float, 128>(k, st);
   if (a.type == PIPE_F16) return a.D == 64 ? run<f16, 64>(k, st) : run<f16, 128>(k, st);

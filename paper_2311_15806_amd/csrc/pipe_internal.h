@@ -273,6 +273,8 @@ struct PipeWorkspace {
 // stream is being captured and the block would have to grow).
 void* pipe_ws_get(int slot, size_t bytes);
 int pipe_ws_error();
+// The same for a slot of one size whose first `zero` bytes are zero when it is first handed out; nullptr and *rc on failure.
+void* pipe_ws_zeroed(int slot, size_t bytes, size_t zero, int* rc);
 // true while a pipe_prepare* call walks a forward entry point: sizes and schedules are set up,
 // nothing is launched or copied
 bool pipe_dry_run();
