@@ -743,17 +743,36 @@ def _type(dtype: torch.dtype) -> int:
     return t
 
 
+# (These calls are a few microseconds on the device at decode sizes: what they ask of a tensor they ask once.)
 def _heads(t: torch.Tensor, name: str):
     """(address, token stride, head stride) of [tokens, heads, head_dim] with a dense last axis."""
-    if not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+    s = t.stride()
+    if len(s) != 3 or not t.is_cuda or (s[2] != 1 and t.shape[2] > 1):
         raise ValueError("%s must be a device tensor [tokens, heads, head_dim] with a dense last axis" % name)
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    return t.data_ptr(), s[0], s[1]
 
 
-def _cache_pages(cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int) -> int:
-    if cache.dim() != 2 or cache.shape[1] != pipe_cache_page_bytes(kv_heads, head_dim, page_size):
-        raise ValueError("the cache must be uint8 [pages, pipe_cache_page_bytes(kv_heads, head_dim, page_size)]")
-    return cache.shape[0]
+def _ints(t: torch.Tensor) -> int:
+    if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous int32 device tensor")
+    return t.data_ptr()
+
+
+def _cache(cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int):
+    """(address, pages)"""
+    shape = cache.shape
+    if len(shape) != 2 or shape[1] != kv_heads * page_size * (head_dim + 8) or cache.dtype is not torch.uint8 or not cache.is_cuda \
+            or not cache.is_contiguous():
+        raise ValueError("the cache must be a contiguous uint8 device tensor [pages, pipe_cache_page_bytes(kv_heads, head_dim, page_size)]")
+    return cache.data_ptr(), shape[0]
+
+
+def _attention_out(q: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
+    if out is None:
+        return torch.empty_like(q, memory_format=torch.contiguous_format)
+    if out.shape != q.shape or out.dtype is not q.dtype or not out.is_cuda or not out.is_contiguous():
+        raise ValueError("output has the wrong shape or type, or is not contiguous")
+    return out
 
 
 def pipe_cache_page_bytes(kv_heads: int, head_dim: int, page_size: int) -> int:
@@ -769,15 +788,15 @@ def pipe_cache_plan(cached: torch.Tensor, fresh: torch.Tensor, page_size: int, f
     """Tables of the next step (all int32): request b holds cached[b] tokens and brings fresh[b]; new pages come from free[used[0]:]
     and enter table [B, width] in place.  Returns (lengths [B], starts [B+1], slots [tokens], positions [tokens], counts [3]);
     counts -- pages used, pages missing, tokens cut off -- is the next step's `used`."""
-    B, i32 = cached.shape[0], torch.int32
+    B = cached.shape[0]
     if cached.dim() != 1 or fresh.shape != cached.shape or table.dim() != 2 or table.shape[0] != B or free.dim() != 1 or used.numel() < 1:
         raise ValueError("cached and fresh are [B], table is [B, width], free is [pages], used holds a number")
     if tokens < 0:
         raise ValueError("tokens must not be negative")
     lengths, starts, slots, positions, counts = cached.new_empty(2 * B + 4 + 2 * tokens).split([B, B + 1, tokens, tokens, 3])
-    _check(_lib.pipe_cache_plan(_ptr(cached, i32), _ptr(fresh, i32), B, int(page_size), _ptr(free, i32), free.shape[0], _ptr(used, i32),
-                                _ptr(table, i32), table.shape[1], int(tokens), lengths.data_ptr(), starts.data_ptr(), slots.data_ptr(),
-                                positions.data_ptr(), counts.data_ptr(), _stream()), "pipe_cache_plan")
+    _check(_lib.pipe_cache_plan(_ints(cached), _ints(fresh), B, page_size, _ints(free), free.shape[0], _ints(used), _ints(table),
+                                table.shape[1], tokens, lengths.data_ptr(), starts.data_ptr(), slots.data_ptr(), positions.data_ptr(),
+                                counts.data_ptr(), _stream()), "pipe_cache_plan")
     return lengths, starts, slots, positions, counts
 
 
@@ -786,20 +805,20 @@ def pipe_cache_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cach
     kp, kt, kh = _heads(k, "k")
     vp, vt, vh = _heads(v, "v")
     T, H, D = k.shape
-    if v.shape != k.shape or v.dtype != k.dtype or tuple(slots.shape) != (T,):
+    if v.shape != k.shape or v.dtype is not k.dtype or slots.shape != (T,):
         raise ValueError("k and v must have one shape and type, slots one entry a token")
-    _check(_lib.pipe_cache_write(kp, vp, _type(k.dtype), T, H, D, kt, kh, vt, vh, _ptr(slots, torch.int32), _ptr(cache, torch.uint8),
-                                 _cache_pages(cache, page_size, H, D), int(page_size), _stream()), "pipe_cache_write")
+    cp, pages = _cache(cache, page_size, H, D)
+    _check(_lib.pipe_cache_write(kp, vp, _type(k.dtype), T, H, D, kt, kh, vt, vh, _ints(slots), cp, pages, page_size, _stream()),
+           "pipe_cache_write")
 
 
 def pipe_cache_read(slots: torch.Tensor, cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int,
                     dtype: torch.dtype = torch.float32):
     """(k, v) [T, kv_heads, head_dim]: the values that the codes at slots [T] stand for (zeros for a slot outside the cache)."""
     T = slots.shape[0]
-    k = torch.empty((T, kv_heads, head_dim), dtype=dtype, device=cache.device)
-    v = torch.empty_like(k)
-    _check(_lib.pipe_cache_read(_ptr(cache, torch.uint8), _cache_pages(cache, page_size, kv_heads, head_dim), int(page_size),
-                                _ptr(slots, torch.int32), T, int(kv_heads), int(head_dim), _type(dtype), k.data_ptr(), v.data_ptr(),
+    cp, pages = _cache(cache, page_size, kv_heads, head_dim)
+    k, v = torch.empty((2, T, kv_heads, head_dim), dtype=dtype, device=cache.device).unbind(0)
+    _check(_lib.pipe_cache_read(cp, pages, page_size, _ints(slots), T, kv_heads, head_dim, _type(dtype), k.data_ptr(), v.data_ptr(),
                                 _stream()), "pipe_cache_read")
     return k, v
 
@@ -812,16 +831,13 @@ def pipe_cache_attention(q: torch.Tensor, starts: torch.Tensor, lengths: torch.T
     qp, qt, qh = _heads(q, "q")
     T, H, D = q.shape
     B = lengths.shape[0]
-    if tuple(starts.shape) != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
+    if starts.shape != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
         raise ValueError("starts is [B + 1], lengths [B], table [B, width]")
-    y = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
-    if y.shape != q.shape or y.dtype != q.dtype:
-        raise ValueError("output has the wrong shape or type")
-    i32 = torch.int32
-    _check(_lib.pipe_cache_attention(qp, _type(q.dtype), T, H, int(kv_heads), D, qt, qh, _ptr(starts, i32), _ptr(lengths, i32), B,
-                                     _ptr(cache, torch.uint8), _cache_pages(cache, page_size, kv_heads, D), int(page_size),
-                                     _ptr(table, i32), table.shape[1], D ** -0.5 if scale is None else float(scale), int(max_length),
-                                     _ptr(y), _stream()), "pipe_cache_attention")
+    cp, pages = _cache(cache, page_size, kv_heads, D)
+    y = _attention_out(q, out)
+    _check(_lib.pipe_cache_attention(qp, _type(q.dtype), T, H, kv_heads, D, qt, qh, _ints(starts), _ints(lengths), B, cp, pages, page_size,
+                                     _ints(table), table.shape[1], D ** -0.5 if scale is None else scale, max_length, y.data_ptr(),
+                                     _stream()), "pipe_cache_attention")
     return y
 
 
@@ -840,15 +856,14 @@ def pipe_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sta
     kp, kt, kh = _heads(k, "k")
     vp, vt, vh = _heads(v, "v")
     T, H, D = q.shape
-    if k.shape != v.shape or k.shape[2] != D or k.dtype != q.dtype or v.dtype != q.dtype:
+    Tk, Hkv, Dk = k.shape
+    if v.shape != (Tk, Hkv, D) or Dk != D or k.dtype is not q.dtype or v.dtype is not q.dtype:
         raise ValueError("k and v must have one shape, and q's head_dim and type")
-    if starts.dim() != 1 or starts.shape[0] < 2 or (starts_k is not None and starts_k.shape != starts.shape):
+    B = starts.shape[0] - 1
+    if starts.dim() != 1 or B < 1 or (starts_k is not None and starts_k.shape != starts.shape):
         raise ValueError("starts and starts_k are [sequences + 1]")
-    y = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
-    if y.shape != q.shape or y.dtype != q.dtype:
-        raise ValueError("output has the wrong shape or type")
-    i32 = torch.int32
-    _check(_lib.pipe_prompt_attention(qp, kp, vp, _type(q.dtype), T, k.shape[0], H, k.shape[1], D, qt, qh, kt, kh, vt, vh,
-                                      _ptr(starts, i32), _ptr(starts_k, i32), starts.shape[0] - 1, 1 if causal else 0,
-                                      D ** -0.5 if scale is None else float(scale), _ptr(y), _stream()), "pipe_prompt_attention")
+    y = _attention_out(q, out)
+    _check(_lib.pipe_prompt_attention(qp, kp, vp, _type(q.dtype), T, Tk, H, Hkv, D, qt, qh, kt, kh, vt, vh, _ints(starts),
+                                      None if starts_k is None else _ints(starts_k), B, 1 if causal else 0,
+                                      D ** -0.5 if scale is None else scale, y.data_ptr(), _stream()), "pipe_prompt_attention")
     return y

@@ -45,7 +45,8 @@ constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE
 
 struct Kernel {
   CacheAttnArgs a;
-  int G, n_share;   // workgroups of a key/value head
+  int G;
+  uint32_t n_share; // workgroups of a key/value head
   bool wide;        // 16-byte loads of q
   uint64_t* part_o;     // [Hkv][n_share][2][16 rows][D/32][16]: pairs of outputs
   uint64_t* part_ml;    // [Hkv][n_share][2][16 rows]: log2 of the reference weight, sum of weights
@@ -58,52 +59,78 @@ struct Kernel {
 // to place 0, of its last to place 1 -- and whoever comes last sums them, in the shares' order.
 struct Request {
   int b, start, n;              // its fresh tokens (b = B: the rows behind the last request, which see nothing)
-  int length;
+  int length, held;             // cached tokens, and those of them that its table has room for
   uint32_t tiles, steps;        // ... each of so many steps
 };
+__device__ __forceinline__ Request make_request(const Kernel& k, int b, int start, int n, int length) {
+  Request r;
+  r.b = b; r.start = start; r.n = n; r.length = length;
+  r.held = (int)min((int64_t)length, min((int64_t)k.a.width << k.a.cache.shift, (int64_t)0x7ffff000));
+  r.tiles = ((uint32_t)n * (uint32_t)k.G + ROWS - 1) / ROWS;
+  r.steps = max(1u, ((uint32_t)r.held + UNIT - 1) / UNIT);
+  return r;
+}
 __device__ __forceinline__ Request request(const Kernel& k, int b) {
   const CacheAttnArgs& a = k.a;
   auto start_of = [&](int i) { return i > 0 ? min(max(a.starts[i], 0), a.T) : 0; };
-  Request r;
-  r.b = b;
-  r.start = start_of(b);
-  r.n = max(0, (b < a.B ? start_of(b + 1) : a.T) - r.start);
-  r.length = b < a.B ? (int)min((int64_t)max(0, a.lengths[b]), min((int64_t)a.width << a.cache.shift, (int64_t)0x7ffff000)) : 0;
-  r.tiles = ((uint32_t)r.n * (uint32_t)k.G + ROWS - 1) / ROWS;
-  r.steps = max(1u, ((uint32_t)r.length + UNIT - 1) / UNIT);
-  return r;
+  const int start = start_of(b);
+  return make_request(k, b, start, max(0, (b < a.B ? start_of(b + 1) : a.T) - start), b < a.B ? max(0, a.lengths[b]) : 0);
+}
+// Where a share begins.  (All steps of a head together are under 2^31: the launch sees to it.)
+__device__ __forceinline__ uint32_t share_begin(uint32_t total, uint32_t n_share, uint32_t share) {
+  return (uint32_t)((uint64_t)total * share / n_share);
+}
+// the share that holds a step: the last one that begins at or before it
+__device__ __forceinline__ uint32_t share_of(uint32_t total, uint32_t n_share, uint32_t step) {
+  return (uint32_t)(((uint64_t)(step + 1) * n_share - 1) / total);
 }
 struct Place {
-  uint64_t total;               // steps of the head
-  uint64_t at;                  // the place looked for ...
-  int b;                        // ... lies in request b,
-  uint64_t step;                // ... this many of its steps on
+  uint32_t total, at;           // steps of the head, and the first of the share,
+  uint32_t step;                // which is this step
+  Request r;                    // of this request
 };
-__device__ __forceinline__ uint64_t share_begin(uint64_t total, uint32_t n_share, uint32_t share) { return total * share / n_share; }
-
-// The first place of a share.  By the whole workgroup: every thread sums up to 17 requests, and the one whose sum
-// holds the place walks them again.
-__device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
-  __shared__ uint64_t s_sum[4], s_step;
-  __shared__ int s_b;
-  const int B1 = k.a.B + 1, per = (B1 + 255) / 256, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int b0 = min(B1, (int)threadIdx.x * per), b1 = min(B1, b0 + per);
-  uint64_t mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const Request r = request(k, b);
-    mine += (uint64_t)r.tiles * r.steps;
-  }
-  uint64_t inc = mine;
+template <typename T>
+__device__ __forceinline__ T of_lane(T x, int lane) { return (T)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {     // inclusive
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = __shfl_up(inc, d);
-    if (lane >= d) inc += o;
+    const uint32_t o = __shfl_up(x, d);
+    if (lane >= d) x += o;
   }
+  return x;
+}
+
+// The first place of a share.  Up to 63 requests: every wave for itself, a lane a request.  More: the workgroup together, a thread sums
+// every 256th part of them, and the one whose sum holds the place walks them again.
+__device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
+  __shared__ uint32_t s_sum[4], s_step;
+  __shared__ int s_b;
+  const int B1 = k.a.B + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Place p;
+  if (B1 <= 64) {
+    const Request r = request(k, min(lane, k.a.B));
+    const uint32_t mine = lane < B1 ? r.tiles * r.steps : 0u, inc = wave_scan(mine);
+    p.total = of_lane(inc, 63);
+    p.at = share_begin(p.total, k.n_share, share);
+    const unsigned long long behind = __ballot(inc > p.at);
+    const int b = behind ? __builtin_ctzll(behind) : 0;
+    p.step = p.at - of_lane(inc - mine, b);
+    p.r = make_request(k, b, of_lane(r.start, b), of_lane(r.n, b), of_lane(r.length, b));
+    return p;
+  }
+  const int per = (B1 + 255) / 256;
+  const int b0 = min(B1, (int)threadIdx.x * per), b1 = min(B1, b0 + per);
+  uint32_t mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const Request r = request(k, b);
+    mine += r.tiles * r.steps;
+  }
+  const uint32_t inc = wave_scan(mine);
   if (lane == 63) s_sum[wave] = inc;
   if (threadIdx.x == 0) s_b = 0;
   __syncthreads();
-  uint64_t before = inc - mine;
-  Place p;
+  uint32_t before = inc - mine;
   p.total = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -114,7 +141,7 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
   if (before <= p.at && p.at < before + mine) {
     for (int b = b0; b < b1; ++b) {
       const Request r = request(k, b);
-      const uint64_t c = (uint64_t)r.tiles * r.steps;
+      const uint32_t c = r.tiles * r.steps;
       if (p.at < before + c) {
         s_b = b;
         s_step = p.at - before;
@@ -124,8 +151,10 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
     }
   }
   __syncthreads();
-  p.b = __builtin_amdgcn_readfirstlane(s_b);
-  p.step = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(s_step >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)s_step);
+  p.total = __builtin_amdgcn_readfirstlane(p.total);
+  p.at = __builtin_amdgcn_readfirstlane(p.at);
+  p.step = __builtin_amdgcn_readfirstlane(s_step);
+  p.r = request(k, __builtin_amdgcn_readfirstlane(s_b));
   return p;
 }
 
@@ -137,9 +166,8 @@ struct Tile {
     row0 = (int)(i * ROWS);
     n_rows = min(ROWS, r.n * k.G - row0);
     // (the table's width cuts a length short, not the places of the queries)
-    const int length = r.b < k.a.B ? max(0, k.a.lengths[r.b]) : 0;
-    first_seen = length - r.n + 1;
-    end = min(r.length, max(0, first_seen + (row0 + n_rows - 1) / k.G));
+    first_seen = r.length - r.n + 1;
+    end = min(r.held, max(0, first_seen + (row0 + n_rows - 1) / k.G));
   }
 };
 
@@ -307,7 +335,7 @@ __device__ __forceinline__ float2 get_pair(const uint64_t* p) {
 // The parts of a tile together, in the shares' order: the tile's steps begin at t0, in share p0; n_part shares from there on (empty ones among
 // them).  scratch: 16 * 16 * (D/16 + 1) + 32 floats of LDS.
 template <typename T, int D>
-__device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, uint64_t total, uint64_t t0, uint32_t p0, uint32_t n_part, float* scratch) {
+__device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, uint32_t total, uint32_t t0, uint32_t p0, uint32_t n_part, float* scratch) {
   constexpr int MT = D / 16;
   float (*s_y)[16][MT + 1] = reinterpret_cast<float (*)[16][MT + 1]>(scratch);
   float* s_ref = scratch + 16 * 16 * (MT + 1);
@@ -323,7 +351,7 @@ __device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, u
 #pragma unroll
       for (int u = 0; u < AT_ONCE; ++u) {
         const uint32_t p = min(q + u * groups, n_part - 1) + p0;
-        const uint64_t b0 = share_begin(total, kr.n_share, p);
+        const uint32_t b0 = share_begin(total, kr.n_share, p);
         const bool there = q + u * groups < n_part && b0 < share_begin(total, kr.n_share, p + 1);
         const int64_t at = (((int64_t)kvh * kr.n_share + p) * 2 + (b0 < t0 ? 1 : 0)) * ROWS + r;
         const float2 m = there ? get_pair(kr.part_ml + at) : make_float2(-INFINITY, 0.f);
@@ -375,7 +403,7 @@ __device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, u
 }
 
 template <typename T, int D, int NB>
-__global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel kr) {
+__global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel(const Kernel kr) {
   constexpr bool FINE = sizeof(T) == 4;                // fp32: centred codes, two terms
   constexpr int KS = D / 32, MT = D / 16, NT = FINE ? 2 : 1;
   __shared__ float s_o[WAVES][ROWS][D + 4];
@@ -385,17 +413,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   const uint32_t share = blockIdx.x / a.cache.Hkv;
   const int kvh = blockIdx.x % a.cache.Hkv;
   const Place first = locate(kr, share);
-  uint64_t pos = first.at, left = share_begin(first.total, kr.n_share, share + 1) - pos;
+  uint32_t pos = first.at, left = share_begin(first.total, kr.n_share, share + 1) - pos;
   if (left == 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
   const Bits bits;
-  Request rq = request(kr, first.b);
-  uint32_t tile = (uint32_t)(first.step / rq.steps), step0 = (uint32_t)(first.step % rq.steps);
+  Request rq = first.r;
+  uint32_t tile = first.step / rq.steps, step0 = first.step % rq.steps;
 
   for (int place = 0;; place = 1) {        // one tile's part after the other
   const Tile t(kr, rq, tile);
-  const uint32_t n_steps = (uint32_t)min((uint64_t)(rq.steps - step0), left);
+  const uint32_t n_steps = min(rq.steps - step0, left);
   const Walk<D, NB> w(a, t.b, kvh, l16, kg);
 
   // q: row l16, the values that meet the words kg * KS .. of a token
@@ -641,8 +669,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void cache_attn_kernel(const Kernel 
   }
   if (n_steps != rq.steps) {
     // Every wave's stores have reached the device's scope before the count says so.
-    const uint64_t t0 = pos - step0, t1 = t0 + rq.steps;
-    const uint32_t p0 = (uint32_t)(((t0 + 1) * kr.n_share - 1) / first.total), p1 = (uint32_t)((t1 * kr.n_share - 1) / first.total);
+    const uint32_t t0 = pos - step0, t1 = t0 + rq.steps;
+    const uint32_t p0 = share_of(first.total, kr.n_share, t0), p1 = share_of(first.total, kr.n_share, t1 - 1);
     __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
     __syncthreads();
     // (parts: the shares from p0 to p1; where there are fewer steps than shares, as many as the tile has steps)
@@ -684,11 +712,14 @@ int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   k.a = a;
   k.G = a.Hq / a.cache.Hkv;
   k.wide = rows_wide(a.q, a.qs, a.type);
-  // No more shares than there are steps, as far as the longest request is known.
+  // No more shares than there are steps, as far as the longest request is known; tiles of up to 3 steps stay whole (300 tokens: 9.8 us a
+  // call whole, 11.0 in parts; 777 tokens 12.5 and 11.1).
   const int64_t longest = a.max_length > 0 ? a.max_length : (int64_t)a.width << a.cache.shift;
   const int64_t tiles = std::max<int64_t>(((int64_t)a.T * k.G + ROWS - 1) / ROWS, std::min(a.B, a.T));
   const int64_t most = (a.D == 64 ? SHARES_64 : SHARES_128) / a.cache.Hkv;
-  k.n_share = (int)std::max<int64_t>(1, std::min(most, tiles * ((longest + UNIT - 1) / UNIT)));
+  const int64_t room = std::min<int64_t>((int64_t)a.width << a.cache.shift, 0x7ffff000);
+  if ((((int64_t)a.T * k.G + ROWS - 1) / ROWS + a.B + 1) * (room / UNIT + 1) > 0x7fffffff) return PIPE_ESHAPE;
+  k.n_share = (uint32_t)std::max<int64_t>(1, std::min(most, tiles * (longest <= 3 * UNIT ? 1 : (longest + UNIT - 1) / UNIT)));
   if (k.n_share > 1) {
     const size_t parts = (size_t)SHARES_64 * 2 * ROWS;       // one size serves every call
     int rc = PIPE_OK;
