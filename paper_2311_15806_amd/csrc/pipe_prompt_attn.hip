@@ -24,9 +24,10 @@ __device__ __forceinline__ f16v mfma(u4 x, u4 y, f16v c, bf16) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, x), __builtin_bit_cast(b8, y), c, 0, 0, 0);
 }
 template <typename T>
-__device__ __forceinline__ uint32_t pack(float x, float y) {
-  struct { T a, b; } v = {(T)x, (T)y};
-  return __builtin_bit_cast(uint32_t, v);
+__device__ __forceinline__ uint32_t pack(float x, float y) {      // (as a vector: one conversion for both)
+  typedef T T2 __attribute__((ext_vector_type(2)));
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){x, y}, T2));
 }
 
 struct Kernel {
@@ -74,7 +75,7 @@ struct Row {
   const T* q;
   T* out;
   int seen;                   // keys this row sees
-  int end;                    // keys any row of the workgroup sees
+  int end, full;              // keys any row of the workgroup sees, and keys that all of them see
   int wave_end, wave_full;    // keys any row of the wave sees, and keys that all of them see
   __device__ __forceinline__ Row(const Kernel& k, const Tile& t, int wave, int n, int kvh) {
     const PromptAttnArgs& a = k.a;
@@ -87,6 +88,7 @@ struct Row {
     q = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)head * a.qs.head;
     out = (T*)a.out + ((int64_t)(t.start + token) * a.Hq + head) * a.D;
     end = seen_by((t.row0 + t.n_rows - 1) / k.G);
+    full = seen_by(t.row0 / k.G);
     const int rows = min(WROWS, t.n_rows - wave * WROWS);
     wave_end = rows > 0 ? seen_by((t.row0 + wave * WROWS + rows - 1) / k.G) : 0;
     wave_full = rows > 0 ? seen_by((t.row0 + wave * WROWS) / k.G) : 0;
@@ -171,13 +173,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   // of row i / 4, and gets column i of the 4 rows.
   const int vr = 4 * h + ((lane >> 2) & 3), vc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);
   int k_at = (n * CH + swizzle<D>(n, h)) * 16, v_at = (vr * CH + swizzle<D>(vr, vc)) * 16 + (lane & 1) * 8;
-  auto step = [&](const u4* ks, const u4* vs, u4* kn, u4* vn, int key0) {
+  // MASKED: some row may not see some key of the tile
+  auto step = [&](auto MASKED, const u4* ks, const u4* vs, u4* kn, u4* vn, int key0) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // this tile is there, and the other slot free
     if (key0 + KEYS < w.end) {
       fetch(a.k, a.ks, kn, key0 + KEYS);
       fetch(a.v, a.vs, vn, key0 + KEYS);
     }
-    if (key0 >= w.wave_end) return;
+    if (MASKED && key0 >= w.wave_end) return;
     asm volatile("" : "+v"(k_at), "+v"(v_at));        // (the places are made here, not kept in 40 registers)
     // scores, keys in the rows: lane (row n, h) holds keys 32 b + 8 (i / 4) + 4 h + i % 4
     f16v s[2];
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         s[b] = mfma(*reinterpret_cast<const u4*>(reinterpret_cast<const char*>(ks) + (k_at ^ (j << 5)) + b * 32 * CH * 16), q[j], s[b], T());
       }
     }
-    const bool some = key0 + KEYS > w.wave_full;            // some row does not see some key
+    const bool some = MASKED && key0 + KEYS > w.wave_full;
     if (some) {
       const int lim = w.seen - key0 - 4 * h;
 #pragma unroll
@@ -222,12 +225,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         sum += e0 + e1;
         p[b][i >> 3][(i >> 1) & 3] = pack<T>(e0, e1);
       }
+    asm volatile("" : "+v"(sum));                     // (summed here: 32 weights would live on into the next step)
     // V's operand: its column d = 32 e + n, keys 16 g + 8 u + 4 h + 0..3, read transposed
     auto column = [&](int g, int u, int e) {
       const char* at = reinterpret_cast<const char*>(vs) + (v_at ^ (e << 6) ^ (u << 5)) + (16 * g + 8 * u) * CH * 16;
       return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)at));
     };
-    if (some) {
+    if constexpr (MASKED) if (some) {
       // A row that does not see a key gives it the weight 0, and 0 times an infinity or a NaN would still reach it.
       uint32_t big = 0;
 #pragma unroll 1
@@ -281,10 +285,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
     fetch(a.k, a.ks, k_a, 0);
     fetch(a.v, a.vs, v_a, 0);
   }
-  for (int key0 = 0; key0 < w.end; key0 += 2 * KEYS) {
-    step(k_a, v_a, k_b, v_b, key0);
+  int key0 = 0;
+  for (; key0 + 2 * KEYS <= w.full; key0 += 2 * KEYS) {
+    step(std::false_type{}, k_a, v_a, k_b, v_b, key0);
+    step(std::false_type{}, k_b, v_b, k_a, v_a, key0 + KEYS);
+  }
+  for (; key0 < w.end; key0 += 2 * KEYS) {
+    step(std::true_type{}, k_a, v_a, k_b, v_b, key0);
     if (key0 + KEYS >= w.end) break;
-    step(k_b, v_b, k_a, v_a, key0 + KEYS);
+    step(std::true_type{}, k_b, v_b, k_a, v_a, key0 + KEYS);
   }
 
   sum += __shfl_xor(sum, 32);
@@ -370,13 +379,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f;
   int k_at = (n * CH + swizzle32<D>(n, h)) * 16, v_at = 4 * h * CH * 16 + ((n >> 2) ^ (4 * h)) * 16 + (n & 3) * 4;   // places in a tile, in bytes: chunk h of K's row n, value n of V's row 4 h
 
-  auto step = [&](const f4* ks, const f4* vs, f4* kn, f4* vn, int key0) {
+  auto step = [&](auto MASKED, const f4* ks, const f4* vs, f4* kn, f4* vn, int key0) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // this tile is there, and the other slot free
     if (key0 + KEYS32 < w.end) {
       fetch(a.k, a.ks, kn, key0 + KEYS32);
       fetch(a.v, a.vs, vn, key0 + KEYS32);
     }
-    if (key0 >= w.wave_end) return;
+    if (MASKED && key0 >= w.wave_end) return;
     asm volatile("" : "+v"(k_at), "+v"(v_at));
     f16v s;
 #pragma unroll
@@ -387,7 +396,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
 #pragma unroll
       for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[i], q[j][i], s, 0, 0, 0);
     }
-    const bool some = key0 + KEYS32 > w.wave_full;
+    const bool some = MASKED && key0 + KEYS32 > w.wave_full;
     if (some) {
       const int lim = w.seen - key0 - 4 * h;
 #pragma unroll
@@ -416,7 +425,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
       const int r = 8 * (i >> 2) + (i & 3);                                // the row of h = 0; the one 4 further differs by an exclusive or of 4
       return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(vs) + (v_at ^ (((8 * e) ^ (r & 15)) << 4)) + r * CH * 16);
     };
-    if (some) {
+    if constexpr (MASKED) if (some) {
       // (a weight of 0 times an infinity or a NaN: see the 16-bit kernel)
       bool bad = false;
 #pragma unroll 1
@@ -454,10 +463,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
     fetch(a.k, a.ks, k_a, 0);
     fetch(a.v, a.vs, v_a, 0);
   }
-  for (int key0 = 0; key0 < w.end; key0 += 2 * KEYS32) {
-    step(k_a, v_a, k_b, v_b, key0);
+  int key0 = 0;
+  for (; key0 + 2 * KEYS32 <= w.full; key0 += 2 * KEYS32) {
+    step(std::false_type{}, k_a, v_a, k_b, v_b, key0);
+    step(std::false_type{}, k_b, v_b, k_a, v_a, key0 + KEYS32);
+  }
+  for (; key0 < w.end; key0 += 2 * KEYS32) {
+    step(std::true_type{}, k_a, v_a, k_b, v_b, key0);
     if (key0 + KEYS32 >= w.end) break;
-    step(k_b, v_b, k_a, v_a, key0 + KEYS32);
+    step(std::true_type{}, k_b, v_b, k_a, v_a, key0 + KEYS32);
   }
   sum += __shfl_xor(sum, 32);
   const float inv = ref == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
