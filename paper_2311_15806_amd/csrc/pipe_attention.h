@@ -89,6 +89,20 @@ __device__ __forceinline__ void store_row(T* p, const float* x) {
   for (int i = 0; i < N; ++i) r.v[i] = from_f<T>(x[i]);
   *reinterpret_cast<Row*>(p) = r;
 }
+// minimum / maximum over the LANES (8 or 16) lanes of a row
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int LANES, bool MAX>
+__device__ __forceinline__ float row_reduce(float x) {
+  auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : fminf(a, b); };
+  x = op(x, dpp<0xB1>(x));    // lane ^ 1
+  x = op(x, dpp<0x4E>(x));    // lane ^ 2
+  x = op(x, dpp<0x141>(x));   // 7 - lane within 8
+  if (LANES == 16) x = op(x, dpp<0x140>(x));   // 15 - lane
+  return x;
+}
 __device__ __forceinline__ float word_scale(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float word_offset(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 #endif

@@ -145,21 +145,6 @@ __global__ __launch_bounds__(PLAN_NT) void cache_plan_kernel(
 // ------------------------------------------------------------------ rows into the cache and back
 // A row (one token's one head) of D values is D/8 lanes of 8 values; a lane's codes are one 32-bit word of the page, so that a
 // row's words are one store of D/2 contiguous bytes.  Bound by the bytes: D values in, D/2 + 4 bytes out.
-// minimum / maximum over the LANES (8 or 16) lanes of a row
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
-}
-template <int LANES, bool MAX>
-__device__ __forceinline__ float row_reduce(float x) {
-  auto op = [](float a, float b) { return MAX ? fmaxf(a, b) : fminf(a, b); };
-  x = op(x, dpp<0xB1>(x));    // lane ^ 1
-  x = op(x, dpp<0x4E>(x));    // lane ^ 2
-  x = op(x, dpp<0x141>(x));   // 7 - lane within 8
-  if (LANES == 16) x = op(x, dpp<0x140>(x));   // 15 - lane
-  return x;
-}
-
 // the bf16 value next to x below or equal / above or equal, as fp32
 __device__ __forceinline__ float bf16_down(float x) {
   const uint32_t u = __float_as_uint(x);

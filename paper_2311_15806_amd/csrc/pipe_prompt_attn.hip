@@ -6,6 +6,7 @@
 namespace {
 
 // ------------------------------------------------------------------ 16-bit types
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
@@ -161,12 +162,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   };
 
   f16v o[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   constexpr float P_LOG = sizeof(T) == 2 && std::is_same_v<T, f16> ? 7.f : 0.f;    // fp16: weights up to 2^15, so that small ones keep their digits
-  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f;
+  float ref, nref, lift, sum;
+  bool careful = false;       // a second pass: some output of the first is not finite
 
   // Places in a tile, in bytes: of K the chunk h of row n -- chunk 2 j + h of row 32 b + n is j and b further, by an exclusive or and an
   // addition --, of V the piece that this lane brings to a transposed read: of every 16 lanes, lane i brings 4 columns from 4 (i % 4) on
@@ -182,6 +180,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
     }
     if (MASKED && key0 >= w.wave_end) return;
     asm volatile("" : "+v"(k_at), "+v"(v_at));        // (the places are made here, not kept in 40 registers)
+    __builtin_amdgcn_s_setprio(1);                    // (the products before the other waves' softmax)
     // scores, keys in the rows: lane (row n, h) holds keys 32 b + 8 (i / 4) + 4 h + i % 4
     f16v s[2];
 #pragma unroll
@@ -193,6 +192,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         s[b] = mfma(*reinterpret_cast<const u4*>(reinterpret_cast<const char*>(ks) + (k_at ^ (j << 5)) + b * 32 * CH * 16), q[j], s[b], T());
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     const bool some = MASKED && key0 + KEYS > w.wave_full;
     if (some) {
       const int lim = w.seen - key0 - 4 * h;
@@ -231,8 +231,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       const char* at = reinterpret_cast<const char*>(vs) + (v_at ^ (e << 6) ^ (u << 5)) + (16 * g + 8 * u) * CH * 16;
       return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)at));
     };
-    if constexpr (MASKED) if (some) {
-      // A row that does not see a key gives it the weight 0, and 0 times an infinity or a NaN would still reach it.
+    if constexpr (MASKED) if (some && careful) {
       uint32_t big = 0;
 #pragma unroll 1
       for (int g = 0; g < KEYS / 16; ++g)
@@ -249,7 +248,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
           }
       constexpr uint32_t INF_BITS = std::is_same_v<T, f16> ? 0x7c00u : 0x7f80u;
       if (__any(big >= INF_BITS)) {
-        // ... so such a tile is summed key by key, each row over the keys that it sees
+        // such a tile is summed key by key, each row over the keys that it sees
 #pragma unroll 1
         for (int k = 0; k < KEYS; ++k) {
           uint32_t pw = 0;
@@ -272,6 +271,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         return;
       }
     }
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int g = 0; g < KEYS / 16; ++g)
 #pragma unroll
@@ -281,21 +281,38 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       }
   };
 
-  if (w.end > 0) {
-    fetch(a.k, a.ks, k_a, 0);
-    fetch(a.v, a.vs, v_a, 0);
+  for (;;) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    ref = lift = -INFINITY;
+    nref = sum = 0.f;
+    if (w.end > 0) {
+      fetch(a.k, a.ks, k_a, 0);
+      fetch(a.v, a.vs, v_a, 0);
+    }
+    int key0 = 0;
+    for (; key0 + 2 * KEYS <= w.full; key0 += 2 * KEYS) {
+      step(std::false_type{}, k_a, v_a, k_b, v_b, key0);
+      step(std::false_type{}, k_b, v_b, k_a, v_a, key0 + KEYS);
+    }
+    for (; key0 < w.end; key0 += 2 * KEYS) {
+      step(std::true_type{}, k_a, v_a, k_b, v_b, key0);
+      if (key0 + KEYS >= w.end) break;
+      step(std::true_type{}, k_b, v_b, k_a, v_a, key0 + KEYS);
+    }
+    // A row that does not see a key gives it the weight 0, and 0 times an infinity or a NaN of V would still reach it: where an output is
+    // not finite, all is done once more, with care for such tiles.
+    if (careful) break;
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bad |= !(fabsf(o[d][i]) < INFINITY);
+    if (!__syncthreads_or(bad)) break;
+    careful = true;
   }
-  int key0 = 0;
-  for (; key0 + 2 * KEYS <= w.full; key0 += 2 * KEYS) {
-    step(std::false_type{}, k_a, v_a, k_b, v_b, key0);
-    step(std::false_type{}, k_b, v_b, k_a, v_a, key0 + KEYS);
-  }
-  for (; key0 < w.end; key0 += 2 * KEYS) {
-    step(std::true_type{}, k_a, v_a, k_b, v_b, key0);
-    if (key0 + KEYS >= w.end) break;
-    step(std::true_type{}, k_b, v_b, k_a, v_a, key0 + KEYS);
-  }
-
   sum += __shfl_xor(sum, 32);
   const float inv = ref == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
   // 4 values of this lane's columns 8 g + 4 h and 4 of lane ^ 32's make 16 bytes: even groups go to the lower lanes, odd ones to the upper
@@ -318,17 +335,31 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
 }
 
 // ------------------------------------------------------------------ fp32
-// The same on the fp32 matrix instruction, 32 x 32 with two values of the summed axis: a lane's four values of K (a 16-byte read) meet four
-// of q, in any order that both keep; a lane's weight of key i meets V's row of that key.  Tiles of 32 keys; matrix instructions take 64 cycles
-// each, so that everything else hides behind them.
-template <int D>
-__device__ __forceinline__ int swizzle32(int r, int c) { return c ^ (r & 15); }     // (16 rows' same chunk in different banks)
+// fp32 goes through the fp16 matrix instruction as two terms, x = 2^-e (hi + lo) with hi = fp16(2^e x) and lo = fp16(2^e x - hi): 22 bits of
+// every value down to 2^-17 of the largest one of its row, for which e is chosen, and a b = hi hi + hi lo + lo hi, what is left out being
+// 2^-22 of it.  Three instructions of 32 cycles for what the fp32 instruction does in 512: 4096 tokens of 32 heads 1.15 ms there.  A key's
+// factor of K goes back into its scores, that of V into its weight.  A tile of 32 keys is loaded one ahead into registers and split on its
+// way into LDS, once for all waves.
+
+// the exponent field of 2^e, for e that brings `largest` (finite, >= 0) to 2^14 .. 2^15
+__device__ __forceinline__ int scale_of(float largest) { return min(253, 268 - (int)(__float_as_uint(largest) >> 23)); }
+__device__ __forceinline__ float power_of(int scale) { return __uint_as_float((uint32_t)scale << 23); }
+
+// Two values in two terms of fp16 each.  (The first rounding is done once: the compiler's single and packed conversions break ties
+// differently, and a rest taken from the other's result is off by a unit.)
+__device__ __forceinline__ void two_terms(float x, float y, uint32_t& hi, uint32_t& lo) {
+  hi = pack<f16>(x, y);
+  asm volatile("" : "+v"(hi));
+  const h2 v = __builtin_bit_cast(h2, hi);
+  lo = pack<f16>(x - (float)v[0], y - (float)v[1]);
+}
 
 template <int D, bool WIDE>
 __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel kr) {
-  constexpr int CH = D / 4, KS = D / 8, DB = D / 32, KEYS32 = 32;
-  constexpr int LOADS = KEYS32 * CH / 256;
-  __shared__ alignas(1024) f4 k_a[KEYS32 * CH], k_b[KEYS32 * CH], v_a[KEYS32 * CH], v_b[KEYS32 * CH];
+  constexpr int CH = D / 8, KS = D / 16, DB = D / 32, KEYS32 = 32;
+  constexpr int LOADS = KEYS32 * CH / 256;               // chunks of 8 values a lane brings of a tile of K (and of V)
+  __shared__ alignas(1024) u4 k_hi[KEYS32 * CH], k_lo[KEYS32 * CH], v_hi[KEYS32 * CH], v_lo[KEYS32 * CH];
+  __shared__ alignas(16) float k_unit[KEYS32], v_unit[KEYS32];     // what a key's scaled values are multiples of
   const PromptAttnArgs& a = kr.a;
   const int id = blockIdx.x, kvh = id % a.Hkv;
   const Tile t = find_tile(kr, kr.n_tiles - 1 - id / a.Hkv);
@@ -336,153 +367,228 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
   const Row<float> w(kr, t, wave, n, kvh);
-  const float* qp = w.q + 4 * h;
-  f4 q[KS];
-  const float sgn = a.scale < 0.f ? -1.f : 1.f;
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    if constexpr (WIDE) {
-      q[s] = *reinterpret_cast<const f4*>(qp + 8 * s);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) q[s][i] = qp[8 * s + i];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q[s][i] = w.real && a.scale != 0.f ? sgn * q[s][i] : 0.f;
-  }
-  const float rs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
 
-  auto fetch = [&](const void* src, const HeadStrides& st, f4* dst, int key0) {
-    const float* base = (const float*)src + (int64_t)(t.k0 + key0) * st.token + (int64_t)kvh * st.head;
+  float kx[LOADS][8], vx[LOADS][8];
+  auto fetch = [&](int key0) {
+    const float* kb = (const float*)a.k + (int64_t)(t.k0 + key0) * a.ks.token + (int64_t)kvh * a.ks.head;
+    const float* vb = (const float*)a.v + (int64_t)(t.k0 + key0) * a.vs.token + (int64_t)kvh * a.vs.head;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int at = (i * WAVES + wave) * 64 + lane, r = at / CH, c = swizzle32<D>(r, at % CH);
-      const int rr = min(r, t.nk - 1 - key0);
-      if constexpr (WIDE) {
-        const uint32_t off = (uint32_t)rr * (uint32_t)st.token * 4u + c * 16;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)((const char*)base + off),
-                                         (__attribute__((address_space(3))) void*)(dst + (i * WAVES + wave) * 64), 16, 0, 0);
-      } else {
-        f4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = base[(int64_t)rr * st.token + c * 4 + e];
-        dst[at] = v;
-      }
+      const int at = i * 256 + threadIdx.x, r = min(at / CH, t.nk - 1 - key0), c = at % CH;   // (rows behind the last key: the last key again)
+      load8<float, WIDE>(kb + (int64_t)r * a.ks.token + c * 8, kx[i]);
+      load8<float, WIDE>(vb + (int64_t)r * a.vs.token + c * 8, vx[i]);
     }
   };
+  if (w.end > 0) fetch(0);
+
+  // q: row n, in two terms
+  float qv[KS][8], qmax = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    load8<float, WIDE>(w.q + 16 * s + 8 * h, qv[s]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      qv[s][i] = w.real && a.scale != 0.f ? qv[s][i] : 0.f;
+      qmax = fmaxf(qmax, fabsf(qv[s][i]));
+    }
+  }
+  qmax = fmaxf(qmax, __shfl_xor(qmax, 32));
+  const int qe = qmax < INFINITY ? scale_of(qmax) : 127;
+  const float qf = a.scale < 0.f ? -power_of(qe) : power_of(qe);
+  u4 q_hi[KS], q_lo[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t hi, lo;
+      two_terms(qf * qv[s][2 * i], qf * qv[s][2 * i + 1], hi, lo);
+      q_hi[s][i] = hi;
+      q_lo[s][i] = lo;
+    }
+  const float scale2 = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
 
   f16v o[DB];
-#pragma unroll
-  for (int d = 0; d < DB; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f;
-  int k_at = (n * CH + swizzle32<D>(n, h)) * 16, v_at = 4 * h * CH * 16 + ((n >> 2) ^ (4 * h)) * 16 + (n & 3) * 4;   // places in a tile, in bytes: chunk h of K's row n, value n of V's row 4 h
+  // weights exp2(rs * score + nref), outputs in units of sigma / P_SCALE: sigma a power of two, no unit of a key that this row sees above U_SLACK of it
+  float ref, nref, lift, sum, sigma, per;
+  bool careful = false;            // a second pass: some output of the first is not finite
+  const int vr = 4 * h + ((lane >> 2) & 3), vc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);      // (places as in the 16-bit kernel)
+  int k_at = (n * CH + swizzle<D>(n, h)) * 16, v_at = (vr * CH + swizzle<D>(vr, vc)) * 16 + (lane & 1) * 8;
+  constexpr float U_SLACK = 8.f, P_SCALE = 16.f;        // 2^REF_SLACK * U_SLACK * P_SCALE fits fp16
+  const float rs = ldexpf(scale2, 127 - qe);
 
-  auto step = [&](auto MASKED, const f4* ks, const f4* vs, f4* kn, f4* vn, int key0) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");     // this tile is there, and the other slot free
-    if (key0 + KEYS32 < w.end) {
-      fetch(a.k, a.ks, kn, key0 + KEYS32);
-      fetch(a.v, a.vs, vn, key0 + KEYS32);
+  auto step = [&](auto MASKED, int key0) {
+    // ---- the loaded tile's terms into LDS, once every wave is done with the tile before
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int at = i * 256 + threadIdx.x, r = at / CH, c = at % CH, to = r * CH + swizzle<D>(r, c);
+      float km = 0.f, vm = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = fabsf(kx[i][e]), y = fabsf(vx[i][e]);
+        km = fmaxf(km, x < INFINITY ? x : 0.f);
+        vm = fmaxf(vm, y < INFINITY ? y : 0.f);
+      }
+      const int ke = scale_of(row_reduce<CH, true>(km)), ve = scale_of(row_reduce<CH, true>(vm));
+      if (c == 0) { k_unit[r] = power_of(254 - ke); v_unit[r] = power_of(254 - ve); }
+      const float kf = power_of(ke), vf = power_of(ve);
+      u4 kh, kl, vh, vl;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t hi, lo;
+        two_terms(kf * kx[i][2 * e], kf * kx[i][2 * e + 1], hi, lo);
+        kh[e] = hi; kl[e] = lo;
+        two_terms(vf * vx[i][2 * e], vf * vx[i][2 * e + 1], hi, lo);
+        vh[e] = hi; vl[e] = lo;
+      }
+      k_hi[to] = kh; k_lo[to] = kl; v_hi[to] = vh; v_lo[to] = vl;
     }
+    if (key0 + KEYS32 < w.end) fetch(key0 + KEYS32);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");     // (the loads of the next tile fly on)
     if (MASKED && key0 >= w.wave_end) return;
     asm volatile("" : "+v"(k_at), "+v"(v_at));
+    // ---- scores of 32 keys
     f16v s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
-      const f4 kv = *reinterpret_cast<const f4*>(reinterpret_cast<const char*>(ks) + (k_at ^ (j << 5)));
+      const u4 kh = *reinterpret_cast<const u4*>(reinterpret_cast<const char*>(k_hi) + (k_at ^ (j << 5)));
+      const u4 kl = *reinterpret_cast<const u4*>(reinterpret_cast<const char*>(k_lo) + (k_at ^ (j << 5)));
+      s = mfma(kl, q_hi[j], s, f16());
+      s = mfma(kh, q_lo[j], s, f16());
+      s = mfma(kh, q_hi[j], s, f16());
+    }
+    float unit[16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[i], q[j][i], s, 0, 0, 0);
+    for (int i = 0; i < 16; i += 4) {
+      const f4 ku = *reinterpret_cast<const f4*>(&k_unit[2 * i + 4 * h]), vu = *reinterpret_cast<const f4*>(&v_unit[2 * i + 4 * h]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        s[i + u] *= ku[u];
+        unit[i + u] = vu[u];
+      }
     }
     const bool some = MASKED && key0 + KEYS32 > w.wave_full;
     if (some) {
       const int lim = w.seen - key0 - 4 * h;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < lim ? s[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        const bool yes = 8 * (i >> 2) + (i & 3) < lim;
+        s[i] = yes ? s[i] : -INFINITY;
+        unit[i] = yes ? unit[i] : 0.f;
+      }
     }
-    float smax = s[0];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) smax = fmaxf(smax, s[i]);
-    if (__any(smax > lift)) {
-      const float nr = fmaxf(ref, fmaxf(smax, __shfl_xor(smax, 32)));
-      const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr));
-      sum *= f;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) o[d] *= f;
-      ref = nr;
-      nref = nr == -INFINITY ? 0.f : -nr * rs;
-      lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
-    }
+    float smax = s[0], umax = unit[0];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], rs, nref));
-      sum += s[i];
+      smax = fmaxf(smax, s[i]);
+      umax = fmaxf(umax, unit[i]);
     }
-    // value n of block e of the row of key 8 (i / 4) + 4 h + i % 4
-    auto value = [&](int i, int e) {
-      const int r = 8 * (i >> 2) + (i & 3);                                // the row of h = 0; the one 4 further differs by an exclusive or of 4
-      return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(vs) + (v_at ^ (((8 * e) ^ (r & 15)) << 4)) + r * CH * 16);
-    };
-    if constexpr (MASKED) if (some) {
-      // (a weight of 0 times an infinity or a NaN: see the 16-bit kernel)
+    smax *= rs;
+    if (__any(smax > lift || umax > U_SLACK * sigma)) {
+      const float nr = fmaxf(ref, fmaxf(smax, __shfl_xor(smax, 32))), ns = fmaxf(sigma, fmaxf(umax, __shfl_xor(umax, 32)));
+      const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - nr), fo = f * (sigma / ns);
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[d] *= fo;
+      ref = nr;
+      nref = nr == -INFINITY ? 0.f : -nr;
+      lift = nr + REF_SLACK;
+      sigma = ns;
+      per = P_SCALE / ns;
+    }
+    u4 p_hi[2], p_lo[2];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], rs, nref));
+      s[i + 1] = __builtin_amdgcn_exp2f(fmaf(s[i + 1], rs, nref));
+      sum += s[i] + s[i + 1];
+      uint32_t hi, lo;
+      two_terms(s[i] * (unit[i] * per), s[i + 1] * (unit[i + 1] * per), hi, lo);
+      p_hi[i >> 3][(i >> 1) & 3] = hi;
+      p_lo[i >> 3][(i >> 1) & 3] = lo;
+    }
+    if constexpr (MASKED) if (some && careful) {
       bool bad = false;
 #pragma unroll 1
-      for (int r = h; r < KEYS32; r += 2)
-#pragma unroll
-        for (int e = 0; e < DB; ++e) bad |= !(fabsf(reinterpret_cast<const float*>(vs)[r * D + 32 * e + n]) < INFINITY);
+      for (int i = lane; i < KEYS32 * CH * 4; i += 64) {
+        const uint32_t x = reinterpret_cast<const uint32_t*>(v_hi)[i];
+        bad |= (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u;
+      }
       if (__any(bad)) {
+        // such a tile is summed key by key, each row over the keys that it sees
 #pragma unroll 1
         for (int k = 0; k < KEYS32; ++k) {
           float p = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) p = k / 8 * 4 + k % 4 == i ? s[i] : p;
-          p = __shfl(p, n + 32 * ((k >> 2) & 1));
+          p = __shfl(p, n + 32 * ((k >> 2) & 1)) * (v_unit[k] * per);
           const bool yes = key0 + k < w.seen;
-          const float* row_at = reinterpret_cast<const float*>(vs) + k * D;
+          const f16* hi_at = reinterpret_cast<const f16*>(v_hi) + k * D;
+          const f16* lo_at = reinterpret_cast<const f16*>(v_lo) + k * D;
 #pragma unroll
           for (int e = 0; e < DB; ++e)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int d = 32 * e + 8 * (i >> 2) + 4 * h + (i & 3);
-              const float v = row_at[swizzle32<D>(k, d >> 2) * 4 + (d & 3)];
+              const int d = 32 * e + 8 * (i >> 2) + 4 * h + (i & 3), at = swizzle<D>(k, d >> 3) * 8 + (d & 7);
+              const float x = (float)hi_at[at], v = fabsf(x) < INFINITY ? x + (float)lo_at[at] : x;
               o[e][i] = yes ? fmaf(p, v, o[e][i]) : o[e][i];
             }
         }
         return;
       }
     }
+    // ---- outputs
+    auto column = [&](const u4* plane, int g, int u, int e) {
+      const char* at = reinterpret_cast<const char*>(plane) + (v_at ^ (e << 6) ^ (u << 5)) + (16 * g + 8 * u) * CH * 16;
+      return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)at));
+    };
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int g = 0; g < KEYS32 / 16; ++g)
 #pragma unroll
-      for (int e = 0; e < DB; ++e) o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(i, e), s[i], o[e], 0, 0, 0);
+      for (int e = 0; e < DB; ++e) {
+        const u2 x = column(v_hi, g, 0, e), y = column(v_hi, g, 1, e), z = column(v_lo, g, 0, e), u = column(v_lo, g, 1, e);
+        o[e] = mfma((u4){z[0], z[1], u[0], u[1]}, p_hi[g], o[e], f16());
+        o[e] = mfma((u4){x[0], x[1], y[0], y[1]}, p_lo[g], o[e], f16());
+        o[e] = mfma((u4){x[0], x[1], y[0], y[1]}, p_hi[g], o[e], f16());
+      }
   };
 
-  if (w.end > 0) {
-    fetch(a.k, a.ks, k_a, 0);
-    fetch(a.v, a.vs, v_a, 0);
-  }
-  int key0 = 0;
-  for (; key0 + 2 * KEYS32 <= w.full; key0 += 2 * KEYS32) {
-    step(std::false_type{}, k_a, v_a, k_b, v_b, key0);
-    step(std::false_type{}, k_b, v_b, k_a, v_a, key0 + KEYS32);
-  }
-  for (; key0 < w.end; key0 += 2 * KEYS32) {
-    step(std::true_type{}, k_a, v_a, k_b, v_b, key0);
-    if (key0 + KEYS32 >= w.end) break;
-    step(std::true_type{}, k_b, v_b, k_a, v_a, key0 + KEYS32);
+  for (;;) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    ref = lift = -INFINITY;
+    nref = sum = 0.f;
+    sigma = 0x1p-126f;
+    per = P_SCALE * 0x1p126f;
+    int key0 = 0;
+    for (; key0 + KEYS32 <= w.full; key0 += KEYS32) step(std::false_type{}, key0);
+    for (; key0 < w.end; key0 += KEYS32) step(std::true_type{}, key0);
+    // (a weight of 0 times an infinity or a NaN: see the 16-bit kernel)
+    if (careful) break;
+    bool bad = false;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bad |= !(fabsf(o[d][i]) < INFINITY);
+    if (!__syncthreads_or(bad)) break;
+    careful = true;
+    fetch(0);
   }
   sum += __shfl_xor(sum, 32);
-  const float inv = ref == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
   if (!w.real) return;
+  const bool none = ref == -INFINITY && sum == 0.f;
+  const float inv = none ? 0.f : 1.f / sum, unit = sigma * (1.f / P_SCALE);
 #pragma unroll
   for (int e = 0; e < DB; ++e)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       f4 y;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = inv == 0.f ? 0.f : o[e][4 * g + i] * inv;
+      for (int i = 0; i < 4; ++i) y[i] = none ? 0.f : o[e][4 * g + i] * inv * unit;
       *reinterpret_cast<f4*>(w.out + 32 * e + 8 * g + 4 * h) = y;
     }
 }
