@@ -7,7 +7,8 @@ namespace {
 // Every workgroup scans the requests for itself (at most 4096 of them, 16 KiB from L2) and then makes its own share of the
 // slots and of the new table entries: one launch, nothing passed between workgroups, no order of theirs in the result.
 constexpr int PLAN_NT = 256;
-constexpr int PLAN_TOKENS = 4096;   // slots of one workgroup
+constexpr int PLAN_EACH = 4;                      // consecutive slots of a thread: one search for their request
+constexpr int PLAN_TOKENS = PLAN_EACH * PLAN_NT;  // slots of a workgroup
 
 __device__ __forceinline__ uint32_t capped_add(uint32_t a, uint32_t b, uint32_t cap) {   // both <= cap < 2^31
   const uint32_t s = a + b;
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(PLAN_NT) void cache_plan_kernel(
     const int32_t* __restrict__ free_list, int n_free, const int32_t* __restrict__ used, int32_t* table, int width, int T,
     int32_t* __restrict__ lengths, int32_t* __restrict__ starts, int32_t* __restrict__ slots,
     int32_t* __restrict__ positions, int32_t* __restrict__ counts) {
-  __shared__ uint32_t tok0[PIPE_PLAN_MAX_B + 1], page0[PIPE_PLAN_MAX_B + 1];
+  __shared__ uint32_t tok0[PIPE_PLAN_MAX_B + 1], page0[PIPE_PLAN_MAX_B + 1], held[PIPE_PLAN_MAX_B];
   __shared__ uint32_t wave_sum[PLAN_NT / 64];
   const int per = (B + PLAN_NT - 1) / PLAN_NT;
   const int b0 = min(B, (int)threadIdx.x * per), b1 = min(B, b0 + per);
@@ -72,6 +73,7 @@ __global__ __launch_bounds__(PLAN_NT) void cache_plan_kernel(
     const uint32_t end = capped_add(at, min(n, cap), cap);
     const uint32_t len = c + (end - at);
     tok0[b] = at;
+    held[b] = c;
     // pages: whole ones up to the cached end are there, those up to the new end are wanted
     const uint32_t P = 1u << shift;
     const uint32_t have = (c >> shift) + ((c & (P - 1)) != 0), need = (len >> shift) + ((len & (P - 1)) != 0);
@@ -113,19 +115,22 @@ __global__ __launch_bounds__(PLAN_NT) void cache_plan_kernel(
   // new table entries
   for (uint32_t j = blockIdx.x * PLAN_NT + threadIdx.x; j < all_pages; j += gridDim.x * PLAN_NT) {
     const int b = owner_of(page0, B, j);
-    const uint32_t c = (uint32_t)max(0, cached[b]), P = 1u << shift;
+    const uint32_t c = held[b], P = 1u << shift;
     const uint32_t have = (c >> shift) + ((c & (P - 1)) != 0);
     const uint32_t f = first_free + j;
     table[(int64_t)b * width + have + (j - page0[b])] = f < (uint32_t)n_free ? free_list[f] : -1;
   }
   // slots and positions
-  const uint32_t t_end = (uint32_t)min((int64_t)T, ((int64_t)blockIdx.x + 1) * PLAN_TOKENS);
-  for (uint32_t t = blockIdx.x * PLAN_TOKENS + threadIdx.x; t < t_end; t += PLAN_NT) {
+  const uint32_t t0 = blockIdx.x * PLAN_TOKENS + threadIdx.x * PLAN_EACH, P = 1u << shift;
+  int b = t0 < total ? owner_of(tok0, B, t0) : B;
+#pragma unroll
+  for (uint32_t u = 0; u < PLAN_EACH; ++u) {
+    const uint32_t t = t0 + u;
+    if (t >= (uint32_t)T) break;
     int32_t slot = -1, pos = -1;
     if (t < total) {
-      const int b = owner_of(tok0, B, t);
-      const uint32_t c = (uint32_t)max(0, cached[b]), P = 1u << shift;
-      const uint32_t p = c + (t - tok0[b]), col = p >> shift;
+      while (t >= tok0[b + 1]) ++b;           // (tok0[B] is the total)
+      const uint32_t c = held[b], p = c + (t - tok0[b]), col = p >> shift;
       const uint32_t have = (c >> shift) + ((c & (P - 1)) != 0);
       int32_t page = -1;
       if (col < have) {
