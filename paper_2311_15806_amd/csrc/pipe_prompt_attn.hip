@@ -31,6 +31,19 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {      // (as a vecto
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){x, y}, T2));
 }
 
+// Order of N products that read READS times each from LDS: the reads AHEAD of the products that wait for them.
+template <int N, int READS, int AHEAD>
+__device__ __forceinline__ void in_turn() {
+  constexpr int DS_READ = 0x100, MFMA = 0x8, FIRST = AHEAD / READS;
+  __builtin_amdgcn_sched_group_barrier(DS_READ, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < N - FIRST; ++i) {
+    __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(DS_READ, READS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(MFMA, FIRST, 0);
+}
+
 struct Kernel {
   PromptAttnArgs a;
   int G, n_tiles;
@@ -184,14 +197,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
     // scores, keys in the rows: lane (row n, h) holds keys 32 b + 8 (i / 4) + 4 h + i % 4
     f16v s[2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
 #pragma unroll
-      for (int j = 0; j < KS; ++j) {
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
         s[b] = mfma(*reinterpret_cast<const u4*>(reinterpret_cast<const char*>(ks) + (k_at ^ (j << 5)) + b * 32 * CH * 16), q[j], s[b], T());
-      }
-    }
+    in_turn<2 * KS, 1, 6>();
     __builtin_amdgcn_s_setprio(0);
     const bool some = MASKED && key0 + KEYS > w.wave_full;
     if (some) {
@@ -279,6 +293,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
         const u2 x = column(g, 0, e), y = column(g, 1, e);
         o[e] = mfma((u4){x[0], x[1], y[0], y[1]}, p[g >> 1][g & 1], o[e], T());
       }
+    in_turn<KEYS / 16 * DB, 2, 8>();
   };
 
   for (;;) {

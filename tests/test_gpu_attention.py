@@ -265,6 +265,25 @@ def test_cache_attention_of_a_long_request(pipe, kind):
         assert np.abs(got.double().cpu().numpy() - want).max() <= limit
 
 
+@pytest.mark.parametrize("B", [62, 63, 64, 65, 300, 1100])
+def test_cache_attention_of_many_requests(pipe, B):
+    """A share finds its place among up to 63 requests in one wave, among more in the workgroup; some hold nothing, some bring nothing."""
+    Hq, Hkv, D, P = 3, 1, 64, 16
+    rng = np.random.default_rng(B)
+    fresh = rng.integers(0, 3, B)
+    lens = np.where(rng.random(B) < 0.2, 0, rng.integers(0, 60, B))
+    lens[B // 2], lens[-1], fresh[0], fresh[-1] = 700, 150, 0, 2
+    cache, table, kv = random_cache(pipe, rng, list(lens), Hkv, D, P)
+    q, qf = typed(rng, (int(fresh.sum()) + 2, Hq, D), "f32")
+    starts = np.concatenate([[0], np.cumsum(fresh)])
+    want = cache_reference(qf, fresh, lens, kv, D ** -0.5)
+    limit = cache_far("f32", D, qf, list(lens), D ** -0.5)
+    for hint in (0, 700, 10, 100000):
+        got = pipe.pipe_cache_attention(q, ints(starts), ints(lens), cache, table, P, Hkv, max_length=hint).double().cpu().numpy()
+        assert np.abs(got - want).max() <= limit, hint
+        assert not got[int(fresh.sum()):].any()
+
+
 def test_cache_attention_of_padded_steps_missing_pages_and_strided_queries(pipe):
     Hq, Hkv, D, P, lens = 8, 2, 64, 16, [40, 70]
     rng = np.random.default_rng(9)
@@ -382,6 +401,24 @@ def test_prompt_attention(pipe, kind, layout, case):
     err = np.abs(got.double().cpu().numpy() - want).max()
     assert err <= ref.far(kind, D, max(nk or nq), a, float(np.abs(vf).max())), err
     assert torch.equal(got, pipe.pipe_prompt_attention(q, k, v, starts, starts_k, causal=causal))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("B", [63, 64, 65, 200])
+def test_prompt_attention_of_many_sequences(pipe, B, kind):
+    Hq, Hkv, D = 3, 1, 64
+    rng = np.random.default_rng(B)
+    nq, nk = rng.integers(0, 9, B), rng.integers(0, 12, B)
+    nq[B // 3] = 140
+    q, qf = typed(rng, (int(nq.sum()) + 1, Hq, D), kind)
+    k, kf = typed(rng, (int(nk.sum()), Hkv, D), kind)
+    v, vf = typed(rng, (int(nk.sum()), Hkv, D), kind)
+    starts, starts_k = (ints(np.concatenate([[0], np.cumsum(n)])) for n in (nq, nk))
+    got = pipe.pipe_prompt_attention(q, k, v, starts, starts_k).double().cpu().numpy()
+    want = prompt_reference(qf, kf, vf, nq, nk, True, D ** -0.5)
+    a = D ** -0.5 * float(np.abs(qf).max()) * float(np.abs(kf).sum(-1).max())
+    assert np.abs(got - want).max() <= ref.far(kind, D, 12, a, float(np.abs(vf).max()))
+    assert not got[-1].any()
 
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
