@@ -628,17 +628,17 @@ int pipe_cache_read(const void* cache_dev, int n_pages, int P, const int32_t* sl
  *   queries than cached tokens) and for rows of q that belong to no request.
  *   max_length: about the longest length, a hint for splitting the work (any value gives the same result up to rounding);
  *   0: table_width * P.
- * Scores, maxima, sums and outputs are fp32.  The codes meet q in fp16 products summed in fp32: q of 16 bits as it is
- * (bf16 with a power of two per row that brings its largest value to 2^12 or so: values under 2^-26 of it are rounded), fp32 as
- * the sum of two fp16 values; the weights of the softmax times V's scales likewise: one fp16 value with 11 significant
- * bits for 16-bit outputs, two for fp32.
- * Errors: PIPE_EINVAL (NULL, type, P, scale not finite), PIPE_ESHAPE (T < 0, B < 1, heads, D, table_width < 1, cache too large),
+ * Scores, maxima, sums and outputs are fp32.  The codes meet q in fp16 products that are summed in fp32: q of 16 bits as it is
+ * (under a power of two that brings its row's largest value to 2^14: what is 2^-28 of that or less is rounded), fp32 as the sum
+ * of two fp16 values (22 bits); the softmax's weights times V's scales likewise, one fp16 value (11 bits) for 16-bit outputs,
+ * two for fp32.  |q| up to 2^94.
+ * Errors: PIPE_EINVAL (NULL, type, P, scale not finite), PIPE_ESHAPE (T < 0, B < 1, heads, D, table_width < 1, cache or table too large),
  * PIPE_ENOTREADY (scratch would have to grow during a capture).                                                   */
 int pipe_cache_attention(const void* q_dev, int type, int T, int Hq, int Hkv, int D, int64_t q_token_stride,
                          int64_t q_head_stride, const int32_t* starts_dev, const int32_t* lengths_dev, int B,
                          const void* cache_dev, int n_pages, int P, const int32_t* table_dev, int table_width,
                          float scale, int max_length, void* out_dev, void* stream);
-/* Scratch of pipe_cache_attention on this stream for up to these sizes.                                            */
+/* Scratch of pipe_cache_attention on this stream, whatever the sizes of the calls to come.                         */
 int pipe_prepare_cache_attention(int T, int Hq, int Hkv, int D, int B, int max_length, void* stream);
 
 /* Attention over packed sequences: sequence b has queries q_starts_dev[b] .. q_starts_dev[b+1]-1 and keys
@@ -646,8 +646,10 @@ int pipe_prepare_cache_attention(int T, int Hq, int Hkv, int D, int B, int max_l
  * m keys, query i sees keys 0 .. m - n + i (aligned at the end: new tokens behind a prefix); otherwise all m.
  *   out [Tq][Hq][D] dense, of the same type as q, k and v; zeros for a query that sees nothing and for rows of q that
  *   belong to no sequence.
- * Scores, maxima, sums and outputs are fp32; for 16-bit types the softmax weights are rounded to that type for the
- * product with V.
+ * Scores, maxima, sums and outputs are fp32.  16-bit types: the softmax's weights are rounded to that type for the product
+ * with V.  fp32: q, k, v and the weights enter the products as the sum of two fp16 values each (22 bits of what is no less than
+ * 2^-17 of the largest value of its row).  A key that a query does not see -- a later one, another sequence's -- does not
+ * reach its output, whatever it holds; infinities and NaN of V cost the tiles around them a second pass.
  * Errors: PIPE_EINVAL (NULL, type, scale not finite), PIPE_ESHAPE (Tq or Tk < 0, B < 1, heads, D, strides).       */
 int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_dev, int type, int Tq, int Tk, int Hq,
                           int Hkv, int D, int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride,

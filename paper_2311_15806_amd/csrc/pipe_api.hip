@@ -32,8 +32,8 @@ extern "C" const char* pipe_last_device_error(void) { return g_last_hip_error.c_
 extern "C" const char* pipe_strerror(int code) {
   switch (code) {
     case PIPE_OK: return "ok";
-    case PIPE_EINVAL: return "invalid argument (NULL pointer or bits/K/gamma/group out of range)";
-    case PIPE_ESHAPE: return "invalid shape (out % group != 0, group % 16 != 0, size <= 0 or too large)";
+    case PIPE_EINVAL: return "invalid argument (NULL pointer, bits/K/gamma/group, type, page size, scale or alignment out of range)";
+    case PIPE_ESHAPE: return "invalid shape (out % group != 0, group % 16 != 0, heads, head_dim, size <= 0 or too large)";
     case PIPE_ENOMEM: return "out of memory";
     case PIPE_EDEVICE: return "HIP call failed";
     case PIPE_ESPLIT: return "ensemble split must be positive and sum to K";
@@ -2383,8 +2383,8 @@ static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 
 // heads and head_dim of the attention calls
 static bool heads_ok(int Hq, int Hkv, int D) { return Hkv >= 1 && Hq >= Hkv && Hq <= 65535 && Hq % Hkv == 0 && (D == 64 || D == 128); }
 
-// (rows of a kernel's grid stay below 2^31)
-static bool rows_ok(int T, int H) { return T >= 0 && (int64_t)T * H <= 0x7fffffff; }
+// (16 threads a row: a launch holds fewer than 2^32)
+static bool rows_ok(int T, int H) { return T >= 0 && (int64_t)T * H < 1 << 28; }
 
 static int cache_view(const void* cache_dev, int n_pages, int P, int Hkv, int D, CacheView* c) {
   const int shift = pipe_page_shift(P);

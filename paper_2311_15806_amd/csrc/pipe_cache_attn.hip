@@ -720,7 +720,7 @@ int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   const int64_t room = std::min<int64_t>((int64_t)a.width << a.cache.shift, 0x7ffff000);
   if ((((int64_t)a.T * k.G + ROWS - 1) / ROWS + a.B + 1) * (room / UNIT + 1) > 0x7fffffff) return PIPE_ESHAPE;
   k.n_share = (uint32_t)std::max<int64_t>(1, std::min(most, tiles * (longest <= 3 * UNIT ? 1 : (longest + UNIT - 1) / UNIT)));
-  if (k.n_share > 1) {
+  if (k.n_share > 1 || pipe_dry_run()) {
     const size_t parts = (size_t)SHARES_64 * 2 * ROWS;       // one size serves every call
     int rc = PIPE_OK;
     uint8_t* ws = (uint8_t*)pipe_ws_zeroed(WS_ATTN, ATTN_COUNTS + parts * (128 + 2) * sizeof(float), ATTN_COUNTS, &rc);

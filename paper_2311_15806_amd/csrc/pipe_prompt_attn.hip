@@ -61,23 +61,38 @@ struct Tile {
 __device__ __forceinline__ Tile find_tile(const Kernel& k, int id) {
   const PromptAttnArgs& a = k.a;
   const int lane = threadIdx.x & 63;
-  auto start_of = [&](int b) { return b > 0 ? min(max(a.q_starts[b], 0), a.Tq) : 0; };
-  int b = -1;
-  for (int i0 = 0; i0 <= a.B; i0 += 64) {
-    const int i = i0 + lane;
-    const bool le = i <= a.B && (int)(((int64_t)start_of(min(i, a.B)) * k.G) / QROWS) + i <= id;
-    const int n = __popcll(__ballot(le));
-    b += n;
-    if (n < 64) break;
+  auto start_of = [&](int i) { return i > 0 ? min(max(a.q_starts[min(i, a.B)], 0), a.Tq) : 0; };
+  auto key_of = [&](int i) { return min(max(a.k_starts[min(i, a.B)], 0), a.Tk); };
+  auto first_id = [&](int start, int i) { return (int)(((int64_t)start * k.G) / QROWS) + i; };
+  int b, start, next, k0, k1;      // the sequence, its queries and its keys
+  if (a.B < 64) {                  // a lane a sequence: nothing is looked up twice
+    const int s = start_of(lane), key = key_of(lane);
+    b = __popcll(__ballot(lane <= a.B && first_id(s, lane) <= id)) - 1;
+    start = __builtin_amdgcn_readlane(s, b);
+    next = b < a.B ? __builtin_amdgcn_readlane(s, b + 1 < 64 ? b + 1 : 63) : a.Tq;
+    k0 = __builtin_amdgcn_readlane(key, b);
+    k1 = b < a.B ? __builtin_amdgcn_readlane(key, b + 1 < 64 ? b + 1 : 63) : k0;
+  } else {
+    b = -1;
+    for (int i0 = 0; i0 <= a.B; i0 += 64) {
+      const int i = i0 + lane;
+      const int n = __popcll(__ballot(i <= a.B && first_id(start_of(i), i) <= id));
+      b += n;
+      if (n < 64) break;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
+    start = start_of(b);
+    next = b < a.B ? start_of(b + 1) : a.Tq;
+    k0 = key_of(b);
+    k1 = b < a.B ? key_of(b + 1) : k0;
   }
-  b = __builtin_amdgcn_readfirstlane(b);
+  const int n = next - start;
   Tile t;
-  t.start = start_of(b);
-  const int n = (b < a.B ? start_of(b + 1) : a.Tq) - t.start;
-  t.row0 = (id - ((int)(((int64_t)t.start * k.G) / QROWS) + b)) * QROWS;
+  t.start = start;
+  t.row0 = (id - first_id(start, b)) * QROWS;
   t.n_rows = t.row0 < 0 ? 0 : min(QROWS, max(0, n * k.G - t.row0));
-  t.k0 = b < a.B ? min(max(a.k_starts[b], 0), a.Tk) : 0;
-  t.nk = b < a.B ? max(0, min(a.k_starts[b + 1], a.Tk) - t.k0) : 0;
+  t.k0 = k0;
+  t.nk = max(0, k1 - k0);
   t.first_seen = t.nk - n + 1;
   return t;
 }
@@ -132,26 +147,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   const int n = lane & 31, h = lane >> 5;
 
   const Row<T> w(kr, t, wave, n, kvh);
-  const T* qp = w.q + 8 * h;
-  u4 q[KS];
-  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = w.real && a.scale != 0.f ? ~0u : 0u;
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    if constexpr (WIDE) {
-      q[s] = *reinterpret_cast<const u4*>(qp + 16 * s);
-    } else {
-      T v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = qp[16 * s + i];
-      __builtin_memcpy(&q[s], v, 16);
-    }
-  }
-#pragma unroll
-  for (int s = 0; s < KS; ++s)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) q[s][i] = (q[s][i] ^ flip) & keep;
-  const float rs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
-
   // ---- loads of a tile: LDS in the order of the lanes, so that a lane picks what belongs at its place
   auto fetch = [&](const void* src, const HeadStrides& st, u4* dst, int key0) {
     const T* base = (const T*)src + (int64_t)(t.k0 + key0) * st.token + (int64_t)kvh * st.head;
@@ -173,6 +168,33 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       }
     }
   };
+
+  auto first_tile = [&]() {
+    if (w.end > 0) {
+      fetch(a.k, a.ks, k_a, 0);
+      fetch(a.v, a.vs, v_a, 0);
+    }
+  };
+  first_tile();
+  const T* qp = w.q + 8 * h;
+  u4 q[KS];
+  const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u, keep = w.real && a.scale != 0.f ? ~0u : 0u;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    if constexpr (WIDE) {
+      q[s] = *reinterpret_cast<const u4*>(qp + 16 * s);
+    } else {
+      T v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = qp[16 * s + i];
+      __builtin_memcpy(&q[s], v, 16);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[s][i] = (q[s][i] ^ flip) & keep;
+  const float rs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
 
   f16v o[DB];
   constexpr float P_LOG = sizeof(T) == 2 && std::is_same_v<T, f16> ? 7.f : 0.f;    // fp16: weights up to 2^15, so that small ones keep their digits
@@ -303,10 +325,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     ref = lift = -INFINITY;
     nref = sum = 0.f;
-    if (w.end > 0) {
-      fetch(a.k, a.ks, k_a, 0);
-      fetch(a.v, a.vs, v_a, 0);
-    }
     int key0 = 0;
     for (; key0 + 2 * KEYS <= w.full; key0 += 2 * KEYS) {
       step(std::false_type{}, k_a, v_a, k_b, v_b, key0);
@@ -327,6 +345,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       for (int i = 0; i < 16; ++i) bad |= !(fabsf(o[d][i]) < INFINITY);
     if (!__syncthreads_or(bad)) break;
     careful = true;
+    first_tile();
   }
   sum += __shfl_xor(sum, 32);
   const float inv = ref == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
