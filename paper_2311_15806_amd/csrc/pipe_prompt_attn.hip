@@ -379,13 +379,26 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
 __device__ __forceinline__ int scale_of(float largest) { return min(253, 268 - (int)(__float_as_uint(largest) >> 23)); }
 __device__ __forceinline__ float power_of(int scale) { return __uint_as_float((uint32_t)scale << 23); }
 
-// Two values in two terms of fp16 each.  (The first rounding is done once: the compiler's single and packed conversions break ties
-// differently, and a rest taken from the other's result is off by a unit.)
-__device__ __forceinline__ void two_terms(float x, float y, uint32_t& hi, uint32_t& lo) {
-  hi = pack<f16>(x, y);
+// f x and f y in two terms of fp16 each; the rest is taken from the rounded value itself, whichever way that fell.
+__device__ __forceinline__ void two_terms(float x, float y, float f, uint32_t& hi, uint32_t& lo) {
+  h2 a = {(f16)__builtin_fmaf(x, f, 0.f), (f16)__builtin_fmaf(y, f, 0.f)};
+  hi = __builtin_bit_cast(uint32_t, a);
   asm volatile("" : "+v"(hi));
-  const h2 v = __builtin_bit_cast(h2, hi);
-  lo = pack<f16>(x - (float)v[0], y - (float)v[1]);
+  a = __builtin_bit_cast(h2, hi);
+  const h2 b = {(f16)__builtin_fmaf(x, f, -(float)a[0]), (f16)__builtin_fmaf(y, f, -(float)a[1])};
+  lo = __builtin_bit_cast(uint32_t, b);
+}
+// the largest finite magnitude of 8 values
+__device__ __forceinline__ float largest8(const float* x) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = __builtin_amdgcn_fmed3f(fabsf(x[e]), m, 0x1.fffffep127f);   // (NaN leaves m)
+  if (__any(m == 0x1.fffffep127f)) {                    // an infinity, most likely: once more without
+    m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]) < INFINITY ? fabsf(x[e]) : 0.f);
+  }
+  return m;
 }
 
 template <int D, bool WIDE>
@@ -393,6 +406,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   constexpr int CH = D / 8, KS = D / 16, DB = D / 32, KEYS32 = 32;
   constexpr int LOADS = KEYS32 * CH / 256;               // chunks of 8 values a lane brings of a tile of K (and of V)
   __shared__ alignas(1024) u4 k_hi[KEYS32 * CH], k_lo[KEYS32 * CH], v_hi[KEYS32 * CH], v_lo[KEYS32 * CH];
+  __shared__ u4 q_rest[D == 128 ? WAVES * KS * 64 : 1];      // the second terms of q, where registers do not hold them too
   __shared__ alignas(16) float k_unit[KEYS32], v_unit[KEYS32];     // what a key's scaled values are multiples of
   const PromptAttnArgs& a = kr.a;
   const int id = blockIdx.x, kvh = id % a.Hkv;
@@ -429,16 +443,20 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   qmax = fmaxf(qmax, __shfl_xor(qmax, 32));
   const int qe = qmax < INFINITY ? scale_of(qmax) : 127;
   const float qf = a.scale < 0.f ? -power_of(qe) : power_of(qe);
-  u4 q_hi[KS], q_lo[KS];
+  u4 q_hi[KS], q_lo[D == 128 ? 1 : KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s)
+  for (int s = 0; s < KS; ++s) {
+    u4 rest;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t hi, lo;
-      two_terms(qf * qv[s][2 * i], qf * qv[s][2 * i + 1], hi, lo);
+      two_terms(qv[s][2 * i], qv[s][2 * i + 1], qf, hi, lo);
       q_hi[s][i] = hi;
-      q_lo[s][i] = lo;
+      rest[i] = lo;
     }
+    if constexpr (D == 128) q_rest[(wave * KS + s) * 64 + lane] = rest;      // (read by this lane alone)
+    else q_lo[s] = rest;
+  }
   const float scale2 = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
 
   f16v o[DB];
@@ -456,13 +474,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int at = i * 256 + threadIdx.x, r = at / CH, c = at % CH, to = r * CH + swizzle<D>(r, c);
-      float km = 0.f, vm = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = fabsf(kx[i][e]), y = fabsf(vx[i][e]);
-        km = fmaxf(km, x < INFINITY ? x : 0.f);
-        vm = fmaxf(vm, y < INFINITY ? y : 0.f);
-      }
+      const float km = largest8(kx[i]), vm = largest8(vx[i]);
       const int ke = scale_of(row_reduce<CH, true>(km)), ve = scale_of(row_reduce<CH, true>(vm));
       if (c == 0) { k_unit[r] = power_of(254 - ke); v_unit[r] = power_of(254 - ve); }
       const float kf = power_of(ke), vf = power_of(ve);
@@ -470,9 +482,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         uint32_t hi, lo;
-        two_terms(kf * kx[i][2 * e], kf * kx[i][2 * e + 1], hi, lo);
+        two_terms(kx[i][2 * e], kx[i][2 * e + 1], kf, hi, lo);
         kh[e] = hi; kl[e] = lo;
-        two_terms(vf * vx[i][2 * e], vf * vx[i][2 * e + 1], hi, lo);
+        two_terms(vx[i][2 * e], vx[i][2 * e + 1], vf, hi, lo);
         vh[e] = hi; vl[e] = lo;
       }
       k_hi[to] = kh; k_lo[to] = kl; v_hi[to] = vh; v_lo[to] = vl;
@@ -482,17 +494,21 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
     if (MASKED && key0 >= w.wave_end) return;
     asm volatile("" : "+v"(k_at), "+v"(v_at));
     // ---- scores of 32 keys
-    f16v s;
+    f16v s, s2;                                      // (two sums: products that wait for one another stand half as close)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    for (int i = 0; i < 16; ++i) s[i] = s2[i] = 0.f;
 #pragma unroll
     for (int j = 0; j < KS; ++j) {
       const u4 kh = *reinterpret_cast<const u4*>(reinterpret_cast<const char*>(k_hi) + (k_at ^ (j << 5)));
       const u4 kl = *reinterpret_cast<const u4*>(reinterpret_cast<const char*>(k_lo) + (k_at ^ (j << 5)));
+      u4 ql;
+      if constexpr (D == 128) ql = q_rest[(wave * KS + j) * 64 + lane];
+      else ql = q_lo[j];
       s = mfma(kl, q_hi[j], s, f16());
-      s = mfma(kh, q_lo[j], s, f16());
-      s = mfma(kh, q_hi[j], s, f16());
+      s2 = mfma(kh, q_hi[j], s2, f16());
+      s = mfma(kh, ql, s, f16());
     }
+    s += s2;
     float unit[16];
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
@@ -539,7 +555,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
       s[i + 1] = __builtin_amdgcn_exp2f(fmaf(s[i + 1], rs, nref));
       sum += s[i] + s[i + 1];
       uint32_t hi, lo;
-      two_terms(s[i] * (unit[i] * per), s[i + 1] * (unit[i + 1] * per), hi, lo);
+      two_terms(s[i] * unit[i], s[i + 1] * unit[i + 1], per, hi, lo);
       p_hi[i >> 3][(i >> 1) & 3] = hi;
       p_lo[i >> 3][(i >> 1) & 3] = lo;
     }
