@@ -599,7 +599,8 @@ int64_t pipe_cache_page_bytes(int Hkv, int D, int P);
  *     counts_dev [3]       pages used so far (the next call's used_dev; at most n_free); pages that are missing
  *                          because the free list or the table's width ended; tokens cut off because they exceed T
  *                          (they count as not brought: lengths, starts and pages leave them out)
- *   counts_dev and used_dev must not overlap (several workgroups read the one and write the other).  Negative
+ *   No output may overlap an input (several workgroups read the one and write the other); the two that a caller might
+ *   confuse, counts_dev and used_dev, are checked.  Negative
  *   entries of cached_dev and fresh_dev count as 0.  The outcome does not depend on the launch.  B <= 4096.
  * Errors: PIPE_EINVAL (NULL, P), PIPE_ESHAPE (B outside 1..4096, T < 0, table_width < 1, n_free < 0).              */
 int pipe_cache_plan(const int32_t* cached_dev, const int32_t* fresh_dev, int B, int P, const int32_t* free_dev,

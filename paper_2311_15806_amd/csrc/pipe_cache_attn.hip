@@ -16,7 +16,13 @@
 // fp32 takes the codes as c - 8, subtracted in fp16 (exact), and q and P in two terms.
 // The offsets' part of the output is P (m + 8 s), with m about -8 s: no large sums that cancel.
 //
-// Bound by the bytes of the codes as long as a tile holds all rows of the head: see the figures at the launch rules.
+// Every byte of the cache is read once as long as a tile holds all rows of the head (tokens * G <= 16), and those bytes bound it:
+// two requests of 131072 tokens, 8 heads of 128, take 63 us = 4.5 TB/s, 48 of 33 to 8000 tokens 54 us = 4.0 TB/s (a large copy: 4.8).
+// To reach that: steps of 32 tokens with two in flight beside the one worked on, the table through scalar loads, a step's words in one
+// register spread by DPP (the 131072s 86 us; 64 tokens and one in flight, words and addresses in each lane: 134); equal shares of all
+// steps to as many workgroups as the chip holds (67); joined by whichever of a tile's shares ends last (one request of 777 tokens
+// 10.8 us; in a second launch 13.3).  One request of 777 tokens is eight trips to memory in a row, 10 us.  fp32 is bound by its instructions: two terms of q
+// and of the weights; 16 requests of 100 to 3000 tokens with 5 rows a tile, 32 heads of 64, take 29 us at 2.0 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -422,276 +428,276 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
   uint32_t tile = first.step / rq.steps, step0 = first.step % rq.steps;
 
   for (int place = 0;; place = 1) {        // one tile's part after the other
-  const Tile t(kr, rq, tile);
-  const uint32_t n_steps = min(rq.steps - step0, left);
-  const Walk<D, NB> w(a, t.b, kvh, l16, kg);
+    const Tile t(kr, rq, tile);
+    const uint32_t n_steps = min(rq.steps - step0, left);
+    const Walk<D, NB> w(a, t.b, kvh, l16, kg);
 
-  // q: row l16, the values that meet the words kg * KS .. of a token
-  const int row = t.row0 + l16;
-  const bool real = l16 < t.n_rows;
-  const int token = real ? row / kr.G : 0, head = real ? row % kr.G : 0;
-  const int seen = real ? t.first_seen + token : 0;      // cached tokens this row sees
-  const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)(kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
-  float qv[KS * 8], qmax = 0, qsum = 0;
-  if (kr.wide) {
+    // q: row l16, the values that meet the words kg * KS .. of a token
+    const int row = t.row0 + l16;
+    const bool real = l16 < t.n_rows;
+    const int token = real ? row / kr.G : 0, head = real ? row % kr.G : 0;
+    const int seen = real ? t.first_seen + token : 0;      // cached tokens this row sees
+    const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)(kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
+    float qv[KS * 8], qmax = 0, qsum = 0;
+    if (kr.wide) {
 #pragma unroll
-    for (int i = 0; i < KS * 8; i += 8) load8<T, true>(qp + i, qv + i);
-  } else {
+      for (int i = 0; i < KS * 8; i += 8) load8<T, true>(qp + i, qv + i);
+    } else {
 #pragma unroll
-    for (int i = 0; i < KS * 8; i += 8) load8<T, false>(qp + i, qv + i);
-  }
-  // the first steps' loads fly while q is made ready
-  const int end = (int)min((int64_t)t.end, (int64_t)(step0 + n_steps) * UNIT);
-  const int full = max(0, t.first_seen + t.row0 / kr.G);   // tokens that every row sees
-  int tok = (int)step0 * UNIT + wave * STEP, steps = 0;
-  int32_t pages[NB];
-  Tokens<D> r0, r1, r2;      // AHEAD + 1 of them, in turn
-  auto fetch = [&](Tokens<D>& x, int from) {
-    Places<NB> at;
-    w.find(at, pages, from);
-    w.load(x, at);
-  };
-  w.pages_of(pages, tok, end);
-  if (tok < end) {
-    fetch(r0, tok);
-    w.pages_of(pages, tok + UNIT, end);
-    fetch(r1, tok + UNIT);
-    w.pages_of(pages, tok + AHEAD * UNIT, end);
-  }
-#pragma unroll
-  for (int i = 0; i < KS * 8; ++i) {
-    qv[i] = real ? qv[i] : 0.f;
-    qmax = fmaxf(qmax, fabsf(qv[i]));
-  }
-  qmax = max_over_kg(qmax);
-  // a power of two that brings the row's largest value to 2^14 .. 2^15, and with it the sign of the scale
-  const int qe = qmax > 0.f && qmax < INFINITY ? max(-80, min(100, 14 - ((int)(__float_as_uint(qmax) >> 23) - 127))) : 0;
-  const float sgn = a.scale < 0.f ? -1.f : 1.f;
-  h8 q[NT][KS];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    u4 hi, lo;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {                // nibbles n and n + 4 are a register of the operand
-      const float x = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n], qe), y = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n + 4], qe);
-      qsum += x + y;
-      hi[n] = half_pair(x, y);
-      lo[n] = half_rest(x, y, hi[n]);
+      for (int i = 0; i < KS * 8; i += 8) load8<T, false>(qp + i, qv + i);
     }
-    q[0][s] = __builtin_bit_cast(h8, hi);
-    if constexpr (FINE) q[1][s] = __builtin_bit_cast(h8, lo);
-  }
-  qsum = sum_over_kg(qsum);
-  // scores in units of q * 2^qe; rs turns them into log2 of a weight
-  const float rs = a.scale == 0.f ? 1.f : ldexpf(fabsf(a.scale) * 1.44269504f, -qe);
-  const float acc0 = FINE ? 0.f : -64.f * qsum;
-
-  f4 o[MT], ones = {0.f, 0.f, 0.f, 0.f};
+    // the first steps' loads fly while q is made ready
+    const int end = (int)min((int64_t)t.end, (int64_t)(step0 + n_steps) * UNIT);
+    const int full = max(0, t.first_seen + t.row0 / kr.G);   // tokens that every row sees
+    int tok = (int)step0 * UNIT + wave * STEP, steps = 0;
+    int32_t pages[NB];
+    Tokens<D> r0, r1, r2;      // AHEAD + 1 of them, in turn
+    auto fetch = [&](Tokens<D>& x, int from) {
+      Places<NB> at;
+      w.find(at, pages, from);
+      w.load(x, at);
+    };
+    w.pages_of(pages, tok, end);
+    if (tok < end) {
+      fetch(r0, tok);
+      w.pages_of(pages, tok + UNIT, end);
+      fetch(r1, tok + UNIT);
+      w.pages_of(pages, tok + AHEAD * UNIT, end);
+    }
 #pragma unroll
-  for (int i = 0; i < MT; ++i) o[i] = (f4){0.f, 0.f, 0.f, 0.f};
-  // weights are exp2(rs * T + nref), nref = -rs * ref + log2(P_SCALE / sigma) with sigma a power of two, all scales of V under 2 sigma
-  float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = 0x1p-100f;
-
-  // one step on `c`, while the next ones' loads fly, AHEAD steps on to `n`
-  auto step = [&](const Tokens<D>& c, Tokens<D>& n) {
-    // (behind the end they read page 0, which the caches hold: behind a branch, the wait for this step's would wait for all)
-    fetch(n, tok + AHEAD * UNIT);
-    w.pages_of(pages, tok + (AHEAD + 1) * UNIT, end);
-    // scores
-    float s[2][4];
-    float ws = word_scale(c.w), wo = word_offset(c.w), wm = fmaf(8.f, ws, wo);      // scale, offset, and the offset of c - 8
-    const float ko = FINE ? wm : wo;
-    each<2>([&](auto J) {
-      constexpr int j = J;
-      f4 acc = {acc0, acc0, acc0, acc0};
+    for (int i = 0; i < KS * 8; ++i) {
+      qv[i] = real ? qv[i] : 0.f;
+      qmax = fmaxf(qmax, fabsf(qv[i]));
+    }
+    qmax = max_over_kg(qmax);
+    // a power of two that brings the row's largest value to 2^14 .. 2^15, and with it the sign of the scale
+    const int qe = qmax > 0.f && qmax < INFINITY ? max(-80, min(100, 14 - ((int)(__float_as_uint(qmax) >> 23) - 127))) : 0;
+    const float sgn = a.scale < 0.f ? -1.f : 1.f;
+    h8 q[NT][KS];
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        uint32_t e[4];
-        expand<FINE>(c.k[j][i], bits, e);
-        const h8 op = __builtin_bit_cast(h8, (u4){e[0], e[1], e[2], e[3]});
+    for (int s = 0; s < KS; ++s) {
+      u4 hi, lo;
 #pragma unroll
-        for (int m = 0; m < NT; ++m) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[m][i], acc, 0, 0, 0);
+      for (int n = 0; n < 4; ++n) {                // nibbles n and n + 4 are a register of the operand
+        const float x = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n], qe), y = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n + 4], qe);
+        qsum += x + y;
+        hi[n] = half_pair(x, y);
+        lo[n] = half_rest(x, y, hi[n]);
       }
-      each<4>([&](auto I) {
-        constexpr int i = I;
-        s[j][i] = fmaf(from_lane<4 * j + i>(ws), acc[i], from_lane<4 * j + i>(ko) * qsum);
+      q[0][s] = __builtin_bit_cast(h8, hi);
+      if constexpr (FINE) q[1][s] = __builtin_bit_cast(h8, lo);
+    }
+    qsum = sum_over_kg(qsum);
+    // scores in units of q * 2^qe; rs turns them into log2 of a weight
+    const float rs = a.scale == 0.f ? 1.f : ldexpf(fabsf(a.scale) * 1.44269504f, -qe);
+    const float acc0 = FINE ? 0.f : -64.f * qsum;
+
+    f4 o[MT], ones = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < MT; ++i) o[i] = (f4){0.f, 0.f, 0.f, 0.f};
+    // weights are exp2(rs * T + nref), nref = -rs * ref + log2(P_SCALE / sigma) with sigma a power of two, all scales of V under 2 sigma
+    float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = 0x1p-100f;
+
+    // one step on `c`, while the next ones' loads fly, AHEAD steps on to `n`
+    auto step = [&](const Tokens<D>& c, Tokens<D>& n) {
+      // (behind the end they read page 0, which the caches hold: behind a branch, the wait for this step's would wait for all)
+      fetch(n, tok + AHEAD * UNIT);
+      w.pages_of(pages, tok + (AHEAD + 1) * UNIT, end);
+      // scores
+      float s[2][4];
+      float ws = word_scale(c.w), wo = word_offset(c.w), wm = fmaf(8.f, ws, wo);      // scale, offset, and the offset of c - 8
+      const float ko = FINE ? wm : wo;
+      each<2>([&](auto J) {
+        constexpr int j = J;
+        f4 acc = {acc0, acc0, acc0, acc0};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          uint32_t e[4];
+          expand<FINE>(c.k[j][i], bits, e);
+          const h8 op = __builtin_bit_cast(h8, (u4){e[0], e[1], e[2], e[3]});
+#pragma unroll
+          for (int m = 0; m < NT; ++m) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, q[m][i], acc, 0, 0, 0);
+        }
+        each<4>([&](auto I) {
+          constexpr int i = I;
+          s[j][i] = fmaf(from_lane<4 * j + i>(ws), acc[i], from_lane<4 * j + i>(ko) * qsum);
+        });
       });
-    });
-    uint32_t vis = 0xffu;                                             // tokens that this row sees, bit 4 j + i
-    const bool some = tok + STEP > full || tok + STEP > end || c.there != (1u << NB) - 1;      // some row does not see some token
-    if (some) {
-      const int lim = min(seen, end) - tok - 4 * kg;
+      uint32_t vis = 0xffu;                                             // tokens that this row sees, bit 4 j + i
+      const bool some = tok + STEP > full || tok + STEP > end || c.there != (1u << NB) - 1;      // some row does not see some token
+      if (some) {
+        const int lim = min(seen, end) - tok - 4 * kg;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool yes = 16 * j + i < lim && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
+            s[j][i] = yes ? s[j][i] : -INFINITY;
+            vis &= yes ? ~0u : ~(1u << (4 * j + i));
+          }
+        // words that nobody sees may hold anything
+        const int j = l16 >> 2 & 1;
+        const bool live = tok + 16 * j + 4 * kg + (l16 & 3) < end && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
+        ws = live ? ws : 0.f;
+        wm = live ? wm : 0.f;
+      }
+      float smax = s[0][0];
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bool yes = 16 * j + i < lim && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
-          s[j][i] = yes ? s[j][i] : -INFINITY;
-          vis &= yes ? ~0u : ~(1u << (4 * j + i));
-        }
-      // words that nobody sees may hold anything
-      const int j = l16 >> 2 & 1;
-      const bool live = tok + 16 * j + 4 * kg + (l16 & 3) < end && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
-      ws = live ? ws : 0.f;
-      wm = live ? wm : 0.f;
-    }
-    float smax = s[0][0];
+        for (int i = 0; i < 4; ++i) smax = fmaxf(smax, s[j][i]);
+      const float vs = l16 < 8 ? 0.f : fabsf(ws);
+      if (__any(smax > lift || vs > 2.f * sigma)) {
+        const float nr = fmaxf(ref, max_over_kg(smax));
+        float top = vs;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(top) & 0x7f800000u));
+        const float f = (ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr))) * (sigma / nsigma);
+        sum *= f;
+        osum *= f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) smax = fmaxf(smax, s[j][i]);
-    const float vs = l16 < 8 ? 0.f : fabsf(ws);
-    if (__any(smax > lift || vs > 2.f * sigma)) {
-      const float nr = fmaxf(ref, max_over_kg(smax));
-      float top = vs;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-      const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(top) & 0x7f800000u));
-      const float f = (ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr))) * (sigma / nsigma);
-      sum *= f;
-      osum *= f;
-#pragma unroll
-      for (int i = 0; i < MT; ++i) o[i] *= f;
-      ones *= f;
-      ref = nr;
-      sigma = nsigma;
-      nref = (nr == -INFINITY ? 0.f : -nr * rs) + __builtin_amdgcn_logf(P_SCALE / nsigma);
-      lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
-    }
-    // weights
-    u4 p[NT];
-    auto weights = [&](auto SOME) {
-      each<2>([&](auto J) {
-        each<2>([&](auto H) {
-          constexpr int j = J, i = 2 * H;
-          float y[2];
-          each<2>([&](auto U) {
-            constexpr int u = U, bit = 4 * j + i + u, lane_of = 8 + bit;
-            const float e = __builtin_amdgcn_exp2f(fmaf(s[j][i + u], rs, nref));
-            sum += e;
-            if constexpr (SOME) {
-              const bool yes = (vis >> bit) & 1u;
-              const float m = from_lane<lane_of>(wm), g = from_lane<lane_of>(ws);
-              osum = fmaf(e, yes ? m : 0.f, osum);
-              y[u] = e * (yes ? g : 0.f);
-            } else {
-              osum = fmaf(from_lane<lane_of>(wm), e, osum);
-              y[u] = from_lane<lane_of>(ws) * e;
-            }
-          });
-          const uint32_t u = half_pair(y[0], y[1]);
-          p[0][j * 2 + (i >> 1)] = u;
-          if constexpr (FINE) p[1][j * 2 + (i >> 1)] = half_rest(y[0], y[1], u);
-        });
-      });
-    };
-    if (some) weights(std::true_type{});
-    else weights(std::false_type{});
-    if constexpr (!FINE) {
-      // the 72s of the sums so far come out now and then: over thousands of tokens of equal weight they would cost fp32 its last digits
-      if ((++steps & 7) == 0) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) o[i] = o[i] - 72.f * ones;
-        ones = (f4){0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < MT; ++i) o[i] *= f;
+        ones *= f;
+        ref = nr;
+        sigma = nsigma;
+        nref = (nr == -INFINITY ? 0.f : -nr * rs) + __builtin_amdgcn_logf(P_SCALE / nsigma);
+        lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
       }
-    }
-    // outputs
-    constexpr int NH = D / 64;       // halves of a V word: 4 codes each
-    uint32_t e[NH][4][4];            // [half][pair of tokens][nibble]
+      // weights
+      u4 p[NT];
+      auto weights = [&](auto SOME) {
+        each<2>([&](auto J) {
+          each<2>([&](auto H) {
+            constexpr int j = J, i = 2 * H;
+            float y[2];
+            each<2>([&](auto U) {
+              constexpr int u = U, bit = 4 * j + i + u, lane_of = 8 + bit;
+              const float e = __builtin_amdgcn_exp2f(fmaf(s[j][i + u], rs, nref));
+              sum += e;
+              if constexpr (SOME) {
+                const bool yes = (vis >> bit) & 1u;
+                const float m = from_lane<lane_of>(wm), g = from_lane<lane_of>(ws);
+                osum = fmaf(e, yes ? m : 0.f, osum);
+                y[u] = e * (yes ? g : 0.f);
+              } else {
+                osum = fmaf(from_lane<lane_of>(wm), e, osum);
+                y[u] = from_lane<lane_of>(ws) * e;
+              }
+            });
+            const uint32_t u = half_pair(y[0], y[1]);
+            p[0][j * 2 + (i >> 1)] = u;
+            if constexpr (FINE) p[1][j * 2 + (i >> 1)] = half_rest(y[0], y[1], u);
+          });
+        });
+      };
+      if (some) weights(std::true_type{});
+      else weights(std::false_type{});
+      if constexpr (!FINE) {
+        // the 72s of the sums so far come out now and then: over thousands of tokens of equal weight they would cost fp32 its last digits
+        if ((++steps & 7) == 0) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {    // tokens (0,1) (2,3) of one block, then of the other
-      const uint32_t x0 = c.v[u >> 1][2 * (u & 1)], x1 = c.v[u >> 1][2 * (u & 1) + 1];
-      expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x05040100u), bits, e[0][u]);
-      if constexpr (NH == 2) expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x07060302u), bits, e[1][u]);
-    }
+          for (int i = 0; i < MT; ++i) o[i] = o[i] - 72.f * ones;
+          ones = (f4){0.f, 0.f, 0.f, 0.f};
+        }
+      }
+      // outputs
+      constexpr int NH = D / 64;       // halves of a V word: 4 codes each
+      uint32_t e[NH][4][4];            // [half][pair of tokens][nibble]
 #pragma unroll
-    for (int m = 0; m < NT; ++m) {
+      for (int u = 0; u < 4; ++u) {    // tokens (0,1) (2,3) of one block, then of the other
+        const uint32_t x0 = c.v[u >> 1][2 * (u & 1)], x1 = c.v[u >> 1][2 * (u & 1) + 1];
+        expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x05040100u), bits, e[0][u]);
+        if constexpr (NH == 2) expand<FINE>(__builtin_amdgcn_perm(x1, x0, 0x07060302u), bits, e[1][u]);
+      }
+#pragma unroll
+      for (int m = 0; m < NT; ++m) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int hf = i >> 2, nb = i & 3;
+          const h8 op = __builtin_bit_cast(h8, (u4){e[hf][0][nb], e[hf][1][nb], e[hf][2][nb], e[hf][3][nb]});
+          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, __builtin_bit_cast(h8, p[m]), o[i], 0, 0, 0);
+        }
+      }
+      if constexpr (!FINE) {
+        const h8 one = {1, 1, 1, 1, 1, 1, 1, 1};
+        ones = __builtin_amdgcn_mfma_f32_16x16x32_f16(one, __builtin_bit_cast(h8, p[0]), ones, 0, 0, 0);
+      }
+      tok += UNIT;
+    };
+    while (tok < end) {
+      step(r0, r2);
+      if (tok >= end) break;
+      step(r1, r0);
+      if (tok >= end) break;
+      step(r2, r1);
+    }
+
+    // a wave's outputs as they are, O[d][row] at d = MT * (4 kg + j) + i, over the reference weight
+    sum = sum_over_kg(sum);
+    osum = sum_over_kg(osum);
+    const float lref = ref == -INFINITY ? -INFINITY : -nref;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        const int hf = i >> 2, nb = i & 3;
-        const h8 op = __builtin_bit_cast(h8, (u4){e[hf][0][nb], e[hf][1][nb], e[hf][2][nb], e[hf][3][nb]});
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(op, __builtin_bit_cast(h8, p[m]), o[i], 0, 0, 0);
+        float y = o[i][j] + osum;
+        if constexpr (!FINE) y = fmaf(-72.f, ones[j], y);
+        s_o[wave][l16][MT * (4 * kg + j) + i] = y;
+      }
+    if (kg == 0) { s_ref[wave][l16] = lref; s_sum[wave][l16] = sum; }
+    __syncthreads();
+    // the waves' parts together: a thread has D/16 values of a row
+    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * MT;
+    if (r < t.n_rows) {
+      float top = s_ref[0][r];
+#pragma unroll
+      for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_ref[i][r]);
+      float y[MT] = {}, all = 0.f;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        const float f = part_weight(s_ref[i][r], s_sum[i][r], top);
+        all = fmaf(f, s_sum[i][r], all);
+#pragma unroll
+        for (int d = 0; d < MT; ++d) y[d] = fmaf(f, s_o[i][r][d0 + d], y[d]);
+      }
+      if (n_steps == rq.steps) {
+        const float inv = top == -INFINITY && all == 0.f ? 0.f : 1.f / all;
+#pragma unroll
+        for (int d = 0; d < MT; ++d) y[d] = inv == 0.f ? 0.f : y[d] * inv;
+        store_row<T, MT>(out_row<T, D>(kr, t, kvh, r) + d0, y);
+      } else {
+        const int64_t at = (((int64_t)kvh * kr.n_share + share) * 2 + place) * ROWS + r;
+#pragma unroll
+        for (int d = 0; d < MT / 2; ++d) put_pair(kr.part_o + (at * (MT / 2) + d) * 16 + (threadIdx.x & 15), y[2 * d], y[2 * d + 1]);
+        if (d0 == 0) put_pair(kr.part_ml + at, top, all);
       }
     }
-    if constexpr (!FINE) {
-      const h8 one = {1, 1, 1, 1, 1, 1, 1, 1};
-      ones = __builtin_amdgcn_mfma_f32_16x16x32_f16(one, __builtin_bit_cast(h8, p[0]), ones, 0, 0, 0);
+    if (n_steps != rq.steps) {
+      // Every wave's stores have reached the device's scope before the count says so.
+      const uint32_t t0 = pos - step0, t1 = t0 + rq.steps;
+      const uint32_t p0 = share_of(first.total, kr.n_share, t0), p1 = share_of(first.total, kr.n_share, t1 - 1);
+      __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
+      __syncthreads();
+      // (parts: the shares from p0 to p1; where there are fewer steps than shares, as many as the tile has steps)
+      uint32_t* count = kr.arrived + kvh * kr.n_share + p0;
+      if (threadIdx.x == 0) s_last = atomicAdd(count, 1u) == (first.total < kr.n_share ? rq.steps : p1 - p0 + 1) - 1;
+      __syncthreads();
+      if (s_last) {
+        join<T, D>(kr, t, kvh, first.total, t0, p0, p1 - p0 + 1, &s_o[0][0][0]);
+        if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
     }
-    tok += UNIT;
-  };
-  while (tok < end) {
-    step(r0, r2);
-    if (tok >= end) break;
-    step(r1, r0);
-    if (tok >= end) break;
-    step(r2, r1);
-  }
-
-  // a wave's outputs as they are, O[d][row] at d = MT * (4 kg + j) + i, over the reference weight
-  sum = sum_over_kg(sum);
-  osum = sum_over_kg(osum);
-  const float lref = ref == -INFINITY ? -INFINITY : -nref;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      float y = o[i][j] + osum;
-      if constexpr (!FINE) y = fmaf(-72.f, ones[j], y);
-      s_o[wave][l16][MT * (4 * kg + j) + i] = y;
+    pos += n_steps;
+    left -= n_steps;
+    if (left == 0) break;
+    __syncthreads();                         // (the next part's outputs come to the same places)
+    step0 = 0;
+    if (++tile >= rq.tiles) {
+      tile = 0;
+      do rq = request(kr, rq.b + 1);         // (steps are left: there is a request)
+      while (rq.tiles == 0);
     }
-  if (kg == 0) { s_ref[wave][l16] = lref; s_sum[wave][l16] = sum; }
-  __syncthreads();
-  // the waves' parts together: a thread has D/16 values of a row
-  const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * MT;
-  if (r < t.n_rows) {
-    float top = s_ref[0][r];
-#pragma unroll
-    for (int i = 1; i < WAVES; ++i) top = fmaxf(top, s_ref[i][r]);
-    float y[MT] = {}, all = 0.f;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-      const float f = part_weight(s_ref[i][r], s_sum[i][r], top);
-      all = fmaf(f, s_sum[i][r], all);
-#pragma unroll
-      for (int d = 0; d < MT; ++d) y[d] = fmaf(f, s_o[i][r][d0 + d], y[d]);
-    }
-    if (n_steps == rq.steps) {
-      const float inv = top == -INFINITY && all == 0.f ? 0.f : 1.f / all;
-#pragma unroll
-      for (int d = 0; d < MT; ++d) y[d] = inv == 0.f ? 0.f : y[d] * inv;
-      store_row<T, MT>(out_row<T, D>(kr, t, kvh, r) + d0, y);
-    } else {
-      const int64_t at = (((int64_t)kvh * kr.n_share + share) * 2 + place) * ROWS + r;
-#pragma unroll
-      for (int d = 0; d < MT / 2; ++d) put_pair(kr.part_o + (at * (MT / 2) + d) * 16 + (threadIdx.x & 15), y[2 * d], y[2 * d + 1]);
-      if (d0 == 0) put_pair(kr.part_ml + at, top, all);
-    }
-  }
-  if (n_steps != rq.steps) {
-    // Every wave's stores have reached the device's scope before the count says so.
-    const uint32_t t0 = pos - step0, t1 = t0 + rq.steps;
-    const uint32_t p0 = share_of(first.total, kr.n_share, t0), p1 = share_of(first.total, kr.n_share, t1 - 1);
-    __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
-    __syncthreads();
-    // (parts: the shares from p0 to p1; where there are fewer steps than shares, as many as the tile has steps)
-    uint32_t* count = kr.arrived + kvh * kr.n_share + p0;
-    if (threadIdx.x == 0) s_last = atomicAdd(count, 1u) == (first.total < kr.n_share ? rq.steps : p1 - p0 + 1) - 1;
-    __syncthreads();
-    if (s_last) {
-      join<T, D>(kr, t, kvh, first.total, t0, p0, p1 - p0 + 1, &s_o[0][0][0]);
-      if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-  }
-  pos += n_steps;
-  left -= n_steps;
-  if (left == 0) break;
-  __syncthreads();                         // (the next part's outputs come to the same places)
-  step0 = 0;
-  if (++tile >= rq.tiles) {
-    tile = 0;
-    do rq = request(kr, rq.b + 1);         // (steps are left: there is a request)
-    while (rq.tiles == 0);
-  }
   }
 }
 

@@ -1,4 +1,18 @@
-// Attention over packed sequences.
+// Attention over packed sequences: out = softmax(scale q K^T) V in one pass over the keys, with a running reference and sum a row.
+//
+// The rows of a key/value head of a sequence are its queries' heads (row = query * G + head in the group), so that every tile of keys
+// serves the whole group.  A workgroup has 128 rows, 32 a wave, and walks its keys 64 at a time (fp32: 32):
+//   S^T[key][row] = K q^T,  P = exp2(scale log2(e) (S - ref)),  O^T[d][row] += V^T P^T
+// Both products are taken transposed: a lane then holds scores of one row only, maxima and sums need one exchange between two lanes, and the
+// scores' accumulator layout is, up to the order of the keys, that of the second product's operand: weights never go through LDS.
+//
+// The floor is the products', 4 D operations a pair of query and key that sees it: 8192 tokens, 32 heads over 8 of 128, in bf16 take
+// 0.53 ms = 1035 TFLOP/s, where a matrix product of 8192^3 reaches 1182.  At that size the matrix units and the LDS reads
+// are busy half of the time each and the softmax's instructions 45 %, between two waves a SIMD.  Seven packed prompts of 3 to 2500 tokens:
+// 0.2 ms, 750 TFLOP/s: short sequences and the causal edge leave rows and tiles unused.  fp32, 4096 tokens, 32 heads over 8 of 128: 0.54 ms,
+// 253 TFLOP/s counted once, three products each; 97 tokens 12 us, four tiles of keys in a row.
+// The tallest tiles are launched first, so that the short ones fill the end; workgroups that follow each other have different heads of the
+// same rows, which keeps the heads' keys in one XCD each where Hkv is 8.
 #include <type_traits>
 
 #include "pipe_attention.h"
@@ -371,7 +385,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
 // ------------------------------------------------------------------ fp32
 // fp32 goes through the fp16 matrix instruction as two terms, x = 2^-e (hi + lo) with hi = fp16(2^e x) and lo = fp16(2^e x - hi): 22 bits of
 // every value down to 2^-17 of the largest one of its row, for which e is chosen, and a b = hi hi + hi lo + lo hi, what is left out being
-// 2^-22 of it.  Three instructions of 32 cycles for what the fp32 instruction does in 512: 4096 tokens of 32 heads 1.15 ms there.  A key's
+// 2^-22 of it.  Three instructions of 32 cycles for what the fp32 instruction does in 512: 4096 tokens of 32 heads 1.15 ms there, 0.54 here.  A key's
 // factor of K goes back into its scores, that of V into its weight.  A tile of 32 keys is loaded one ahead into registers and split on its
 // way into LDS, once for all waves.
 
