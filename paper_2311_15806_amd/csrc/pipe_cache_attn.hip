@@ -64,7 +64,7 @@ struct Kernel {
 // workgroups busy to the end, and one long request is split.  Of a tile that several shares hold, each writes its part -- of its first tile
 // to place 0, of its last to place 1 -- and whoever comes last sums them, in the shares' order.
 struct Request {
-  int b, start, n;              // its fresh tokens (b = B: the rows behind the last request, which see nothing)
+  int b, start, n;              // its fresh tokens (b = B: the rows behind the last request and, after those, the ones before the first: they see nothing)
   int length, held;             // cached tokens, and those of them that its table has room for
   uint32_t tiles, steps;        // ... each of so many steps
 };
@@ -78,9 +78,9 @@ __device__ __forceinline__ Request make_request(const Kernel& k, int b, int star
 }
 __device__ __forceinline__ Request request(const Kernel& k, int b) {
   const CacheAttnArgs& a = k.a;
-  auto start_of = [&](int i) { return i > 0 ? min(max(a.starts[i], 0), a.T) : 0; };
-  const int start = start_of(b);
-  return make_request(k, b, start, max(0, (b < a.B ? start_of(b + 1) : a.T) - start), b < a.B ? max(0, a.lengths[b]) : 0);
+  auto start_of = [&](int i) { return min(max(a.starts[i], 0), a.T); };
+  const int start = start_of(b), first = start_of(0);
+  return make_request(k, b, start, max(0, (b < a.B ? start_of(b + 1) : a.T + min(first, start)) - start), b < a.B ? max(0, a.lengths[b]) : 0);
 }
 // Where a share begins.  (All steps of a head together are under 2^31: the launch sees to it.)
 __device__ __forceinline__ uint32_t share_begin(uint32_t total, uint32_t n_share, uint32_t share) {
@@ -177,10 +177,15 @@ struct Tile {
   }
 };
 
+// its i-th token's row of q and of the output
+__device__ __forceinline__ int token_row(const Kernel& k, const Tile& t, int i) {
+  const int at = t.start + i;
+  return at < k.a.T ? at : at - k.a.T;
+}
 template <typename T, int D>
 __device__ __forceinline__ T* out_row(const Kernel& k, const Tile& t, int kvh, int r) {
   const int row = t.row0 + r;
-  return (T*)k.a.out + ((int64_t)(t.start + row / k.G) * k.a.Hq + (int64_t)kvh * k.G + row % k.G) * D;
+  return (T*)k.a.out + ((int64_t)token_row(k, t, row / k.G) * k.a.Hq + (int64_t)kvh * k.G + row % k.G) * D;
 }
 
 // what a part counts, beside the largest reference: nothing if it saw nothing (and NaN if it saw nothing but NaN)
@@ -437,7 +442,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     const bool real = l16 < t.n_rows;
     const int token = real ? row / kr.G : 0, head = real ? row % kr.G : 0;
     const int seen = real ? t.first_seen + token : 0;      // cached tokens this row sees
-    const T* qp = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)(kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
+    const T* qp = (const T*)a.q + (int64_t)token_row(kr, t, token) * a.qs.token + (int64_t)(kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
     float qv[KS * 8], qmax = 0, qsum = 0;
     if (kr.wide) {
 #pragma unroll

@@ -68,13 +68,16 @@ struct Tile {
   int row0, n_rows, start;    // rows row0 .. of a sequence whose queries start at `start`; row = query * G + head in the group
   int k0, nk;                 // its keys
   int first_seen;             // keys that its first query sees (causal; may be negative)
+  int none;                   // queries that see nothing ahead of them: the rows before the first sequence are counted to it
 };
 
 // Tile `id` of the launch: sequence b (B: the rows behind the last one, which see nothing) owns the ids from
 // floor(start_b * G / QROWS) + b on.
-__device__ __forceinline__ Tile find_tile(const Kernel& k, int id) {
+__device__ __forceinline__ Tile find_tile(const Kernel& k, int place) {
   const PromptAttnArgs& a = k.a;
+  const int id = k.n_tiles - 1 - place;       // (long tiles first: the last queries see most)
   const int lane = threadIdx.x & 63;
+  const int none = min(max(a.q_starts[0], 0), a.Tq);
   auto start_of = [&](int i) { return i > 0 ? min(max(a.q_starts[min(i, a.B)], 0), a.Tq) : 0; };
   auto key_of = [&](int i) { return min(max(a.k_starts[min(i, a.B)], 0), a.Tk); };
   auto first_id = [&](int start, int i) { return (int)(((int64_t)start * k.G) / QROWS) + i; };
@@ -108,6 +111,7 @@ __device__ __forceinline__ Tile find_tile(const Kernel& k, int id) {
   t.k0 = k0;
   t.nk = max(0, k1 - k0);
   t.first_seen = t.nk - n + 1;
+  t.none = b > 0 ? 0 : none;
   return t;
 }
 
@@ -126,7 +130,7 @@ struct Row {
     real = lrow < t.n_rows;
     const int row = t.row0 + (real ? lrow : 0);
     const int token = row / k.G, head = kvh * k.G + row % k.G;
-    auto seen_by = [&](int query) { return a.causal ? max(0, min(t.nk, t.first_seen + query)) : t.nk; };
+    auto seen_by = [&](int query) { return query < t.none ? 0 : a.causal ? max(0, min(t.nk, t.first_seen + query)) : t.nk; };
     seen = real ? seen_by(token) : 0;
     q = (const T*)a.q + (int64_t)(t.start + token) * a.qs.token + (int64_t)head * a.qs.head;
     out = (T*)a.out + ((int64_t)(t.start + token) * a.Hq + head) * a.D;
@@ -153,9 +157,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   // one array per slot: the compiler tells loads into one from reads of another by the array
   __shared__ alignas(1024) u4 k_a[KEYS * CH], k_b[KEYS * CH], v_a[KEYS * CH], v_b[KEYS * CH];
   const PromptAttnArgs& a = kr.a;
-  // (long tiles first: the last queries see most)
   const int id = blockIdx.x, kvh = id % a.Hkv;
-  const Tile t = find_tile(kr, kr.n_tiles - 1 - id / a.Hkv);
+  const Tile t = find_tile(kr, id / a.Hkv);
   if (t.n_rows == 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;
@@ -424,7 +427,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   __shared__ alignas(16) float k_unit[KEYS32], v_unit[KEYS32];     // what a key's scaled values are multiples of
   const PromptAttnArgs& a = kr.a;
   const int id = blockIdx.x, kvh = id % a.Hkv;
-  const Tile t = find_tile(kr, kr.n_tiles - 1 - id / a.Hkv);
+  const Tile t = find_tile(kr, id / a.Hkv);
   if (t.n_rows == 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 31, h = lane >> 5;

@@ -464,6 +464,73 @@ def test_rows_of_no_sequence_are_zeros(pipe):
     assert torch.isfinite(out).all() and not out[11:].any() and out[:11].any()
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("first", [3, 40])
+def test_rows_before_the_first_sequence_are_zeros(pipe, kind, causal, first):
+    Hq, Hkv, D, nq, nk = 4, 2, 64, [50, 9], [130, 9]
+    rng = np.random.default_rng(first)
+    q, qf = typed(rng, (first + sum(nq), Hq, D), kind)
+    k, kf = typed(rng, (5 + sum(nk), Hkv, D), kind)
+    v, vf = typed(rng, (5 + sum(nk), Hkv, D), kind)
+    got = pipe.pipe_prompt_attention(q, k, v, ints(first + np.array([0, 50, 59])), ints(5 + np.array([0, 130, 139])), causal=causal)
+    got = got.double().cpu().numpy()
+    want = prompt_reference(qf[first:], kf[5:], vf[5:], nq, nk, causal, D ** -0.5)
+    a = D ** -0.5 * float(np.abs(qf).max()) * float(np.abs(kf).sum(-1).max())
+    assert not got[:first].any()
+    assert np.abs(got[first:] - want).max() <= ref.far(kind, D, 130, a, float(np.abs(vf).max()))
+
+
+@pytest.mark.parametrize("B", [2, 70])
+@pytest.mark.parametrize("first", [3, 40])
+def test_rows_before_the_first_request_are_zeros(pipe, B, first):
+    Hq, Hkv, D, P = 8, 2, 64, 16
+    rng = np.random.default_rng(B + first)
+    lens = [200] + list(rng.integers(1, 300, B - 1))
+    cache, table, kv = random_cache(pipe, rng, lens, Hkv, D, P)
+    q, qf = typed(rng, (first + B, Hq, D), "f16")
+    got = pipe.pipe_cache_attention(q, ints(first + np.arange(B + 1)), ints(lens), cache, table, P, Hkv).double().cpu().numpy()
+    want = cache_reference(qf[first:], [1] * B, lens, kv, D ** -0.5)
+    assert not got[:first].any()
+    assert np.abs(got[first:] - want).max() <= cache_far("f16", D, qf, lens, D ** -0.5)
+
+
+def lengths_of_many_tiles(B, T, rng):
+    n = np.floor(rng.dirichlet(np.full(B, 0.5)) * T).astype(int)
+    if B > 2:
+        n[B // 2] = 0
+    return list(n)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("B", [2, 9, 31])
+def test_prompt_attention_of_many_tiles(pipe, B, causal, kind):
+    """More tiles than the chip holds at once, of sequences of very different lengths, some with a prefix, some with fewer keys than queries,
+    rows of none before and behind them: every row is computed once, by the tile that owns it.  Heads repeat, so that one reference serves."""
+    Hkv, G, D, T = 150, 2, 64, 600
+    rng = np.random.default_rng(B)
+    nq = lengths_of_many_tiles(B, T, rng)
+    nk = [int(n * f) for n, f in zip(nq, rng.choice([0.5, 1.0, 1.0, 2.5], B))]
+    first, Tq, Tk = 2, 5 + sum(nq), sum(nk)
+    q1, qf = typed(rng, (Tq, G, D), kind)
+    k1, kf = typed(rng, (Tk, 1, D), kind)
+    v1, vf = typed(rng, (Tk, 1, D), kind)
+    assert (Tq * G // 128 + B + 1) * Hkv > 512
+    q, k, v = q1.repeat(1, Hkv, 1), k1.expand(Tk, Hkv, D), v1.expand(Tk, Hkv, D)
+    starts, starts_k = ints(first + np.concatenate([[0], np.cumsum(nq)])), ints(np.concatenate([[0], np.cumsum(nk)]))
+    out = torch.full((Tq, Hkv * G, D), float("nan"), dtype=DT[kind], device="cuda")
+    pipe.pipe_prompt_attention(q, k, v, starts, starts_k, causal=causal, out=out)
+    got = out.view(Tq, Hkv, G, D)
+    assert torch.equal(got, got[:, :1].expand_as(got))
+    got = got[:, 0].double().cpu().numpy()
+    want = prompt_reference(qf[first:], kf, vf, nq, nk, causal, D ** -0.5)
+    a = D ** -0.5 * float(np.abs(qf).max()) * float(np.abs(kf).sum(-1).max())
+    n = first + sum(nq)
+    assert not got[:first].any() and not got[n:].any()
+    assert np.abs(got[first:n] - want[:sum(nq)]).max() <= ref.far(kind, D, max(nk), a, float(np.abs(vf).max()))
+
+
 # ------------------------------------------------------------------ graphs, streams, refusals
 
 def test_a_step_in_a_graph(pipe):
