@@ -17,7 +17,7 @@
 // The offsets' part of the output is P (m + 8 s), with m about -8 s: no large sums that cancel.
 //
 // Every byte of the cache is read once as long as a tile holds all rows of the head (tokens * G <= 16), and those bytes bound it:
-// two requests of 131072 tokens, 8 heads of 128, take 63 us = 4.5 TB/s, 48 of 33 to 8000 tokens 54 us = 4.0 TB/s (a large copy: 4.8).
+// two requests of 131072 tokens, 8 heads of 128, take 62 us = 4.6 TB/s, 48 of 33 to 8000 tokens 54 us = 4.0 TB/s (a large copy: 4.8).
 // To reach that: steps of 32 tokens with two in flight beside the one worked on, the table through scalar loads, a step's words in one
 // register spread by DPP (the 131072s 86 us; 64 tokens and one in flight, words and addresses in each lane: 134); equal shares of all
 // steps to as many workgroups as the chip holds (67); joined by whichever of a tile's shares ends last (one request of 777 tokens
@@ -53,6 +53,7 @@ struct Kernel {
   CacheAttnArgs a;
   int G;
   uint32_t n_share; // workgroups of a key/value head
+  float load;       // of one of them on a compute unit, for each key/value head
   bool wide;        // 16-byte loads of q
   uint64_t* part_o;     // [Hkv][n_share][2][16 rows][D/32][16]: pairs of outputs
   uint64_t* part_ml;    // [Hkv][n_share][2][16 rows]: log2 of the reference weight, sum of weights
@@ -60,9 +61,12 @@ struct Kernel {
 };
 
 // The work of a key/value head is the tiles of all requests one after the other, a tile of request b counting the steps of UNIT tokens that
-// its cache has; every workgroup takes an equal share of the steps, wherever it begins and ends.  So requests of any lengths keep all
-// workgroups busy to the end, and one long request is split.  Of a tile that several shares hold, each writes its part -- of its first tile
-// to place 0, of its last to place 1 -- and whoever comes last sums them, in the shares' order.
+// its cache has.  A workgroup takes one of two kinds of share, whichever `locate` reckons to end first:
+//   equal ones of all steps, wherever they begin and end: requests of any lengths keep all workgroups busy to the end;
+//   one tile, or one of the parts of `each` steps that a tile is cut into: no share then ends one tile and begins the next, which is a chain of
+//   trips to memory of its own, and a tile in one piece needs no parts joined.
+// Of a tile that several shares hold, each writes its part -- of its first tile to place 0, of its last to place 1 -- and whoever comes last
+// sums them, in the shares' order.
 struct Request {
   int b, start, n;              // its fresh tokens (b = B: the rows behind the last request and, after those, the ones before the first: they see nothing)
   int length, held;             // cached tokens, and those of them that its table has room for
@@ -92,20 +96,37 @@ __device__ __forceinline__ uint32_t share_of(uint32_t total, uint32_t n_share, u
 }
 struct Place {
   uint32_t total, at;           // steps of the head, and the first of the share,
-  uint32_t step;                // which is this step
+  uint32_t step, n;             // which is this step; the steps of the share
+  uint32_t each;                // steps of a part; 0: equal shares
   Request r;                    // of this request
 };
 template <typename T>
 __device__ __forceinline__ T of_lane(T x, int lane) { return (T)__builtin_amdgcn_readlane((int)x, lane); }
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {     // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_up(x, d);
-    if (lane >= d) x += o;
-  }
-  return x;
+// f over the lanes up to each one (the last lane: over all), f(0, x) = x
+template <int CTRL, int ROWS_OF_16>
+__device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS_OF_16, 0xf, false); }
+template <typename F>
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, F f) {
+  x = f(x, moved<0x111, 0xf>(x));      // from 1, 2, 4 and 8 lanes below within 16
+  x = f(x, moved<0x112, 0xf>(x));
+  x = f(x, moved<0x114, 0xf>(x));
+  x = f(x, moved<0x118, 0xf>(x));
+  x = f(x, moved<0x142, 0xa>(x));      // the last lane of the 16 below to every second 16
+  return f(x, moved<0x143, 0xc>(x));   // lane 31 to the upper half
 }
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  return wave_scan(x, [](uint32_t a, uint32_t b) { return a + b; });
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  return of_lane(wave_scan(x, [](uint32_t a, uint32_t b) { return max(a, b); }), 63);
+}
+
+// What the kinds of shares cost, in steps of a workgroup that has a compute unit to itself (0.7 us): LOAD steps' worth of every unit's time goes
+// into each, the more of them at once the slower; JOIN for the trips of parts to memory and back, BREAK for a tile's end and the next one's
+// begin in a share.  16 requests of 750 tokens, 32 heads of 64 in bf16: whole 12.8 us, in equal shares 21.1; of 3000 tokens, 29 and 34; of 100 to 3000
+// in fp32, 31 and 30; 8 heads of 128, 750 tokens: whole 11.2, in parts 13.0; 3000 tokens: 24 and 19.
+constexpr int UNITS = 256;
+constexpr float LOAD_64 = 0.67f, LOAD_128 = 1.f, JOIN = 4.f, BREAK = 8.f;
 
 // The first place of a share.  Up to 63 requests: every wave for itself, a lane a request.  More: the workgroup together, a thread sums
 // every 256th part of them, and the one whose sum holds the place walks them again.
@@ -118,7 +139,37 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
     const Request r = request(k, min(lane, k.a.B));
     const uint32_t mine = lane < B1 ? r.tiles * r.steps : 0u, inc = wave_scan(mine);
     p.total = of_lane(inc, 63);
+    if (k.n_share > 1) {
+      const uint32_t tiles = lane < B1 ? r.tiles : 0u, inc_t = wave_scan(tiles), all = of_lane(inc_t, 63);
+      const uint32_t longest = wave_max(tiles > 0 ? r.steps : 0u);
+      if (all > 0 && all <= k.n_share) {
+        // parts of as few steps as will do: of the average of a share, or if that makes too many of them, of so many that it cannot, a tile
+        // of s steps having (s + cut - 1) / cut parts at most
+        auto parts_of = [&](uint32_t cut) { return (r.steps + cut - 1) / cut; };
+        uint32_t cut = (p.total + k.n_share - 1) / k.n_share;
+        const uint32_t spare = k.n_share - all;
+        if (of_lane(wave_scan(tiles * parts_of(cut)), 63) > k.n_share) cut = spare > 0 ? min(longest, (p.total - all + spare - 1) / spare) : longest;
+        const float load = k.load;
+        const float whole = longest * fmaxf(1.f, all * load);
+        const float parts = cut * fmaxf(1.f, min(k.n_share, p.total / cut + all) * load) + JOIN;
+        const float equal = (float)p.total / k.n_share * fmaxf(1.f, k.n_share * load) + JOIN + BREAK;
+        if (fminf(whole, parts) <= equal) {
+          p.each = whole <= parts ? longest : cut;
+          const uint32_t per = parts_of(p.each), n = tiles * per, inc_p = wave_scan(n);
+          const unsigned long long behind = __ballot(inc_p > share);
+          const int b = behind ? __builtin_ctzll(behind) : 0;
+          p.r = make_request(k, b, of_lane(r.start, b), of_lane(r.n, b), of_lane(r.length, b));
+          const uint32_t at = share - of_lane(inc_p - n, b), per_b = of_lane(per, b), cut_at = at % per_b * p.each;
+          p.at = 0;
+          p.step = at / per_b * p.r.steps + cut_at;
+          p.n = behind ? min(p.each, p.r.steps - cut_at) : 0;
+          return p;
+        }
+      }
+    }
+    p.each = 0;
     p.at = share_begin(p.total, k.n_share, share);
+    p.n = share_begin(p.total, k.n_share, share + 1) - p.at;
     const unsigned long long behind = __ballot(inc > p.at);
     const int b = behind ? __builtin_ctzll(behind) : 0;
     p.step = p.at - of_lane(inc - mine, b);
@@ -143,7 +194,9 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
     before += w < wave ? s_sum[w] : 0;
     p.total += s_sum[w];
   }
+  p.each = 0;
   p.at = share_begin(p.total, k.n_share, share);
+  p.n = share_begin(p.total, k.n_share, share + 1) - p.at;
   if (before <= p.at && p.at < before + mine) {
     for (int b = b0; b < b1; ++b) {
       const Request r = request(k, b);
@@ -159,6 +212,7 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
   __syncthreads();
   p.total = __builtin_amdgcn_readfirstlane(p.total);
   p.at = __builtin_amdgcn_readfirstlane(p.at);
+  p.n = __builtin_amdgcn_readfirstlane(p.n);
   p.step = __builtin_amdgcn_readfirstlane(s_step);
   p.r = request(k, __builtin_amdgcn_readfirstlane(s_b));
   return p;
@@ -343,8 +397,8 @@ __device__ __forceinline__ float2 get_pair(const uint64_t* p) {
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
-// The parts of a tile together, in the shares' order: the tile's steps begin at t0, in share p0; n_part shares from there on (empty ones among
-// them).  scratch: 16 * 16 * (D/16 + 1) + 32 floats of LDS.
+// The parts of a tile together, in the shares' order: n_part shares from share p0 on.  Equal shares of `total` steps: the tile's steps begin at t0,
+// and empty shares may be among them; total = 0: a part a share.  scratch: 16 * 16 * (D/16 + 1) + 32 floats of LDS.
 template <typename T, int D>
 __device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, uint32_t total, uint32_t t0, uint32_t p0, uint32_t n_part, float* scratch) {
   constexpr int MT = D / 16;
@@ -363,8 +417,8 @@ __device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, u
       for (int u = 0; u < AT_ONCE; ++u) {
         const uint32_t p = min(q + u * groups, n_part - 1) + p0;
         const uint32_t b0 = share_begin(total, kr.n_share, p);
-        const bool there = q + u * groups < n_part && b0 < share_begin(total, kr.n_share, p + 1);
-        const int64_t at = (((int64_t)kvh * kr.n_share + p) * 2 + (b0 < t0 ? 1 : 0)) * ROWS + r;
+        const bool there = q + u * groups < n_part && (total == 0 || b0 < share_begin(total, kr.n_share, p + 1));
+        const int64_t at = (((int64_t)kvh * kr.n_share + p) * 2 + (total > 0 && b0 < t0 ? 1 : 0)) * ROWS + r;
         const float2 m = there ? get_pair(kr.part_ml + at) : make_float2(-INFINITY, 0.f);
         lref[u] = m.x;
         sum[u] = m.y;
@@ -424,7 +478,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
   const uint32_t share = blockIdx.x / a.cache.Hkv;
   const int kvh = blockIdx.x % a.cache.Hkv;
   const Place first = locate(kr, share);
-  uint32_t pos = first.at, left = share_begin(first.total, kr.n_share, share + 1) - pos;
+  uint32_t pos = first.at, left = first.n;
   if (left == 0) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
@@ -681,15 +735,17 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     if (n_steps != rq.steps) {
       // Every wave's stores have reached the device's scope before the count says so.
       const uint32_t t0 = pos - step0, t1 = t0 + rq.steps;
-      const uint32_t p0 = share_of(first.total, kr.n_share, t0), p1 = share_of(first.total, kr.n_share, t1 - 1);
+      const bool cut = first.each > 0;
+      const uint32_t p0 = cut ? share - step0 / first.each : share_of(first.total, kr.n_share, t0);
+      const uint32_t n_part = cut ? (rq.steps + first.each - 1) / first.each : share_of(first.total, kr.n_share, t1 - 1) - p0 + 1;
       __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
       __syncthreads();
-      // (parts: the shares from p0 to p1; where there are fewer steps than shares, as many as the tile has steps)
+      // (equal shares, fewer steps than them: as many parts as the tile has steps)
       uint32_t* count = kr.arrived + kvh * kr.n_share + p0;
-      if (threadIdx.x == 0) s_last = atomicAdd(count, 1u) == (first.total < kr.n_share ? rq.steps : p1 - p0 + 1) - 1;
+      if (threadIdx.x == 0) s_last = atomicAdd(count, 1u) == (!cut && first.total < kr.n_share ? rq.steps : n_part) - 1;
       __syncthreads();
       if (s_last) {
-        join<T, D>(kr, t, kvh, first.total, t0, p0, p1 - p0 + 1, &s_o[0][0][0]);
+        join<T, D>(kr, t, kvh, cut ? 0 : first.total, t0, p0, n_part, &s_o[0][0][0]);
         if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
@@ -726,11 +782,12 @@ int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   // No more shares than there are steps, as far as the longest request is known; tiles of up to 3 steps stay whole (300 tokens: 9.8 us a
   // call whole, 11.0 in parts; 777 tokens 12.5 and 11.1).
   const int64_t longest = a.max_length > 0 ? a.max_length : (int64_t)a.width << a.cache.shift;
-  const int64_t tiles = std::max<int64_t>(((int64_t)a.T * k.G + ROWS - 1) / ROWS, std::min(a.B, a.T));
+  const int64_t tiles = ((int64_t)a.T * k.G + std::min<int64_t>((int64_t)a.B + 1, a.T) * (ROWS - 1)) / ROWS;      // at most: those of a request round up
   const int64_t most = (a.D == 64 ? SHARES_64 : SHARES_128) / a.cache.Hkv;
   const int64_t room = std::min<int64_t>((int64_t)a.width << a.cache.shift, 0x7ffff000);
   if ((((int64_t)a.T * k.G + ROWS - 1) / ROWS + a.B + 1) * (room / UNIT + 1) > 0x7fffffff) return PIPE_ESHAPE;
   k.n_share = (uint32_t)std::max<int64_t>(1, std::min(most, tiles * (longest <= 3 * UNIT ? 1 : (longest + UNIT - 1) / UNIT)));
+  k.load = (a.D == 64 ? LOAD_64 : LOAD_128) * a.cache.Hkv / UNITS;
   if (k.n_share > 1 || pipe_dry_run()) {
     const size_t parts = (size_t)SHARES_64 * 2 * ROWS;       // one size serves every call
     int rc = PIPE_OK;

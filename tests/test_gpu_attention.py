@@ -284,6 +284,31 @@ def test_cache_attention_of_many_requests(pipe, B):
         assert not got[int(fresh.sum()):].any()
 
 
+SHARES = {
+    # Hq, Hkv, lengths, fresh: what a workgroup gets
+    "one tile each": (32, 32, [640 + 7 * i for i in range(16)], [1] * 16),
+    "parts of one tile": (8, 2, [100, 2000, 3001], [1, 1, 1]),
+    "parts of requests of several tiles": (4, 2, [2000, 130, 900], [40, 1, 3]),
+    "equal shares": (8, 8, [300 + 150 * (i % 7) + 3200 * (i % 9 == 0) for i in range(60)], [1 + (i % 5 == 0) for i in range(60)]),
+}
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("shares", SHARES)
+def test_cache_attention_in_shares(pipe, kind, shares):
+    Hq, Hkv, lens, fresh = SHARES[shares]
+    D, P = 64, 16
+    rng = np.random.default_rng(len(lens))
+    cache, table, kv = random_cache(pipe, rng, lens, Hkv, D, P)
+    q, qf = typed(rng, (sum(fresh) + 3, Hq, D), kind)        # rows of no request behind them
+    starts = ints(np.concatenate([[0], np.cumsum(fresh)]))
+    got = pipe.pipe_cache_attention(q, starts, ints(lens), cache, table, P, Hkv, max_length=max(lens))
+    want = cache_reference(qf, fresh, lens, kv, D ** -0.5)
+    assert np.abs(got.double().cpu().numpy() - want).max() <= cache_far(kind, D, qf, lens, D ** -0.5)
+    for _ in range(3):                                       # the counts of parts are back at zero, and the order of arrival does not matter
+        assert torch.equal(got, pipe.pipe_cache_attention(q, starts, ints(lens), cache, table, P, Hkv, max_length=max(lens)))
+
+
 def test_cache_attention_of_padded_steps_missing_pages_and_strided_queries(pipe):
     Hq, Hkv, D, P, lens = 8, 2, 64, 16, [40, 70]
     rng = np.random.default_rng(9)
