@@ -62,7 +62,8 @@ struct Kernel {
 
 // The work of a key/value head is the tiles of all requests one after the other, a tile of request b counting the steps of UNIT tokens that
 // its cache has.  A workgroup takes one of two kinds of share, whichever `locate` reckons to end first:
-//   equal ones of all steps, wherever they begin and end: requests of any lengths keep all workgroups busy to the end;
+//   equal ones of all steps, wherever they begin and end: requests of any lengths keep all workgroups busy to the end.  A tile counts GAP steps
+//   more ahead of its own, for the work of beginning it;
 //   one tile, or one of the parts of `each` steps that a tile is cut into: no share then ends one tile and begins the next, which is a chain of
 //   trips to memory of its own, and a tile in one piece needs no parts joined.
 // Of a tile that several shares hold, each writes its part -- of its first tile to place 0, of its last to place 1 -- and whoever comes last
@@ -95,9 +96,9 @@ __device__ __forceinline__ uint32_t share_of(uint32_t total, uint32_t n_share, u
   return (uint32_t)(((uint64_t)(step + 1) * n_share - 1) / total);
 }
 struct Place {
-  uint32_t total, at;           // steps of the head, and the first of the share,
+  uint32_t total, at;           // steps of the head, and the first of the share, gaps included (`at`: equal shares only),
   uint32_t step, n;             // which is this step; the steps of the share
-  uint32_t each;                // steps of a part; 0: equal shares
+  uint32_t each;                // steps of a part, no gaps; 0: equal shares
   Request r;                    // of this request
 };
 template <typename T>
@@ -122,11 +123,11 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 }
 
 // What the kinds of shares cost, in steps of a workgroup that has a compute unit to itself (0.7 us): LOAD steps' worth of every unit's time goes
-// into each, the more of them at once the slower; JOIN for the trips of parts to memory and back, BREAK for a tile's end and the next one's
-// begin in a share.  16 requests of 750 tokens, 32 heads of 64 in bf16: whole 12.8 us, in equal shares 21.1; of 3000 tokens, 29 and 34; of 100 to 3000
+// into each, the more of them at once the slower; JOIN for the trips of parts to memory and back, and a GAP a tile that equal shares begin.  16 requests of 750 tokens, 32 heads of 64 in bf16: whole 12.8 us, in equal shares 21.1; of 3000 tokens, 29 and 34; of 100 to 3000
 // in fp32, 31 and 30; 8 heads of 128, 750 tokens: whole 11.2, in parts 13.0; 3000 tokens: 24 and 19.
 constexpr int UNITS = 256;
-constexpr float LOAD_64 = 0.67f, LOAD_128 = 1.f, JOIN = 4.f, BREAK = 8.f;
+constexpr float LOAD_64 = 0.67f, LOAD_128 = 1.f, JOIN = 4.f;
+constexpr uint32_t GAP = 4;      // 48 requests of 33 to 8000 tokens: 54.8 us with 0, 53.6 with 2, 51.8 with 4, 53.0 with 6
 
 // The first place of a share.  Up to 63 requests: every wave for itself, a lane a request.  More: the workgroup together, a thread sums
 // every 256th part of them, and the one whose sum holds the place walks them again.
@@ -138,21 +139,22 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
   if (B1 <= 64) {
     const Request r = request(k, min(lane, k.a.B));
     const uint32_t mine = lane < B1 ? r.tiles * r.steps : 0u, inc = wave_scan(mine);
-    p.total = of_lane(inc, 63);
+    const uint32_t tiles = lane < B1 ? r.tiles : 0u, inc_t = wave_scan(tiles), all = of_lane(inc_t, 63);
+    const uint32_t total = of_lane(inc, 63);
+    p.total = total + GAP * all;
     if (k.n_share > 1) {
-      const uint32_t tiles = lane < B1 ? r.tiles : 0u, inc_t = wave_scan(tiles), all = of_lane(inc_t, 63);
       const uint32_t longest = wave_max(tiles > 0 ? r.steps : 0u);
       if (all > 0 && all <= k.n_share) {
         // parts of as few steps as will do: of the average of a share, or if that makes too many of them, of so many that it cannot, a tile
         // of s steps having (s + cut - 1) / cut parts at most
         auto parts_of = [&](uint32_t cut) { return (r.steps + cut - 1) / cut; };
-        uint32_t cut = (p.total + k.n_share - 1) / k.n_share;
+        uint32_t cut = (total + k.n_share - 1) / k.n_share;
         const uint32_t spare = k.n_share - all;
-        if (of_lane(wave_scan(tiles * parts_of(cut)), 63) > k.n_share) cut = spare > 0 ? min(longest, (p.total - all + spare - 1) / spare) : longest;
+        if (of_lane(wave_scan(tiles * parts_of(cut)), 63) > k.n_share) cut = spare > 0 ? min(longest, (total - all + spare - 1) / spare) : longest;
         const float load = k.load;
         const float whole = longest * fmaxf(1.f, all * load);
-        const float parts = cut * fmaxf(1.f, min(k.n_share, p.total / cut + all) * load) + JOIN;
-        const float equal = (float)p.total / k.n_share * fmaxf(1.f, k.n_share * load) + JOIN + BREAK;
+        const float parts = cut * fmaxf(1.f, min(k.n_share, total / cut + all) * load) + JOIN;
+        const float equal = (float)p.total / k.n_share * fmaxf(1.f, k.n_share * load) + JOIN;
         if (fminf(whole, parts) <= equal) {
           p.each = whole <= parts ? longest : cut;
           const uint32_t per = parts_of(p.each), n = tiles * per, inc_p = wave_scan(n);
@@ -170,9 +172,10 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
     p.each = 0;
     p.at = share_begin(p.total, k.n_share, share);
     p.n = share_begin(p.total, k.n_share, share + 1) - p.at;
-    const unsigned long long behind = __ballot(inc > p.at);
+    const uint32_t inc_w = inc + GAP * inc_t, before_w = inc_w - mine - GAP * tiles;
+    const unsigned long long behind = __ballot(inc_w > p.at);
     const int b = behind ? __builtin_ctzll(behind) : 0;
-    p.step = p.at - of_lane(inc - mine, b);
+    p.step = p.at - of_lane(before_w, b);
     p.r = make_request(k, b, of_lane(r.start, b), of_lane(r.n, b), of_lane(r.length, b));
     return p;
   }
@@ -181,7 +184,7 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
   uint32_t mine = 0;
   for (int b = b0; b < b1; ++b) {
     const Request r = request(k, b);
-    mine += r.tiles * r.steps;
+    mine += r.tiles * (r.steps + GAP);
   }
   const uint32_t inc = wave_scan(mine);
   if (lane == 63) s_sum[wave] = inc;
@@ -200,7 +203,7 @@ __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
   if (before <= p.at && p.at < before + mine) {
     for (int b = b0; b < b1; ++b) {
       const Request r = request(k, b);
-      const uint32_t c = r.tiles * r.steps;
+      const uint32_t c = r.tiles * (r.steps + GAP);
       if (p.at < before + c) {
         s_b = b;
         s_step = p.at - before;
@@ -397,7 +400,7 @@ __device__ __forceinline__ float2 get_pair(const uint64_t* p) {
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
-// The parts of a tile together, in the shares' order: n_part shares from share p0 on.  Equal shares of `total` steps: the tile's steps begin at t0,
+// The parts of a tile together, in the shares' order: n_part shares from share p0 on.  Equal shares of `total` steps: the tile begins at t0,
 // and empty shares may be among them; total = 0: a part a share.  scratch: 16 * 16 * (D/16 + 1) + 32 floats of LDS.
 template <typename T, int D>
 __device__ __forceinline__ void join(const Kernel& kr, const Tile& t, int kvh, uint32_t total, uint32_t t0, uint32_t p0, uint32_t n_part, float* scratch) {
@@ -484,11 +487,13 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
   const int l16 = lane & 15, kg = lane >> 4;
   const Bits bits;
   Request rq = first.r;
-  uint32_t tile = first.step / rq.steps, step0 = first.step % rq.steps;
+  const uint32_t gap = first.each > 0 ? 0 : GAP;
+  uint32_t tile = first.step / (rq.steps + gap), at = first.step % (rq.steps + gap);
 
   for (int place = 0;; place = 1) {        // one tile's part after the other
+    const uint32_t to = min(rq.steps + gap, at + left), step0 = max(at, gap) - gap, n_steps = max(to, gap) - gap - step0;
+    if (n_steps == 0) break;               // (the share ends ahead of the tile's steps)
     const Tile t(kr, rq, tile);
-    const uint32_t n_steps = min(rq.steps - step0, left);
     const Walk<D, NB> w(a, t.b, kvh, l16, kg);
 
     // q: row l16, the values that meet the words kg * KS .. of a token
@@ -734,9 +739,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     }
     if (n_steps != rq.steps) {
       // Every wave's stores have reached the device's scope before the count says so.
-      const uint32_t t0 = pos - step0, t1 = t0 + rq.steps;
+      const uint32_t t0 = pos - at, t1 = t0 + gap + rq.steps;
       const bool cut = first.each > 0;
-      const uint32_t p0 = cut ? share - step0 / first.each : share_of(first.total, kr.n_share, t0);
+      const uint32_t p0 = cut ? share - step0 / first.each : share_of(first.total, kr.n_share, t0 + gap);
       const uint32_t n_part = cut ? (rq.steps + first.each - 1) / first.each : share_of(first.total, kr.n_share, t1 - 1) - p0 + 1;
       __builtin_amdgcn_s_waitcnt(0x0F70);    // vmcnt(0)
       __syncthreads();
@@ -749,11 +754,11 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
         if (threadIdx.x == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
-    pos += n_steps;
-    left -= n_steps;
+    pos += to - at;
+    left -= to - at;
     if (left == 0) break;
     __syncthreads();                         // (the next part's outputs come to the same places)
-    step0 = 0;
+    at = 0;
     if (++tile >= rq.tiles) {
       tile = 0;
       do rq = request(kr, rq.b + 1);         // (steps are left: there is a request)
@@ -785,7 +790,7 @@ int launch_cache_attention(const CacheAttnArgs& a, hipStream_t st) {
   const int64_t tiles = ((int64_t)a.T * k.G + std::min<int64_t>((int64_t)a.B + 1, a.T) * (ROWS - 1)) / ROWS;      // at most: those of a request round up
   const int64_t most = (a.D == 64 ? SHARES_64 : SHARES_128) / a.cache.Hkv;
   const int64_t room = std::min<int64_t>((int64_t)a.width << a.cache.shift, 0x7ffff000);
-  if ((((int64_t)a.T * k.G + ROWS - 1) / ROWS + a.B + 1) * (room / UNIT + 1) > 0x7fffffff) return PIPE_ESHAPE;
+  if ((((int64_t)a.T * k.G + ROWS - 1) / ROWS + a.B + 1) * (room / UNIT + 1 + GAP) > 0x7fffffff) return PIPE_ESHAPE;
   k.n_share = (uint32_t)std::max<int64_t>(1, std::min(most, tiles * (longest <= 3 * UNIT ? 1 : (longest + UNIT - 1) / UNIT)));
   k.load = (a.D == 64 ? LOAD_64 : LOAD_128) * a.cache.Hkv / UNITS;
   if (k.n_share > 1 || pipe_dry_run()) {
