@@ -17,12 +17,12 @@
 // The offsets' part of the output is P (m + 8 s), with m about -8 s: no large sums that cancel.
 //
 // Every byte of the cache is read once as long as a tile holds all rows of the head (tokens * G <= 16), and those bytes bound it:
-// two requests of 131072 tokens, 8 heads of 128, take 62 us = 4.6 TB/s, 48 of 33 to 8000 tokens 54 us = 4.0 TB/s (a large copy: 4.8).
+// two requests of 131072 tokens, 8 heads of 128, take 62 us = 4.6 TB/s, 48 of 33 to 8000 tokens 52 us = 4.1 TB/s (a large copy: 4.8).
 // To reach that: steps of 32 tokens with two in flight beside the one worked on, the table through scalar loads, a step's words in one
 // register spread by DPP (the 131072s 86 us; 64 tokens and one in flight, words and addresses in each lane: 134); equal shares of all
 // steps to as many workgroups as the chip holds (67); joined by whichever of a tile's shares ends last (one request of 777 tokens
 // 10.8 us; in a second launch 13.3).  One request of 777 tokens is eight trips to memory in a row, 10 us.  fp32 is bound by its instructions: two terms of q
-// and of the weights; 16 requests of 100 to 3000 tokens with 5 rows a tile, 32 heads of 64, take 29 us at 2.0 TB/s.
+// and of the weights; 16 requests of 100 to 3000 tokens with 5 rows a tile, 32 heads of 64, take 27 us at 2.2 TB/s.
 #include <algorithm>
 #include <type_traits>
 
