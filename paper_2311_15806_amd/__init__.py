@@ -9,7 +9,7 @@ from . import workloads  # noqa: F401
 _BINDING_NAMES = (
     "Expansion", "PipeError", "pipe_expand", "pipe_expand_with_operator", "pipe_expansion_order", "pipe_forward", "pipe_forward_acc",
     "pipe_forward_conv2d", "pipe_mlp_forward", "pipe_chain_forward", "pipe_chain_forward_conv", "pipe_set_kernel", "pipe_timing_enable", "pipe_timing_read", "PIPE_ACT_NONE", "PIPE_ACT_GELU", "PIPE_ACT_SILU_GATED", "PIPE_ACT_RELU",
-    "pipe_cache_page_bytes", "pipe_cache_plan", "pipe_cache_write", "pipe_cache_read", "pipe_cache_attention", "pipe_prompt_attention",
+    "pipe_cache_page_bytes", "pipe_cache_plan", "pipe_cache_write", "pipe_cache_read", "pipe_cache_attention", "pipe_prepare_cache_attention", "pipe_prompt_attention",
 )
 
 
