@@ -360,7 +360,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) bad |= !(fabsf(o[d][i]) < INFINITY);
-    if (!__syncthreads_or(bad)) break;
+    if (!__syncthreads_or(bad && w.seen > 0)) break;       // (a row that sees nothing gives zeros whatever it summed)
     careful = true;
     first_tile();
   }
@@ -483,6 +483,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   const int vr = 4 * h + ((lane >> 2) & 3), vc = ((lane >> 4) & 1) * 2 + ((lane >> 1) & 1);      // (places as in the 16-bit kernel)
   int k_at = (n * CH + swizzle<D>(n, h)) * 16, v_at = (vr * CH + swizzle<D>(vr, vc)) * 16 + (lane & 1) * 8;
   constexpr float U_SLACK = 8.f, P_SCALE = 16.f;        // 2^REF_SLACK * U_SLACK * P_SCALE fits fp16
+  constexpr float U_LEAST = 0x1p-120f;                  // sigma at first: P_SCALE over it is finite, whatever V's units (of zeros: 2^-126)
   const float rs = ldexpf(scale2, 127 - qe);
 
   auto step = [&](auto MASKED, int key0) {
@@ -629,8 +630,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
       for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     ref = lift = -INFINITY;
     nref = sum = 0.f;
-    sigma = 0x1p-126f;
-    per = P_SCALE * 0x1p126f;
+    sigma = U_LEAST;
+    per = P_SCALE / U_LEAST;
     int key0 = 0;
     for (; key0 + KEYS32 <= w.full; key0 += KEYS32) step(std::false_type{}, key0);
     for (; key0 < w.end; key0 += KEYS32) step(std::true_type{}, key0);
@@ -641,7 +642,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
     for (int d = 0; d < DB; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) bad |= !(fabsf(o[d][i]) < INFINITY);
-    if (!__syncthreads_or(bad)) break;
+    if (!__syncthreads_or(bad && w.seen > 0)) break;       // (a row that sees nothing gives zeros whatever it summed)
     careful = true;
     fetch(0);
   }

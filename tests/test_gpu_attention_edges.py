@@ -1,0 +1,56 @@
+"""Attention at the edges of its number range: zero, constant, huge and infinite keys and values, empty and tiny queries, scales far from one;
+and what the binding refuses.  Against the definitions in numpy."""
+import numpy as np
+import pytest
+
+import _attention as ref
+from test_gpu_attention import ints, pipe, prompt_reference, typed  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def prompt_limit(kind, q, k, v, scale):
+    D, n = q.shape[-1], k.shape[0]
+    a = abs(scale) * float(np.abs(q).max()) * float(np.abs(k).sum(-1).max())
+    return ref.far(kind, D, n, a, float(np.abs(v).max()))
+
+
+# ------------------------------------------------------------------ prompts
+
+ZEROS = {
+    "all": lambda v: v.zero_(),
+    "first": lambda v: v[0].zero_(),
+    "a tile": lambda v: v[:32].zero_(),
+    "two tiles": lambda v: v[:64].zero_(),
+    "one head": lambda v: v[:, 1].zero_(),
+}
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("zero", ZEROS)
+@pytest.mark.parametrize("D,causal,n", [(64, True, 100), (128, True, 100), (64, False, 70), (128, False, 5)])
+def test_prompts_of_zero_values(pipe, kind, zero, D, causal, n):
+    rng = np.random.default_rng(D + n)
+    q, qf = typed(rng, (n, 4, D), kind)
+    k, kf = typed(rng, (n, 2, D), kind)
+    v, _ = typed(rng, (n, 2, D), kind)
+    ZEROS[zero](v)
+    vf = v.double().cpu().numpy()
+    got = pipe.pipe_prompt_attention(q, k, v, ints([0, n]), causal=causal).double().cpu().numpy()
+    want = prompt_reference(qf, kf, vf, [n], [n], causal, D ** -0.5)
+    assert np.abs(got - want).max() <= prompt_limit(kind, qf, kf, vf, D ** -0.5)
+
+
+@pytest.mark.parametrize("gain", [1e-30, 1.5e-33, 1e-35, 1e-37])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_of_tiny_values(pipe, D, gain):
+    """Weights times values of that size are multiples of some 2^-149: 2^-22 a key beside the bound of other values."""
+    n = 90
+    rng = np.random.default_rng(D)
+    q, qf = typed(rng, (n, 2, D), "f32")
+    k, kf = typed(rng, (n, 2, D), "f32")
+    v, vf = typed(rng, (n, 2, D), "f32", gain=gain)
+    got = pipe.pipe_prompt_attention(q, k, v, ints([0, n])).double().cpu().numpy()
+    want = prompt_reference(qf, kf, vf, [n], [n], True, D ** -0.5)
+    top = float(np.abs(vf).max())
+    assert np.abs(got - want).max() <= prompt_limit("f32", qf, kf, vf, D ** -0.5) + n * 2.0 ** -22 * top + 2.0 ** -140
