@@ -211,7 +211,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   for (int s = 0; s < KS; ++s)
 #pragma unroll
     for (int i = 0; i < 4; ++i) q[s][i] = (q[s][i] ^ flip) & keep;
-  const float rs = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
+  const float rs = a.scale == 0.f ? 1.f : fminf(fabsf(a.scale) * 1.44269504f, 0x1.fffffep127f);    // (finite: 0 times it is 0)
 
   f16v o[DB];
   constexpr float P_LOG = sizeof(T) == 2 && std::is_same_v<T, f16> ? 7.f : 0.f;    // fp16: weights up to 2^15, so that small ones keep their digits
@@ -459,7 +459,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   }
   qmax = fmaxf(qmax, __shfl_xor(qmax, 32));
   const int qe = qmax < INFINITY ? scale_of(qmax) : 127;
-  const float qf = a.scale < 0.f ? -power_of(qe) : power_of(qe);
+  // log2 of a weight per unit of a score, 2^-e * |scale| * log2(e).  It is finite, and where it would be 0 -- all scores are next to nothing
+  // then -- the scores are: 0 times an infinity, or a masked score times 0, would be NaN.
+  const float rs0 = fminf(ldexpf(fabsf(a.scale) * 0.72134752f, 128 - qe), 0x1.fffffep127f), rs = rs0 > 0.f ? rs0 : 1.f;
+  const float qf = rs0 > 0.f ? copysignf(power_of(qe), a.scale) : 0.f;
   u4 q_hi[KS], q_lo[D == 128 ? 1 : KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
@@ -474,7 +477,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
     if constexpr (D == 128) q_rest[(wave * KS + s) * 64 + lane] = rest;      // (read by this lane alone)
     else q_lo[s] = rest;
   }
-  const float scale2 = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504f;
 
   f16v o[DB];
   // weights exp2(rs * score + nref), outputs in units of sigma / P_SCALE: sigma a power of two, no unit of a key that this row sees above U_SLACK of it
@@ -484,7 +486,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   int k_at = (n * CH + swizzle<D>(n, h)) * 16, v_at = (vr * CH + swizzle<D>(vr, vc)) * 16 + (lane & 1) * 8;
   constexpr float U_SLACK = 8.f, P_SCALE = 16.f;        // 2^REF_SLACK * U_SLACK * P_SCALE fits fp16
   constexpr float U_LEAST = 0x1p-120f;                  // sigma at first: P_SCALE over it is finite, whatever V's units (of zeros: 2^-126)
-  const float rs = ldexpf(scale2, 127 - qe);
 
   auto step = [&](auto MASKED, int key0) {
     // ---- the loaded tile's terms into LDS, once every wave is done with the tile before

@@ -54,3 +54,37 @@ def test_prompts_of_tiny_values(pipe, D, gain):
     want = prompt_reference(qf, kf, vf, [n], [n], True, D ** -0.5)
     top = float(np.abs(vf).max())
     assert np.abs(got - want).max() <= prompt_limit("f32", qf, kf, vf, D ** -0.5) + n * 2.0 ** -22 * top + 2.0 ** -140
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("scale", [1e-8, -1e-20, 1e-44])
+def test_prompts_of_zero_queries_and_small_scales(pipe, kind, scale):
+    """Scores of (next to) nothing: every query gives the mean of the values it sees."""
+    D, n = 64, 80
+    rng = np.random.default_rng(3)
+    q, _ = typed(rng, (n, 2, D), kind)
+    q[::2] = 0
+    qf = q.double().cpu().numpy()
+    k, kf = typed(rng, (n, 2, D), kind)
+    v, vf = typed(rng, (n, 2, D), kind)
+    got = pipe.pipe_prompt_attention(q, k, v, ints([0, n]), scale=scale).double().cpu().numpy()
+    want = prompt_reference(qf, kf, vf, [n], [n], True, scale)
+    assert np.abs(got - want).max() <= prompt_limit(kind, qf, kf, vf, scale)
+
+
+def far_factors(pipe, kind, q_gain, k_gain, scale, D):
+    n = 70
+    rng = np.random.default_rng(4)
+    q, qf = typed(rng, (n, 2, D), kind, gain=q_gain)
+    k, kf = typed(rng, (n, 2, D), kind, gain=k_gain)
+    v, vf = typed(rng, (n, 2, D), kind)
+    got = pipe.pipe_prompt_attention(q, k, v, ints([0, n]), scale=scale).double().cpu().numpy()
+    want = prompt_reference(qf, kf, vf, [n], [n], True, scale)
+    assert np.abs(got - want).max() <= prompt_limit(kind, qf, kf, vf, scale)
+
+
+@pytest.mark.parametrize("kind,q_gain,k_gain,scale", [("f32", 1e-38, 1.0, 3e38), ("f32", 1e-20, 1e-20, 1e38), ("f32", 0.0, 1.0, -3e38), ("bf16", 0.0, 1.0, 3e38),
+                                                      ("f16", 1e-4, 1e-3, 1e6)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_of_huge_scales(pipe, kind, q_gain, k_gain, scale, D):
+    far_factors(pipe, kind, q_gain, k_gain, scale, D)
