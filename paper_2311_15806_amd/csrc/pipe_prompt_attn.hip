@@ -393,7 +393,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
 // way into LDS, once for all waves.
 
 // the exponent field of 2^e, for e that brings `largest` (finite, >= 0) to 2^14 .. 2^15
-__device__ __forceinline__ int scale_of(float largest) { return min(253, 268 - (int)(__float_as_uint(largest) >> 23)); }
+__device__ __forceinline__ int scale_of(float largest, int most = 253) { return min(most, 268 - (int)(__float_as_uint(largest) >> 23)); }
 __device__ __forceinline__ float power_of(int scale) { return __uint_as_float((uint32_t)scale << 23); }
 
 // f x and f y in two terms of fp16 each; the rest is taken from the rounded value itself, whichever way that fell.
@@ -459,9 +459,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
   }
   qmax = fmaxf(qmax, __shfl_xor(qmax, 32));
   const int qe = qmax < INFINITY ? scale_of(qmax) : 127;
-  // log2 of a weight per unit of a score, 2^-e * |scale| * log2(e).  It is finite, and where it would be 0 -- all scores are next to nothing
+  // Scores are kept in multiples of 2^K_SHIFT: the sums of up to 2^37 times the unit of a key of up to 2^113 are finite then.  (Keys under 2^-88
+  // are held to multiples of 2^-126.)
+  constexpr int K_SHIFT = 24;
+  // log2 of a weight per unit of a score, 2^(K_SHIFT - e) * |scale| * log2(e).  It is finite, and where it would be 0 -- all scores are next to nothing
   // then -- the scores are: 0 times an infinity, or a masked score times 0, would be NaN.
-  const float rs0 = fminf(ldexpf(fabsf(a.scale) * 0.72134752f, 128 - qe), 0x1.fffffep127f), rs = rs0 > 0.f ? rs0 : 1.f;
+  const float rs0 = fminf(ldexpf(fabsf(a.scale) * 0.72134752f, 128 + K_SHIFT - qe), 0x1.fffffep127f), rs = rs0 > 0.f ? rs0 : 1.f;
   const float qf = rs0 > 0.f ? copysignf(power_of(qe), a.scale) : 0.f;
   u4 q_hi[KS], q_lo[D == 128 ? 1 : KS];
 #pragma unroll
@@ -494,8 +497,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
     for (int i = 0; i < LOADS; ++i) {
       const int at = i * 256 + threadIdx.x, r = at / CH, c = at % CH, to = r * CH + swizzle<D>(r, c);
       const float km = largest8(kx[i]), vm = largest8(vx[i]);
-      const int ke = scale_of(row_reduce<CH, true>(km)), ve = scale_of(row_reduce<CH, true>(vm));
-      if (c == 0) { k_unit[r] = power_of(254 - ke); v_unit[r] = power_of(254 - ve); }
+      const int ke = scale_of(row_reduce<CH, true>(km), 253 - K_SHIFT), ve = scale_of(row_reduce<CH, true>(vm));
+      if (c == 0) { k_unit[r] = power_of(254 - K_SHIFT - ke); v_unit[r] = power_of(254 - ve); }
       const float kf = power_of(ke), vf = power_of(ve);
       u4 kh, kl, vh, vl;
 #pragma unroll

@@ -88,3 +88,10 @@ def far_factors(pipe, kind, q_gain, k_gain, scale, D):
 @pytest.mark.parametrize("D", [64, 128])
 def test_prompts_of_huge_scales(pipe, kind, q_gain, k_gain, scale, D):
     far_factors(pipe, kind, q_gain, k_gain, scale, D)
+
+
+@pytest.mark.parametrize("kind,q_gain,k_gain", [("f32", 1e-33, 1e33), ("f32", 1e33, 1e-33), ("f32", 1e-37, 6e37), ("bf16", 1e-33, 1e33), ("bf16", 1e30, 1e-30)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_of_far_factors(pipe, kind, q_gain, k_gain, D):
+    """Factors at the ends of the range whose product is an ordinary score."""
+    far_factors(pipe, kind, q_gain, k_gain, D ** -0.5, D)
