@@ -581,7 +581,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
       p_hi[i >> 3][(i >> 1) & 3] = hi;
       p_lo[i >> 3][(i >> 1) & 3] = lo;
     }
-    if constexpr (MASKED) if (some && careful) {
+    if constexpr (MASKED) if (careful) {
       bool bad = false;
 #pragma unroll 1
       for (int i = lane; i < KEYS32 * CH * 4; i += 64) {
@@ -637,9 +637,10 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
     sigma = U_LEAST;
     per = P_SCALE / U_LEAST;
     int key0 = 0;
-    for (; key0 + KEYS32 <= w.full; key0 += KEYS32) step(std::false_type{}, key0);
+    for (; !careful && key0 + KEYS32 <= w.full; key0 += KEYS32) step(std::false_type{}, key0);
     for (; key0 < w.end; key0 += KEYS32) step(std::true_type{}, key0);
-    // (a weight of 0 times an infinity or a NaN: see the 16-bit kernel)
+    // A weight of 0 times an infinity or a NaN: see the 16-bit kernel.  Here an infinity that is seen needs the second pass too: its second
+    // term is NaN.
     if (careful) break;
     bool bad = false;
 #pragma unroll

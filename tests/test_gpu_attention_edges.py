@@ -95,3 +95,28 @@ def test_prompts_of_huge_scales(pipe, kind, q_gain, k_gain, scale, D):
 def test_prompts_of_far_factors(pipe, kind, q_gain, k_gain, D):
     """Factors at the ends of the range whose product is an ordinary score."""
     far_factors(pipe, kind, q_gain, k_gain, D ** -0.5, D)
+
+
+def close(got, want, limit):
+    """Equal where not finite, within the limit elsewhere."""
+    odd = ~np.isfinite(want)
+    assert np.array_equal(got[odd], want[odd], equal_nan=True)
+    assert np.isfinite(got[~odd]).all() and np.abs(got[~odd] - want[~odd]).max() <= limit
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("at", [0, 31, 70, 299])
+def test_prompts_with_an_infinite_value(pipe, kind, D, causal, at):
+    """An infinity of V is one in its column of every query that sees it, wherever its tile lies, and nowhere else."""
+    n, H = 300, 2
+    rng = np.random.default_rng(at + D)
+    q, qf = typed(rng, (n, H, D), kind)
+    k, kf = typed(rng, (n, H, D), kind)
+    v, vf = typed(rng, (n, H, D), kind)
+    limit = prompt_limit(kind, qf, kf, vf, D ** -0.5)
+    v[at, 0, 5], v[at, 1, 3] = float("inf"), -float("inf")
+    vf[at, 0, 5], vf[at, 1, 3] = np.inf, -np.inf
+    got = pipe.pipe_prompt_attention(q, k, v, ints([0, n]), causal=causal).double().cpu().numpy()
+    close(got, prompt_reference(qf, kf, vf, [n], [n], causal, D ** -0.5), limit)
