@@ -509,6 +509,16 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
         two_terms(vx[i][2 * e], vx[i][2 * e + 1], vf, hi, lo);
         vh[e] = hi; vl[e] = lo;
       }
+      if constexpr (MASKED) if (careful) {
+        // an infinity of K becomes the second term, which only q's first one meets: the others would add infinities of either sign, or NaN
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t half = 0xffffu << 16 * (e & 1), x = kh[e >> 1] & half;
+          const bool inf = (x & 0x7fff7fffu) == (0x7c007c00u & half);
+          kl[e >> 1] = inf ? (kl[e >> 1] & ~half) | x : kl[e >> 1];
+          kh[e >> 1] = inf ? kh[e >> 1] & ~half : kh[e >> 1];
+        }
+      }
       k_hi[to] = kh; k_lo[to] = kl; v_hi[to] = vh; v_lo[to] = vl;
     }
     if (key0 + KEYS32 < w.end) fetch(key0 + KEYS32);
@@ -639,8 +649,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_f32_kernel(const Kernel 
     int key0 = 0;
     for (; !careful && key0 + KEYS32 <= w.full; key0 += KEYS32) step(std::false_type{}, key0);
     for (; key0 < w.end; key0 += KEYS32) step(std::true_type{}, key0);
-    // A weight of 0 times an infinity or a NaN: see the 16-bit kernel.  Here an infinity that is seen needs the second pass too: its second
-    // term is NaN.
+    // A weight of 0 times an infinity or a NaN: see the 16-bit kernel.  Here an infinity of K or V that is seen needs the second pass too: its
+    // second term is NaN.
     if (careful) break;
     bool bad = false;
 #pragma unroll

@@ -106,6 +106,30 @@ def close(got, want, limit):
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("at", [0, 40, 149])
+@pytest.mark.parametrize("scale", [None, -0.1])
+def test_prompts_with_an_infinite_key(pipe, kind, D, at, scale):
+    """A key with an infinity: a score of -infinity is a weight of 0, one of +infinity is NaN."""
+    n, H = 150, 2
+    rng = np.random.default_rng(at + D)
+    q, qf = typed(rng, (n, H, D), kind)
+    k, kf = typed(rng, (n, H, D), kind)
+    v, vf = typed(rng, (n, H, D), kind)
+    sc = D ** -0.5 if scale is None else scale
+    limit = prompt_limit(kind, qf, kf, vf, sc)
+    k[at, 0, 5], k[at, 1, 3] = float("inf"), -float("inf")
+    kf[at, 0, 5], kf[at, 1, 3] = np.inf, -np.inf
+    got = pipe.pipe_prompt_attention(q, k, v, ints([0, n]), scale=scale).double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want = prompt_reference(qf, kf, vf, [n], [n], True, sc)
+    if at == 0:
+        got, want = got[1:], want[1:]            # (a query whose only score is -infinity has no weights at all)
+    assert at == 149 or (np.isnan(want).any() and np.isfinite(want[at:]).any())
+    close(got, want, limit)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("at", [0, 31, 70, 299])
 def test_prompts_with_an_infinite_value(pipe, kind, D, causal, at):
