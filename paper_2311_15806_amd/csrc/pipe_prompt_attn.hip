@@ -214,9 +214,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   const float rs = a.scale == 0.f ? 1.f : fminf(fabsf(a.scale) * 1.44269504f, 0x1.fffffep127f);    // (finite: 0 times it is 0)
 
   f16v o[DB];
-  constexpr float P_LOG = sizeof(T) == 2 && std::is_same_v<T, f16> ? 7.f : 0.f;    // fp16: weights up to 2^15, so that small ones keep their digits
   float ref, nref, lift, sum;
   bool careful = false;       // a second pass: some output of the first is not finite
+  // log2 of a weight at the reference.  fp16: weights up to 2^15, so that small ones keep their digits.  bf16 has fp32's range, and sums over
+  // values next to the end of it do not: weights up to 2^-24 in the second pass, for sums over 2^24 keys.
+  auto p_log = [&]() { return std::is_same_v<T, f16> ? 7.f : careful ? -32.f : 0.f; };
 
   // Places in a tile, in bytes: of K the chunk h of row n -- chunk 2 j + h of row 32 b + n is j and b further, by an exclusive or and an
   // addition --, of V the piece that this lane brings to a transposed read: of every 16 lanes, lane i brings 4 columns from 4 (i % 4) on
@@ -266,7 +268,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[d] *= f;
       ref = nr;
-      nref = P_LOG - (nr == -INFINITY ? 0.f : nr * rs);
+      nref = p_log() - (nr == -INFINITY ? 0.f : nr * rs);
       lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
     }
     u4 p[2][2];
@@ -353,7 +355,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       step(std::true_type{}, k_b, v_b, k_a, v_a, key0 + KEYS);
     }
     // A row that does not see a key gives it the weight 0, and 0 times an infinity or a NaN of V would still reach it: where an output is
-    // not finite, all is done once more, with care for such tiles.
+    // not finite, all is done once more, with care for such tiles (and in bf16 with smaller weights).
     if (careful) break;
     bool bad = false;
 #pragma unroll

@@ -2,9 +2,10 @@
 and what the binding refuses.  Against the definitions in numpy."""
 import numpy as np
 import pytest
+import torch
 
 import _attention as ref
-from test_gpu_attention import ints, pipe, prompt_reference, typed  # noqa: F401
+from test_gpu_attention import DT, ints, pipe, prompt_reference, typed  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -95,6 +96,21 @@ def test_prompts_of_huge_scales(pipe, kind, q_gain, k_gain, scale, D):
 def test_prompts_of_far_factors(pipe, kind, q_gain, k_gain, D):
     """Factors at the ends of the range whose product is an ordinary score."""
     far_factors(pipe, kind, q_gain, k_gain, D ** -0.5, D)
+
+
+@pytest.mark.parametrize("kind,gain", [("f32", 3e37), ("bf16", 3e37), ("f16", 1.3e4)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompts_of_huge_values(pipe, kind, gain, D):
+    """Sums over values next to the type's largest: the result is one of them on average, though their sum is beyond fp32."""
+    n = 150
+    rng = np.random.default_rng(5)
+    q, qf = typed(rng, (n, 2, D), kind)
+    k, kf = typed(rng, (n, 2, D), kind)
+    v = torch.from_numpy(np.clip(rng.standard_normal((n, 2, D)), -4, 4).astype(np.float32) * np.float32(gain)).to(DT[kind]).abs().cuda()
+    vf = v.double().cpu().numpy()
+    got = pipe.pipe_prompt_attention(q, k, v, ints([0, n])).double().cpu().numpy()
+    want = prompt_reference(qf, kf, vf, [n], [n], True, D ** -0.5)
+    assert np.abs(got - want).max() <= prompt_limit(kind, qf, kf, vf, D ** -0.5)
 
 
 def close(got, want, limit):
