@@ -48,6 +48,8 @@ constexpr size_t ATTN_COUNTS = 4096;                // bytes of the counts of pa
 static_assert(SHARES_64 * sizeof(uint32_t) <= ATTN_COUNTS && SHARES_128 <= SHARES_64);
 constexpr float REF_SLACK = 6.f;                    // log2: a row's reference rises only when a score exceeds it by this
 constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE fits fp16
+constexpr int W_LOG = 32;                           // weights are 2^-W_LOG at the reference: times offsets next to bf16's largest they sum up over 2^26 tokens
+constexpr float S_LEAST = 0x1p-80f;                 // least unit of V's scales: 2^W_LOG * P_SCALE over it is finite
 
 struct Kernel {
   CacheAttnArgs a;
@@ -559,8 +561,11 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     f4 o[MT], ones = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < MT; ++i) o[i] = (f4){0.f, 0.f, 0.f, 0.f};
-    // weights are exp2(rs * T + nref), nref = -rs * ref + log2(P_SCALE / sigma) with sigma a power of two, all scales of V under 2 sigma
-    float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = 0x1p-100f;
+    // weights are exp2(rs * T + nref), nref = -rs * ref - W_LOG.  The operand of the second product is a weight times V's scale in units of sigma,
+    // times `lev` = 2^W_LOG * P_SCALE / sigma: a power of two, all scales of V under 2 sigma.  Offsets are summed as they are: rows of V without
+    // a scale say nothing of sigma.
+    float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = S_LEAST, lev = P_SCALE * 0x1p32f / S_LEAST;
+    static_assert(W_LOG == 32);
 
     // one step on `c`, while the next ones' loads fly, AHEAD steps on to `n`
     auto step = [&](const Tokens<D>& c, Tokens<D>& n) {
@@ -617,18 +622,20 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
         const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(top) & 0x7f800000u));
-        const float f = (ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr))) * (sigma / nsigma);
+        const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr)), fo = f * (sigma / nsigma);
         sum *= f;
         osum *= f;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) o[i] *= f;
-        ones *= f;
+        for (int i = 0; i < MT; ++i) o[i] *= fo;
+        ones *= fo;
         ref = nr;
         sigma = nsigma;
-        nref = (nr == -INFINITY ? 0.f : -nr * rs) + __builtin_amdgcn_logf(P_SCALE / nsigma);
+        lev = P_SCALE * 0x1p32f / nsigma;
+        nref = (nr == -INFINITY ? 0.f : -nr * rs) - W_LOG;
         lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
       }
       // weights
+      ws *= lev;
       u4 p[NT];
       auto weights = [&](auto SOME) {
         each<2>([&](auto J) {
@@ -700,14 +707,14 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     // a wave's outputs as they are, O[d][row] at d = MT * (4 kg + j) + i, over the reference weight
     sum = sum_over_kg(sum);
     osum = sum_over_kg(osum);
-    const float lref = ref == -INFINITY ? -INFINITY : -nref;
+    const float lref = ref == -INFINITY ? -INFINITY : -nref, unit = sigma * (0x1p-32f / P_SCALE);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        float y = o[i][j] + osum;
+        float y = o[i][j];
         if constexpr (!FINE) y = fmaf(-72.f, ones[j], y);
-        s_o[wave][l16][MT * (4 * kg + j) + i] = y;
+        s_o[wave][l16][MT * (4 * kg + j) + i] = fmaf(y, unit, osum);
       }
     if (kg == 0) { s_ref[wave][l16] = lref; s_sum[wave][l16] = sum; }
     __syncthreads();

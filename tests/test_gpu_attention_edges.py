@@ -160,3 +160,38 @@ def test_prompts_with_an_infinite_value(pipe, kind, D, causal, at):
     vf[at, 0, 5], vf[at, 1, 3] = np.inf, -np.inf
     got = pipe.pipe_prompt_attention(q, k, v, ints([0, n]), causal=causal).double().cpu().numpy()
     close(got, prompt_reference(qf, kf, vf, [n], [n], causal, D ** -0.5), limit)
+
+
+# ------------------------------------------------------------------ the cache
+
+def filled(pipe, k, v, P):
+    """(cache, table, K and V as the cache holds them in fp64) of one request with the rows k and v [n, Hkv, D], fp32."""
+    n, Hkv, D = k.shape
+    pages = -(-n // P)
+    cache = torch.zeros((pages, pipe.pipe_cache_page_bytes(Hkv, D, P)), dtype=torch.uint8, device="cuda")
+    slots = ints(np.arange(n))
+    pipe.pipe_cache_write(torch.from_numpy(k.astype(np.float32)).cuda(), torch.from_numpy(v.astype(np.float32)).cuda(), slots, cache, P)
+    kk, vv = (x.double().cpu().numpy() for x in pipe.pipe_cache_read(slots, cache, P, Hkv, D))
+    return cache, ints(np.arange(pages)[None]), kk, vv
+
+
+CONSTANTS = (2.0 ** -90, 1.0, 1000.0, 2.0 ** 20, -2.0 ** 100, 2.0 ** 126)
+
+
+@pytest.mark.parametrize("kind,values", [("f32", CONSTANTS), ("bf16", CONSTANTS), ("f16", (1.0, 1000.0, 57344.0))])
+@pytest.mark.parametrize("n", [3, 1100, 20000])
+@pytest.mark.parametrize("rise", [0.0, 0.003])
+@pytest.mark.parametrize("D", [64, 128])
+def test_cache_of_constant_values(pipe, kind, values, n, rise, D):
+    """Rows of V without a scale, under equal scores and under slowly rising (for other queries falling) ones."""
+    P, Hq, Hkv = 64, 4, 2
+    rng = np.random.default_rng(n)
+    k = np.broadcast_to((np.arange(n) * rise)[:, None, None], (n, Hkv, D))
+    q, qf = typed(rng, (1, Hq, D), kind)
+    limit = 2 * ref.UNIT[kind] + 2 * (n + 16) * ref.U32
+    for c in values:
+        cache, table, _, vv = filled(pipe, k, np.full((n, Hkv, D), c), P)
+        assert (vv == c).all()
+        for hint in (0, 1):
+            got = pipe.pipe_cache_attention(q, ints([0, 1]), ints([n]), cache, table, P, Hkv, scale=0.1, max_length=hint).double().cpu().numpy()
+            assert np.abs(got / c - 1).max() <= limit, (c, hint)
