@@ -502,7 +502,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     const int row = t.row0 + l16;
     const bool real = l16 < t.n_rows;
     const int token = real ? row / kr.G : 0, head = real ? row % kr.G : 0;
-    const int seen = real ? t.first_seen + token : 0;      // cached tokens this row sees
+    const int seen = real ? t.first_seen + token : 0x7fffffff;      // cached tokens this row sees (one that is not there: as many as any)
     const T* qp = (const T*)a.q + (int64_t)token_row(kr, t, token) * a.qs.token + (int64_t)(kvh * kr.G + head) * a.qs.head + kg * (KS * 8);
     float qv[KS * 8], qmax = 0, qsum = 0;
     if (kr.wide) {
@@ -562,8 +562,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
 #pragma unroll
     for (int i = 0; i < MT; ++i) o[i] = (f4){0.f, 0.f, 0.f, 0.f};
     // weights are exp2(rs * T + nref), nref = -rs * ref - W_LOG.  The operand of the second product is a weight times V's scale in units of sigma,
-    // times `lev` = 2^W_LOG * P_SCALE / sigma: a power of two, all scales of V under 2 sigma.  Offsets are summed as they are: rows of V without
-    // a scale say nothing of sigma.
+    // times `lev` = 2^W_LOG * P_SCALE / sigma: a power of two, all scales of V that the row has seen under 2 sigma.  (Up to the tokens that every
+    // row sees all rows have one sigma.)  Offsets are summed as they are: rows of V without a scale say nothing of sigma.
     float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = S_LEAST, lev = P_SCALE * 0x1p32f / S_LEAST;
     static_assert(W_LOG == 32);
 
@@ -615,12 +615,23 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) smax = fmaxf(smax, s[j][i]);
-      const float vs = l16 < 8 ? 0.f : fabsf(ws);
+      // V's scales: of a token in each lane, or of the tokens that this row sees where the rows differ
+      float vs = l16 < 8 ? 0.f : fabsf(ws);
+      if (some) {
+        vs = 0.f;
+        each<8>([&](auto B) {
+          constexpr int bit = B;
+          const float g = fabsf(from_lane<8 + bit>(ws));
+          vs = fmaxf(vs, (vis >> bit) & 1u ? g : 0.f);
+        });
+      }
       if (__any(smax > lift || vs > 2.f * sigma)) {
         const float nr = fmaxf(ref, max_over_kg(smax));
-        float top = vs;
+        float top = max_over_kg(vs);
+        if (!some) {
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+          for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        }
         const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(top) & 0x7f800000u));
         const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr)), fo = f * (sigma / nsigma);
         sum *= f;
@@ -635,7 +646,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
         lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
       }
       // weights
-      ws *= lev;
+      if (!some) ws *= lev;
       u4 p[NT];
       auto weights = [&](auto SOME) {
         each<2>([&](auto J) {
@@ -650,7 +661,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
                 const bool yes = (vis >> bit) & 1u;
                 const float m = from_lane<lane_of>(wm), g = from_lane<lane_of>(ws);
                 osum = fmaf(e, yes ? m : 0.f, osum);
-                y[u] = e * (yes ? g : 0.f);
+                y[u] = e * (yes ? g * lev : 0.f);
               } else {
                 osum = fmaf(from_lane<lane_of>(wm), e, osum);
                 y[u] = from_lane<lane_of>(ws) * e;

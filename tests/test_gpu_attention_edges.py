@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import _attention as ref
-from test_gpu_attention import DT, ints, pipe, prompt_reference, typed  # noqa: F401
+from test_gpu_attention import DT, cache_reference, ints, pipe, prompt_reference, typed  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -195,3 +195,23 @@ def test_cache_of_constant_values(pipe, kind, values, n, rise, D):
         for hint in (0, 1):
             got = pipe.pipe_cache_attention(q, ints([0, 1]), ints([n]), cache, table, P, Hkv, scale=0.1, max_length=hint).double().cpu().numpy()
             assert np.abs(got / c - 1).max() <= limit, (c, hint)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("huge", [1e9, 1e30])
+@pytest.mark.parametrize("n", [5, 300, 317])
+def test_a_later_draft_stays_out_of_earlier_ones(pipe, kind, D, huge, n):
+    """Values of the last fresh tokens that are far beyond the others' reach the queries that see them and leave the others' digits alone."""
+    P, Hq, Hkv, fresh = 16, 4, 2, 4
+    rng = np.random.default_rng(n)
+    k, v = rng.standard_normal((n, Hkv, D)), rng.standard_normal((n, Hkv, D))
+    v[-2:] *= huge
+    cache, table, kk, vv = filled(pipe, k, v, P)
+    q, qf = typed(rng, (fresh, Hq, D), kind)
+    got = pipe.pipe_cache_attention(q, ints([0, fresh]), ints([n]), cache, table, P, Hkv).double().cpu().numpy()
+    want = cache_reference(qf, [fresh], [n], [(kk, vv)], D ** -0.5)
+    a = D ** -0.5 * float(np.abs(qf).sum(-1).max()) * 2 * float(np.abs(kk).max())
+    for i in range(fresh):
+        top = 2 * float(np.abs(vv[:n - fresh + i + 1]).max())
+        assert np.abs(got[i] - want[i]).max() <= ref.far(kind, D, n, a, top), i
