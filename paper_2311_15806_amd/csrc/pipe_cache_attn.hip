@@ -49,6 +49,7 @@ static_assert(SHARES_64 * sizeof(uint32_t) <= ATTN_COUNTS && SHARES_128 <= SHARE
 constexpr float REF_SLACK = 6.f;                    // log2: a row's reference rises only when a score exceeds it by this
 constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE fits fp16
 constexpr int W_LOG = 32;                           // weights are 2^-W_LOG at the reference: times offsets next to bf16's largest they sum up over 2^26 tokens
+constexpr int K_LOG = 28;                           // a code's sums with q, up to 2^26, and q's, up to 2^22, meet K's scale and offset in units of 2^28: finite
 constexpr float S_LEAST = 0x1p-80f;                 // least unit of V's scales: 2^W_LOG * P_SCALE over it is finite
 
 struct Kernel {
@@ -537,7 +538,10 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     }
     qmax = max_over_kg(qmax);
     // a power of two that brings the row's largest value to 2^14 .. 2^15, and with it the sign of the scale
-    const int qe = qmax > 0.f && qmax < INFINITY ? max(-80, min(100, 14 - ((int)(__float_as_uint(qmax) >> 23) - 127))) : 0;
+    const int qe = qmax > 0.f && qmax < INFINITY ? 14 - ((int)(__float_as_uint(qmax) >> 23) - 127) : 0;
+    // scores are in units of 2^(K_LOG - qe), in which they are finite; rs turns them into log2 of a weight.  rs is finite, and where it would be 0 --
+    // all scores are next to nothing then -- the scores are: 0 times an infinity, or a masked score times 0, would be NaN.
+    const float rs0 = fminf(ldexpf(fabsf(a.scale) * 0.72134752f, 1 + K_LOG - qe), 0x1.fffffep127f), rs = rs0 > 0.f ? rs0 : 1.f;
     const float sgn = a.scale < 0.f ? -1.f : 1.f;
     h8 q[NT][KS];
 #pragma unroll
@@ -545,7 +549,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
       u4 hi, lo;
 #pragma unroll
       for (int n = 0; n < 4; ++n) {                // nibbles n and n + 4 are a register of the operand
-        const float x = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n], qe), y = a.scale == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n + 4], qe);
+        const float x = rs0 == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n], qe), y = rs0 == 0.f ? 0.f : sgn * ldexpf(qv[8 * s + n + 4], qe);
         qsum += x + y;
         hi[n] = half_pair(x, y);
         lo[n] = half_rest(x, y, hi[n]);
@@ -554,8 +558,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
       if constexpr (FINE) q[1][s] = __builtin_bit_cast(h8, lo);
     }
     qsum = sum_over_kg(qsum);
-    // scores in units of q * 2^qe; rs turns them into log2 of a weight
-    const float rs = a.scale == 0.f ? 1.f : ldexpf(fabsf(a.scale) * 1.44269504f, -qe);
+    const float word_unit = l16 < 8 ? 1.f / (1 << K_LOG) : 1.f;      // (words of K in lanes l16 < 8, of V in the others)
     const float acc0 = FINE ? 0.f : -64.f * qsum;
 
     f4 o[MT], ones = {0.f, 0.f, 0.f, 0.f};
@@ -574,7 +577,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
       w.pages_of(pages, tok + (AHEAD + 1) * UNIT, end);
       // scores
       float s[2][4];
-      float ws = word_scale(c.w), wo = word_offset(c.w), wm = fmaf(8.f, ws, wo);      // scale, offset, and the offset of c - 8
+      float ws = word_scale(c.w) * word_unit, wo = word_offset(c.w) * word_unit, wm = fmaf(8.f, ws, wo);      // scale, offset, and the offset of c - 8
       const float ko = FINE ? wm : wo;
       each<2>([&](auto J) {
         constexpr int j = J;

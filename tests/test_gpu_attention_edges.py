@@ -215,3 +215,19 @@ def test_a_later_draft_stays_out_of_earlier_ones(pipe, kind, D, huge, n):
     for i in range(fresh):
         top = 2 * float(np.abs(vv[:n - fresh + i + 1]).max())
         assert np.abs(got[i] - want[i]).max() <= ref.far(kind, D, n, a, top), i
+
+
+@pytest.mark.parametrize("kind,q_gain,k_gain,scale", [
+    ("f32", 1e-33, 1e33, None), ("f32", 1e33, 1e-33, None), ("f32", 1e-37, 3e37, None), ("f32", 1e-30, 1.0, 1e-20), ("f32", 1e-38, 1.0, 3e38),
+    ("f32", 0.0, 1.0, 1e-44), ("bf16", 1e33, 1e-33, None), ("bf16", 1e-33, 1e33, None), ("bf16", 1e-37, 3e37, None), ("bf16", 1e-30, 1.0, 1e-20), ("f16", 0.0, 1.0, 1e-44)])
+def test_cache_of_far_factors(pipe, kind, q_gain, k_gain, scale):
+    """Factors at the ends of the range whose product is an ordinary score, or none at all."""
+    P, Hq, Hkv, D, n, fresh = 16, 4, 2, 64, 75, 3
+    rng = np.random.default_rng(7)
+    cache, table, kk, vv = filled(pipe, np.clip(rng.standard_normal((n, Hkv, D)), -4, 4) * k_gain, rng.standard_normal((n, Hkv, D)), P)
+    q, qf = typed(rng, (fresh, Hq, D), kind, gain=q_gain)
+    sc = D ** -0.5 if scale is None else scale
+    got = pipe.pipe_cache_attention(q, ints([0, fresh]), ints([n]), cache, table, P, Hkv, scale=scale).double().cpu().numpy()
+    want = cache_reference(qf, [fresh], [n], [(kk, vv)], sc)
+    a = sc * float(np.abs(qf).sum(-1).max()) * 2 * float(np.abs(kk).max())
+    assert np.abs(got - want).max() <= ref.far(kind, D, n, a, 2 * float(np.abs(vv).max()))
