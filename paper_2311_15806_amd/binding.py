@@ -788,7 +788,7 @@ def pipe_cache_plan(cached: torch.Tensor, fresh: torch.Tensor, page_size: int, f
     """Tables of the next step (all int32): request b holds cached[b] tokens and brings fresh[b]; new pages come from free[used[0]:]
     and enter table [B, width] in place.  Returns (lengths [B], starts [B+1], slots [tokens], positions [tokens], counts [3]);
     counts -- pages used, pages missing, tokens cut off -- is the next step's `used`."""
-    B = cached.shape[0]
+    B = cached.numel()
     if cached.dim() != 1 or fresh.shape != cached.shape or table.dim() != 2 or table.shape[0] != B or free.dim() != 1 or used.numel() < 1:
         raise ValueError("cached and fresh are [B], table is [B, width], free is [pages], used holds a number")
     if tokens < 0:
@@ -815,6 +815,8 @@ def pipe_cache_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cach
 def pipe_cache_read(slots: torch.Tensor, cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int,
                     dtype: torch.dtype = torch.float32):
     """(k, v) [T, kv_heads, head_dim]: the values that the codes at slots [T] stand for (zeros for a slot outside the cache)."""
+    if slots.dim() != 1:
+        raise ValueError("slots has one entry a token")
     T = slots.shape[0]
     cp, pages = _cache(cache, page_size, kv_heads, head_dim)
     k, v = torch.empty((2, T, kv_heads, head_dim), dtype=dtype, device=cache.device).unbind(0)
@@ -830,8 +832,8 @@ def pipe_cache_attention(q: torch.Tensor, starts: torch.Tensor, lengths: torch.T
     of them the last of its lengths[b] cached tokens.  scale: None = head_dim ** -0.5; max_length: about the longest length (a hint)."""
     qp, qt, qh = _heads(q, "q")
     T, H, D = q.shape
-    B = lengths.shape[0]
-    if starts.shape != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
+    B = lengths.numel()
+    if lengths.dim() != 1 or starts.shape != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
         raise ValueError("starts is [B + 1], lengths [B], table [B, width]")
     cp, pages = _cache(cache, page_size, kv_heads, D)
     y = _attention_out(q, out)
@@ -859,7 +861,7 @@ def pipe_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sta
     Tk, Hkv, Dk = k.shape
     if v.shape != (Tk, Hkv, D) or Dk != D or k.dtype is not q.dtype or v.dtype is not q.dtype:
         raise ValueError("k and v must have one shape, and q's head_dim and type")
-    B = starts.shape[0] - 1
+    B = starts.numel() - 1
     if starts.dim() != 1 or B < 1 or (starts_k is not None and starts_k.shape != starts.shape):
         raise ValueError("starts and starts_k are [sequences + 1]")
     y = _attention_out(q, out)

@@ -231,3 +231,32 @@ def test_cache_of_far_factors(pipe, kind, q_gain, k_gain, scale):
     want = cache_reference(qf, [fresh], [n], [(kk, vv)], sc)
     a = sc * float(np.abs(qf).sum(-1).max()) * 2 * float(np.abs(kk).max())
     assert np.abs(got - want).max() <= ref.far(kind, D, n, a, 2 * float(np.abs(vv).max()))
+
+
+# ------------------------------------------------------------------ refusals
+
+def small_call(pipe):
+    """What a call of each kind takes: two requests of one fresh token."""
+    q, k = torch.randn(2, 4, 64, device="cuda"), torch.randn(2, 2, 64, device="cuda")
+    cache = torch.zeros((4, pipe.pipe_cache_page_bytes(2, 64, 16)), dtype=torch.uint8, device="cuda")
+    starts, lengths, table, slots = ints([0, 1, 2]), ints([1, 1]), ints([[0], [1]]), ints([0, 16])
+    return q, k, cache, starts, lengths, table, slots
+
+
+def test_tables_of_other_ranks_are_refused(pipe):
+    q, k, cache, starts, lengths, table, slots = small_call(pipe)
+    pipe.pipe_cache_write(k, k, slots, cache, 16)
+    for bad in (slots[None], slots[:, None], slots.view(2, 1, 1), slots[0]):
+        with pytest.raises(ValueError):
+            pipe.pipe_cache_read(bad, cache, 16, 2, 64)
+        with pytest.raises(ValueError):
+            pipe.pipe_cache_write(k, k, bad, cache, 16)
+    for bad in (lengths[:, None], torch.stack([lengths, lengths], dim=1), lengths[0]):
+        with pytest.raises(ValueError):
+            pipe.pipe_cache_attention(q, starts, bad, cache, table, 16, 2)
+    for bad in (starts[:, None], starts[0], starts[None]):
+        with pytest.raises(ValueError):
+            pipe.pipe_prompt_attention(q, k, k, bad)
+    for bad in (lengths[:, None], lengths[0]):
+        with pytest.raises(ValueError):
+            pipe.pipe_cache_plan(bad, bad, 16, slots, ints([0]), table, 2)
