@@ -744,34 +744,38 @@ def _type(dtype: torch.dtype) -> int:
 
 
 # (These calls are a few microseconds on the device at decode sizes: what they ask of a tensor they ask once.)
-def _heads(t: torch.Tensor, name: str):
+# The number of the current device, on whose stream the kernels run: tensors of another one, or of none (-1), are refused.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _heads(t: torch.Tensor, name: str, dev: int):
     """(address, token stride, head stride) of [tokens, heads, head_dim] with a dense last axis."""
     s = t.stride()
-    if len(s) != 3 or not t.is_cuda or (s[2] != 1 and t.shape[2] > 1):
-        raise ValueError("%s must be a device tensor [tokens, heads, head_dim] with a dense last axis" % name)
+    if len(s) != 3 or t.get_device() != dev or (s[2] != 1 and t.shape[2] > 1):
+        raise ValueError("%s must be a tensor [tokens, heads, head_dim] of the current device with a dense last axis" % name)
     return t.data_ptr(), s[0], s[1]
 
 
-def _ints(t: torch.Tensor) -> int:
-    if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous int32 device tensor")
+def _ints(t: torch.Tensor, dev: int) -> int:
+    if t.dtype is not torch.int32 or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("expected a contiguous int32 tensor of the current device")
     return t.data_ptr()
 
 
-def _cache(cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int):
+def _cache(cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int, dev: int):
     """(address, pages)"""
     shape = cache.shape
-    if len(shape) != 2 or shape[1] != kv_heads * page_size * (head_dim + 8) or cache.dtype is not torch.uint8 or not cache.is_cuda \
-            or not cache.is_contiguous():
-        raise ValueError("the cache must be a contiguous uint8 device tensor [pages, pipe_cache_page_bytes(kv_heads, head_dim, page_size)]")
+    if len(shape) != 2 or shape[1] != kv_heads * page_size * (head_dim + 8) or cache.dtype is not torch.uint8 \
+            or cache.get_device() != dev or not cache.is_contiguous():
+        raise ValueError("the cache must be a contiguous uint8 tensor of the current device [pages, pipe_cache_page_bytes(kv_heads, head_dim, page_size)]")
     return cache.data_ptr(), shape[0]
 
 
-def _attention_out(q: torch.Tensor, out: Optional[torch.Tensor]) -> torch.Tensor:
+def _attention_out(q: torch.Tensor, out: Optional[torch.Tensor], dev: int) -> torch.Tensor:
     if out is None:
         return torch.empty_like(q, memory_format=torch.contiguous_format)
-    if out.shape != q.shape or out.dtype is not q.dtype or not out.is_cuda or not out.is_contiguous():
-        raise ValueError("output has the wrong shape or type, or is not contiguous")
+    if out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != dev or not out.is_contiguous():
+        raise ValueError("output has the wrong shape, type or device, or is not contiguous")
     return out
 
 
@@ -788,39 +792,42 @@ def pipe_cache_plan(cached: torch.Tensor, fresh: torch.Tensor, page_size: int, f
     """Tables of the next step (all int32): request b holds cached[b] tokens and brings fresh[b]; new pages come from free[used[0]:]
     and enter table [B, width] in place.  Returns (lengths [B], starts [B+1], slots [tokens], positions [tokens], counts [3]);
     counts -- pages used, pages missing, tokens cut off -- is the next step's `used`."""
+    dev = _device()
     B = cached.numel()
     if cached.dim() != 1 or fresh.shape != cached.shape or table.dim() != 2 or table.shape[0] != B or free.dim() != 1 or used.numel() < 1:
         raise ValueError("cached and fresh are [B], table is [B, width], free is [pages], used holds a number")
     if tokens < 0:
         raise ValueError("tokens must not be negative")
     lengths, starts, slots, positions, counts = cached.new_empty(2 * B + 4 + 2 * tokens).split([B, B + 1, tokens, tokens, 3])
-    _check(_lib.pipe_cache_plan(_ints(cached), _ints(fresh), B, page_size, _ints(free), free.shape[0], _ints(used), _ints(table),
-                                table.shape[1], tokens, lengths.data_ptr(), starts.data_ptr(), slots.data_ptr(), positions.data_ptr(),
-                                counts.data_ptr(), _stream()), "pipe_cache_plan")
+    _check(_lib.pipe_cache_plan(_ints(cached, dev), _ints(fresh, dev), B, page_size, _ints(free, dev), free.shape[0], _ints(used, dev),
+                                _ints(table, dev), table.shape[1], tokens, lengths.data_ptr(), starts.data_ptr(), slots.data_ptr(),
+                                positions.data_ptr(), counts.data_ptr(), _stream()), "pipe_cache_plan")
     return lengths, starts, slots, positions, counts
 
 
 def pipe_cache_write(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor, page_size: int) -> None:
     """Keys and values [T, kv_heads, head_dim] in 4 bits to slots [T] (int32; a slot outside the cache is skipped)."""
-    kp, kt, kh = _heads(k, "k")
-    vp, vt, vh = _heads(v, "v")
+    dev = _device()
+    kp, kt, kh = _heads(k, "k", dev)
+    vp, vt, vh = _heads(v, "v", dev)
     T, H, D = k.shape
     if v.shape != k.shape or v.dtype is not k.dtype or slots.shape != (T,):
         raise ValueError("k and v must have one shape and type, slots one entry a token")
-    cp, pages = _cache(cache, page_size, H, D)
-    _check(_lib.pipe_cache_write(kp, vp, _type(k.dtype), T, H, D, kt, kh, vt, vh, _ints(slots), cp, pages, page_size, _stream()),
+    cp, pages = _cache(cache, page_size, H, D, dev)
+    _check(_lib.pipe_cache_write(kp, vp, _type(k.dtype), T, H, D, kt, kh, vt, vh, _ints(slots, dev), cp, pages, page_size, _stream()),
            "pipe_cache_write")
 
 
 def pipe_cache_read(slots: torch.Tensor, cache: torch.Tensor, page_size: int, kv_heads: int, head_dim: int,
                     dtype: torch.dtype = torch.float32):
     """(k, v) [T, kv_heads, head_dim]: the values that the codes at slots [T] stand for (zeros for a slot outside the cache)."""
+    dev = _device()
     if slots.dim() != 1:
         raise ValueError("slots has one entry a token")
     T = slots.shape[0]
-    cp, pages = _cache(cache, page_size, kv_heads, head_dim)
+    cp, pages = _cache(cache, page_size, kv_heads, head_dim, dev)
     k, v = torch.empty((2, T, kv_heads, head_dim), dtype=dtype, device=cache.device).unbind(0)
-    _check(_lib.pipe_cache_read(cp, pages, page_size, _ints(slots), T, kv_heads, head_dim, _type(dtype), k.data_ptr(), v.data_ptr(),
+    _check(_lib.pipe_cache_read(cp, pages, page_size, _ints(slots, dev), T, kv_heads, head_dim, _type(dtype), k.data_ptr(), v.data_ptr(),
                                 _stream()), "pipe_cache_read")
     return k, v
 
@@ -830,15 +837,16 @@ def pipe_cache_attention(q: torch.Tensor, starts: torch.Tensor, lengths: torch.T
                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the fresh tokens q [T, heads, head_dim] over the cache: request b's queries are starts[b] .. starts[b+1]-1, the last
     of them the last of its lengths[b] cached tokens.  scale: None = head_dim ** -0.5; max_length: about the longest length (a hint)."""
-    qp, qt, qh = _heads(q, "q")
+    dev = _device()
+    qp, qt, qh = _heads(q, "q", dev)
     T, H, D = q.shape
     B = lengths.numel()
     if lengths.dim() != 1 or starts.shape != (B + 1,) or table.dim() != 2 or table.shape[0] != B:
         raise ValueError("starts is [B + 1], lengths [B], table [B, width]")
-    cp, pages = _cache(cache, page_size, kv_heads, D)
-    y = _attention_out(q, out)
-    _check(_lib.pipe_cache_attention(qp, _type(q.dtype), T, H, kv_heads, D, qt, qh, _ints(starts), _ints(lengths), B, cp, pages, page_size,
-                                     _ints(table), table.shape[1], D ** -0.5 if scale is None else scale, max_length, y.data_ptr(),
+    cp, pages = _cache(cache, page_size, kv_heads, D, dev)
+    y = _attention_out(q, out, dev)
+    _check(_lib.pipe_cache_attention(qp, _type(q.dtype), T, H, kv_heads, D, qt, qh, _ints(starts, dev), _ints(lengths, dev), B, cp, pages, page_size,
+                                     _ints(table, dev), table.shape[1], D ** -0.5 if scale is None else scale, max_length, y.data_ptr(),
                                      _stream()), "pipe_cache_attention")
     return y
 
@@ -854,9 +862,10 @@ def pipe_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sta
                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention over packed sequences: q [Tq, heads, head_dim], k and v [Tk, kv_heads, head_dim]; sequence b is starts[b] ..
     starts[b+1]-1 of q and starts_k (None: starts) of k and v.  causal: aligned at the end.  scale: None = head_dim ** -0.5."""
-    qp, qt, qh = _heads(q, "q")
-    kp, kt, kh = _heads(k, "k")
-    vp, vt, vh = _heads(v, "v")
+    dev = _device()
+    qp, qt, qh = _heads(q, "q", dev)
+    kp, kt, kh = _heads(k, "k", dev)
+    vp, vt, vh = _heads(v, "v", dev)
     T, H, D = q.shape
     Tk, Hkv, Dk = k.shape
     if v.shape != (Tk, Hkv, D) or Dk != D or k.dtype is not q.dtype or v.dtype is not q.dtype:
@@ -864,8 +873,8 @@ def pipe_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sta
     B = starts.numel() - 1
     if starts.dim() != 1 or B < 1 or (starts_k is not None and starts_k.shape != starts.shape):
         raise ValueError("starts and starts_k are [sequences + 1]")
-    y = _attention_out(q, out)
-    _check(_lib.pipe_prompt_attention(qp, kp, vp, _type(q.dtype), T, Tk, H, Hkv, D, qt, qh, kt, kh, vt, vh, _ints(starts),
-                                      None if starts_k is None else _ints(starts_k), B, 1 if causal else 0,
+    y = _attention_out(q, out, dev)
+    _check(_lib.pipe_prompt_attention(qp, kp, vp, _type(q.dtype), T, Tk, H, Hkv, D, qt, qh, kt, kh, vt, vh, _ints(starts, dev),
+                                      None if starts_k is None else _ints(starts_k, dev), B, 1 if causal else 0,
                                       D ** -0.5 if scale is None else scale, y.data_ptr(), _stream()), "pipe_prompt_attention")
     return y

@@ -260,3 +260,17 @@ def test_tables_of_other_ranks_are_refused(pipe):
     for bad in (lengths[:, None], lengths[0]):
         with pytest.raises(ValueError):
             pipe.pipe_cache_plan(bad, bad, 16, slots, ints([0]), table, 2)
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(pipe, monkeypatch):
+    """The kernels run on the current device; one card is enough to ask: another one is said to be current."""
+    q, k, cache, starts, lengths, table, slots = small_call(pipe)
+    calls = [lambda: pipe.pipe_cache_plan(lengths, lengths, 16, slots, ints([0]), table, 2), lambda: pipe.pipe_cache_write(k, k, slots, cache, 16),
+             lambda: pipe.pipe_cache_read(slots, cache, 16, 2, 64), lambda: pipe.pipe_cache_attention(q, starts, lengths, cache, table, 16, 2),
+             lambda: pipe.pipe_prompt_attention(q, k, k, starts)]
+    for call in calls:
+        call()
+    monkeypatch.setattr(pipe, "_device", lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
