@@ -632,7 +632,7 @@ int pipe_cache_read(const void* cache_dev, int n_pages, int P, const int32_t* sl
  * Scores, maxima, sums and outputs are fp32.  The codes meet q in fp16 products that are summed in fp32: q of 16 bits as it is
  * (under a power of two that brings its row's largest value to 2^14: what is 2^-28 of that or less is rounded), fp32 as the sum
  * of two fp16 values (22 bits); the softmax's weights times V's scales likewise, one fp16 value (11 bits) for 16-bit outputs,
- * two for fp32.  Any finite q and scale; rows of K and V under 2^-90 lose digits (they count to about 2^-117).
+ * two for fp32.  Any finite q and scale; keys under 2^-110 lose digits.
  * Errors: PIPE_EINVAL (NULL, type, P, scale not finite), PIPE_ESHAPE (T < 0, B < 1, heads, D, table_width < 1, cache or table too large),
  * PIPE_ENOTREADY (scratch would have to grow during a capture).                                                   */
 int pipe_cache_attention(const void* q_dev, int type, int T, int Hq, int Hkv, int D, int64_t q_token_stride,

@@ -48,9 +48,12 @@ constexpr size_t ATTN_COUNTS = 4096;                // bytes of the counts of pa
 static_assert(SHARES_64 * sizeof(uint32_t) <= ATTN_COUNTS && SHARES_128 <= SHARES_64);
 constexpr float REF_SLACK = 6.f;                    // log2: a row's reference rises only when a score exceeds it by this
 constexpr float P_SCALE = 256.f;                    // 2^REF_SLACK * 2 * P_SCALE fits fp16
-constexpr int W_LOG = 32;                           // weights are 2^-W_LOG at the reference: times offsets next to bf16's largest they sum up over 2^26 tokens
 constexpr int K_LOG = 28;                           // a code's sums with q, up to 2^26, and q's, up to 2^22, meet K's scale and offset in units of 2^28: finite
-constexpr float S_LEAST = 0x1p-80f;                 // least unit of V's scales: 2^W_LOG * P_SCALE over it is finite
+constexpr float S_LEAST = 0x1p-116f;                // least unit of V's scales and offsets
+constexpr float OFFSETS = 0x1p-8f;                  // an offset counts as a scale of so much of it: little beside a scale, which is 2^-12 of it or none
+// log2 of a weight at the reference: weights times offsets stay well inside fp32's range, tiny ones and those next to its end.  (No more apart than
+// that parts of different units are joined without losing a weight.)
+__device__ __forceinline__ int level_of(float sigma) { return max(-32, min(16, 8 + 127 - (int)(__float_as_uint(sigma) >> 23))); }
 
 struct Kernel {
   CacheAttnArgs a;
@@ -564,11 +567,12 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     f4 o[MT], ones = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < MT; ++i) o[i] = (f4){0.f, 0.f, 0.f, 0.f};
-    // weights are exp2(rs * T + nref), nref = -rs * ref - W_LOG.  The operand of the second product is a weight times V's scale in units of sigma,
-    // times `lev` = 2^W_LOG * P_SCALE / sigma: a power of two, all scales of V that the row has seen under 2 sigma.  (Up to the tokens that every
-    // row sees all rows have one sigma.)  Offsets are summed as they are: rows of V without a scale say nothing of sigma.
-    float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = S_LEAST, lev = P_SCALE * 0x1p32f / S_LEAST;
-    static_assert(W_LOG == 32);
+    // weights are exp2(rs * T + nref), nref = -rs * ref + level_of(sigma), sigma a power of two: all scales of V that the row has seen are under
+    // 2 sigma, all offsets under 2 sigma / OFFSETS.  The operand of the second product is a weight times a scale times `lev` = P_SCALE / sigma /
+    // 2^level_of(sigma), under 2^15.  (Up to the tokens that every row sees all rows have one sigma.)
+    float ref = -INFINITY, nref = 0.f, lift = -INFINITY, sum = 0.f, osum = 0.f, sigma = S_LEAST;
+    auto lev_of = [](float sigma) { return ldexpf(P_SCALE / sigma, -level_of(sigma)); };
+    float lev = lev_of(S_LEAST);
 
     // one step on `c`, while the next ones' loads fly, AHEAD steps on to `n`
     auto step = [&](const Tokens<D>& c, Tokens<D>& n) {
@@ -611,6 +615,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
         const int j = l16 >> 2 & 1;
         const bool live = tok + 16 * j + 4 * kg + (l16 & 3) < end && ((c.there >> (NB == 1 ? 0 : j)) & 1u);
         ws = live ? ws : 0.f;
+        wo = live ? wo : 0.f;
         wm = live ? wm : 0.f;
       }
       float smax = s[0][0];
@@ -618,13 +623,14 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) smax = fmaxf(smax, s[j][i]);
-      // V's scales: of a token in each lane, or of the tokens that this row sees where the rows differ
-      float vs = l16 < 8 ? 0.f : fabsf(ws);
+      // V's scales and offsets: of a token in each lane, or of the tokens that this row sees where the rows differ
+      const float v_size = fmaf(fabsf(wo), OFFSETS, fabsf(ws));
+      float vs = l16 < 8 ? 0.f : v_size;
       if (some) {
         vs = 0.f;
         each<8>([&](auto B) {
           constexpr int bit = B;
-          const float g = fabsf(from_lane<8 + bit>(ws));
+          const float g = from_lane<8 + bit>(v_size);
           vs = fmaxf(vs, (vis >> bit) & 1u ? g : 0.f);
         });
       }
@@ -637,15 +643,16 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
         }
         const float nsigma = fmaxf(sigma, __uint_as_float(__float_as_uint(top) & 0x7f800000u));
         const float f = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rs * (ref - nr)), fo = f * (sigma / nsigma);
-        sum *= f;
-        osum *= f;
+        const int down = level_of(nsigma) - level_of(sigma);
+        sum = ldexpf(sum * f, down);
+        osum = ldexpf(osum * f, down);
 #pragma unroll
         for (int i = 0; i < MT; ++i) o[i] *= fo;
         ones *= fo;
         ref = nr;
         sigma = nsigma;
-        lev = P_SCALE * 0x1p32f / nsigma;
-        nref = (nr == -INFINITY ? 0.f : -nr * rs) - W_LOG;
+        lev = lev_of(nsigma);
+        nref = (nr == -INFINITY ? 0.f : -nr * rs) + level_of(nsigma);
         lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
       }
       // weights
@@ -721,7 +728,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
     // a wave's outputs as they are, O[d][row] at d = MT * (4 kg + j) + i, over the reference weight
     sum = sum_over_kg(sum);
     osum = sum_over_kg(osum);
-    const float lref = ref == -INFINITY ? -INFINITY : -nref, unit = sigma * (0x1p-32f / P_SCALE);
+    const float lref = ref == -INFINITY ? -INFINITY : -nref, unit = ldexpf(sigma / P_SCALE, level_of(sigma));
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll

@@ -197,6 +197,24 @@ def test_cache_of_constant_values(pipe, kind, values, n, rise, D):
             assert np.abs(got / c - 1).max() <= limit, (c, hint)
 
 
+@pytest.mark.parametrize("kind,gain", [(k, g) for k in ("f32", "bf16") for g in (1e-36, 1e-30, 1e-20, 1e30, 3e37)] + [("f16", 1e-4), ("f16", 1.5e4)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_cache_of_small_and_large_values(pipe, kind, gain, D):
+    """Values of any size keep their digits, in one piece and in parts."""
+    P, Hq, Hkv, n, fresh = 32, 4, 2, 1500, 2
+    rng = np.random.default_rng(D)
+    cache, table, kk, vv = filled(pipe, rng.standard_normal((n, Hkv, D)), np.clip(rng.standard_normal((n, Hkv, D)), -4, 4) * gain, P)
+    q, qf = typed(rng, (fresh, Hq, D), kind)
+    want = cache_reference(qf, [fresh], [n], [(kk, vv)], D ** -0.5)
+    a = D ** -0.5 * float(np.abs(qf).sum(-1).max()) * 2 * float(np.abs(kk).max())
+    limit = ref.far(kind, D, n, a, 2 * float(np.abs(vv).max()))
+    if kind == "f16":
+        limit += 2.0 ** -25                     # (an output under 2^-14 is rounded to a multiple of 2^-24)
+    for hint in (0, 1):
+        got = pipe.pipe_cache_attention(q, ints([0, fresh]), ints([n]), cache, table, P, Hkv, max_length=hint).double().cpu().numpy()
+        assert np.abs(got - want).max() <= limit, hint
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("huge", [1e9, 1e30])
