@@ -1,11 +1,13 @@
 """Attention at the edges of its number range: zero, constant, huge and infinite keys and values, empty and tiny queries, scales far from one;
 and what the binding refuses.  Against the definitions in numpy."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 import _attention as ref
-from test_gpu_attention import DT, cache_reference, ints, pipe, prompt_reference, typed  # noqa: F401
+from test_gpu_attention import DT, cache_reference, ints, pipe, prompt_reference, random_cache, typed  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -249,6 +251,70 @@ def test_cache_of_far_factors(pipe, kind, q_gain, k_gain, scale):
     want = cache_reference(qf, [fresh], [n], [(kk, vv)], sc)
     a = sc * float(np.abs(qf).sum(-1).max()) * 2 * float(np.abs(kk).max())
     assert np.abs(got - want).max() <= ref.far(kind, D, n, a, 2 * float(np.abs(vv).max()))
+
+
+# ------------------------------------------------------------------ graphs
+
+def fresh_stream():
+    """A stream that no earlier call can have used (torch's own come from a pool)."""
+    hip = ctypes.CDLL("libamdhip64.so")
+    s = ctypes.c_void_p()
+    assert hip.hipStreamCreate(ctypes.byref(s)) == 0
+    return torch.cuda.ExternalStream(s.value)
+
+
+def test_a_stream_without_scratch_is_refused_in_a_capture_and_served_once_prepared(pipe):
+    rng = np.random.default_rng(1)
+    lens = [2000, 300]
+    cache, table, _ = random_cache(pipe, rng, lens, 2, 64, 16)
+    q, _ = typed(rng, (2, 8, 64), "f32")
+    starts, lengths = ints([0, 1, 2]), ints(lens)
+    want = pipe.pipe_cache_attention(q, starts, lengths, cache, table, 16, 2)
+    out = torch.full_like(want, float("nan"))
+    side = fresh_stream()
+    torch.cuda.synchronize()
+    codes = []
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        try:
+            pipe.pipe_cache_attention(q, starts, lengths, cache, table, 16, 2, out=out)
+        except pipe.PipeError as e:
+            codes.append(e.code)
+        q.add(1)
+    assert codes == [-6]
+    with torch.cuda.stream(side):
+        pipe.pipe_prepare_cache_attention(2, 8, 2, 64, 2, max(lens))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        pipe.pipe_cache_attention(q, starts, lengths, cache, table, 16, 2, out=out)
+    for _ in range(4):
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_prompts_in_a_graph(pipe, kind):
+    """Captured once, replayed on other values and other lengths, with the caller's work between."""
+    n, D = 200, 64
+    rng = np.random.default_rng(2)
+    x, _ = typed(rng, (n, 8, D), kind)
+    starts = ints([0, 50, 120, n])
+    out = torch.empty((n, 4, D), dtype=DT[kind], device="cuda")
+    call = lambda o=None: pipe.pipe_prompt_attention(x[:, :4], x[:, 4:6], x[:, 6:], starts, out=o)      # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for i in range(4):
+        x.copy_(typed(rng, (n, 8, D), kind)[0])
+        starts.copy_(ints([0, 10 * i, 60 + 35 * i, n - i]))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(got, call()), i
 
 
 # ------------------------------------------------------------------ refusals
