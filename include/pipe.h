@@ -581,7 +581,8 @@ int pipe_hbm_probe(int64_t bytes, double* gbps_out, void* stream);
  * is outside is not written, reads as zeros and is left out of the attention.
  *
  * All calls are asynchronous on `stream`, allocate nothing but library scratch, and may be captured into a graph
- * (pipe_cache_attention after pipe_prepare_cache_attention on that stream).                                        */
+ * (pipe_cache_attention after pipe_prepare_cache_attention on that stream; a captured call uses the scratch of the stream
+ * that it was captured on, so its replays must not overlap in time with that stream's other calls).                 */
 enum { PIPE_F32 = 0, PIPE_F16 = 1, PIPE_BF16 = 2 };
 
 /* Bytes of one page; 0 if the cache has no such page (Hkv < 1, D not 64 or 128, P not one of the above). */
@@ -649,8 +650,10 @@ int pipe_prepare_cache_attention(int T, int Hq, int Hkv, int D, int B, int max_l
  *   belong to no sequence.
  * Scores, maxima, sums and outputs are fp32.  16-bit types: the softmax's weights are rounded to that type for the product
  * with V.  fp32: q, k, v and the weights enter the products as the sum of two fp16 values each (22 bits of what is no less than
- * 2^-17 of the largest value of its row).  A key that a query does not see -- a later one, another sequence's -- does not
- * reach its output, whatever it holds; infinities and NaN of V cost the tiles around them a second pass.
+ * 2^-17 of the largest value of its row; keys and values under 2^-88 and 2^-105 lose digits).  A key that a query does not see --
+ * a later one, another sequence's -- does not reach its output, whatever it holds.  One that it sees counts by the formula: an
+ * infinity of V is one in its column, a score of -infinity a weight of 0, one of +infinity NaN.  Where an output is not finite, or
+ * the sums over values next to bf16's largest are not, 128 rows of a head are computed once more.
  * Errors: PIPE_EINVAL (NULL, type, scale not finite), PIPE_ESHAPE (Tq or Tk < 0, B < 1, heads, D, strides).       */
 int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_dev, int type, int Tq, int Tk, int Hq,
                           int Hkv, int D, int64_t q_token_stride, int64_t q_head_stride, int64_t k_token_stride,

@@ -743,7 +743,8 @@ def _type(dtype: torch.dtype) -> int:
     return t
 
 
-# (These calls are a few microseconds on the device at decode sizes: what they ask of a tensor they ask once.)
+# Inference only, as all of this module: no gradient passes through these calls, their outputs require none.
+# (They are a few microseconds on the device at decode sizes: what they ask of a tensor they ask once.)
 # The number of the current device, on whose stream the kernels run: tensors of another one, or of none (-1), are refused.
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
@@ -836,7 +837,8 @@ def pipe_cache_attention(q: torch.Tensor, starts: torch.Tensor, lengths: torch.T
                          page_size: int, kv_heads: int, scale: Optional[float] = None, max_length: int = 0,
                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the fresh tokens q [T, heads, head_dim] over the cache: request b's queries are starts[b] .. starts[b+1]-1, the last
-    of them the last of its lengths[b] cached tokens.  scale: None = head_dim ** -0.5; max_length: about the longest length (a hint)."""
+    of them the last of its lengths[b] cached tokens.  scale: None = head_dim ** -0.5; max_length: about the longest length (a hint).
+    The output has no gradient, also where q requires one."""
     dev = _device()
     qp, qt, qh = _heads(q, "q", dev)
     T, H, D = q.shape
@@ -861,7 +863,8 @@ def pipe_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sta
                           starts_k: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
                           out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention over packed sequences: q [Tq, heads, head_dim], k and v [Tk, kv_heads, head_dim]; sequence b is starts[b] ..
-    starts[b+1]-1 of q and starts_k (None: starts) of k and v.  causal: aligned at the end.  scale: None = head_dim ** -0.5."""
+    starts[b+1]-1 of q and starts_k (None: starts) of k and v.  causal: aligned at the end.  scale: None = head_dim ** -0.5.
+    The output has no gradient, also where an input requires one."""
     dev = _device()
     qp, qt, qh = _heads(q, "q", dev)
     kp, kt, kh = _heads(k, "k", dev)

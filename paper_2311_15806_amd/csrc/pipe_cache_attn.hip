@@ -17,12 +17,13 @@
 // The offsets' part of the output is P (m + 8 s), with m about -8 s: no large sums that cancel.
 //
 // Every byte of the cache is read once as long as a tile holds all rows of the head (tokens * G <= 16), and those bytes bound it:
-// two requests of 131072 tokens, 8 heads of 128, take 62 us = 4.6 TB/s, 48 of 33 to 8000 tokens 52 us = 4.1 TB/s (a large copy: 4.8).
+// two requests of 131072 tokens, 8 heads of 128, take 62 us = 4.6 TB/s, 48 of 33 to 8000 tokens 51 us = 4.1 TB/s (a large copy: 4.8).
 // To reach that: steps of 32 tokens with two in flight beside the one worked on, the table through scalar loads, a step's words in one
 // register spread by DPP (the 131072s 86 us; 64 tokens and one in flight, words and addresses in each lane: 134); equal shares of all
 // steps to as many workgroups as the chip holds (67); joined by whichever of a tile's shares ends last (one request of 777 tokens
 // 10.8 us; in a second launch 13.3).  One request of 777 tokens is eight trips to memory in a row, 10 us.  fp32 is bound by its instructions: two terms of q
-// and of the weights; 16 requests of 100 to 3000 tokens with 5 rows a tile, 32 heads of 64, take 27 us at 2.2 TB/s.
+// and of the weights, made for 16 rows a tile whatever is real; 16 requests of 100 to 3000 tokens with 5 rows a tile, 32 heads of 64, take
+// 27 us at 2.2 TB/s.  (Every instance keeps 13 to 33 scalar registers in lanes of vector ones.)
 #include <algorithm>
 #include <type_traits>
 
@@ -136,7 +137,9 @@ constexpr float LOAD_64 = 0.67f, LOAD_128 = 1.f, JOIN = 4.f;
 constexpr uint32_t GAP = 4;      // 48 requests of 33 to 8000 tokens: 54.8 us with 0, 53.6 with 2, 51.8 with 4, 53.0 with 6
 
 // The first place of a share.  Up to 63 requests: every wave for itself, a lane a request.  More: the workgroup together, a thread sums
-// every 256th part of them, and the one whose sum holds the place walks them again.
+// every 256th part of them, and the one whose sum holds the place walks them again; those get equal shares only, because the search of one wave
+// ends there, not because they were the better ones: 63 and 64 requests of 750 tokens in bf16, 32 heads over 8 of 64, take 12.8 and 15.8 us, of
+// 3000 tokens 29.6 and 35.5; 16 heads over one of 128, 13.5 and 15.8, 16.3 and 18.3.
 __device__ __forceinline__ Place locate(const Kernel& k, uint32_t share) {
   __shared__ uint32_t s_sum[4], s_step;
   __shared__ int s_b;
@@ -655,7 +658,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void cache_attn_kernel
         nref = (nr == -INFINITY ? 0.f : -nr * rs) + level_of(nsigma);
         lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
       }
-      // weights
+      // weights times V's scales: one fp16 value for outputs of 16 bits (2^-12 of each, at random, less than such an output's own rounding), two
+      // for fp32; their sums take them unrounded
       if (!some) ws *= lev;
       u4 p[NT];
       auto weights = [&](auto SOME) {

@@ -7,10 +7,12 @@
 // scores' accumulator layout is, up to the order of the keys, that of the second product's operand: weights never go through LDS.
 //
 // The floor is the products', 4 D operations a pair of query and key that sees it: 8192 tokens, 32 heads over 8 of 128, in bf16 take
-// 0.53 ms = 1035 TFLOP/s, where a matrix product of 8192^3 reaches 1182.  At that size the matrix units and the LDS reads
-// are busy half of the time each and the softmax's instructions 45 %, between two waves a SIMD.  Seven packed prompts of 3 to 2500 tokens:
-// 0.2 ms, 750 TFLOP/s: short sequences and the causal edge leave rows and tiles unused.  fp32, 4096 tokens, 32 heads over 8 of 128: 0.54 ms,
-// 253 TFLOP/s counted once, three products each; 97 tokens 12 us, four tiles of keys in a row.
+// 0.53 to 0.55 ms = 1000 to 1035 TFLOP/s, where a matrix product of 8192^3 reaches 1182.  At that size the matrix units and the LDS reads
+// are busy half of the time each and the softmax's instructions 45 %, between two waves a SIMD.  Seven packed prompts of 228 to 2500 tokens
+// take 0.2 ms, 730 to 750 TFLOP/s, about 98 steps of 64 keys (2.05 us each) one after the other at every place of the chip: 69 are the pairs that
+// are seen, 4 the causal edges of tiles, 15 the beginnings of tiles (3 steps each, of 15 on average), 10 an end that is not even.
+// fp32, 4096 tokens, 32 heads over 8 of 128: 0.54 ms, 253 TFLOP/s counted once, three products each (at head_dim 128 150 registers a lane are
+// spilled); 97 tokens 12 us, one workgroup's four tiles of keys in a row, where keys are not split between waves.
 // The tallest tiles are launched first, so that the short ones fill the end; workgroups that follow each other have different heads of the
 // same rows, which keeps the heads' keys in one XCD each where Hkv is 8.
 #include <type_traits>
@@ -211,6 +213,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
   for (int s = 0; s < KS; ++s)
 #pragma unroll
     for (int i = 0; i < 4; ++i) q[s][i] = (q[s][i] ^ flip) & keep;
+  // log2 of a weight per unit of a score
   const float rs = a.scale == 0.f ? 1.f : fminf(fabsf(a.scale) * 1.44269504f, 0x1.fffffep127f);    // (finite: 0 times it is 0)
 
   f16v o[DB];
@@ -271,6 +274,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_mfma_kernel(const Kernel
       nref = p_log() - (nr == -INFINITY ? 0.f : nr * rs);
       lift = nr == -INFINITY ? -INFINITY : nr + REF_SLACK / rs;
     }
+    // (weights are rounded to the inputs' type, the only one that the matrix unit multiplies with V's: 2^-12 or 2^-9 of each, at random; their
+    // sum takes them unrounded)
     u4 p[2][2];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
