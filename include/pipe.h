@@ -661,6 +661,64 @@ int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_de
                           const int32_t* q_starts_dev, const int32_t* k_starts_dev, int B, int causal, float scale,
                           void* out_dev, void* stream);
 
+/* ---- Layers in 8-bit integers with a scale for each token, and a router's experts ----
+ *
+ * pipe_forward's activations have one scale a call, the largest value's: a token's result depends on the others of its batch.  Here every token has
+ * its own, and every output channel of the weights one: y[t][o] = act( s_t * s_o * sum_i c_t[i] w_o[i] + b_o ).  The sum is exact.
+ *
+ * Rows and codes: a row x of `in` values (fp32, fp16 or bf16) has s = max|x| / 127 in fp32 (0 if under 2^-126), c = clamp(rint(x / s), -127, 127)
+ * with the correctly rounded fp32 quotient, rint to even, c = 0 where s = 0.  A row that holds a NaN or an infinity has s = NaN and c = 0: all its
+ * outputs are NaN (ReLU's too), other tokens' are not touched.  Always 8 bits, whatever pipe_set_activation_bits says.  Codes are rows of
+ * pipe_token_pitch(in) bytes, `in` rounded up to a multiple of 128, 16-byte aligned; pipe_token_quantize writes zeros behind the
+ * row's end; what weights hold there does not matter.  Weights are such rows too, [out][pitch] and [out] scales: made by
+ * pipe_token_quantize from W [out, in], or any codes (-128 as well) and any scales of another origin.
+ *
+ * Activations of `act`: PIPE_ACT_NONE, PIPE_ACT_GELU (erf), PIPE_ACT_RELU, and PIPE_ACT_SILU_GATED: 2 * out rows of weights, scales and bias, the
+ * gate's first, y = SiLU(gate) * up.  scale and bias vectors are fp32, bias_dev NULL = none; everything behind the sum is fp32, y is rounded once to x's
+ * type.  Any finite scales whose product with the sum is finite.
+ *
+ * x has a row stride in elements (>= 0), its rows are dense; 16-byte aligned addresses and strides are read with wider loads.  y is dense, 16-byte aligned, and must not
+ * overlap an input.  1 <= in <= 130944.  All calls are asynchronous on `stream`, allocate nothing, use no library scratch and may be captured
+ * into a graph at any time.  scratch_dev: pipe_token_scratch(T, in) bytes, 16-byte aligned, of the caller's, in use until the call has run on the stream.    */
+int pipe_token_pitch(int in);                                  /* 0: no such row */
+int64_t pipe_token_scratch(int64_t rows, int in);              /* -1: no such rows */
+/* Errors: PIPE_EINVAL (NULL, type, alignment), PIPE_ESHAPE (rows < 0 or >= 2^30, in, stride).                       */
+int pipe_token_quantize(const void* x_dev, int type, int64_t rows, int in, int64_t row_stride, int8_t* codes_dev,
+                        float* scales_dev, void* stream);
+/* Errors: PIPE_EINVAL (NULL, type, act, alignment), PIPE_ESHAPE (T, in, out, stride).                              */
+int pipe_token_forward(const void* x_dev, int type, int64_t T, int in, int64_t row_stride, const int8_t* codes_dev,
+                       const float* scales_dev, const float* bias_dev, int out, int act, void* scratch_dev, void* y_dev, void* stream);
+
+/* The router: of each token's E logits the top_k largest, largest first, ties to the lower expert, and their weights exp(l - max) / sum, the sum over the chosen
+ * ones (renormalize 1) or over all E (0).  An expert with the logit -infinity or NaN is never chosen; where fewer than top_k are left the rest are
+ * expert -1 with weight 0.  (A NaN beside them, or +infinity, makes weights NaN by the formula.)
+ *   experts_dev, weights_dev [T][top_k];  starts_dev, order_dev, places_dev: as pipe_expert_sort, of these experts.
+ * pipe_expert_sort: the T * top_k pairs (token, choice) by expert, in the pairs' order within an expert; pairs whose expert is outside 0 .. E-1 (another
+ * device's, -1) have no row.
+ *   starts_dev [E+1]      first row of each expert, and their total
+ *   order_dev  [T*top_k]  row -> pair token * top_k + choice; -1 from the total on
+ *   places_dev [T][top_k] pair -> row, or -1
+ * Errors: PIPE_EINVAL (NULL, type, renormalize), PIPE_ESHAPE (T < 0, T * top_k >= 2^30, E outside 1..1024, top_k outside 1..32 or over E, stride).
+ * (pipe_expert_sort: top_k may exceed E.)                                                                           */
+int pipe_expert_route(const void* logits_dev, int type, int T, int E, int64_t row_stride, int top_k, int renormalize,
+                      int32_t* experts_dev, float* weights_dev, int32_t* starts_dev, int32_t* order_dev, int32_t* places_dev, void* stream);
+int pipe_expert_sort(const int32_t* experts_dev, int T, int top_k, int E, int32_t* starts_dev, int32_t* order_dev,
+                     int32_t* places_dev, void* stream);
+
+/* pipe_token_forward of each expert on its rows: codes_dev [E][out or 2 out][pitch], scales_dev and bias_dev [E][out or 2 out].  Rows starts_dev[e] ..
+ * starts_dev[e+1]-1 of y (ascending from 0, at most `rows`) are expert e's.  Row r is token order_dev[r] / top_k of x [T]; order_dev NULL: row r of x, then
+ * rows = T.  Rows from starts_dev[E] on, and rows whose order is outside 0 .. T*top_k-1, are zeros.
+ * Errors: as pipe_token_forward; PIPE_ESHAPE also for E outside 1..1024, top_k outside 1..32, rows.                 */
+int pipe_expert_forward(const void* x_dev, int type, int64_t T, int in, int64_t row_stride, const int8_t* codes_dev,
+                        const float* scales_dev, const float* bias_dev, int E, int out, const int32_t* starts_dev,
+                        const int32_t* order_dev, int64_t rows, int top_k, int act, void* scratch_dev, void* y_dev, void* stream);
+
+/* Back to the tokens: out[t] = sum_j weights[t][j] * y[places[t][j]] in fp32, j ascending, rounded once to y's type (out_dev dense [T][out]); a choice
+ * whose place is outside 0 .. rows-1 is left out, whatever its weight; a token without any is zeros.
+ * Errors: PIPE_EINVAL (NULL, type), PIPE_ESHAPE (T, top_k, rows, out, stride).                                     */
+int pipe_expert_combine(const void* y_dev, int type, int64_t rows, int out, int64_t row_stride, const int32_t* places_dev,
+                        const float* weights_dev, int T, int top_k, void* out_dev, void* stream);
+
 const char* pipe_strerror(int code);
 /* Text of the last HIP error seen by this thread ("" if none). */
 const char* pipe_last_device_error(void);

@@ -99,6 +99,15 @@ def _load():
     lib.pipe_cache_attention.argtypes = [vp, ci, ci, ci, ci, ci, i64, i64, vp, vp, ci, vp, ci, ci, vp, ci, cf, ci, vp, vp]
     lib.pipe_prepare_cache_attention.argtypes = [ci, ci, ci, ci, ci, ci, vp]
     lib.pipe_prompt_attention.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, i64, i64, i64, i64, i64, i64, vp, vp, ci, ci, cf, vp, vp]
+    lib.pipe_token_pitch.argtypes = [ci]
+    lib.pipe_token_scratch.argtypes = [i64, ci]
+    lib.pipe_token_scratch.restype = i64
+    lib.pipe_token_quantize.argtypes = [vp, ci, i64, ci, i64, vp, vp, vp]
+    lib.pipe_token_forward.argtypes = [vp, ci, i64, ci, i64, vp, vp, vp, ci, ci, vp, vp, vp]
+    lib.pipe_expert_route.argtypes = [vp, ci, ci, ci, i64, ci, ci, vp, vp, vp, vp, vp, vp]
+    lib.pipe_expert_sort.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp]
+    lib.pipe_expert_forward.argtypes = [vp, ci, i64, ci, i64, vp, vp, vp, ci, ci, vp, vp, i64, ci, ci, vp, vp, vp]
+    lib.pipe_expert_combine.argtypes = [vp, ci, i64, ci, i64, vp, vp, ci, ci, vp, vp]
     lib.pipe_strerror.argtypes = [ci]
     lib.pipe_strerror.restype = C.c_char_p
     lib.pipe_last_device_error.restype = C.c_char_p
@@ -881,3 +890,153 @@ def pipe_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sta
                                       None if starts_k is None else _ints(starts_k, dev), B, 1 if causal else 0,
                                       D ** -0.5 if scale is None else scale, y.data_ptr(), _stream()), "pipe_prompt_attention")
     return y
+
+
+# ---------------------------------------------------------------- 8-bit layers with a scale for each token, and a router's experts
+
+
+def _rows(x: torch.Tensor, name: str, dev: int):
+    """(address, row stride) of [rows, n] with dense rows."""
+    s = x.stride()
+    if len(s) != 2 or x.get_device() != dev or (s[1] != 1 and x.shape[1] > 1):
+        raise ValueError("%s must be a matrix on the current device with dense rows" % name)
+    return x.data_ptr(), s[0]
+
+
+def _dense(t: torch.Tensor, dtype: torch.dtype, shape, name: str, dev: int) -> int:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s of the current device" % (name, dtype, list(shape)))
+    return t.data_ptr()
+
+
+def _result(out: Optional[torch.Tensor], x: torch.Tensor, rows: int, width: int, dev: int) -> torch.Tensor:
+    if out is None:
+        return x.new_empty((rows, width))
+    if out.shape != (rows, width) or out.dtype is not x.dtype or out.get_device() != dev or not out.is_contiguous():
+        raise ValueError("output has the wrong shape, type or device, or is not contiguous")
+    return out
+
+
+def pipe_token_pitch(in_features: int) -> int:
+    """Bytes of a row of codes: in_features rounded up to a multiple of 128."""
+    n = _lib.pipe_token_pitch(int(in_features))
+    if n == 0:
+        raise ValueError("1 <= in_features <= 130944")
+    return n
+
+
+def pipe_token_scratch(rows: int, in_features: int) -> int:
+    """Bytes of the codes and scales of rows inputs, which the calls below keep in a tensor of their own while they run."""
+    n = _lib.pipe_token_scratch(int(rows), int(in_features))
+    if n < 0:
+        raise ValueError("0 <= rows < 2**30, 1 <= in_features <= 130944")
+    return n
+
+
+def pipe_token_quantize(x: torch.Tensor):
+    """(codes [rows, pitch] int8, scales [rows] fp32) of the rows x [rows, n]: activations, or weights [out, in] for the calls below."""
+    dev = _device()
+    xp, stride = _rows(x, "x", dev)
+    rows, n = x.shape
+    codes = torch.empty((rows, pipe_token_pitch(n)), dtype=torch.int8, device=x.device)
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _check(_lib.pipe_token_quantize(xp, _type(x.dtype), rows, n, stride, codes.data_ptr(), scales.data_ptr(), _stream()), "pipe_token_quantize")
+    return codes, scales
+
+
+def _layer_width(codes: torch.Tensor, n_in: int, act: int, lead: int) -> int:
+    shape = codes.shape
+    if len(shape) != lead + 2 or shape[-1] != (n_in + 127) // 128 * 128:
+        raise ValueError("codes must be %s[rows, pipe_token_pitch(in_features)]" % ("[experts] x " if lead else ""))
+    if act != PIPE_ACT_SILU_GATED:
+        return shape[-2]
+    if shape[-2] % 2:
+        raise ValueError("a gated layer has as many rows of the gate as of the other half")
+    return shape[-2] // 2
+
+
+def pipe_token_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                       act: int = PIPE_ACT_NONE, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(x W^T + bias) [T, out] of x's type, both sides in 8 bits: x [T, in] with a scale for each token (pipe_token_quantize, inside), W as
+    codes [out, pitch] with scales [out] (PIPE_ACT_SILU_GATED: 2 * out rows, the gate's first).  The output has no gradient."""
+    dev = _device()
+    xp, stride = _rows(x, "x", dev)
+    T, n = x.shape
+    width = _layer_width(codes, n, act, 0)
+    y = _result(out, x, T, width, dev)
+    cp = _dense(codes, torch.int8, codes.shape, "codes", dev)
+    lead = codes.shape[:-1]
+    sp = _dense(scales, torch.float32, lead, "scales", dev)
+    bp = None if bias is None else _dense(bias, torch.float32, lead, "bias", dev)
+    scratch = torch.empty(T * (codes.shape[-1] + 4), dtype=torch.uint8, device=x.device)
+    _check(_lib.pipe_token_forward(xp, _type(x.dtype), T, n, stride, cp, sp, bp, width, act, scratch.data_ptr(), y.data_ptr(), _stream()),
+           "pipe_token_forward")
+    return y
+
+
+def pipe_expert_route(logits: torch.Tensor, top_k: int, renormalize: bool = True):
+    """Of each token's logits [T, E] the top_k largest: (experts [T, top_k], weights [T, top_k], starts [E + 1], order [T * top_k], places
+    [T, top_k]), the tables as pipe_expert_sort gives them.  weights: softmax over the chosen (renormalize) or over all."""
+    dev = _device()
+    lp, stride = _rows(logits, "logits", dev)
+    T, E = logits.shape
+    if not 1 <= top_k <= 32:
+        raise ValueError("top_k must be 1 to 32")
+    n = T * top_k
+    experts, weights, order, places, starts = torch.empty(4 * n + E + 1, dtype=torch.int32, device=logits.device).split([n, n, n, n, E + 1])
+    weights = weights.view(torch.float32)
+    _check(_lib.pipe_expert_route(lp, _type(logits.dtype), T, E, stride, top_k, 1 if renormalize else 0, experts.data_ptr(), weights.data_ptr(),
+                                  starts.data_ptr(), order.data_ptr(), places.data_ptr(), _stream()), "pipe_expert_route")
+    return experts.view(T, top_k), weights.view(T, top_k), starts, order, places.view(T, top_k)
+
+
+def pipe_expert_sort(experts: torch.Tensor, num_experts: int):
+    """The pairs of experts [T, top_k] (int32; outside 0 .. num_experts - 1: no row) by expert: (starts [num_experts + 1], order [T * top_k]: row ->
+    pair, -1 behind the last, places [T, top_k]: pair -> row or -1)."""
+    dev = _device()
+    if experts.dim() != 2:
+        raise ValueError("experts is [tokens, top_k]")
+    T, k = experts.shape
+    n = T * k
+    ep = _ints(experts, dev)
+    order, places, starts = torch.empty(2 * n + max(0, num_experts) + 1, dtype=torch.int32, device=experts.device).split([n, n, max(0, num_experts) + 1])
+    _check(_lib.pipe_expert_sort(ep, T, k, num_experts, starts.data_ptr(), order.data_ptr(), places.data_ptr(), _stream()), "pipe_expert_sort")
+    return starts, order, places.view(T, k)
+
+
+def pipe_expert_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, starts: torch.Tensor, order: Optional[torch.Tensor] = None,
+                        top_k: int = 1, bias: Optional[torch.Tensor] = None, act: int = PIPE_ACT_NONE,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """pipe_token_forward of every expert on its rows, starts[e] .. starts[e+1]-1 of the result [rows, out].  codes [E, out, pitch], scales and bias
+    [E, out] (gated: 2 * out).  order [rows]: row r is token order[r] // top_k of x; None: row r of x.  Rows behind starts[E] are zeros."""
+    dev = _device()
+    xp, stride = _rows(x, "x", dev)
+    T, n = x.shape
+    width = _layer_width(codes, n, act, 1)
+    E = codes.shape[0]
+    if starts.shape != (E + 1,) or (order is not None and order.dim() != 1):
+        raise ValueError("starts is [experts + 1], order [rows]")
+    rows = T if order is None else order.shape[0]
+    y = _result(out, x, rows, width, dev)
+    cp = _dense(codes, torch.int8, codes.shape, "codes", dev)
+    lead = codes.shape[:-1]
+    sp = _dense(scales, torch.float32, lead, "scales", dev)
+    bp = None if bias is None else _dense(bias, torch.float32, lead, "bias", dev)
+    scratch = torch.empty(T * (codes.shape[-1] + 4), dtype=torch.uint8, device=x.device)
+    _check(_lib.pipe_expert_forward(xp, _type(x.dtype), T, n, stride, cp, sp, bp, E, width, _ints(starts, dev), None if order is None else _ints(order, dev),
+                                    rows, top_k, act, scratch.data_ptr(), y.data_ptr(), _stream()), "pipe_expert_forward")
+    return y
+
+
+def pipe_expert_combine(y: torch.Tensor, places: torch.Tensor, weights: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[t] = sum_j weights[t, j] * y[places[t, j]] [T, width] of y's type (places [T, top_k] int32, weights fp32; a place outside y's rows is left out)."""
+    dev = _device()
+    yp, stride = _rows(y, "y", dev)
+    if places.dim() != 2:
+        raise ValueError("places is [tokens, top_k]")
+    T, k = places.shape
+    wp = _dense(weights, torch.float32, places.shape, "weights", dev)
+    r = _result(out, y, T, y.shape[1], dev)
+    _check(_lib.pipe_expert_combine(yp, _type(y.dtype), y.shape[0], y.shape[1], stride, _ints(places, dev), wp, T, k, r.data_ptr(), _stream()),
+           "pipe_expert_combine")
+    return r

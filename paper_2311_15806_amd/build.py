@@ -30,6 +30,8 @@ SOURCES = [
     ("pipe_cache.hip", PRELOAD),
     ("pipe_cache_attn.hip", []),
     ("pipe_prompt_attn.hip", []),
+    ("pipe_token.hip", PRELOAD),
+    ("pipe_token_gemm.hip", []),
 ]
 
 COMMON = [

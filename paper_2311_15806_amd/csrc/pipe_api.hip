@@ -13,6 +13,7 @@
 
 #include "pipe_attention.h"
 #include "pipe_internal.h"
+#include "pipe_token.h"
 
 // ------------------------------------------------------------------ errors
 static thread_local std::string g_last_hip_error;
@@ -2492,4 +2493,104 @@ extern "C" int pipe_prompt_attention(const void* q_dev, const void* k_dev, const
   a.type = type; a.Tq = Tq; a.Tk = Tk; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.B = B; a.causal = causal; a.scale = scale;
   a.out = out_dev;
   return launch_prompt_attention(a, (hipStream_t)stream);
+}
+
+// ------------------------------------------------------------------ a scale for each token; experts
+extern "C" int pipe_token_pitch(int in) {
+  return in < 1 || in > PIPE_TOKEN_MAX_IN ? 0 : (int)round_up64(in, PIPE_TOKEN_PITCH);
+}
+
+static bool rows_fit(int64_t rows) { return rows >= 0 && rows < 1 << 30; }
+
+extern "C" int pipe_token_quantize(const void* x_dev, int type, int64_t rows, int in, int64_t row_stride, int8_t* codes_dev,
+                                   float* scales_dev, void* stream) {
+  if (!known_type(type)) return PIPE_EINVAL;
+  const int pitch = pipe_token_pitch(in);
+  if (pitch == 0 || !rows_fit(rows) || row_stride < 0) return PIPE_ESHAPE;
+  if (rows == 0) return PIPE_OK;
+  if (!x_dev || !codes_dev || !scales_dev || !aligned16(codes_dev)) return PIPE_EINVAL;
+  return launch_token_quantize(x_dev, type, rows, in, row_stride, pitch, codes_dev, scales_dev, (hipStream_t)stream);
+}
+
+extern "C" int64_t pipe_token_scratch(int64_t rows, int in) {
+  const int pitch = pipe_token_pitch(in);
+  return pitch == 0 || !rows_fit(rows) ? -1 : rows * ((int64_t)pitch + (int64_t)sizeof(float));
+}
+
+// the layer or the experts on the rows x, whose codes and scales go to the caller's scratch
+static int token_layer(const void* x_dev, int type, int64_t rows, int in, int64_t row_stride, void* scratch_dev, TokenProductArgs a, void* stream) {
+  if (!known_type(type) || a.act < PIPE_ACT_NONE || a.act > PIPE_ACT_RELU) return PIPE_EINVAL;
+  a.pitch = pipe_token_pitch(in);
+  if (a.pitch == 0 || !rows_fit(rows) || !rows_fit(a.n) || row_stride < 0 || a.out < 1 || a.out > 1 << 28 || a.E < 1 || a.E > PIPE_EXPERTS_MAX ||
+      a.top_k < 1 || a.top_k > PIPE_TOP_K_MAX)
+    return PIPE_ESHAPE;
+  if (a.n == 0) return PIPE_OK;
+  if (!a.w || !a.sw || !a.y || !aligned16(a.w) || !aligned16(a.y)) return PIPE_EINVAL;
+  if (rows > 0 && (!x_dev || !scratch_dev || !aligned16(scratch_dev))) return PIPE_EINVAL;
+  if (rows == 0) return PIPE_ESHAPE;      // rows of y without an input
+  a.type = type;
+  a.n_x = rows;
+  int8_t* codes = (int8_t*)scratch_dev;
+  float* scales = (float*)(codes + rows * a.pitch);
+  a.qx = codes;
+  a.sx = scales;
+  const int rc = launch_token_quantize(x_dev, type, rows, in, row_stride, a.pitch, codes, scales, (hipStream_t)stream);
+  return rc ? rc : launch_token_product(a, (hipStream_t)stream);
+}
+
+extern "C" int pipe_token_forward(const void* x_dev, int type, int64_t T, int in, int64_t row_stride, const int8_t* codes_dev,
+                                  const float* scales_dev, const float* bias_dev, int out, int act, void* scratch_dev, void* y_dev, void* stream) {
+  TokenProductArgs a{};
+  a.w = codes_dev; a.sw = scales_dev; a.bias = bias_dev;
+  a.n = T; a.top_k = 1; a.E = 1; a.out = out; a.act = act; a.y = y_dev;
+  return token_layer(x_dev, type, T, in, row_stride, scratch_dev, a, stream);
+}
+
+extern "C" int pipe_expert_forward(const void* x_dev, int type, int64_t T, int in, int64_t row_stride, const int8_t* codes_dev,
+                                   const float* scales_dev, const float* bias_dev, int E, int out, const int32_t* starts_dev,
+                                   const int32_t* order_dev, int64_t rows, int top_k, int act, void* scratch_dev, void* y_dev, void* stream) {
+  TokenProductArgs a{};
+  a.w = codes_dev; a.sw = scales_dev; a.bias = bias_dev;
+  a.starts = starts_dev; a.order = order_dev;
+  a.n = rows; a.top_k = top_k; a.E = E; a.out = out; a.act = act; a.y = y_dev;
+  if (rows > 0 && !starts_dev) return PIPE_EINVAL;
+  if (!order_dev && rows != T) return PIPE_ESHAPE;
+  return token_layer(x_dev, type, T, in, row_stride, scratch_dev, a, stream);
+}
+
+static bool router_ok(int T, int E, int top_k) {
+  return T >= 0 && E >= 1 && E <= PIPE_EXPERTS_MAX && top_k >= 1 && top_k <= PIPE_TOP_K_MAX && (int64_t)T * top_k < 1 << 30;
+}
+
+extern "C" int pipe_expert_sort(const int32_t* experts_dev, int T, int top_k, int E, int32_t* starts_dev, int32_t* order_dev,
+                                int32_t* places_dev, void* stream) {
+  if (!router_ok(T, E, top_k)) return PIPE_ESHAPE;
+  if (!starts_dev || (T > 0 && (!experts_dev || !order_dev || !places_dev))) return PIPE_EINVAL;
+  return launch_expert_sort(experts_dev, T * top_k, E, starts_dev, order_dev, places_dev, (hipStream_t)stream);
+}
+
+extern "C" int pipe_expert_route(const void* logits_dev, int type, int T, int E, int64_t row_stride, int top_k, int renormalize,
+                                 int32_t* experts_dev, float* weights_dev, int32_t* starts_dev, int32_t* order_dev, int32_t* places_dev,
+                                 void* stream) {
+  if (!known_type(type) || (renormalize != 0 && renormalize != 1)) return PIPE_EINVAL;
+  if (!router_ok(T, E, top_k) || top_k > E || row_stride < 0) return PIPE_ESHAPE;
+  if (!starts_dev || (T > 0 && (!logits_dev || !experts_dev || !weights_dev || !order_dev || !places_dev))) return PIPE_EINVAL;
+  if (T > 0) {
+    ExpertRouteArgs a{};
+    a.logits = logits_dev; a.type = type; a.T = T; a.E = E; a.top_k = top_k; a.renormalize = renormalize; a.row_stride = row_stride;
+    a.experts = experts_dev; a.weights = weights_dev;
+    const int rc = launch_expert_route(a, (hipStream_t)stream);
+    if (rc) return rc;
+  }
+  return launch_expert_sort(experts_dev, T * top_k, E, starts_dev, order_dev, places_dev, (hipStream_t)stream);
+}
+
+extern "C" int pipe_expert_combine(const void* y_dev, int type, int64_t rows, int out, int64_t row_stride, const int32_t* places_dev,
+                                   const float* weights_dev, int T, int top_k, void* out_dev, void* stream) {
+  if (!known_type(type)) return PIPE_EINVAL;
+  if (!router_ok(T, 1, top_k) || !rows_fit(rows) || out < 1 || out > 1 << 28 || row_stride < 0 || (int64_t)T * ((out + 7) / 8) >= (int64_t)1 << 38)
+    return PIPE_ESHAPE;
+  if (T == 0) return PIPE_OK;
+  if (!places_dev || !weights_dev || !out_dev || (rows > 0 && !y_dev)) return PIPE_EINVAL;
+  return launch_expert_combine(y_dev, type, rows, out, row_stride, places_dev, weights_dev, T, top_k, out_dev, (hipStream_t)stream);
 }
