@@ -99,6 +99,7 @@ def _load():
     lib.pipe_cache_attention.argtypes = [vp, ci, ci, ci, ci, ci, i64, i64, vp, vp, ci, vp, ci, ci, vp, ci, cf, ci, vp, vp]
     lib.pipe_prepare_cache_attention.argtypes = [ci, ci, ci, ci, ci, ci, vp]
     lib.pipe_prompt_attention.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, i64, i64, i64, i64, i64, i64, vp, vp, ci, ci, cf, vp, vp]
+    lib.pipe_set_token_kernel.argtypes = [ci]
     lib.pipe_token_pitch.argtypes = [ci]
     lib.pipe_token_scratch.argtypes = [i64, ci]
     lib.pipe_token_scratch.restype = i64
@@ -972,6 +973,10 @@ def pipe_token_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
     _check(_lib.pipe_token_forward(xp, _type(x.dtype), T, n, stride, cp, sp, bp, width, act, scratch.data_ptr(), y.data_ptr(), _stream()),
            "pipe_token_forward")
     return y
+
+
+def pipe_set_token_kernel(which: int) -> None:
+    _check(_lib.pipe_set_token_kernel(int(which)), "pipe_set_token_kernel")
 
 
 def pipe_expert_route(logits: torch.Tensor, top_k: int, renormalize: bool = True):

@@ -2558,6 +2558,12 @@ extern "C" int pipe_expert_forward(const void* x_dev, int type, int64_t T, int i
   return token_layer(x_dev, type, T, in, row_stride, scratch_dev, a, stream);
 }
 
+extern "C" int pipe_set_token_kernel(int which) {
+  if (which < 0 || which > 4) return PIPE_EINVAL;
+  g_token_kernel = which;
+  return PIPE_OK;
+}
+
 static bool router_ok(int T, int E, int top_k) {
   return T >= 0 && E >= 1 && E <= PIPE_EXPERTS_MAX && top_k >= 1 && top_k <= PIPE_TOP_K_MAX && (int64_t)T * top_k < 1 << 30;
 }

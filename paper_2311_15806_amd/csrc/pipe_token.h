@@ -22,6 +22,7 @@ struct TokenProductArgs {
   void* y;                 // [n][out]
 };
 int launch_token_product(const TokenProductArgs& a, hipStream_t st);
+extern int g_token_kernel;   // 0: by the sizes; 1 to 4: see pipe_set_token_kernel
 
 struct ExpertRouteArgs {
   const void* logits;

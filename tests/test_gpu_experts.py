@@ -17,6 +17,14 @@ def pipe():
     return b
 
 
+@pytest.fixture(params=[0, 1, 2, 3, 4], ids=["automatic", "streamed", "tiles64", "tiles128", "tiles256"])
+def kernel(pipe, request):
+    """The layers' kernels, each on everything."""
+    pipe.pipe_set_token_kernel(request.param)
+    yield request.param
+    pipe.pipe_set_token_kernel(0)
+
+
 def ints(v):
     return torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
 
@@ -131,7 +139,7 @@ LINEAR = [
 
 
 @pytest.mark.parametrize("case", LINEAR, ids=["-".join(str(v) for v in c) for c in LINEAR])
-def test_forward(pipe, case):
+def test_forward(pipe, kernel, case):
     T, n, out, act, bias, kind = case
     rng = np.random.default_rng(T * 1000 + n + out)
     rows = out * (2 if act == "gated" else 1)
@@ -148,9 +156,22 @@ def test_forward_of_no_tokens(pipe):
     assert y.shape == (0, 8)
 
 
+def test_every_kernel_gives_the_same_bits(pipe):
+    rng = np.random.default_rng(6)
+    x, _ = typed(rng, (200, 777), "f32")
+    cw, sw, _, _ = weights(rng, (3,), 300, 777)
+    b = torch.from_numpy(rng.standard_normal((3, 300)).astype(np.float32)).cuda()
+    for act in ref.ACTS.values():
+        got = []
+        for which in (1, 2, 3, 4, 0):
+            pipe.pipe_set_token_kernel(which)
+            got.append(pipe.pipe_expert_forward(x, cw, sw, ints([0, 30, 170, 198]), bias=b, act=act))
+        assert all(torch.equal(g, got[0]) for g in got[1:]), act
+
+
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ["none", "gated"])
-def test_a_token_alone_is_the_token_in_its_batch(pipe, kind, act):
+def test_a_token_alone_is_the_token_in_its_batch(pipe, kernel, kind, act):
     """Whatever kernel a batch's size takes, a token's output is the same bits."""
     rng = np.random.default_rng(5)
     x, _ = typed(rng, (700, 1000), kind)
@@ -161,7 +182,7 @@ def test_a_token_alone_is_the_token_in_its_batch(pipe, kind, act):
 
 
 @pytest.mark.parametrize("T", [1, 20, 300])
-def test_longest_rows(pipe, T):
+def test_longest_rows(pipe, kernel, T):
     """Sums next to 2^31."""
     n, rng = 130944, np.random.default_rng(0)
     x = torch.ones(T, n, device="cuda")
@@ -177,7 +198,7 @@ def test_longest_rows(pipe, T):
 
 
 @pytest.mark.parametrize("T", [3, 40, 400])
-def test_scales_of_any_size(pipe, T):
+def test_scales_of_any_size(pipe, kernel, T):
     """The product of a sum with one of the scales may leave fp32's range where the whole does not."""
     rng = np.random.default_rng(T)
     n, out = 500, 72
@@ -196,7 +217,7 @@ def test_scales_of_any_size(pipe, T):
 
 @pytest.mark.parametrize("act", ["none", "gelu", "gated", "relu"])
 @pytest.mark.parametrize("T", [6, 50, 300])
-def test_tokens_with_nan_or_infinity(pipe, T, act):
+def test_tokens_with_nan_or_infinity(pipe, kernel, T, act):
     rng = np.random.default_rng(7)
     x, v = typed(rng, (T, 333), "f32")
     x[1, 5], x[4, 332], x[T - 1, 0] = float("nan"), float("inf"), -float("inf")
@@ -304,7 +325,7 @@ EXPERTS = [
 
 
 @pytest.mark.parametrize("case", EXPERTS, ids=["-".join(str(v) for v in c) for c in EXPERTS])
-def test_experts(pipe, case):
+def test_experts(pipe, kernel, case):
     T, k, E, absent, n, out, act, bias, gather, kind = case
     rng = np.random.default_rng(T * 100 + E)
     skew = rng.standard_normal(E + absent)
@@ -321,7 +342,7 @@ def test_experts(pipe, case):
 
 
 @pytest.mark.parametrize("T", [4, 300])
-def test_experts_of_uneven_rows(pipe, T):
+def test_experts_of_uneven_rows(pipe, kernel, T):
     """All rows to one expert, the first, the last; none at all; an expert's row count next to a tile's."""
     rng = np.random.default_rng(T)
     E, n, out = 5, 200, 90
@@ -337,7 +358,7 @@ def test_experts_of_uneven_rows(pipe, T):
 
 
 @pytest.mark.parametrize("n_rows", [24, 600])
-def test_experts_of_orders_outside(pipe, n_rows):
+def test_experts_of_orders_outside(pipe, kernel, n_rows):
     """Rows whose order names no pair are zeros, also with a bias; the same pair twice is served twice."""
     rng = np.random.default_rng(3)
     T, k, E, n, out = 10, 2, 3, 150, 40
@@ -356,7 +377,7 @@ def test_experts_of_orders_outside(pipe, n_rows):
 
 
 @pytest.mark.parametrize("T", [4, 40, 300])
-def test_experts_of_starts_that_do_not_ascend(pipe, T):
+def test_experts_of_starts_that_do_not_ascend(pipe, kernel, T):
     """Any table ends the call in bounds: nothing outside y is written, and no expert's rows are another's by more than the table says."""
     rng = np.random.default_rng(4)
     x, _ = typed(rng, (T, 128), "f32")
@@ -367,7 +388,7 @@ def test_experts_of_starts_that_do_not_ascend(pipe, T):
         assert bool((guard[:16] == 7).all()) and bool((guard[16 + T:] == 7).all()), starts
 
 
-def test_experts_beyond_4_gib(pipe):
+def test_experts_beyond_4_gib(pipe, kernel):
     """Weights past 32-bit offsets: the last expert's rows are read where they lie."""
     E, out, n = 3, 180000, 8192                       # 4.4e9 bytes
     codes = torch.zeros(E, out, n, dtype=torch.int8, device="cuda")
@@ -533,7 +554,8 @@ def test_refusals(pipe):
         with pytest.raises(ValueError):
             call()
     for call in (lambda: pipe.pipe_token_forward(x, codes, scales, act=7), lambda: pipe.pipe_expert_route(x[:, :3], 4), lambda: pipe.pipe_expert_sort(e, 0),
-                 lambda: pipe.pipe_expert_sort(e, 1025), lambda: pipe.pipe_expert_forward(x, codes[None], scales[None], starts, order=e.flatten(), top_k=0),
+                 lambda: pipe.pipe_expert_sort(e, 1025), lambda: pipe.pipe_set_token_kernel(5), lambda: pipe.pipe_set_token_kernel(-1),
+                 lambda: pipe.pipe_expert_forward(x, codes[None], scales[None], starts, order=e.flatten(), top_k=0),
                  lambda: pipe.pipe_expert_forward(x, codes[None], scales[None], starts, order=e.flatten(), top_k=33)):
         with pytest.raises(pipe.PipeError):
             call()
