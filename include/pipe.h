@@ -689,7 +689,7 @@ int pipe_token_quantize(const void* x_dev, int type, int64_t rows, int in, int64
 int pipe_token_forward(const void* x_dev, int type, int64_t T, int in, int64_t row_stride, const int8_t* codes_dev,
                        const float* scales_dev, const float* bias_dev, int out, int act, void* scratch_dev, void* y_dev, void* stream);
 
-/* Kernel of pipe_token_forward and pipe_expert_forward (tuning and tests): 0 = by the sizes (default), 1 = weights streamed past up to 64 tokens at a
+/* Kernel of pipe_token_forward and pipe_expert_forward (tuning and tests): 0 = by the sizes (default), 1 = weights streamed past up to 32 tokens at a
  * time, 2, 3, 4 = tiles of 64, 128, 256 tokens.  (Gathered inputs of more than 4 GiB of codes are always streamed past.)  Results do not depend on the
  * setting.  Returns PIPE_EINVAL for other values.                                                                   */
 int pipe_set_token_kernel(int which);

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void token_quantize_kernel(const T* __restrict
 template <typename T, bool WIDE>
 int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitch, int8_t* codes, float* scales, hipStream_t st) {
   const T* p = (const T*)x;
-  if (pitch <= 2048)
+  if (pitch <= 2048 && rows > 512)
     PIPE_KLAUNCH((token_quantize_kernel<T, 64, 4, WIDE>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p, rows, in, stride, pitch, codes, scales);
   else
     PIPE_KLAUNCH((token_quantize_kernel<T, 256, 4, WIDE>), dim3((unsigned)rows), dim3(256), 0, st, p, rows, in, stride, pitch, codes, scales);

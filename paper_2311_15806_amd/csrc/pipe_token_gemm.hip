@@ -4,6 +4,8 @@
 // Sums are exact in 32 bits.  Both scales' exponents are kept apart from their mantissas until the end, so that no product of a sum and one of
 // the scales leaves fp32's range where the whole does not.  Every kernel here computes an output by the same operations: which one serves a call
 // changes no bit.
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "pipe_attention.h"
@@ -15,40 +17,75 @@ int g_token_kernel = 0;
 namespace {
 
 // ------------------------------------------------------------------ what the kernels share
-// A tile's rows of y: those of expert e from `row` on, n of them; e == E: rows without an expert.
+// A tile's rows of y: those of expert e from `row` on, n of them.
 struct Rows {
   int e, n;
   int64_t row;
 };
-// Tile `id`: expert e owns the ids from floor(starts[e] / BT) + e on, which are at least as many as its tiles; called by whole waves.
+// sums over a wave's lanes up to and with each, by moves within the vector unit
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int wave_sums(int v) {
+  v = dpp_add<0x111, 0xf>(v);   // row_shr 1, 2, 4, 8
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);   // row_bcast 15, 31
+  return dpp_add<0x143, 0xc>(v);
+}
+// How many tiles of BT rows the experts have, one expert's after the other's.  Called by whole waves, a lane an expert; so is what follows.
+template <int BT>
+struct Experts {
+  int start, end, tiles, upto;      // of the lane's expert: its rows, its tiles, all up to with them
+  __device__ __forceinline__ Experts(const TokenProductArgs& a, int e0, int before) {
+    const int e = e0 + (threadIdx.x & 63), n = (int)a.n;
+    start = e > 0 ? min(max(a.starts[min(e, a.E)], 0), n) : 0;
+    end = min(max(a.starts[min(e + 1, a.E)], 0), n);
+    tiles = e < a.E && end > start ? (end - start + BT - 1) / BT : 0;
+    upto = before + wave_sums(tiles);
+  }
+};
+template <int BT>
+__device__ __forceinline__ int live_tiles(const TokenProductArgs& a) {
+  if (a.starts == nullptr) return (int)((a.n + BT - 1) / BT);
+  int before = 0;
+  for (int e0 = 0; e0 < a.E; e0 += 64) before = __builtin_amdgcn_readlane(Experts<BT>(a, e0, before).upto, 63);
+  return before;
+}
+// Tile `id` of them; no rows: there is none.
 template <int BT>
 __device__ __forceinline__ Rows find_rows(const TokenProductArgs& a, int id) {
   if (a.starts == nullptr) return Rows{0, (int)min((int64_t)BT, a.n - (int64_t)id * BT), (int64_t)id * BT};
-  const int lane = threadIdx.x & 63, n = (int)a.n;
-  auto start_of = [&](int e) { return e <= 0 ? 0 : min(max(a.starts[min(e, a.E)], 0), n); };
-  int e = -1, start, end;
-  if (a.E < 63) {      // a lane an expert: nothing is looked up twice
-    const int s = start_of(lane);
-    e = __popcll(__ballot(lane <= a.E && s / BT + lane <= id)) - 1;
-    start = __builtin_amdgcn_readlane(s, e);
-    end = e < a.E ? __builtin_amdgcn_readlane(s, e + 1) : n;
-  } else {
-    for (int i0 = 0; i0 <= a.E; i0 += 64) {
-      const int i = i0 + lane;
-      const int found = __popcll(__ballot(i <= a.E && start_of(i) / BT + i <= id));
-      e += found;
-      if (found < 64) break;
+  int before = 0;
+  for (int e0 = 0; e0 < a.E; e0 += 64) {
+    const Experts<BT> x(a, e0, before);
+    const int at = __popcll(__ballot(x.upto <= id));
+    if (at < 64) {
+      const int s = __builtin_amdgcn_readlane(x.start, at) + (id - __builtin_amdgcn_readlane(x.upto - x.tiles, at)) * BT;
+      return Rows{e0 + at, min(BT, __builtin_amdgcn_readlane(x.end, at) - s), s};
     }
-    e = __builtin_amdgcn_readfirstlane(e);
-    start = __builtin_amdgcn_readfirstlane(start_of(e));
-    end = e < a.E ? __builtin_amdgcn_readfirstlane(start_of(e + 1)) : n;
+    before = __builtin_amdgcn_readlane(x.upto, 63);
   }
-  const int skip = (id - start / BT - e) * BT;
-  return Rows{e, skip < 0 ? 0 : min(BT, end - start - skip), (int64_t)start + skip};
+  return Rows{0, 0, 0};
 }
+// (never more tiles than this)
 template <int BT>
 int64_t row_tiles(const TokenProductArgs& a) {
-  return a.starts == nullptr ? (a.n + BT - 1) / BT : a.n / BT + a.E + 1;
+  return a.starts == nullptr ? (a.n + BT - 1) / BT : a.n / BT + std::min<int64_t>(a.E, a.n);
+}
+// The rows of y behind the last expert's, zeros: a share for every workgroup of the launch.
+template <int NT>
+__device__ __forceinline__ void zero_rest(const TokenProductArgs& a) {
+  if (a.starts == nullptr) return;
+  const int64_t size = a.type == PIPE_F32 ? 4 : 2, first = (int64_t)min(max(a.starts[a.E], 0), (int)a.n) * a.out * size, end = a.n * a.out * size;
+  const int64_t lo = (first + 15) / 16, hi = end / 16;      // whole pieces; what lies before and behind them is the first workgroup's
+  char* y = (char*)a.y;
+  for (int64_t i = lo + (int64_t)blockIdx.x * NT + threadIdx.x; i < hi; i += (int64_t)gridDim.x * NT) reinterpret_cast<uint4*>(y)[i] = make_uint4(0, 0, 0, 0);
+  if (blockIdx.x == 0 && threadIdx.x < 16) {
+    const int64_t before = first + threadIdx.x * 2, behind = max(hi * 16, first) + threadIdx.x * 2;
+    if (before < min(lo * 16, end)) *reinterpret_cast<uint16_t*>(y + before) = 0;
+    if (behind < end) *reinterpret_cast<uint16_t*>(y + behind) = 0;
+  }
 }
 // the input behind row i of a tile, -1: none
 __device__ __forceinline__ int64_t input_of(const TokenProductArgs& a, const Rows& r, int i) {
@@ -114,16 +151,6 @@ __device__ __forceinline__ void put4(void* y, int type, int64_t at, const float*
   else if (type == PIPE_F16) put4_typed((f16*)y + at, z, have, wide);
   else put4_typed((bf16*)y + at, z, have, wide);
 }
-// zeros of the columns from o0 on, WIDTH of them, of a tile of rows without an expert
-template <int WIDTH, int NT>
-__device__ __forceinline__ void put_zeros(const TokenProductArgs& a, const Rows& r, int o0) {
-  const float zero = 0.f;
-  for (int i = threadIdx.x; i < r.n * WIDTH; i += NT) {
-    const int t = i / WIDTH, o = o0 + i % WIDTH;
-    if (o < a.out) put4(a.y, a.type, (r.row + t) * a.out + o, &zero, 1, false);
-  }
-}
-
 // Scales and bias of a tile's BO rows of weights, scales of its BT tokens (negative: no input), by all NT threads.
 template <int BO, int BT>
 struct Side {
@@ -193,199 +220,231 @@ __device__ __forceinline__ void finish(const TokenProductArgs& a, const Rows& r,
   }
 }
 
+// an address that is the same in every lane, in scalar registers
+__device__ __forceinline__ const int8_t* uniform(const int8_t* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return reinterpret_cast<const int8_t*>((uint64_t)hi << 32 | lo);
+}
 // Where a wave's loads of 8 rows x 128 codes come from: row `first` + 8 p + (lane >> 3) of the tile's B rows of weights (first < B) or of its tokens.
 // Addresses are a resource's base and 32 bits; of a gated layer 16 rows of the gate and of the other half in turn.
 template <bool GATED, int B, int P>
 struct Source {
-  __amdgpu_buffer_rsrc_t from0, from1;
+  const int8_t *b0, *b1;
   unsigned off[P];
   __device__ __forceinline__ Source(const TokenProductArgs& a, const Rows& r, int o0, int first) {
     const int lane = threadIdx.x & 63;
     const bool weights = first < B;
-    const int8_t *b0, *b1;
     if (weights) {
       b0 = a.w + ((int64_t)r.e * w_rows_of(a, GATED) + o0) * a.pitch;
       b1 = GATED ? b0 + (int64_t)a.out * a.pitch : b0;
     } else {
       b0 = b1 = a.qx + (a.order ? 0 : r.row) * a.pitch;
     }
-    from0 = __builtin_amdgcn_make_buffer_rsrc((void*)b0, 0, 0xffffffffu, 0x00020000);
-    from1 = __builtin_amdgcn_make_buffer_rsrc((void*)b1, 0, 0xffffffffu, 0x00020000);
+    b0 = uniform(b0);
+    b1 = uniform(b1);
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       const int row = first + p * 8 + (lane >> 3);
       int64_t at;
       if (weights) at = min(o0 + (GATED ? (row >> 5) * 16 + (row & 15) : row), a.out - 1) - o0;
       else at = max(input_of(a, r, row - B), (int64_t)0) - (a.order ? 0 : r.row);
-      off[p] = (unsigned)(at * a.pitch);
+      off[p] = (unsigned)(at * a.pitch) + (lane & 7) * 16;
     }
   }
-  __device__ __forceinline__ const __amdgpu_buffer_rsrc_t& from(int p) const { return ((p >> 1) & 1) ? from1 : from0; }
+  // load p of the codes from k on; zeros, without an access, where there are none
+  __device__ __forceinline__ v4i load(int p, int k, int pitch) const {
+    const __amdgpu_buffer_rsrc_t from =
+        __builtin_amdgcn_make_buffer_rsrc((void*)uniform(((p >> 1) & 1) ? b1 : b0), 0, __builtin_amdgcn_readfirstlane(k < pitch ? 0xffffffffu : 0u), 0x00020000);
+    return (v4i)__builtin_amdgcn_raw_buffer_load_b128(from, off[p], k, 0);
+  }
 };
-// 16 bytes a lane from base + off + k to dst + 16 * lane
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t base, v4i* dst, unsigned off, int k) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(base, (__attribute__((address_space(3))) void*)dst, 16, off, k, 0, 0);
-}
 // whether 32 bits reach every input
 static bool near(const TokenProductArgs& a) { return a.order == nullptr || a.n_x * a.pitch < (int64_t)0xffffffff; }
 
-// Blocks b, b + 8, ... of a launch run on one XCD (one L2): neighbours there are HIGH tiles of tokens x some of weights.
-template <int HIGH>
-struct Order {
-  int o_tiles, t_tiles, per_xcd;
-  __device__ __forceinline__ bool tile(int block, int* ot, int* id) const {
-    const int at = block >> 3;
-    const int64_t place = (int64_t)(block & 7) * per_xcd + at;
-    if (at >= per_xcd || place >= (int64_t)o_tiles * t_tiles) return false;
-    const int band = (int)(place / (HIGH * (int64_t)o_tiles)), in_band = (int)(place - band * (HIGH * (int64_t)o_tiles));
-    const int high = min(HIGH, t_tiles - band * HIGH);
-    *ot = in_band / high;
-    *id = band * HIGH + in_band - *ot * high;
-    return true;
-  }
-};
+// Which tile a workgroup takes, of o_tiles x t_tiles.  Blocks b, b + 8, ... of a launch run on one XCD (one L2), which takes an eighth of all tiles: 8 tiles of
+// tokens x some of weights next to each other.  (Chunks of 8 x 4 tiles dealt to the XCDs in turn: 4096 tokens of 4096-11008 227 us for 217, eight
+// gated experts 905 for 870.)
+__device__ __forceinline__ bool place_of(int o_tiles, int t_tiles, int* ot, int* id) {
+  const int all = o_tiles * t_tiles, per_xcd = (all + 7) / 8, at = blockIdx.x >> 3, place = (blockIdx.x & 7) * per_xcd + at;
+  if (at >= per_xcd || place >= all) return false;
+  const int band = place / (8 * o_tiles), in_band = place - band * 8 * o_tiles, high = min(8, t_tiles - band * 8);
+  *ot = in_band / high;
+  *id = band * 8 + in_band - *ot * high;
+  return true;
+}
 
 // ------------------------------------------------------------------ few tokens
-// Bound by the bytes of the weights.  16 rows (of the gate and of the other half as well) x 16 TB tokens a workgroup of eight waves, which take the
-// steps of 64 codes in turn, straight from memory to operands; their sums meet in LDS.
-template <bool GATED, int TB>
-__global__ __launch_bounds__(512) void token_stream_kernel(const TokenProductArgs a, int o_tiles) {
-  constexpr int NW = 8, G = GATED ? 2 : 1, U = 4;
-  __shared__ v4i part[NW][G * TB][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int id = blockIdx.x / o_tiles, o0 = (blockIdx.x - id * o_tiles) * 16;
-  const Rows r = find_rows<16 * TB>(a, id);
-  if (r.n <= 0) return;
-  if (r.e == a.E) {
-    put_zeros<16, 512>(a, r, o0);
-    return;
-  }
+// Bound by the bytes of the weights, which go straight from memory to operands.  A tile is 16 rows of weights (of the gate and of the other half as well) x
+// 16 TB tokens; S of a workgroup's eight waves take its steps of 64 codes in turn and join their sums in LDS.
+template <bool GATED, int TB, int S>
+__global__ __launch_bounds__(512, 4) void token_stream_kernel(const TokenProductArgs a, int o_tiles, int tiles) {
+  constexpr int G = GATED ? 2 : 1;
+  constexpr int U = TB + G <= 2 ? 4 : TB + G == 3 ? 3 : 2;      // steps of a set of registers: two workgroups a unit
+  __shared__ v4i part[S > 1 ? 8 : 1][G * TB][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave % S;
+  const int tile = blockIdx.x * (8 / S) + wave / S;
+  const int id = tile / o_tiles, o0 = (tile - id * o_tiles) * 16;
+  Rows r{0, 0, 0};
+  if (tile < tiles) r = find_rows<16 * TB>(a, id);
+  zero_rest<512>(a);
+  const bool live = r.n > 0;
+  if (S == 1 && !live) return;
   const int n16 = lane & 15, k16 = lane >> 4;
-  const int64_t w0 = (int64_t)r.e * w_rows_of(a, GATED);
-  // weights through a resource of the 16 rows, behind whose end a step beyond the last reads zeros; tokens at 64 bits
-  __amdgpu_buffer_rsrc_t from[G];
-#pragma unroll
-  for (int h = 0; h < G; ++h)
-    from[h] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + (w0 + h * a.out + o0) * a.pitch), 0, (unsigned)(min(16, a.out - o0) * a.pitch), 0x00020000);
-  const unsigned w_at = (unsigned)(min(n16, a.out - 1 - o0) * a.pitch + k16 * 16);
-  const int8_t* xp[TB];
-#pragma unroll
-  for (int b = 0; b < TB; ++b) xp[b] = a.qx + max(input_of(a, r, 16 * b + n16), (int64_t)0) * a.pitch + k16 * 16;
   v4i acc[G][TB] = {};
-  const int steps = a.pitch / 64;
-  struct Set {
-    v4i w[U][G], x[U][TB];
-  } s0, s1;
-  auto ask = [&](Set& q, int s) __attribute__((always_inline)) {
+  // what the end takes is requested first: scales and biases of the lane's four channels, and of its token the wave's of the blocks it finishes
+  Channels ch[G];
+  float sx = 0.f;
+  bool none = true;
+  const int b_own = S > 1 ? min(sub, TB - 1) : 0;
+  if (live) {
+    const int64_t w0 = (int64_t)r.e * w_rows_of(a, GATED);
+    // weights through a resource of the 16 rows, behind whose end a step beyond the last reads zeros; tokens at 64 bits
+    __amdgpu_buffer_rsrc_t from[G];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = s + u * NW;
+    for (int h = 0; h < G; ++h)
+      from[h] = __builtin_amdgcn_make_buffer_rsrc((void*)uniform(a.w + (w0 + h * a.out + o0) * a.pitch), 0, (unsigned)(min(16, a.out - o0) * a.pitch), 0x00020000);
+    const unsigned w_at = (unsigned)(min(n16, a.out - 1 - o0) * a.pitch + k16 * 16);
+    const int steps = a.pitch / 64;
+    struct Set {
+      v4i w[U][G], x[U][TB];
+    } s0, s1;
+    auto ask_w = [&](Set& q, int s) __attribute__((always_inline)) {
 #pragma unroll
-      for (int h = 0; h < G; ++h) q.w[u][h] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(from[h], w_at + (k < steps ? k * 64u : 0x80000000u), 0, 0);
+      for (int u = 0; u < U; ++u) {
+        const int k = s + u * S;
 #pragma unroll
-      for (int b = 0; b < TB; ++b) q.x[u][b] = (v4i)gload16(xp[b] + min(k, steps - 1) * 64);
+        for (int h = 0; h < G; ++h) q.w[u][h] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(from[h], w_at + (k < steps ? k * 64u : 0x80000000u), 0, 0);
+      }
+    };
+    const int8_t* xp[TB];
+    auto ask_x = [&](Set& q, int s) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int b = 0; b < TB; ++b) q.x[u][b] = (v4i)gload16(xp[b] + min(s + u * S, steps - 1) * 64);
+    };
+    auto mul = [&](const Set& q) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int h = 0; h < G; ++h)
+#pragma unroll
+          for (int b = 0; b < TB; ++b) acc[h][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.w[u][h], q.x[u][b], acc[h][b], 0, 0, 0);
+    };
+    int s = sub;
+    ask_w(s0, s);
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+      const int64_t in = input_of(a, r, 16 * b + n16);
+      xp[b] = a.qx + max(in, (int64_t)0) * a.pitch + k16 * 16;
+      if (TB == 1 || (S > 1 && b == b_own)) { none = in < 0; sx = a.sx[max(in, (int64_t)0)]; }
     }
-  };
-  auto mul = [&](const Set& q) __attribute__((always_inline)) {
+    ask_x(s0, s);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int h = 0; h < G; ++h)
 #pragma unroll
-      for (int h = 0; h < G; ++h)
-#pragma unroll
-        for (int b = 0; b < TB; ++b) acc[h][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q.w[u][h], q.x[u][b], acc[h][b], 0, 0, 0);
-  };
-  int s = wave;
-  ask(s0, s);
-  while (true) {
-    s += U * NW;
-    if (s >= steps) { mul(s0); break; }
-    ask(s1, s);
-    mul(s0);
-    s += U * NW;
-    if (s >= steps) { mul(s1); break; }
-    ask(s0, s);
-    mul(s1);
-  }
-#pragma unroll
-  for (int h = 0; h < G; ++h)
-#pragma unroll
-    for (int b = 0; b < TB; ++b) part[wave][h * TB + b][lane] = acc[h][b];
-  __syncthreads();
-  if (wave >= TB) return;
-  const int b = wave, t = 16 * b + n16;
-  v4i sum[G];
-#pragma unroll
-  for (int h = 0; h < G; ++h) {
-    sum[h] = part[0][h * TB + b][lane];
-#pragma unroll
-    for (int q = 1; q < NW; ++q) sum[h] += part[q][h * TB + b][lane];
-  }
-  if (t >= r.n) return;
-  const int64_t in = input_of(a, r, t);
-  const float sx = in < 0 ? 0.f : a.sx[in];
-  float z[2][4];
-#pragma unroll
-  for (int h = 0; h < G; ++h) {
-    Channels c;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t o = w0 + weight_of<GATED>(a, o0, 16 * h + 4 * k16 + i);
-      c.set(i, a.sw[o], a.bias ? a.bias[o] : 0.f);
+      for (int i = 0; i < 4; ++i) {
+        const int64_t o = w0 + weight_of<GATED>(a, o0, 16 * h + 4 * k16 + i);
+        ch[h].set(i, a.sw[o], a.bias ? a.bias[o] : 0.f);
+      }
+    while (true) {
+      s += U * S;
+      if (s >= steps) { mul(s0); break; }
+      ask_w(s1, s);
+      ask_x(s1, s);
+      mul(s0);
+      s += U * S;
+      if (s >= steps) { mul(s1); break; }
+      ask_w(s0, s);
+      ask_x(s0, s);
+      mul(s1);
     }
-    c.values(sum[h], sx, a.bias != nullptr, z[h]);
   }
-  if (GATED) {
+  auto end = [&](const v4i (&sum)[G], int t, float sx, bool none) __attribute__((always_inline)) {
+    if (t >= r.n) return;
+    float z[2][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) z[0][i] = silu(z[0][i]) * z[1][i];
+    for (int h = 0; h < G; ++h) ch[h].values(sum[h], sx, a.bias != nullptr, z[h]);
+    if (GATED) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[0][i] = silu(z[0][i]) * z[1][i];
+    } else {
+      act4(z[0], a.act);
+    }
+    if (none) z[0][0] = z[0][1] = z[0][2] = z[0][3] = 0.f;
+    const int o = o0 + 4 * k16;
+    put4(a.y, a.type, (r.row + t) * a.out + o, z[0], a.out - o, a.out % 4 == 0);
+  };
+  if constexpr (S == 1) {
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+      if (TB > 1) {
+        const int64_t in = input_of(a, r, 16 * b + n16);
+        none = in < 0;
+        sx = a.sx[max(in, (int64_t)0)];
+      }
+      v4i sum[G];
+#pragma unroll
+      for (int h = 0; h < G; ++h) sum[h] = acc[h][b];
+      end(sum, 16 * b + n16, sx, none);
+    }
   } else {
-    act4(z[0], a.act);
+    static_assert(S >= TB, "a block of tokens a wave");
+#pragma unroll
+    for (int h = 0; h < G; ++h)
+#pragma unroll
+      for (int b = 0; b < TB; ++b) part[wave][h * TB + b][lane] = acc[h][b];
+    __syncthreads();
+    if (!live || sub >= TB) return;
+    v4i sum[G];
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      sum[h] = part[wave - sub][h * TB + sub][lane];
+#pragma unroll
+      for (int q = 1; q < S; ++q) sum[h] += part[wave - sub + q][h * TB + sub][lane];
+    }
+    end(sum, 16 * sub + n16, sx, none);
   }
-  if (in < 0) z[0][0] = z[0][1] = z[0][2] = z[0][3] = 0.f;
-  const int o = o0 + 4 * k16;
-  put4(a.y, a.type, (r.row + t) * a.out + o, z[0], a.out - o, a.out % 4 == 0);
 }
 
 // ------------------------------------------------------------------ tiles
-// B rows of weights x B tokens a workgroup of four waves, a quarter each.  A stage is 128 codes of every row, straight to LDS, one stage ahead; the
-// eight pieces of 16 of a row lie in an order that differs by pairs of rows, so that the reads of 16 rows' same piece meet all banks.
-template <bool GATED, int B>
-__global__ __launch_bounds__(256, 2) void token_tile_kernel(const TokenProductArgs a, const Order<8> order) {
-  constexpr int KB = 128, P = B / 16, F = B / 32, WIDTH = GATED ? B / 2 : B;
-  __shared__ alignas(1024) v4i slot0[2 * B * KB / 16], slot1[2 * B * KB / 16];
-  static_assert(sizeof(slot0) + sizeof(slot1) <= 65536, "loads to LDS reach the first 64 KiB");
+// B rows of weights x B tokens a workgroup of four waves, a quarter each.  A stage is 128 codes of every row; the eight pieces of 16 of a row lie in
+// LDS in an order that differs by pairs of rows, so that the reads of 16 rows' same piece meet all banks.  One stage is in LDS ahead, D more are in
+// registers or on their way there.
+template <bool GATED, int B, int D>
+__global__ __launch_bounds__(256, B == 128 ? 2 : 4) void token_tile_kernel(const TokenProductArgs a, int o_tiles) {
+  constexpr int KB = 128, P = B / 16, F = B / 32, WIDTH = GATED ? B / 2 : B, SLOT = 2 * B * KB / 16;
+  __shared__ alignas(1024) v4i slots[2 * SLOT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int ot, id;
-  if (!order.tile(blockIdx.x, &ot, &id)) return;
+  zero_rest<256>(a);
+  if (!place_of(o_tiles, live_tiles<B>(a), &ot, &id)) return;
   const Rows r = find_rows<B>(a, id);
-  if (r.n <= 0) return;
   const int o0 = ot * WIDTH;
-  if (r.e == a.E) {
-    put_zeros<WIDTH, 256>(a, r, o0);
-    return;
-  }
-  Source<GATED, B, P> src(a, r, o0, wave * (B / 2));
-  // the lane's piece of row (lane >> 3) of an even load; of an odd one it is 4 further
+  const Source<GATED, B, P> src(a, r, o0, wave * (B / 2));
+  v4i st[D][P];
+  auto ask = [&](v4i (&q)[P], int k) __attribute__((always_inline)) {
 #pragma unroll
-  for (int p = 0; p < P; ++p) src.off[p] += (((lane & 7) ^ (lane >> 4)) ^ ((p & 1) * 4)) * 16;
-  int k = 0;
-  auto ask = [&](v4i* slot) __attribute__((always_inline)) {
+    for (int p = 0; p < P; ++p) q[p] = src.load(p, k, a.pitch);
+    __builtin_amdgcn_sched_barrier(0);      // in this order, which the waits count on
+  };
+  const int put_at = wave * (P * 64) + (lane >> 3) * 8, swz = lane >> 4;
+  auto put = [&](int slot, const v4i (&q)[P]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int p = 0; p < P; ++p)
-      load_to_lds(src.from(p), slot + (wave * P + p) * 64, src.off[p], k);
-    k += KB;
-    __builtin_amdgcn_sched_barrier(0);      // requested before the stage that is there is read
+    for (int p = 0; p < P; ++p) slots[slot + put_at + p * 64 + ((lane & 7) ^ (swz + (p & 1) * 4))] = q[p];
   };
   const int wo = (wave & 1) * (B / 2), wt = (wave >> 1) * (B / 2), n16 = lane & 15, k16 = lane >> 4;
   const int at_w = (wo + n16) * 8 + (k16 ^ (n16 >> 1)), at_x = (B + wt + n16) * 8 + (k16 ^ (n16 >> 1));
   v4i acc[F][F] = {};
-  auto mul = [&](const v4i* slot) __attribute__((always_inline)) {
+  auto mul = [&](int slot) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       v4i w[F], x[F];
 #pragma unroll
       for (int f = 0; f < F; ++f) {
-        w[f] = slot[(at_w ^ (4 * j)) + f * 128];
-        x[f] = slot[(at_x ^ (4 * j)) + f * 128];
+        w[f] = slots[slot + (at_w ^ (4 * j)) + f * 128];
+        x[f] = slots[slot + (at_x ^ (4 * j)) + f * 128];
       }
 #pragma unroll
       for (int f = 0; f < F; ++f)
@@ -393,57 +452,56 @@ __global__ __launch_bounds__(256, 2) void token_tile_kernel(const TokenProductAr
         for (int g = 0; g < F; ++g) acc[f][g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[f], x[g], acc[f][g], 0, 0, 0);
     }
   };
-  auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-  const int stages = a.pitch / KB;
-  ask(slot0);
-  for (int i = 0; i + 2 < stages; i += 2) {
-    meet();                       // slot 0 is there, slot 1 free
-    ask(slot1);
-    mul(slot0);
-    meet();
-    ask(slot0);
-    mul(slot1);
-  }
+  auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // set i holds stages i, i + D, ...; in its turn a stage finds its codes in LDS and moves the next one's there, whose registers take the stage D later
+#pragma unroll
+  for (int i = 0; i < D; ++i) ask(st[i], i * KB);
+  put(0, st[0]);
+  ask(st[0], D * KB);
   meet();
-  if (stages & 1) {
-    mul(slot0);
-  } else {
-    ask(slot1);
-    mul(slot0);
-    meet();
-    mul(slot1);
+  int now = 0, k = 0;
+  for (; k + (D - 1) * KB < a.pitch; k += D * KB) {      // (one way through: with an exit in the middle every wait would be for all loads)
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+      put(now ^ SLOT, st[(i + 1) % D]);
+      ask(st[(i + 1) % D], k + (i + 1 + D) * KB);
+      mul(now);
+      meet();
+      now ^= SLOT;
+    }
   }
-  __syncthreads();
-  auto& side = *reinterpret_cast<Side<B, B>*>(slot1);
+#pragma unroll
+  for (int i = 0; i + 1 < D; ++i)
+    if (k + i * KB < a.pitch) {
+      if (i + 2 < D) put(now ^ SLOT, st[(i + 1) % D]);
+      mul(now);
+      meet();
+      now ^= SLOT;
+    }
+  auto& side = *reinterpret_cast<Side<B, B>*>(slots + SLOT);
   side.template load<GATED, 256>(a, r, o0);
   __syncthreads();
-  static_assert(sizeof(slot0) >= 4 * 16 * 4 * F * sizeof(v4i) && sizeof(slot1) >= sizeof(side), "turn");
-  finish<GATED>(a, r, o0, wo, wt, acc, slot0 + wave * (16 * 4 * F), side);
+  static_assert(SLOT >= 4 * 16 * 4 * F && SLOT * sizeof(v4i) >= sizeof(side), "turn");
+  finish<GATED>(a, r, o0, wo, wt, acc, slots + wave * (16 * 4 * F), side);
 }
 
 // ------------------------------------------------------------------ large tiles
 // 256 rows of weights x 256 tokens a workgroup of eight waves, 128 x 64 a wave.
 template <bool GATED>
-__global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArgs a, const Order<8> order) {
+__global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArgs a, int o_tiles) {
   constexpr int N = 256, KB = 128, P = 8, WIDTH = GATED ? N / 2 : N;
   // rows of 128 codes: 256 of the weights, then 256 of the tokens; the eight pieces of 16 of a row in an order that differs by pairs of rows
   constexpr int SLOT = 2 * N * KB / 16;
   __shared__ alignas(1024) v4i slots[2 * SLOT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int ot, id;
-  if (!order.tile(blockIdx.x, &ot, &id)) return;
+  zero_rest<512>(a);
+  if (!place_of(o_tiles, live_tiles<N>(a), &ot, &id)) return;
   const Rows r = find_rows<N>(a, id);
-  if (r.n <= 0) return;
   const int o0 = ot * WIDTH;
-  if (r.e == a.E) {
-    put_zeros<WIDTH, 512>(a, r, o0);
-    return;
-  }
-  Source<GATED, N, P> src(a, r, o0, wave * 64);
-#pragma unroll
-  for (int p = 0; p < P; ++p) src.off[p] += (lane & 7) * 16;
+  const Source<GATED, N, P> src(a, r, o0, wave * 64);
   v4i st[P];
-  auto ask = [&](int p, int k) __attribute__((always_inline)) { st[p] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(src.from(p), src.off[p], k, 0); };
+  auto ask = [&](int p, int k) __attribute__((always_inline)) { st[p] = src.load(p, k, a.pitch); };
   // row wave * 64 + p * 8 + (lane >> 3) has its pieces in the order (row >> 1) & 7
   const int put_at = wave * 512 + (lane >> 3) * 8, swz = lane >> 4;
   auto put = [&](int slot, int p) __attribute__((always_inline)) { slots[slot + put_at + p * 64 + ((lane & 7) ^ (swz + (p & 1) * 4))] = st[p]; };
@@ -501,17 +559,17 @@ __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArg
 #pragma unroll
   for (int p = 0; p < P; ++p) put(0, p);
 #pragma unroll
-  for (int p = 0; p < P; ++p) ask(p, min(KB, last));
+  for (int p = 0; p < P; ++p) ask(p, KB);
   meet();
 #pragma unroll
   for (int i = 0; i < 3; ++i) w[i] = read_w(0, 0, i);
 #pragma unroll
   for (int g = 0; g < 4; ++g) x[g] = read_x(0, 0, g);
-  // (the last two stages request the last one's codes again: one loop, whose sums stay where they are)
+  // (what the last two stages request is none: one loop, whose sums stay where they are)
   int now = 0;
   if (wt < r.n) {
     for (int k = 0; k <= last; k += KB) {
-      half(now, std::integral_constant<int, 0>{}, now, now ^ SLOT, min(k + 2 * KB, last));
+      half(now, std::integral_constant<int, 0>{}, now, now ^ SLOT, k + 2 * KB);
       meet();
       half(now, std::integral_constant<int, 1>{}, now ^ SLOT, 0, 0);
       now ^= SLOT;
@@ -523,7 +581,7 @@ __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArg
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         put(now, p);
-        ask(p, min(k + 2 * KB, last));
+        ask(p, k + 2 * KB);
       }
       meet();
     }
@@ -538,30 +596,38 @@ __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArg
 // ------------------------------------------------------------------ launches
 enum { AUTOMATIC = 0, STREAM = 1, TILES_64 = 2, TILES_128 = 3, TILES_256 = 4 };
 
+template <int TB, int S>
+int launch_stream_split(const TokenProductArgs& a, bool gated, int o_tiles, int tiles, hipStream_t st) {
+  const dim3 grid((unsigned)((tiles + 8 / S - 1) / (8 / S)));
+  if (gated) PIPE_KLAUNCH((token_stream_kernel<true, TB, S>), grid, dim3(512), 0, st, a, o_tiles, tiles);
+  else PIPE_KLAUNCH((token_stream_kernel<false, TB, S>), grid, dim3(512), 0, st, a, o_tiles, tiles);
+  PIPE_HIP(hipGetLastError());
+  return PIPE_OK;
+}
 template <int TB>
 int launch_stream(const TokenProductArgs& a, bool gated, hipStream_t st) {
   const int o_tiles = (a.out + 15) / 16;
-  const int64_t grid = (int64_t)o_tiles * row_tiles<16 * TB>(a);
-  if (grid > 0x7fffffff) return PIPE_ESHAPE;
-  if (gated) PIPE_KLAUNCH((token_stream_kernel<true, TB>), dim3((unsigned)grid), dim3(512), 0, st, a, o_tiles);
-  else PIPE_KLAUNCH((token_stream_kernel<false, TB>), dim3((unsigned)grid), dim3(512), 0, st, a, o_tiles);
-  PIPE_HIP(hipGetLastError());
-  return PIPE_OK;
+  const int64_t tiles = (int64_t)o_tiles * row_tiles<16 * TB>(a);
+  if (tiles > 0x7fffffff - 8) return PIPE_ESHAPE;
+  // as many waves a tile as keep about four to eight a SIMD (32 tokens, six of 64 experts: one wave 80 us, four 100, eight 106; 16 tokens of
+  // 4096-11008, gated: eight 27, four 30, one 48)
+  if (tiles <= 1024) return launch_stream_split<TB, 8>(a, gated, o_tiles, (int)tiles, st);
+  if (tiles <= 2048) return launch_stream_split<TB, 4>(a, gated, o_tiles, (int)tiles, st);
+  return launch_stream_split<TB, 1>(a, gated, o_tiles, (int)tiles, st);
 }
 
 template <int B>
 int launch_tiles(const TokenProductArgs& a, bool gated, hipStream_t st) {
   const int width = gated ? B / 2 : B;
-  const int64_t o_tiles = (a.out + width - 1) / width, t_tiles = row_tiles<B>(a), per = (o_tiles * t_tiles + 7) / 8;
-  if (per * 8 > 0x7fffffff) return PIPE_ESHAPE;
-  const Order<8> order{(int)o_tiles, (int)t_tiles, (int)per};
-  const dim3 grid((unsigned)(8 * per));
+  const int64_t o_tiles = (a.out + width - 1) / width, t_tiles = row_tiles<B>(a);
+  if (o_tiles * t_tiles > 0x7ffffff0) return PIPE_ESHAPE;
+  const dim3 grid((unsigned)((o_tiles * t_tiles + 7) / 8 * 8));
   if constexpr (B == 256) {
-    if (gated) PIPE_KLAUNCH((token_big_kernel<true>), grid, dim3(512), 0, st, a, order);
-    else PIPE_KLAUNCH((token_big_kernel<false>), grid, dim3(512), 0, st, a, order);
+    if (gated) PIPE_KLAUNCH((token_big_kernel<true>), grid, dim3(512), 0, st, a, (int)o_tiles);
+    else PIPE_KLAUNCH((token_big_kernel<false>), grid, dim3(512), 0, st, a, (int)o_tiles);
   } else {
-    if (gated) PIPE_KLAUNCH((token_tile_kernel<true, B>), grid, dim3(256), 0, st, a, order);
-    else PIPE_KLAUNCH((token_tile_kernel<false, B>), grid, dim3(256), 0, st, a, order);
+    if (gated) PIPE_KLAUNCH((token_tile_kernel<true, B, B == 128 ? 2 : 3>), grid, dim3(256), 0, st, a, (int)o_tiles);
+    else PIPE_KLAUNCH((token_tile_kernel<false, B, B == 128 ? 2 : 3>), grid, dim3(256), 0, st, a, (int)o_tiles);
   }
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
@@ -571,20 +637,23 @@ int launch_tiles(const TokenProductArgs& a, bool gated, hipStream_t st) {
 
 int launch_token_product(const TokenProductArgs& a, hipStream_t st) {
   const bool gated = a.act == PIPE_ACT_SILU_GATED;
-  const int64_t w_rows = gated ? 2 * (int64_t)a.out : a.out;
   int which = g_token_kernel;
   const int64_t each = a.n / a.E;       // tokens of an expert, about
   if (which == AUTOMATIC) {
-    if (each <= 64) which = STREAM;
-    else if ((w_rows + 255) / 256 * row_tiles<256>(a) >= 256) which = TILES_256;
-    else if ((w_rows + 127) / 128 * row_tiles<128>(a) >= 256) which = TILES_128;
-    else which = TILES_64;
+    which = STREAM;
+    if (each > 32) {
+      // Microseconds a stage of 128 codes, from what each kernel takes with few tiles and with many (half a tile more for each expert).  Calls of
+      // 64, 128 and 256 tokens a tile: 512 tokens of 4096-4096 27, 37 and 60 us; 1000 42, 40 and 62; 2048 73, 57 and 68; 4096 of 4096-11008 -, 250 and
+      // 215; 512 tokens, six of 64 gated experts of 2048-1408 93, 100 and 114; 2048 201, 176 and 172.
+      const double w_rows = gated ? 2.0 * a.out : a.out, more = a.starts ? 0.5 * a.E : 0.0;
+      auto tiles = [&](int B) { return std::ceil(w_rows / B) * std::ceil((double)a.n / B + more); };
+      const double t64 = std::max(0.45, 0.00096 * tiles(64)), t128 = std::max(0.95, 0.00287 * tiles(128)), t256 = std::max(1.9, 0.0084 * tiles(256));
+      which = t64 <= t128 && t64 <= t256 ? TILES_64 : t128 <= t256 ? TILES_128 : TILES_256;
+    }
   }
   if (!near(a)) which = STREAM;
   if (which == TILES_256) return launch_tiles<256>(a, gated, st);
   if (which == TILES_128) return launch_tiles<128>(a, gated, st);
   if (which == TILES_64) return launch_tiles<64>(a, gated, st);
-  if (each <= 16) return launch_stream<1>(a, gated, st);
-  if (each <= 32) return launch_stream<2>(a, gated, st);
-  return launch_stream<4>(a, gated, st);
+  return each <= 16 ? launch_stream<1>(a, gated, st) : launch_stream<2>(a, gated, st);
 }
