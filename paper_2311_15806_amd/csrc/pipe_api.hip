@@ -2532,10 +2532,8 @@ static int token_layer(const void* x_dev, int type, int64_t rows, int in, int64_
   a.n_x = rows;
   int8_t* codes = (int8_t*)scratch_dev;
   float* scales = (float*)(codes + rows * a.pitch);
-  a.qx = codes;
-  a.sx = scales;
-  const int rc = launch_token_quantize(x_dev, type, rows, in, row_stride, a.pitch, codes, scales, (hipStream_t)stream);
-  return rc ? rc : launch_token_product(a, (hipStream_t)stream);
+  a.x = x_dev; a.x_stride = row_stride; a.in = in;
+  return launch_token_layer(a, codes, scales, (hipStream_t)stream);
 }
 
 extern "C" int pipe_token_forward(const void* x_dev, int type, int64_t T, int in, int64_t row_stride, const int8_t* codes_dev,

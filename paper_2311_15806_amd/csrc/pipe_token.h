@@ -10,7 +10,10 @@ int launch_token_quantize(const void* x, int type, int64_t rows, int in, int64_t
                           hipStream_t st);
 
 struct TokenProductArgs {
-  const int8_t* qx;        // codes [n_x][pitch] and scales [n_x] of the inputs
+  const void* x;           // inputs [n_x], `in` values each
+  int64_t x_stride;
+  int in, x_wide;          // x_wide: rows can be read 16 bytes at a time
+  const int8_t* qx;        // their codes [n_x][pitch] and scales [n_x], where a launch of their own made them
   const float* sx;
   const int8_t* w;         // [E][rows][pitch], rows = out, or 2 out of a gated layer (gate rows first)
   const float* sw;         // [E][rows]
@@ -21,7 +24,7 @@ struct TokenProductArgs {
   int top_k, E, pitch, out, act, type;
   void* y;                 // [n][out]
 };
-int launch_token_product(const TokenProductArgs& a, hipStream_t st);
+int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStream_t st);   // (codes, scales: room for the inputs')
 extern int g_token_kernel;   // 0: by the sizes; 1 to 4: see pipe_set_token_kernel
 
 struct ExpertRouteArgs {
@@ -35,3 +38,30 @@ int launch_expert_route(const ExpertRouteArgs& a, hipStream_t st);
 int launch_expert_sort(const int32_t* experts, int n, int E, int32_t* starts, int32_t* order, int32_t* places, hipStream_t st);
 int launch_expert_combine(const void* y, int type, int64_t n, int H, int64_t row_stride, const int32_t* places, const float* weights, int T,
                           int top_k, void* out, hipStream_t st);
+
+#if defined(__HIPCC__)
+#include "pipe_codes.h"
+// the larger of m and |x|; +infinity from a NaN or an infinity on
+__device__ __forceinline__ float raised(float m, float x) {
+  const float v = fabsf(x);
+  return v < INFINITY ? fmaxf(m, v) : INFINITY;
+}
+// The codes of a row whose largest magnitude is `top` (+infinity: it is not finite as a whole): s = top / 127, c = rint(x / s).
+struct RowScale {
+  float s;
+  bool bad;
+  Divisor d;
+  __device__ __forceinline__ explicit RowScale(float top) : s(normal(__fdiv_rn(top, 127.f))), bad(!(top < INFINITY)), d(s > 0.f && !bad ? s : 1.f) {}
+  static __device__ __forceinline__ float normal(float s) { return s < 0x1p-126f ? 0.f : s; }
+  __device__ __forceinline__ float scale() const { return bad ? __uint_as_float(0x7fc00000u) : s; }
+  __device__ __forceinline__ uint2 codes8(const float* x) const {
+    int q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float r = d.fast ? d.quotient<true>(x[i]) : d.quotient<false>(x[i]);
+      q[i] = s > 0.f && !bad ? (int)__builtin_amdgcn_fmed3f(rintf(r), -127.f, 127.f) : 0;
+    }
+    return make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+  }
+};
+#endif

@@ -31,10 +31,7 @@ __global__ __launch_bounds__(256) void token_quantize_kernel(const T* __restrict
   float top = 0.f;
   auto raise = [&](const float* a) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float m = fabsf(a[i]);
-      top = m < INFINITY ? fmaxf(top, m) : INFINITY;
-    }
+    for (int i = 0; i < 8; ++i) top = raised(top, a[i]);
   };
 #pragma unroll
   for (int j = 0; j < CH; ++j) raise(v[j]);
@@ -44,22 +41,11 @@ __global__ __launch_bounds__(256) void token_quantize_kernel(const T* __restrict
     raise(a);
   }
   top = NT == 64 ? wave_max(top) : block_max(top);
-  const bool bad = !(top < INFINITY);
-  float s = __fdiv_rn(top, 127.f);
-  if (s < 0x1p-126f) s = 0.f;
-  if (tid == 0) scales[row] = bad ? __uint_as_float(0x7fc00000u) : s;
-  const bool live = !bad && s > 0.f;
-  const Divisor d(live ? s : 1.f);
+  const RowScale scale(top);
+  if (tid == 0) scales[row] = scale.scale();
   uint2* dst = reinterpret_cast<uint2*>(codes + row * pitch);
   auto put = [&](int c, const float* a) __attribute__((always_inline)) {
-    if (c * 8 >= pitch) return;
-    int q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float r = d.fast ? d.quotient<true>(a[i]) : d.quotient<false>(a[i]);
-      q[i] = live ? (int)__builtin_amdgcn_fmed3f(rintf(r), -127.f, 127.f) : 0;
-    }
-    dst[c] = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+    if (c * 8 < pitch) dst[c] = scale.codes8(a);
   };
 #pragma unroll
   for (int j = 0; j < CH; ++j) put(tid + j * NT, v[j]);

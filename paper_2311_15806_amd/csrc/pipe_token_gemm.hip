@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "pipe_attention.h"
+#include "pipe_codes.h"
 #include "pipe_tile.h"
 #include "pipe_token.h"
 
@@ -275,6 +276,22 @@ __device__ __forceinline__ bool place_of(int o_tiles, int t_tiles, int* ot, int*
 }
 
 // ------------------------------------------------------------------ few tokens
+// the lane's four channels of token t of a tile
+template <bool GATED>
+__device__ __forceinline__ void outputs(const TokenProductArgs& a, const Rows& r, int o0, int t, const Channels* ch, const v4i* sum, float sx, bool none) {
+  float z[2][4];
+  ch[0].values(sum[0], sx, a.bias != nullptr, z[0]);
+  if (GATED) {
+    ch[GATED].values(sum[GATED], sx, a.bias != nullptr, z[1]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[0][i] = silu(z[0][i]) * z[1][i];
+  } else {
+    act4(z[0], a.act);
+  }
+  if (none) z[0][0] = z[0][1] = z[0][2] = z[0][3] = 0.f;
+  const int o = o0 + 4 * ((threadIdx.x & 63) >> 4);
+  put4(a.y, a.type, (r.row + t) * a.out + o, z[0], a.out - o, a.out % 4 == 0);
+}
 // Bound by the bytes of the weights, which go straight from memory to operands.  A tile is 16 rows of weights (of the gate and of the other half as well) x
 // 16 TB tokens; S of a workgroup's eight waves take its steps of 64 codes in turn and join their sums in LDS.
 template <bool GATED, int TB, int S>
@@ -361,21 +378,6 @@ __global__ __launch_bounds__(512, 4) void token_stream_kernel(const TokenProduct
       mul(s1);
     }
   }
-  auto end = [&](const v4i (&sum)[G], int t, float sx, bool none) __attribute__((always_inline)) {
-    if (t >= r.n) return;
-    float z[2][4];
-#pragma unroll
-    for (int h = 0; h < G; ++h) ch[h].values(sum[h], sx, a.bias != nullptr, z[h]);
-    if (GATED) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z[0][i] = silu(z[0][i]) * z[1][i];
-    } else {
-      act4(z[0], a.act);
-    }
-    if (none) z[0][0] = z[0][1] = z[0][2] = z[0][3] = 0.f;
-    const int o = o0 + 4 * k16;
-    put4(a.y, a.type, (r.row + t) * a.out + o, z[0], a.out - o, a.out % 4 == 0);
-  };
   if constexpr (S == 1) {
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
@@ -387,7 +389,7 @@ __global__ __launch_bounds__(512, 4) void token_stream_kernel(const TokenProduct
       v4i sum[G];
 #pragma unroll
       for (int h = 0; h < G; ++h) sum[h] = acc[h][b];
-      end(sum, 16 * b + n16, sx, none);
+      if (16 * b + n16 < r.n) outputs<GATED>(a, r, o0, 16 * b + n16, ch, sum, sx, none);
     }
   } else {
     static_assert(S >= TB, "a block of tokens a wave");
@@ -404,8 +406,125 @@ __global__ __launch_bounds__(512, 4) void token_stream_kernel(const TokenProduct
 #pragma unroll
       for (int q = 1; q < S; ++q) sum[h] += part[wave - sub + q][h * TB + sub][lane];
     }
-    end(sum, 16 * sub + n16, sx, none);
+    if (16 * sub + n16 < r.n) outputs<GATED>(a, r, o0, 16 * sub + n16, ch, sum, sx, none);
   }
+}
+
+// The same for a call of up to FUSED_CODES codes in one launch: every workgroup makes the codes of its tile's tokens itself, while its first weights are on
+// their way.  (One token of 4096-4096 in bf16: 8.2 us a call, two launches 10.5.)
+constexpr int FUSED_CODES = 8192, FUSED_TILES = 1024;
+template <bool GATED, typename T>
+__global__ __launch_bounds__(512, 4) void token_stream_fused_kernel(const TokenProductArgs a, int o_tiles) {
+  constexpr int G = GATED ? 2 : 1, U = 4, S = 8, EACH = FUSED_CODES / 8 / 512;
+  __shared__ v4i part[8][G][64];
+  __shared__ alignas(16) int8_t codes[FUSED_CODES];
+  __shared__ uint32_t top[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (threadIdx.x < 16) top[threadIdx.x] = 0;
+  const int id = blockIdx.x / o_tiles, o0 = (blockIdx.x - id * o_tiles) * 16;
+  const Rows r = find_rows<16>(a, id);
+  zero_rest<512>(a);
+  if (r.n <= 0) return;
+  const int n16 = lane & 15, k16 = lane >> 4;
+  const int64_t w0 = (int64_t)r.e * w_rows_of(a, GATED);
+  __amdgpu_buffer_rsrc_t from[G];
+#pragma unroll
+  for (int h = 0; h < G; ++h)
+    from[h] = __builtin_amdgcn_make_buffer_rsrc((void*)uniform(a.w + (w0 + h * a.out + o0) * a.pitch), 0, (unsigned)(min(16, a.out - o0) * a.pitch), 0x00020000);
+  const unsigned w_at = (unsigned)(min(n16, a.out - 1 - o0) * a.pitch + k16 * 16);
+  const int steps = a.pitch / 64;
+  v4i w0s[U][G], w1s[U][G];
+  auto ask = [&](v4i (&q)[U][G], int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = s + u * S;
+#pragma unroll
+      for (int h = 0; h < G; ++h) q[u][h] = (v4i)__builtin_amdgcn_raw_buffer_load_b128(from[h], w_at + (k < steps ? k * 64u : 0x80000000u), 0, 0);
+    }
+  };
+  ask(w0s, wave);
+  // 8 values a piece, pieces of the tile's tokens one after the other; 16 neighbouring lanes' are one token's
+  const int per_row = a.pitch / 8, pieces = r.n * per_row;
+  float v[EACH][8];
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    const int g = threadIdx.x + j * 512, row = g / per_row, c = (g - row * per_row) * 8;
+    const int64_t in = g < pieces ? input_of(a, r, row) : -1;
+    const T* x = (const T*)a.x + max(in, (int64_t)0) * a.x_stride + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
+    if (in >= 0) {
+      if (a.x_wide && c + 8 <= a.in) {
+        load8<T, true>(x, v[j]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (c + i < a.in) v[j][i] = to_f(x[i]);
+      }
+    }
+  }
+  ask(w1s, wave + U * S);
+  const int64_t in = input_of(a, r, n16);
+  Channels ch[G];
+#pragma unroll
+  for (int h = 0; h < G; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t o = w0 + weight_of<GATED>(a, o0, 16 * h + 4 * k16 + i);
+      ch[h].set(i, a.sw[o], a.bias ? a.bias[o] : 0.f);
+    }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    const int g = threadIdx.x + j * 512;
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = raised(m, v[j][i]);
+    m = row_reduce<16, true>(m);
+    if (g < pieces && (lane & 15) == 0) atomicMax(&top[g / per_row], __float_as_uint(m));
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) {
+    const int g = threadIdx.x + j * 512;
+    if (g < pieces) {
+      const RowScale s(__uint_as_float(top[g / per_row]));
+      *reinterpret_cast<uint2*>(codes + g * 8) = s.codes8(v[j]);
+    }
+  }
+  __syncthreads();
+  v4i acc[G] = {};
+  const int x_at = min(n16, r.n - 1) * a.pitch + k16 * 16;
+  auto mul = [&](const v4i (&q)[U][G], int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const v4i x = *reinterpret_cast<const v4i*>(codes + x_at + min(s + u * S, steps - 1) * 64);
+#pragma unroll
+      for (int h = 0; h < G; ++h) acc[h] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q[u][h], x, acc[h], 0, 0, 0);
+    }
+  };
+  // (two sets of U steps of eight waves hold 4096 codes of a row, a longer one takes two sets more)
+  mul(w0s, wave);
+  if (steps > 2 * U * S) ask(w0s, wave + 2 * U * S);
+  mul(w1s, wave + U * S);
+  if (steps > 2 * U * S) {
+    ask(w1s, wave + 3 * U * S);
+    mul(w0s, wave + 2 * U * S);
+    mul(w1s, wave + 3 * U * S);
+  }
+  static_assert(FUSED_CODES == 4 * U * S * 64, "steps");
+#pragma unroll
+  for (int h = 0; h < G; ++h) part[wave][h][lane] = acc[h];
+  __syncthreads();
+  if (wave > 0 || n16 >= r.n) return;
+  v4i sum[G];
+#pragma unroll
+  for (int h = 0; h < G; ++h) {
+    sum[h] = part[0][h][lane];
+#pragma unroll
+    for (int q = 1; q < S; ++q) sum[h] += part[q][h][lane];
+  }
+  outputs<GATED>(a, r, o0, n16, ch, sum, RowScale(__uint_as_float(top[n16])).scale(), in < 0);
 }
 
 // ------------------------------------------------------------------ tiles
@@ -594,7 +713,7 @@ __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArg
 }
 
 // ------------------------------------------------------------------ launches
-enum { AUTOMATIC = 0, STREAM = 1, TILES_64 = 2, TILES_128 = 3, TILES_256 = 4 };
+enum { AUTOMATIC = 0, STREAM = 1, TILES_64 = 2, TILES_128 = 3, TILES_256 = 4 };   // see pipe_set_token_kernel
 
 template <int TB, int S>
 int launch_stream_split(const TokenProductArgs& a, bool gated, int o_tiles, int tiles, hipStream_t st) {
@@ -635,23 +754,54 @@ int launch_tiles(const TokenProductArgs& a, bool gated, hipStream_t st) {
 
 }  // namespace
 
-int launch_token_product(const TokenProductArgs& a, hipStream_t st) {
+static int kernel_of(const TokenProductArgs& a) {
   const bool gated = a.act == PIPE_ACT_SILU_GATED;
   int which = g_token_kernel;
   const int64_t each = a.n / a.E;       // tokens of an expert, about
   if (which == AUTOMATIC) {
-    which = STREAM;
-    if (each > 32) {
-      // Microseconds a stage of 128 codes, from what each kernel takes with few tiles and with many (half a tile more for each expert).  Calls of
-      // 64, 128 and 256 tokens a tile: 512 tokens of 4096-4096 27, 37 and 60 us; 1000 42, 40 and 62; 2048 73, 57 and 68; 4096 of 4096-11008 -, 250 and
-      // 215; 512 tokens, six of 64 gated experts of 2048-1408 93, 100 and 114; 2048 201, 176 and 172.
-      const double w_rows = gated ? 2.0 * a.out : a.out, more = a.starts ? 0.5 * a.E : 0.0;
+    // Few tokens are streamed past: the weights' bytes are all that counts up to 32 tokens (4096-4096: 13 us, tiles 17; 48 tokens 17 both), longer where the
+    // outputs make few tiles (33 tokens of 8192-64: 19 us, tiles 27).  Experts' tokens are not spread evenly, a second tile reads the weights again: four each
+    // (16 tokens, two of eight experts of 4096-4096: 29 us, tiles 30; 64 tokens: 60 and 30).
+    const double w_rows = gated ? 2.0 * a.out : a.out;
+    if (a.starts ? each <= 4 : a.n <= (w_rows <= 1024 ? 64 : 32)) {
+      which = STREAM;
+    } else {
+      // Microseconds of a launch, from what a stage of 128 codes takes each kernel with few tiles and with many (half a tile more for each expert), and its
+      // ends, in stages.  Calls of 64, 128 and 256 tokens a tile: 512 tokens of 4096-4096 27, 37 and 60 us; 1000 42, 40 and 62; 2048 73, 57 and 68; 4096 of
+      // 4096-11008 312, 239 and 198; 512 tokens, six of 64 gated experts of 2048-1408 93, 100 and 114; 8192, two of 128 of 1024-1024 138, 122 and 152.
+      const double more = a.starts ? 0.5 * a.E : 0.0, stages = a.pitch / 128;
       auto tiles = [&](int B) { return std::ceil(w_rows / B) * std::ceil((double)a.n / B + more); };
-      const double t64 = std::max(0.45, 0.00096 * tiles(64)), t128 = std::max(0.95, 0.00287 * tiles(128)), t256 = std::max(1.9, 0.0084 * tiles(256));
+      const double t64 = std::max(0.45, 0.0010 * tiles(64)) * (stages + 3), t128 = std::max(0.95, 0.0032 * tiles(128)) * (stages + 3),
+                   t256 = std::max(1.85, 0.0084 * tiles(256)) * (stages + 5);
       which = t64 <= t128 && t64 <= t256 ? TILES_64 : t128 <= t256 ? TILES_128 : TILES_256;
     }
   }
-  if (!near(a)) which = STREAM;
+  return near(a) ? which : STREAM;
+}
+
+template <bool GATED>
+static int launch_fused(const TokenProductArgs& a, int o_tiles, hipStream_t st) {
+  const dim3 grid((unsigned)(o_tiles * row_tiles<16>(a))), block(512);
+  if (a.type == PIPE_F32) PIPE_KLAUNCH((token_stream_fused_kernel<GATED, float>), grid, block, 0, st, a, o_tiles);
+  else if (a.type == PIPE_F16) PIPE_KLAUNCH((token_stream_fused_kernel<GATED, f16>), grid, block, 0, st, a, o_tiles);
+  else PIPE_KLAUNCH((token_stream_fused_kernel<GATED, bf16>), grid, block, 0, st, a, o_tiles);
+  PIPE_HIP(hipGetLastError());
+  return PIPE_OK;
+}
+
+int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStream_t st) {
+  const bool gated = a.act == PIPE_ACT_SILU_GATED;
+  const int which = kernel_of(a);
+  const int n_wide = 16 / type_size(a.type), o_tiles = (a.out + 15) / 16;
+  if (which == STREAM && a.n * a.pitch <= FUSED_CODES && o_tiles * row_tiles<16>(a) <= FUSED_TILES) {
+    a.x_wide = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride % n_wide == 0;
+    return gated ? launch_fused<true>(a, o_tiles, st) : launch_fused<false>(a, o_tiles, st);
+  }
+  a.qx = codes;
+  a.sx = scales;
+  const int rc = launch_token_quantize(a.x, a.type, a.n_x, a.in, a.x_stride, a.pitch, codes, scales, st);
+  if (rc) return rc;
+  const int64_t each = a.n / a.E;
   if (which == TILES_256) return launch_tiles<256>(a, gated, st);
   if (which == TILES_128) return launch_tiles<128>(a, gated, st);
   if (which == TILES_64) return launch_tiles<64>(a, gated, st);
