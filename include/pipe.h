@@ -703,12 +703,16 @@ int pipe_set_token_kernel(int which);
  *   starts_dev [E+1]      first row of each expert, and their total
  *   order_dev  [T*top_k]  row -> pair token * top_k + choice; -1 from the total on
  *   places_dev [T][top_k] pair -> row, or -1
+ *   scratch_dev           pipe_expert_scratch(T, top_k, E) bytes of the caller's, 8-byte aligned, in use until the call has run; NULL where that is 0
+ *                         (up to 481 pairs; -1: no such router)
  * Errors: PIPE_EINVAL (NULL, type, renormalize), PIPE_ESHAPE (T < 0, T * top_k >= 2^30, E outside 1..1024, top_k outside 1..32 or over E, stride).
  * (pipe_expert_sort: top_k may exceed E.)                                                                           */
 int pipe_expert_route(const void* logits_dev, int type, int T, int E, int64_t row_stride, int top_k, int renormalize,
-                      int32_t* experts_dev, float* weights_dev, int32_t* starts_dev, int32_t* order_dev, int32_t* places_dev, void* stream);
+                      int32_t* experts_dev, float* weights_dev, int32_t* starts_dev, int32_t* order_dev, int32_t* places_dev,
+                      void* scratch_dev, void* stream);
 int pipe_expert_sort(const int32_t* experts_dev, int T, int top_k, int E, int32_t* starts_dev, int32_t* order_dev,
-                     int32_t* places_dev, void* stream);
+                     int32_t* places_dev, void* scratch_dev, void* stream);
+int64_t pipe_expert_scratch(int T, int top_k, int E);
 
 /* pipe_token_forward of each expert on its rows: codes_dev [E][out or 2 out][pitch], scales_dev and bias_dev [E][out or 2 out].  Rows starts_dev[e] ..
  * starts_dev[e+1]-1 of y (ascending from 0, at most `rows`) are expert e's.  Row r is token order_dev[r] / top_k of x [T]; order_dev NULL: row r of x, then

@@ -105,8 +105,10 @@ def _load():
     lib.pipe_token_scratch.restype = i64
     lib.pipe_token_quantize.argtypes = [vp, ci, i64, ci, i64, vp, vp, vp]
     lib.pipe_token_forward.argtypes = [vp, ci, i64, ci, i64, vp, vp, vp, ci, ci, vp, vp, vp]
-    lib.pipe_expert_route.argtypes = [vp, ci, ci, ci, i64, ci, ci, vp, vp, vp, vp, vp, vp]
-    lib.pipe_expert_sort.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp]
+    lib.pipe_expert_route.argtypes = [vp, ci, ci, ci, i64, ci, ci, vp, vp, vp, vp, vp, vp, vp]
+    lib.pipe_expert_sort.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp, vp]
+    lib.pipe_expert_scratch.argtypes = [ci, ci, ci]
+    lib.pipe_expert_scratch.restype = i64
     lib.pipe_expert_forward.argtypes = [vp, ci, i64, ci, i64, vp, vp, vp, ci, ci, vp, vp, i64, ci, ci, vp, vp, vp]
     lib.pipe_expert_combine.argtypes = [vp, ci, i64, ci, i64, vp, vp, ci, ci, vp, vp]
     lib.pipe_strerror.argtypes = [ci]
@@ -979,6 +981,24 @@ def pipe_set_token_kernel(which: int) -> None:
     _check(_lib.pipe_set_token_kernel(int(which)), "pipe_set_token_kernel")
 
 
+def pipe_expert_scratch(tokens: int, top_k: int, num_experts: int) -> int:
+    """Bytes that the router's calls keep counts in while they run (in a tensor of their own)."""
+    n = _lib.pipe_expert_scratch(int(tokens), int(top_k), int(num_experts))
+    if n < 0:
+        raise ValueError("1 to 1024 experts, 1 to 32 of them a token, tokens * top_k < 2**30")
+    return n
+
+
+def _tables(n: int, T: int, k: int, E: int, like: torch.Tensor):
+    """(room for starts and scratch, n tables [T, k], addresses of starts and scratch), int32."""
+    pairs = T * k
+    extra = 0 if pairs <= 481 else pipe_expert_scratch(T, k, E) // 4      # (a block is at least 481 pairs)
+    at = (E + 2) // 2 * 2
+    room = torch.empty(at + extra, dtype=torch.int32, device=like.device)
+    starts = room.data_ptr()
+    return room, torch.empty((n, T, k), dtype=torch.int32, device=like.device).unbind(0), starts, starts + 4 * at
+
+
 def pipe_expert_route(logits: torch.Tensor, top_k: int, renormalize: bool = True):
     """Of each token's logits [T, E] the top_k largest: (experts [T, top_k], weights [T, top_k], starts [E + 1], order [T * top_k], places
     [T, top_k]), the tables as pipe_expert_sort gives them.  weights: softmax over the chosen (renormalize) or over all."""
@@ -987,12 +1007,12 @@ def pipe_expert_route(logits: torch.Tensor, top_k: int, renormalize: bool = True
     T, E = logits.shape
     if not 1 <= top_k <= 32:
         raise ValueError("top_k must be 1 to 32")
-    n = T * top_k
-    experts, weights, order, places, starts = torch.empty(4 * n + E + 1, dtype=torch.int32, device=logits.device).split([n, n, n, n, E + 1])
-    weights = weights.view(torch.float32)
-    _check(_lib.pipe_expert_route(lp, _type(logits.dtype), T, E, stride, top_k, 1 if renormalize else 0, experts.data_ptr(), weights.data_ptr(),
-                                  starts.data_ptr(), order.data_ptr(), places.data_ptr(), _stream()), "pipe_expert_route")
-    return experts.view(T, top_k), weights.view(T, top_k), starts, order, places.view(T, top_k)
+    room, tables, sp, cp = _tables(3, T, top_k, E, logits)
+    experts, order, places = tables
+    weights = torch.empty((T, top_k), dtype=torch.float32, device=logits.device)
+    _check(_lib.pipe_expert_route(lp, _type(logits.dtype), T, E, stride, top_k, 1 if renormalize else 0, experts.data_ptr(), weights.data_ptr(), sp,
+                                  order.data_ptr(), places.data_ptr(), cp, _stream()), "pipe_expert_route")
+    return experts, weights, room[:E + 1], order.view(-1), places
 
 
 def pipe_expert_sort(experts: torch.Tensor, num_experts: int):
@@ -1002,11 +1022,13 @@ def pipe_expert_sort(experts: torch.Tensor, num_experts: int):
     if experts.dim() != 2:
         raise ValueError("experts is [tokens, top_k]")
     T, k = experts.shape
-    n = T * k
     ep = _ints(experts, dev)
-    order, places, starts = torch.empty(2 * n + max(0, num_experts) + 1, dtype=torch.int32, device=experts.device).split([n, n, max(0, num_experts) + 1])
-    _check(_lib.pipe_expert_sort(ep, T, k, num_experts, starts.data_ptr(), order.data_ptr(), places.data_ptr(), _stream()), "pipe_expert_sort")
-    return starts, order, places.view(T, k)
+    if not 1 <= num_experts <= 1024 or not 1 <= k <= 32:
+        raise ValueError("1 to 1024 experts, 1 to 32 of them a token")
+    room, (order, places), sp, cp = _tables(2, T, k, num_experts, experts)
+    _check(_lib.pipe_expert_sort(ep, T, k, num_experts, sp, order.data_ptr(), places.data_ptr(), cp, _stream()),
+           "pipe_expert_sort")
+    return room[:num_experts + 1], order.view(-1), places
 
 
 def pipe_expert_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, starts: torch.Tensor, order: Optional[torch.Tensor] = None,

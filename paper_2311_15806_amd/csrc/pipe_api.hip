@@ -2566,27 +2566,30 @@ static bool router_ok(int T, int E, int top_k) {
   return T >= 0 && E >= 1 && E <= PIPE_EXPERTS_MAX && top_k >= 1 && top_k <= PIPE_TOP_K_MAX && (int64_t)T * top_k < 1 << 30;
 }
 
+extern "C" int64_t pipe_expert_scratch(int T, int top_k, int E) {
+  return router_ok(T, E, top_k) ? expert_sort_scratch(T, top_k, E) : -1;
+}
+
 extern "C" int pipe_expert_sort(const int32_t* experts_dev, int T, int top_k, int E, int32_t* starts_dev, int32_t* order_dev,
-                                int32_t* places_dev, void* stream) {
+                                int32_t* places_dev, void* scratch_dev, void* stream) {
   if (!router_ok(T, E, top_k)) return PIPE_ESHAPE;
   if (!starts_dev || (T > 0 && (!experts_dev || !order_dev || !places_dev))) return PIPE_EINVAL;
-  return launch_expert_sort(experts_dev, T * top_k, E, starts_dev, order_dev, places_dev, (hipStream_t)stream);
+  if (expert_sort_scratch(T, top_k, E) > 0 && (!scratch_dev || (reinterpret_cast<uintptr_t>(scratch_dev) & 7) != 0)) return PIPE_EINVAL;
+  return launch_expert_sort(experts_dev, T, top_k, E, starts_dev, order_dev, places_dev, scratch_dev, (hipStream_t)stream);
 }
 
 extern "C" int pipe_expert_route(const void* logits_dev, int type, int T, int E, int64_t row_stride, int top_k, int renormalize,
                                  int32_t* experts_dev, float* weights_dev, int32_t* starts_dev, int32_t* order_dev, int32_t* places_dev,
-                                 void* stream) {
+                                 void* scratch_dev, void* stream) {
   if (!known_type(type) || (renormalize != 0 && renormalize != 1)) return PIPE_EINVAL;
   if (!router_ok(T, E, top_k) || top_k > E || row_stride < 0) return PIPE_ESHAPE;
   if (!starts_dev || (T > 0 && (!logits_dev || !experts_dev || !weights_dev || !order_dev || !places_dev))) return PIPE_EINVAL;
-  if (T > 0) {
-    ExpertRouteArgs a{};
-    a.logits = logits_dev; a.type = type; a.T = T; a.E = E; a.top_k = top_k; a.renormalize = renormalize; a.row_stride = row_stride;
-    a.experts = experts_dev; a.weights = weights_dev;
-    const int rc = launch_expert_route(a, (hipStream_t)stream);
-    if (rc) return rc;
-  }
-  return launch_expert_sort(experts_dev, T * top_k, E, starts_dev, order_dev, places_dev, (hipStream_t)stream);
+  if (expert_sort_scratch(T, top_k, E) > 0 && (!scratch_dev || (reinterpret_cast<uintptr_t>(scratch_dev) & 7) != 0)) return PIPE_EINVAL;
+  if (T == 0) return launch_expert_sort(nullptr, 0, top_k, E, starts_dev, order_dev, places_dev, nullptr, (hipStream_t)stream);
+  ExpertRouteArgs a{};
+  a.logits = logits_dev; a.type = type; a.T = T; a.E = E; a.top_k = top_k; a.renormalize = renormalize; a.row_stride = row_stride;
+  a.experts = experts_dev; a.weights = weights_dev;
+  return launch_expert_route(a, starts_dev, order_dev, places_dev, scratch_dev, (hipStream_t)stream);
 }
 
 extern "C" int pipe_expert_combine(const void* y_dev, int type, int64_t rows, int out, int64_t row_stride, const int32_t* places_dev,

@@ -34,8 +34,10 @@ struct ExpertRouteArgs {
   int32_t* experts;
   float* weights;
 };
-int launch_expert_route(const ExpertRouteArgs& a, hipStream_t st);
-int launch_expert_sort(const int32_t* experts, int n, int E, int32_t* starts, int32_t* order, int32_t* places, hipStream_t st);
+int64_t expert_sort_scratch(int T, int top_k, int E);      // bytes
+int launch_expert_route(const ExpertRouteArgs& a, int32_t* starts, int32_t* order, int32_t* places, void* scratch, hipStream_t st);   // (T > 0)
+int launch_expert_sort(const int32_t* experts, int T, int top_k, int E, int32_t* starts, int32_t* order, int32_t* places, void* scratch,
+                       hipStream_t st);
 int launch_expert_combine(const void* y, int type, int64_t n, int H, int64_t row_stride, const int32_t* places, const float* weights, int T,
                           int top_k, void* out, hipStream_t st);
 

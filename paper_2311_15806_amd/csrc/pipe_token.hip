@@ -1,4 +1,6 @@
 // Rows in 8 bits with a scale each; the router's choice, the order by expert, and the way back.
+#include <algorithm>
+
 #include "pipe_attention.h"
 #include "pipe_codes.h"
 #include "pipe_token.h"
@@ -67,91 +69,215 @@ int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitc
   return PIPE_OK;
 }
 
-// ------------------------------------------------------------------ the choice of experts
-// A wave a token, lane l its logits l, l + 64, ...; each of the top_k steps is a maximum over the wave and a ballot a register, which finds the
-// lowest index that holds it.  A NaN equals nothing and is never chosen.
-template <typename T, int EL>
-__global__ __launch_bounds__(256) void expert_route_kernel(const ExpertRouteArgs a) {
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (t >= a.T) return;
-  const T* row = (const T*)a.logits + (int64_t)t * a.row_stride;
-  float v[EL];
-#pragma unroll
-  for (int i = 0; i < EL; ++i) v[i] = i * 64 + lane < a.E ? to_f(row[i * 64 + lane]) : -INFINITY;
-  float chosen = -INFINITY;      // lane j: the j-th largest logit
-  int expert = -1;
-  float first = 0.f, total = 0.f;
-  for (int j = 0; j < a.top_k; ++j) {
-    float m = v[0];
-#pragma unroll
-    for (int i = 1; i < EL; ++i) m = fmaxf(m, v[i]);
-    m = wave_max(m);
-    if (!(m > -INFINITY)) break;
-    int at = -1;
-#pragma unroll
-    for (int i = 0; i < EL; ++i) {
-      const unsigned long long b = __ballot(v[i] == m);
-      if (at < 0 && b != 0) at = i * 64 + __ffsll(b) - 1;
-    }
-    if (j == 0) {
-      first = m;
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < EL; ++i) sum += expf(v[i] - m);
-      total = sum;
-    }
-    if (lane == j) { chosen = m; expert = at; }
-#pragma unroll
-    for (int i = 0; i < EL; ++i)
-      if (i * 64 + lane == at) v[i] = -INFINITY;
+// ------------------------------------------------------------------ the choice of experts, and the order by expert
+// Pairs (token, choice) go by blocks of up to 512, whole tokens each, a pair a thread.  Where there is one block a single workgroup does all.  Otherwise a
+// launch counts each block's pairs by expert (the router's beside its choice), and another has every workgroup sum the counts of the blocks
+// before its own and of all, which gives its pairs' rows.  Nothing passes between the workgroups of a launch; no order of theirs is in the result.
+constexpr int PAIRS = 512;
+__host__ __device__ constexpr int block_tokens(int top_k) { return PAIRS / top_k; }
+static int block_count(int T, int top_k) { return (T + block_tokens(top_k) - 1) / block_tokens(top_k); }
+
+struct SortArgs {
+  int T, E, top_k, blocks;
+  int32_t *starts, *order, *places;
+  uint16_t* counts;     // [blocks][E + 1, rounded up to four], the last: pairs without an expert
+};
+__host__ __device__ constexpr int count_pitch(int E) { return (E + 4) / 4 * 4; }
+
+// lanes of the wave with the same key (of `bits` bits)
+__device__ __forceinline__ unsigned long long same_key(int key, int bits) {
+  unsigned long long m = ~0ull;
+  for (int i = 0; i < bits; ++i) {
+    const unsigned long long b = __ballot((key >> i) & 1);
+    m &= (key >> i) & 1 ? b : ~b;
   }
-  const float e = chosen > -INFINITY ? expf(chosen - first) : 0.f;
-  if (a.renormalize) total = e;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-  if (lane < a.top_k) {
-    a.experts[(int64_t)t * a.top_k + lane] = expert;
-    a.weights[(int64_t)t * a.top_k + lane] = expert >= 0 ? e / total : 0.f;
-  }
+  return m;
 }
 
-// ------------------------------------------------------------------ the order by expert
-// A workgroup an expert, and one for the pairs without one: it counts the pairs of the experts before it, which gives its first row, and writes
-// the rows of its own in order.  Nothing passes between workgroups.
-constexpr int SORT_NT = 1024;
-__global__ __launch_bounds__(SORT_NT) void expert_sort_kernel(const int32_t* __restrict__ experts, int n, int E, int32_t* __restrict__ starts,
-                                                              int32_t* __restrict__ order, int32_t* __restrict__ places) {
-  __shared__ int below[SORT_NT / 64], own[SORT_NT / 64];
-  const int e = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;      // e == E: none
-  const int share = (n + SORT_NT - 1) / SORT_NT * 64;       // pairs of a wave, whole rounds of 64
-  const int lo = min(n, wave * share), hi = min(n, lo + share);
-  auto key = [&](int i) {
-    const int k = experts[i];
-    return (unsigned)k < (unsigned)E ? k : E;
-  };
-  int b = 0, o = 0;
-  for (int i = lo + lane; i < hi; i += 64) {
-    const int k = key(i);
-    b += k < e;
-    o += k == e;
-  }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) { b += __shfl_xor(b, d, 64); o += __shfl_xor(o, d, 64); }
-  if (lane == 0) { below[wave] = b; own[wave] = o; }
+// The rows of block `b`'s pairs, `n` of them, a pair a thread: `key` is its expert (E: none; E + 1: behind the end).
+__device__ __forceinline__ void place(const SortArgs& a, int b, int n, int key, int* lds) {
+  const int q = a.E + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int *base = lds, *total = lds + q;                                // of each expert
+  uint16_t* cnt = reinterpret_cast<uint16_t*>(lds + 2 * q);         // ... and of each wave's pairs
+  __shared__ int wave_total[PAIRS / 64];
+  for (int i = threadIdx.x; i < PAIRS / 64 * q; i += PAIRS) cnt[i] = 0;
+  for (int e = threadIdx.x; e < q; e += PAIRS) base[e] = total[e] = 0;
   __syncthreads();
-  int row = 0;
-  for (int w = 0; w < SORT_NT / 64; ++w) row += below[w] + (w < wave ? own[w] : 0);
-  if (threadIdx.x == 0) starts[e] = row;
-  for (int i = lo; i < hi; i += 64) {
-    const bool mine = i + lane < hi && key(i + lane) == e;
-    const unsigned long long all = __ballot(mine);
-    const int at = row + __popcll(all & ((1ull << lane) - 1));
-    if (mine) {
-      order[at] = e < E ? i + lane : -1;
-      places[i + lane] = e < E ? at : -1;
+  const bool mine = (int)threadIdx.x < n;
+  const unsigned long long same = same_key(mine ? key : q, 32 - __clz(q));
+  const int before = __popcll(same & ((1ull << lane) - 1));
+  if (mine && before == 0) cnt[wave * q + key] = (uint16_t)__popcll(same);
+  if (a.blocks > 1) {
+    const int quads = count_pitch(a.E) / 4, groups = max(1, PAIRS / quads);      // four experts a thread, the blocks dealt to groups of threads
+    for (int x = threadIdx.x; x < groups * quads; x += PAIRS) {
+      const int g = x / quads, e = (x - g * quads) * 4;
+      int pre[4] = {0, 0, 0, 0}, all[4] = {0, 0, 0, 0};
+#pragma unroll 8
+      for (int r = g; r < a.blocks; r += groups) {
+        const uint2 c = *reinterpret_cast<const uint2*>(a.counts + (int64_t)r * (4 * quads) + e);
+        const int v[4] = {(int)(c.x & 0xffff), (int)(c.x >> 16), (int)(c.y & 0xffff), (int)(c.y >> 16)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          all[i] += v[i];
+          pre[i] += r < b ? v[i] : 0;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (e + i < q) {
+          atomicAdd(&base[e + i], pre[i]);
+          atomicAdd(&total[e + i], all[i]);
+        }
     }
-    row += __popcll(all);
   }
+  __syncthreads();
+  for (int e = threadIdx.x; e < q; e += PAIRS) {      // counts of the waves before
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < PAIRS / 64; ++w) {
+      const int c = cnt[w * q + e];
+      cnt[w * q + e] = (uint16_t)sum;
+      sum += c;
+    }
+    if (a.blocks == 1) total[e] = sum;
+  }
+  __syncthreads();
+  // first rows: all pairs of the experts before, `per` experts a thread
+  const int per = (a.E + PAIRS - 1) / PAIRS, e0 = min((int)threadIdx.x * per, a.E), e1 = min(e0 + per, a.E);
+  int own = 0;
+  for (int e = e0; e < e1; ++e) own += total[e];
+  int upto = own;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d);
+    if (lane >= d) upto += v;
+  }
+  if (lane == 63) wave_total[wave] = upto;
+  __syncthreads();
+  int first = upto - own;
+  for (int w = 0; w < wave; ++w) first += wave_total[w];
+  for (int e = e0; e < e1; ++e) {
+    base[e] += first;
+    if (b == 0) a.starts[e] = first;
+    first += total[e];
+    if (e == a.E - 1) {
+      base[a.E] += first;
+      if (b == 0) a.starts[a.E] = first;
+    }
+  }
+  __syncthreads();
+  if (!mine) return;
+  const int pair = b * (block_tokens(a.top_k) * a.top_k) + threadIdx.x, row = base[key] + cnt[wave * q + key] + before;
+  a.order[row] = key < a.E ? pair : -1;
+  a.places[pair] = key < a.E ? row : -1;
+}
+
+// pairs of block b
+__device__ __forceinline__ int pairs_of(const SortArgs& a, int b) {
+  return min(block_tokens(a.top_k), a.T - b * block_tokens(a.top_k)) * a.top_k;
+}
+__device__ __forceinline__ int key_of(int expert, int E) { return (unsigned)expert < (unsigned)E ? expert : E; }
+extern __shared__ int sort_lds[];
+static size_t sort_lds_bytes(int E) { return (size_t)(E + 1) * (2 * sizeof(int) + PAIRS / 64 * sizeof(uint16_t)); }   // (41 KiB at most)
+
+__global__ __launch_bounds__(PAIRS) void expert_place_kernel(const int32_t* __restrict__ experts, const SortArgs a) {
+  const int b = blockIdx.x, n = pairs_of(a, b);
+  const int key = (int)threadIdx.x < n ? key_of(experts[(int64_t)b * (block_tokens(a.top_k) * a.top_k) + threadIdx.x], a.E) : 0;
+  place(a, b, n, key, sort_lds);
+}
+
+// counts of a block by expert
+__device__ __forceinline__ void count_block(const SortArgs& a, int b, int n, int key, int* hist /* [E + 1] */) {
+  const int q = a.E + 1;
+  for (int e = threadIdx.x; e < q; e += PAIRS) hist[e] = 0;
+  __syncthreads();
+  if ((int)threadIdx.x < n) atomicAdd(&hist[key], 1);
+  __syncthreads();
+  for (int e = threadIdx.x; e < q; e += PAIRS) a.counts[(int64_t)b * count_pitch(a.E) + e] = (uint16_t)hist[e];
+}
+__global__ __launch_bounds__(PAIRS) void expert_count_kernel(const int32_t* __restrict__ experts, const SortArgs a) {
+  const int b = blockIdx.x, n = pairs_of(a, b);
+  const int key = (int)threadIdx.x < n ? key_of(experts[(int64_t)b * (block_tokens(a.top_k) * a.top_k) + threadIdx.x], a.E) : 0;
+  count_block(a, b, n, key, sort_lds);
+}
+
+// over the 16 lanes of a token
+__device__ __forceinline__ float row_sum(float x) {
+  x += dpp<0xB1>(x);
+  x += dpp<0x4E>(x);
+  x += dpp<0x141>(x);
+  return x + dpp<0x140>(x);
+}
+template <int CTRL>
+__device__ __forceinline__ int dpp_i(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ int row_min(int x) {
+  x = min(x, dpp_i<0xB1>(x));
+  x = min(x, dpp_i<0x4E>(x));
+  x = min(x, dpp_i<0x141>(x));
+  return min(x, dpp_i<0x140>(x));
+}
+
+// 16 lanes a token, lane l its logits l, l + 16, ...; each of the top_k steps is a maximum and then the lowest index that holds it.  A NaN equals
+// nothing and is never chosen.  16384 tokens, eight of 128, bf16: 4.6 us (a wave a token: 12.7).
+template <typename T, int EL>
+__global__ __launch_bounds__(PAIRS) void expert_route_kernel(const ExpertRouteArgs a, const SortArgs s) {
+  __shared__ int keys[PAIRS];
+  const int lane = threadIdx.x & 63, l = lane & 15, b = blockIdx.x;
+  const int t0 = b * block_tokens(a.top_k), tokens = min(block_tokens(a.top_k), a.T - t0);
+  for (int i0 = (threadIdx.x >> 6) * 4; i0 < tokens; i0 += PAIRS / 16) {
+    const int i = i0 + (lane >> 4), t = t0 + min(i, tokens - 1);
+    const T* row = (const T*)a.logits + (int64_t)t * a.row_stride;
+    float v[EL];
+#pragma unroll
+    for (int e = 0; e < EL; ++e) v[e] = e * 16 + l < a.E ? to_f(row[e * 16 + l]) : -INFINITY;
+    float chosen[2] = {-INFINITY, -INFINITY};      // lane l: the l-th and the 16 + l-th largest
+    int expert[2] = {-1, -1};
+    float first = 0.f, total = 0.f;
+    for (int j = 0; j < a.top_k; ++j) {
+      float m = v[0];
+#pragma unroll
+      for (int e = 1; e < EL; ++e) m = fmaxf(m, v[e]);
+      m = row_reduce<16, true>(m);
+      int at = 0x7fffffff;
+#pragma unroll
+      for (int e = EL - 1; e >= 0; --e) at = v[e] == m ? e * 16 + l : at;
+      at = row_min(at);
+      const bool there = m > -INFINITY;      // (no logit left: the maximum of NaNs is one, or -infinity)
+      if (j == 0) {
+        first = there ? m : 0.f;
+        if (!a.renormalize) {
+#pragma unroll
+          for (int e = 0; e < EL; ++e) total += expf(v[e] - first);
+        }
+      }
+      if (l == (j & 15) && there) {
+        chosen[j >> 4] = m;
+        expert[j >> 4] = at;
+      }
+#pragma unroll
+      for (int e = 0; e < EL; ++e) v[e] = e * 16 + l == at ? -INFINITY : v[e];
+    }
+    float w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[h] = expert[h] >= 0 ? expf(chosen[h] - first) : 0.f;
+    if (a.renormalize) total = w[0] + w[1];
+    total = row_sum(total);
+    if (i < tokens) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int j = h * 16 + l;
+        if (j < a.top_k) {
+          a.experts[(int64_t)t * a.top_k + j] = expert[h];
+          a.weights[(int64_t)t * a.top_k + j] = expert[h] >= 0 ? w[h] / total : 0.f;
+          keys[i * a.top_k + j] = key_of(expert[h], a.E);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const int n = tokens * a.top_k, key = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;
+  if (s.blocks == 1) place(s, b, n, key, sort_lds);
+  else count_block(s, b, n, key, sort_lds);
 }
 
 // ------------------------------------------------------------------ back to the tokens
@@ -197,13 +323,16 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(const T* __restrict
 }
 
 template <typename T>
-int route_typed(const ExpertRouteArgs& a, hipStream_t st) {
-  const dim3 grid((a.T + 3) / 4), block(256);
-  if (a.E <= 64) PIPE_KLAUNCH((expert_route_kernel<T, 1>), grid, block, 0, st, a);
-  else if (a.E <= 128) PIPE_KLAUNCH((expert_route_kernel<T, 2>), grid, block, 0, st, a);
-  else if (a.E <= 256) PIPE_KLAUNCH((expert_route_kernel<T, 4>), grid, block, 0, st, a);
-  else if (a.E <= 512) PIPE_KLAUNCH((expert_route_kernel<T, 8>), grid, block, 0, st, a);
-  else PIPE_KLAUNCH((expert_route_kernel<T, 16>), grid, block, 0, st, a);
+int route_typed(const ExpertRouteArgs& a, const SortArgs& s, hipStream_t st) {
+  const dim3 grid(s.blocks), block(PAIRS);
+  const size_t lds = sort_lds_bytes(a.E);
+  if (a.E <= 16) PIPE_KLAUNCH((expert_route_kernel<T, 1>), grid, block, lds, st, a, s);
+  else if (a.E <= 32) PIPE_KLAUNCH((expert_route_kernel<T, 2>), grid, block, lds, st, a, s);
+  else if (a.E <= 64) PIPE_KLAUNCH((expert_route_kernel<T, 4>), grid, block, lds, st, a, s);
+  else if (a.E <= 128) PIPE_KLAUNCH((expert_route_kernel<T, 8>), grid, block, lds, st, a, s);
+  else if (a.E <= 256) PIPE_KLAUNCH((expert_route_kernel<T, 16>), grid, block, lds, st, a, s);
+  else if (a.E <= 512) PIPE_KLAUNCH((expert_route_kernel<T, 32>), grid, block, lds, st, a, s);
+  else PIPE_KLAUNCH((expert_route_kernel<T, 64>), grid, block, lds, st, a, s);
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
 }
@@ -233,15 +362,30 @@ int launch_token_quantize(const void* x, int type, int64_t rows, int in, int64_t
   return wide ? quantize_typed<bf16, true>(x, rows, in, stride, pitch, codes, scales, st) : quantize_typed<bf16, false>(x, rows, in, stride, pitch, codes, scales, st);
 }
 
-int launch_expert_route(const ExpertRouteArgs& a, hipStream_t st) {
-  if (a.type == PIPE_F32) return route_typed<float>(a, st);
-  return a.type == PIPE_F16 ? route_typed<f16>(a, st) : route_typed<bf16>(a, st);
+int64_t expert_sort_scratch(int T, int top_k, int E) {
+  const int blocks = block_count(T, top_k);
+  return blocks > 1 ? (int64_t)blocks * count_pitch(E) * sizeof(uint16_t) : 0;
 }
 
-int launch_expert_sort(const int32_t* experts, int n, int E, int32_t* starts, int32_t* order, int32_t* places, hipStream_t st) {
-  PIPE_KLAUNCH(expert_sort_kernel, dim3(E + 1), dim3(SORT_NT), 0, st, experts, n, E, starts, order, places);
+static int launch_place(const int32_t* experts, const SortArgs& s, hipStream_t st) {
+  PIPE_KLAUNCH(expert_place_kernel, dim3(s.blocks), dim3(PAIRS), sort_lds_bytes(s.E), st, experts, s);
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
+}
+
+int launch_expert_route(const ExpertRouteArgs& a, int32_t* starts, int32_t* order, int32_t* places, void* scratch, hipStream_t st) {
+  const SortArgs s{a.T, a.E, a.top_k, block_count(a.T, a.top_k), starts, order, places, (uint16_t*)scratch};
+  const int rc = a.type == PIPE_F32 ? route_typed<float>(a, s, st) : a.type == PIPE_F16 ? route_typed<f16>(a, s, st) : route_typed<bf16>(a, s, st);
+  return rc || s.blocks == 1 ? rc : launch_place(a.experts, s, st);
+}
+
+int launch_expert_sort(const int32_t* experts, int T, int top_k, int E, int32_t* starts, int32_t* order, int32_t* places, void* scratch, hipStream_t st) {
+  const SortArgs s{T, E, top_k, std::max(1, block_count(T, top_k)), starts, order, places, (uint16_t*)scratch};
+  if (s.blocks > 1) {
+    PIPE_KLAUNCH(expert_count_kernel, dim3(s.blocks), dim3(PAIRS), (E + 1) * sizeof(int), st, experts, s);
+    PIPE_HIP(hipGetLastError());
+  }
+  return launch_place(experts, s, st);
 }
 
 int launch_expert_combine(const void* y, int type, int64_t n, int H, int64_t stride, const int32_t* places, const float* weights, int T, int top_k,

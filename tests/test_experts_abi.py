@@ -75,13 +75,13 @@ def test_layer_refusals(lib):
 
 
 def route(lib, **o):
-    a = dict(logits=BUF, type=0, T=4, E=8, stride=I(8), k=2, renormalize=1, experts=BUF, weights=BUF, starts=BUF, order=BUF, places=BUF)
+    a = dict(logits=BUF, type=0, T=4, E=8, stride=I(8), k=2, renormalize=1, experts=BUF, weights=BUF, starts=BUF, order=BUF, places=BUF, scratch=BUF)
     a.update(o)
     return lib.pipe_expert_route(*a.values(), None)
 
 
 def sort(lib, **o):
-    a = dict(experts=BUF, T=4, k=2, E=8, starts=BUF, order=BUF, places=BUF)
+    a = dict(experts=BUF, T=4, k=2, E=8, starts=BUF, order=BUF, places=BUF, scratch=BUF)
     a.update(o)
     return lib.pipe_expert_sort(*a.values(), None)
 
@@ -102,6 +102,14 @@ def test_router_refusals(lib):
     for f in (route, sort):
         for bad in (dict(E=0), dict(E=1025)):
             assert f(lib, **bad) == ESHAPE, bad
+        assert f(lib, T=600, scratch=None) == EINVAL and f(lib, T=600, scratch=C.c_void_p(4100)) == EINVAL
+    lib.pipe_expert_scratch.restype = I
+    for k in range(1, 33):                       # whole tokens of up to 512 pairs a block
+        assert lib.pipe_expert_scratch(481 // k, k, 8) == 0 and lib.pipe_expert_scratch(512 // k, k, 8) == 0
+        assert lib.pipe_expert_scratch(512 // k + 1, k, 8) == 2 * 12 * 2
+    assert lib.pipe_expert_scratch(0, 3, 5) == 0
+    for bad in ((-1, 2, 8), (4, 0, 8), (4, 33, 8), (4, 2, 0), (4, 2, 1025), (1 << 29, 2, 8)):
+        assert lib.pipe_expert_scratch(*bad) == -1
     for bad in (dict(type=3), dict(renormalize=2)):
         assert route(lib, **bad) == EINVAL
     for bad in (dict(k=9), dict(stride=I(-1))):

@@ -544,7 +544,8 @@ def test_refusals(pipe):
             lambda: pipe.pipe_token_forward(x, codes, scales, out=torch.zeros(4, 34, device=dev, dtype=torch.float16)),
             lambda: pipe.pipe_token_forward(x, codes[None], scales), lambda: pipe.pipe_token_forward(torch.zeros(4, 200, device=dev), codes, scales),
             lambda: pipe.pipe_expert_route(x.cpu(), 2), lambda: pipe.pipe_expert_route(x, 0), lambda: pipe.pipe_expert_route(x, 33),
-            lambda: pipe.pipe_expert_sort(e.long(), 8), lambda: pipe.pipe_expert_sort(e.flatten(), 8), lambda: pipe.pipe_expert_sort(e.cpu(), 8),
+            lambda: pipe.pipe_expert_sort(e.long(), 8), lambda: pipe.pipe_expert_sort(e, 0), lambda: pipe.pipe_expert_sort(e, 1025), lambda: pipe.pipe_expert_scratch(-1, 2, 8),
+            lambda: pipe.pipe_expert_sort(torch.zeros(2, 33, dtype=torch.int32, device=dev), 8), lambda: pipe.pipe_expert_sort(e.flatten(), 8), lambda: pipe.pipe_expert_sort(e.cpu(), 8),
             lambda: pipe.pipe_expert_combine(x, e.long(), w), lambda: pipe.pipe_expert_combine(x, e, w[:3]), lambda: pipe.pipe_expert_combine(x.cpu(), e, w),
             lambda: pipe.pipe_expert_combine(x, e, w.half()), lambda: pipe.pipe_expert_combine(x, e, w, out=x[:2]),
             lambda: pipe.pipe_expert_forward(x, codes, scales, starts), lambda: pipe.pipe_expert_forward(x, codes[None], scales[None], starts[:1]),
@@ -553,8 +554,8 @@ def test_refusals(pipe):
             lambda: pipe.pipe_expert_forward(x, codes[None], scales[None], starts, order=e.flatten().long())):
         with pytest.raises(ValueError):
             call()
-    for call in (lambda: pipe.pipe_token_forward(x, codes, scales, act=7), lambda: pipe.pipe_expert_route(x[:, :3], 4), lambda: pipe.pipe_expert_sort(e, 0),
-                 lambda: pipe.pipe_expert_sort(e, 1025), lambda: pipe.pipe_set_token_kernel(5), lambda: pipe.pipe_set_token_kernel(-1),
+    for call in (lambda: pipe.pipe_token_forward(x, codes, scales, act=7), lambda: pipe.pipe_expert_route(x[:, :3], 4),
+                 lambda: pipe.pipe_set_token_kernel(5), lambda: pipe.pipe_set_token_kernel(-1),
                  lambda: pipe.pipe_expert_forward(x, codes[None], scales[None], starts, order=e.flatten(), top_k=0),
                  lambda: pipe.pipe_expert_forward(x, codes[None], scales[None], starts, order=e.flatten(), top_k=33)):
         with pytest.raises(pipe.PipeError):
