@@ -43,27 +43,40 @@ int launch_expert_combine(const void* y, int type, int64_t n, int H, int64_t row
 
 #if defined(__HIPCC__)
 #include "pipe_codes.h"
-// the larger of m and |x|; +infinity from a NaN or an infinity on
-__device__ __forceinline__ float raised(float m, float x) {
-  const float v = fabsf(x);
-  return v < INFINITY ? fmaxf(m, v) : INFINITY;
-}
-// The codes of a row whose largest magnitude is `top` (+infinity: it is not finite as a whole): s = top / 127, c = rint(x / s).
+// The larger of m and |x| as bit patterns, which order as the magnitudes do, an infinity and NaN behind all others.
+__device__ __forceinline__ uint32_t raised(uint32_t m, float x) { return max(m, __float_as_uint(x) & 0x7fffffffu); }
+// ... as a number, +infinity where the row is not finite as a whole
+__device__ __forceinline__ float top_of(uint32_t m) { return __uint_as_float(min(m, 0x7f800000u)); }
+// The codes of a row whose largest magnitude is `top`: s = top / 127, c = rint(x / s).  No quotient lies beyond 127 by more than its own rounding: nothing
+// is bounded but by that.
 struct RowScale {
-  float s;
-  bool bad;
-  Divisor d;
-  __device__ __forceinline__ explicit RowScale(float top) : s(normal(__fdiv_rn(top, 127.f))), bad(!(top < INFINITY)), d(s > 0.f && !bad ? s : 1.f) {}
-  static __device__ __forceinline__ float normal(float s) { return s < 0x1p-126f ? 0.f : s; }
+  float s, y;
+  bool live, bad, fast;
+  __device__ __forceinline__ explicit RowScale(float top) {
+    bad = !(top < INFINITY);
+    s = __fdiv_rn(top, 127.f);
+    if (s < 0x1p-126f) s = 0.f;
+    live = s > 0.f && !bad;
+    y = live ? __fdiv_rn(1.f, s) : 0.f;
+    fast = s > 1e-27f && s < 1e27f;
+  }
   __device__ __forceinline__ float scale() const { return bad ? __uint_as_float(0x7fc00000u) : s; }
+  // (the correctly rounded quotient by two corrections, as Divisor's, within its range; sums are left apart whatever the file's contraction)
+  template <bool FAST>
+  __device__ __forceinline__ int code(float x) const {
+    if (!FAST) return (int)rintf(__fdiv_rn(x, s));
+    float q = __fmul_rn(x, y);
+    q = __fmaf_rn(__fmaf_rn(-q, s, x), y, q);
+    return (int)rintf(__fmaf_rn(__fmaf_rn(-q, s, x), y, q));
+  }
+  template <bool FAST>
+  __device__ __forceinline__ uint2 eight(const float* x) const {
+    return make_uint2(pack4(code<FAST>(x[0]), code<FAST>(x[1]), code<FAST>(x[2]), code<FAST>(x[3])),
+                      pack4(code<FAST>(x[4]), code<FAST>(x[5]), code<FAST>(x[6]), code<FAST>(x[7])));
+  }
   __device__ __forceinline__ uint2 codes8(const float* x) const {
-    int q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float r = d.fast ? d.quotient<true>(x[i]) : d.quotient<false>(x[i]);
-      q[i] = s > 0.f && !bad ? (int)__builtin_amdgcn_fmed3f(rintf(r), -127.f, 127.f) : 0;
-    }
-    return make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+    if (!live) return make_uint2(0, 0);
+    return fast ? eight<true>(x) : eight<false>(x);
   }
 };
 #endif

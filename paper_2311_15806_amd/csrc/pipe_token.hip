@@ -30,10 +30,10 @@ __global__ __launch_bounds__(256) void token_quantize_kernel(const T* __restrict
   float v[CH][8];
 #pragma unroll
   for (int j = 0; j < CH; ++j) fetch(tid + j * NT, v[j]);
-  float top = 0.f;
+  uint32_t bits = 0;
   auto raise = [&](const float* a) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = raised(top, a[i]);
+    for (int i = 0; i < 8; ++i) bits = raised(bits, a[i]);
   };
 #pragma unroll
   for (int j = 0; j < CH; ++j) raise(v[j]);
@@ -42,8 +42,8 @@ __global__ __launch_bounds__(256) void token_quantize_kernel(const T* __restrict
     fetch(c, a);
     raise(a);
   }
-  top = NT == 64 ? wave_max(top) : block_max(top);
-  const RowScale scale(top);
+  const float top = top_of(bits);
+  const RowScale scale(NT == 64 ? wave_max(top) : block_max(top));
   if (tid == 0) scales[row] = scale.scale();
   uint2* dst = reinterpret_cast<uint2*>(codes + row * pitch);
   auto put = [&](int c, const float* a) __attribute__((always_inline)) {
@@ -61,10 +61,12 @@ __global__ __launch_bounds__(256) void token_quantize_kernel(const T* __restrict
 template <typename T, bool WIDE>
 int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitch, int8_t* codes, float* scales, hipStream_t st) {
   const T* p = (const T*)x;
-  if (pitch <= 2048 && rows > 512)
-    PIPE_KLAUNCH((token_quantize_kernel<T, 64, 4, WIDE>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p, rows, in, stride, pitch, codes, scales);
-  else
-    PIPE_KLAUNCH((token_quantize_kernel<T, 256, 4, WIDE>), dim3((unsigned)rows), dim3(256), 0, st, p, rows, in, stride, pitch, codes, scales);
+  // a wave a row where there are many of up to 4096 values: no barrier (4096 rows of 4096: fp32 21.5 -> 19.0 us)
+  const dim3 by_wave((unsigned)((rows + 3) / 4)), by_group((unsigned)rows), block(256);
+  if (pitch <= 2048 && rows > 512) PIPE_KLAUNCH((token_quantize_kernel<T, 64, 4, WIDE>), by_wave, block, 0, st, p, rows, in, stride, pitch, codes, scales);
+  else if (pitch <= 4096 && rows > 512) PIPE_KLAUNCH((token_quantize_kernel<T, 64, 8, WIDE>), by_wave, block, 0, st, p, rows, in, stride, pitch, codes, scales);
+  else if (pitch <= 4096) PIPE_KLAUNCH((token_quantize_kernel<T, 256, 2, WIDE>), by_group, block, 0, st, p, rows, in, stride, pitch, codes, scales);
+  else PIPE_KLAUNCH((token_quantize_kernel<T, 256, 4, WIDE>), by_group, block, 0, st, p, rows, in, stride, pitch, codes, scales);
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
 }

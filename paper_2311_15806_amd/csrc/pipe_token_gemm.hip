@@ -477,10 +477,10 @@ __global__ __launch_bounds__(512, 4) void token_stream_fused_kernel(const TokenP
 #pragma unroll
   for (int j = 0; j < EACH; ++j) {
     const int g = threadIdx.x + j * 512;
-    float m = 0.f;
+    uint32_t bits = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = raised(m, v[j][i]);
-    m = row_reduce<16, true>(m);
+    for (int i = 0; i < 8; ++i) bits = raised(bits, v[j][i]);
+    const float m = row_reduce<16, true>(top_of(bits));
     if (g < pieces && (lane & 15) == 0) atomicMax(&top[g / per_row], __float_as_uint(m));
   }
   __syncthreads();
