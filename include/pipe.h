@@ -679,7 +679,8 @@ int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_de
  *
  * x has a row stride in elements (>= 0), its rows are dense; 16-byte aligned addresses and strides are read with wider loads.  y is dense, 16-byte aligned, and must not
  * overlap an input.  1 <= in <= 130944.  All calls are asynchronous on `stream`, allocate nothing, use no library scratch and may be captured
- * into a graph at any time.  scratch_dev: pipe_token_scratch(T, in) bytes, 16-byte aligned, of the caller's, in use until the call has run on the stream.    */
+ * into a graph at any time.  scratch_dev: pipe_token_scratch(T, in) bytes, 16-byte aligned, of the caller's, in use until the call has run on the stream.
+ * NULL is PIPE_EINVAL unless the call makes its codes in the one launch that also multiplies, which calls of few rows do (rows of y * pitch <= 8192).  */
 int pipe_token_pitch(int in);                                  /* 0: no such row */
 int64_t pipe_token_scratch(int64_t rows, int in);              /* -1: no such rows */
 /* Errors: PIPE_EINVAL (NULL, type, alignment), PIPE_ESHAPE (rows < 0 or >= 2^30, in, stride).                       */

@@ -958,6 +958,15 @@ def _layer_width(codes: torch.Tensor, n_in: int, act: int, lead: int) -> int:
     return shape[-2] // 2
 
 
+def _with_scratch(T: int, pitch: int, rows: int, like: torch.Tensor, where: str, call) -> None:
+    """A layer's call with room for the codes of its T inputs; without, where it may not need any (it says so by refusing)."""
+    code = call(None) if rows * pitch <= 8192 else -1
+    if code == -1:
+        scratch = torch.empty(T * (pitch + 4), dtype=torch.uint8, device=like.device)
+        code = call(scratch.data_ptr())
+    _check(code, where)
+
+
 def pipe_token_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
                        act: int = PIPE_ACT_NONE, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(x W^T + bias) [T, out] of x's type, both sides in 8 bits: x [T, in] with a scale for each token (pipe_token_quantize, inside), W as
@@ -971,9 +980,8 @@ def pipe_token_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
     lead = codes.shape[:-1]
     sp = _dense(scales, torch.float32, lead, "scales", dev)
     bp = None if bias is None else _dense(bias, torch.float32, lead, "bias", dev)
-    scratch = torch.empty(T * (codes.shape[-1] + 4), dtype=torch.uint8, device=x.device)
-    _check(_lib.pipe_token_forward(xp, _type(x.dtype), T, n, stride, cp, sp, bp, width, act, scratch.data_ptr(), y.data_ptr(), _stream()),
-           "pipe_token_forward")
+    _with_scratch(T, codes.shape[-1], T, x, "pipe_token_forward",
+                  lambda scratch: _lib.pipe_token_forward(xp, _type(x.dtype), T, n, stride, cp, sp, bp, width, act, scratch, y.data_ptr(), _stream()))
     return y
 
 
@@ -989,14 +997,14 @@ def pipe_expert_scratch(tokens: int, top_k: int, num_experts: int) -> int:
     return n
 
 
-def _tables(n: int, T: int, k: int, E: int, like: torch.Tensor):
-    """(room for starts and scratch, n tables [T, k], addresses of starts and scratch), int32."""
-    pairs = T * k
-    extra = 0 if pairs <= 481 else pipe_expert_scratch(T, k, E) // 4      # (a block is at least 481 pairs)
+def _starts(T: int, k: int, E: int, like: torch.Tensor):
+    """(starts [E + 1], address of the calls' scratch)"""
+    extra = 0 if T * k <= 481 else pipe_expert_scratch(T, k, E) // 4      # (481 pairs need none, whatever k)
+    if extra == 0:
+        return like.new_empty(E + 1, dtype=torch.int32), None
     at = (E + 2) // 2 * 2
-    room = torch.empty(at + extra, dtype=torch.int32, device=like.device)
-    starts = room.data_ptr()
-    return room, torch.empty((n, T, k), dtype=torch.int32, device=like.device).unbind(0), starts, starts + 4 * at
+    room = like.new_empty(at + extra, dtype=torch.int32)
+    return room[:E + 1], room.data_ptr() + 4 * at
 
 
 def pipe_expert_route(logits: torch.Tensor, top_k: int, renormalize: bool = True):
@@ -1007,12 +1015,11 @@ def pipe_expert_route(logits: torch.Tensor, top_k: int, renormalize: bool = True
     T, E = logits.shape
     if not 1 <= top_k <= 32:
         raise ValueError("top_k must be 1 to 32")
-    room, tables, sp, cp = _tables(3, T, top_k, E, logits)
-    experts, order, places = tables
-    weights = torch.empty((T, top_k), dtype=torch.float32, device=logits.device)
-    _check(_lib.pipe_expert_route(lp, _type(logits.dtype), T, E, stride, top_k, 1 if renormalize else 0, experts.data_ptr(), weights.data_ptr(), sp,
-                                  order.data_ptr(), places.data_ptr(), cp, _stream()), "pipe_expert_route")
-    return experts, weights, room[:E + 1], order.view(-1), places
+    starts, scratch = _starts(T, top_k, E, logits)
+    experts, weights, order, places = logits.new_empty((4, T, top_k), dtype=torch.int32).unbind(0)
+    _check(_lib.pipe_expert_route(lp, _type(logits.dtype), T, E, stride, top_k, 1 if renormalize else 0, experts.data_ptr(), weights.data_ptr(),
+                                  starts.data_ptr(), order.data_ptr(), places.data_ptr(), scratch, _stream()), "pipe_expert_route")
+    return experts, weights.view(torch.float32), starts, order.view(-1), places
 
 
 def pipe_expert_sort(experts: torch.Tensor, num_experts: int):
@@ -1025,10 +1032,10 @@ def pipe_expert_sort(experts: torch.Tensor, num_experts: int):
     ep = _ints(experts, dev)
     if not 1 <= num_experts <= 1024 or not 1 <= k <= 32:
         raise ValueError("1 to 1024 experts, 1 to 32 of them a token")
-    room, (order, places), sp, cp = _tables(2, T, k, num_experts, experts)
-    _check(_lib.pipe_expert_sort(ep, T, k, num_experts, sp, order.data_ptr(), places.data_ptr(), cp, _stream()),
-           "pipe_expert_sort")
-    return room[:num_experts + 1], order.view(-1), places
+    starts, scratch = _starts(T, k, num_experts, experts)
+    order, places = experts.new_empty((2, T, k)).unbind(0)
+    _check(_lib.pipe_expert_sort(ep, T, k, num_experts, starts.data_ptr(), order.data_ptr(), places.data_ptr(), scratch, _stream()), "pipe_expert_sort")
+    return starts, order.view(-1), places
 
 
 def pipe_expert_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, starts: torch.Tensor, order: Optional[torch.Tensor] = None,
@@ -1049,9 +1056,9 @@ def pipe_expert_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tens
     lead = codes.shape[:-1]
     sp = _dense(scales, torch.float32, lead, "scales", dev)
     bp = None if bias is None else _dense(bias, torch.float32, lead, "bias", dev)
-    scratch = torch.empty(T * (codes.shape[-1] + 4), dtype=torch.uint8, device=x.device)
-    _check(_lib.pipe_expert_forward(xp, _type(x.dtype), T, n, stride, cp, sp, bp, E, width, _ints(starts, dev), None if order is None else _ints(order, dev),
-                                    rows, top_k, act, scratch.data_ptr(), y.data_ptr(), _stream()), "pipe_expert_forward")
+    _with_scratch(T, codes.shape[-1], rows, x, "pipe_expert_forward",
+                  lambda scratch: _lib.pipe_expert_forward(xp, _type(x.dtype), T, n, stride, cp, sp, bp, E, width, _ints(starts, dev),
+                                                           None if order is None else _ints(order, dev), rows, top_k, act, scratch, y.data_ptr(), _stream()))
     return y
 
 

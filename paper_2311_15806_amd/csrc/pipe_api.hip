@@ -2526,12 +2526,12 @@ static int token_layer(const void* x_dev, int type, int64_t rows, int in, int64_
     return PIPE_ESHAPE;
   if (a.n == 0) return PIPE_OK;
   if (!a.w || !a.sw || !a.y || !aligned16(a.w) || !aligned16(a.y)) return PIPE_EINVAL;
-  if (rows > 0 && (!x_dev || !scratch_dev || !aligned16(scratch_dev))) return PIPE_EINVAL;
+  if (rows > 0 && (!x_dev || !aligned16(scratch_dev))) return PIPE_EINVAL;
   if (rows == 0) return PIPE_ESHAPE;      // rows of y without an input
   a.type = type;
   a.n_x = rows;
   int8_t* codes = (int8_t*)scratch_dev;
-  float* scales = (float*)(codes + rows * a.pitch);
+  float* scales = codes ? (float*)(codes + rows * a.pitch) : nullptr;
   a.x = x_dev; a.x_stride = row_stride; a.in = in;
   return launch_token_layer(a, codes, scales, (hipStream_t)stream);
 }

@@ -24,7 +24,7 @@ struct TokenProductArgs {
   int top_k, E, pitch, out, act, type;
   void* y;                 // [n][out]
 };
-int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStream_t st);   // (codes, scales: room for the inputs')
+int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStream_t st);   // (codes, scales: room for the inputs', or nullptr)
 extern int g_token_kernel;   // 0: by the sizes; 1 to 4: see pipe_set_token_kernel
 
 struct ExpertRouteArgs {

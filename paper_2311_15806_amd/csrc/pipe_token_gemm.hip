@@ -801,6 +801,7 @@ int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStr
     a.x_wide = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride % n_wide == 0;
     return gated ? launch_fused<true>(a, o_tiles, st) : launch_fused<false>(a, o_tiles, st);
   }
+  if (codes == nullptr) return PIPE_EINVAL;
   a.qx = codes;
   a.sx = scales;
   const int rc = launch_token_quantize(a.x, a.type, a.n_x, a.in, a.x_stride, a.pitch, codes, scales, st);

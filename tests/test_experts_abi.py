@@ -61,8 +61,10 @@ def experts(lib, **o):
 
 def test_layer_refusals(lib):
     for f in (forward, experts):
-        for name in ("x", "codes", "scales", "scratch", "y"):
+        for name in ("x", "codes", "scales", "y"):
             assert f(lib, **{name: None}) == EINVAL, name
+        for T in (65, 100000):                   # more than 8192 codes need room
+            assert f(lib, T=I(T), scratch=None, **({"rows": I(2 * T)} if f is experts else {})) == EINVAL
         for bad in (dict(type=4), dict(act=4), dict(act=-1), dict(codes=ODD), dict(y=ODD), dict(scratch=ODD)):
             assert f(lib, **bad) == EINVAL, bad
         for bad in (dict(T=I(-1)), dict(T=I(1 << 30)), dict(n=0), dict(n=131000), dict(stride=I(-1)), dict(out=0), dict(out=(1 << 28) + 1)):
