@@ -677,10 +677,11 @@ int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_de
  * gate's first, y = SiLU(gate) * up.  scale and bias vectors are fp32, bias_dev NULL = none; everything behind the sum is fp32, y is rounded once to x's
  * type.  Any finite scales whose product with the sum is finite.
  *
- * x has a row stride in elements (>= 0), its rows are dense; 16-byte aligned addresses and strides are read with wider loads.  y is dense, 16-byte aligned, and must not
- * overlap an input.  1 <= in <= 130944.  All calls are asynchronous on `stream`, allocate nothing, use no library scratch and may be captured
+ * x has a row stride in elements (>= 0), its rows are dense; 16-byte aligned addresses and strides are read with wider loads.  y is dense, 16-byte aligned, and may
+ * overlap x, but nothing else that the call reads.  1 <= in <= 130944.  All calls are asynchronous on `stream`, allocate nothing, use no library scratch and may be captured
  * into a graph at any time.  scratch_dev: pipe_token_scratch(T, in) bytes, 16-byte aligned, of the caller's, in use until the call has run on the stream.
- * NULL is PIPE_EINVAL unless the call makes its codes in the one launch that also multiplies, which calls of few rows do (rows of y * pitch <= 8192).  */
+ * NULL is PIPE_EINVAL unless the call makes its codes in the one launch that also multiplies, which calls of few rows do (rows of y * pitch <= 8192).
+ * Launches of 2^23 tiles or more (16 outputs x 16 tokens of few tokens, 64 x 64 and more of many) are refused, PIPE_ESHAPE.                          */
 int pipe_token_pitch(int in);                                  /* 0: no such row */
 int64_t pipe_token_scratch(int64_t rows, int in);              /* -1: no such rows */
 /* Errors: PIPE_EINVAL (NULL, type, alignment), PIPE_ESHAPE (rows < 0 or >= 2^30, in, stride).                       */
@@ -691,7 +692,8 @@ int pipe_token_forward(const void* x_dev, int type, int64_t T, int in, int64_t r
                        const float* scales_dev, const float* bias_dev, int out, int act, void* scratch_dev, void* y_dev, void* stream);
 
 /* Kernel of pipe_token_forward and pipe_expert_forward (tuning and tests): 0 = by the sizes (default), 1 = weights streamed past up to 32 tokens at a
- * time, 2, 3, 4 = tiles of 64, 128, 256 tokens.  (Gathered inputs of more than 4 GiB of codes are always streamed past.)  Results do not depend on the
+ * time, 2, 3, 4 = tiles of 64, 128, 256 tokens.  (Gathered inputs of more than 4 GiB of codes
+ * have tiles of 128 tokens of their own.)  Results do not depend on the
  * setting.  Returns PIPE_EINVAL for other values.                                                                   */
 int pipe_set_token_kernel(int which);
 
@@ -725,6 +727,7 @@ int pipe_expert_forward(const void* x_dev, int type, int64_t T, int in, int64_t 
 
 /* Back to the tokens: out[t] = sum_j weights[t][j] * y[places[t][j]] in fp32, j ascending, rounded once to y's type (out_dev dense [T][out]); a choice
  * whose place is outside 0 .. rows-1 is left out, whatever its weight; a token without any is zeros.
+ * out_dev must not overlap an input.
  * Errors: PIPE_EINVAL (NULL, type), PIPE_ESHAPE (T, top_k, rows, out, stride).                                     */
 int pipe_expert_combine(const void* y_dev, int type, int64_t rows, int out, int64_t row_stride, const int32_t* places_dev,
                         const float* weights_dev, int T, int top_k, void* out_dev, void* stream);

@@ -2595,7 +2595,7 @@ extern "C" int pipe_expert_route(const void* logits_dev, int type, int T, int E,
 extern "C" int pipe_expert_combine(const void* y_dev, int type, int64_t rows, int out, int64_t row_stride, const int32_t* places_dev,
                                    const float* weights_dev, int T, int top_k, void* out_dev, void* stream) {
   if (!known_type(type)) return PIPE_EINVAL;
-  if (!router_ok(T, 1, top_k) || !rows_fit(rows) || out < 1 || out > 1 << 28 || row_stride < 0 || (int64_t)T * ((out + 7) / 8) >= (int64_t)1 << 38)
+  if (!router_ok(T, 1, top_k) || !rows_fit(rows) || out < 1 || out > 1 << 28 || row_stride < 0)
     return PIPE_ESHAPE;
   if (T == 0) return PIPE_OK;
   if (!places_dev || !weights_dev || !out_dev || (rows > 0 && !y_dev)) return PIPE_EINVAL;

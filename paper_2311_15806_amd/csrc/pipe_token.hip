@@ -7,6 +7,8 @@
 
 namespace {
 
+constexpr int64_t MOST_BLOCKS = 1 << 23;      // workgroups of 256 threads a launch
+
 // ------------------------------------------------------------------ rows to codes
 // s = max|x| / 127, c = rint(x / s): NT threads a row, 8 values a thread and step, the first CH steps kept in registers between the maximum
 // and the codes, the rest (rows of more than 8 NT CH values) read again.  A row with a NaN or an infinity has the maximum +infinity here.
@@ -14,47 +16,47 @@ template <typename T, int NT, int CH, bool WIDE>
 __global__ __launch_bounds__(256) void token_quantize_kernel(const T* __restrict__ x, int64_t rows, int in, int64_t stride, int pitch,
                                                              int8_t* __restrict__ codes, float* __restrict__ scales) {
   constexpr int PER = 256 / NT;
-  const int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / NT;
-  const int tid = threadIdx.x % NT;
-  if (PER > 1 && row >= rows) return;      // (a whole wave: no barrier follows)
-  const T* xr = x + row * stride;
-  const int n_chunk = (in + 7) >> 3;
-  auto fetch = [&](int c, float* v) __attribute__((always_inline)) {
-    if (c * 8 + 8 <= in) {
-      load8<T, WIDE>(xr + c * 8, v);
-    } else {
+  const int tid = threadIdx.x % NT, n_chunk = (in + 7) >> 3;
+  // (a launch holds fewer than 2^32 threads, rows are up to 2^30)
+  for (int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / NT; row < rows; row += (int64_t)gridDim.x * PER) {
+    const T* xr = x + row * stride;
+    auto fetch = [&](int c, float* v) __attribute__((always_inline)) {
+      if (c * 8 + 8 <= in) {
+        load8<T, WIDE>(xr + c * 8, v);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = c * 8 + i < in ? to_f(xr[c * 8 + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = c * 8 + i < in ? to_f(xr[c * 8 + i]) : 0.f;
+      }
+    };
+    float v[CH][8];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) fetch(tid + j * NT, v[j]);
+    uint32_t bits = 0;
+    auto raise = [&](const float* a) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) bits = raised(bits, a[i]);
+    };
+#pragma unroll
+    for (int j = 0; j < CH; ++j) raise(v[j]);
+    for (int c = tid + CH * NT; c < n_chunk; c += NT) {
+      float a[8];
+      fetch(c, a);
+      raise(a);
     }
-  };
-  float v[CH][8];
+    const float top = top_of(bits);
+    const RowScale scale(NT == 64 ? wave_max(top) : block_max(top));
+    if (tid == 0) scales[row] = scale.scale();
+    uint2* dst = reinterpret_cast<uint2*>(codes + row * pitch);
+    auto put = [&](int c, const float* a) __attribute__((always_inline)) {
+      if (c * 8 < pitch) dst[c] = scale.codes8(a);
+    };
 #pragma unroll
-  for (int j = 0; j < CH; ++j) fetch(tid + j * NT, v[j]);
-  uint32_t bits = 0;
-  auto raise = [&](const float* a) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) bits = raised(bits, a[i]);
-  };
-#pragma unroll
-  for (int j = 0; j < CH; ++j) raise(v[j]);
-  for (int c = tid + CH * NT; c < n_chunk; c += NT) {
-    float a[8];
-    fetch(c, a);
-    raise(a);
-  }
-  const float top = top_of(bits);
-  const RowScale scale(NT == 64 ? wave_max(top) : block_max(top));
-  if (tid == 0) scales[row] = scale.scale();
-  uint2* dst = reinterpret_cast<uint2*>(codes + row * pitch);
-  auto put = [&](int c, const float* a) __attribute__((always_inline)) {
-    if (c * 8 < pitch) dst[c] = scale.codes8(a);
-  };
-#pragma unroll
-  for (int j = 0; j < CH; ++j) put(tid + j * NT, v[j]);
-  for (int c = tid + CH * NT; c * 8 < pitch; c += NT) {
-    float a[8];
-    fetch(c, a);
-    put(c, a);
+    for (int j = 0; j < CH; ++j) put(tid + j * NT, v[j]);
+    for (int c = tid + CH * NT; c * 8 < pitch; c += NT) {
+      float a[8];
+      fetch(c, a);
+      put(c, a);
+    }
   }
 }
 
@@ -62,7 +64,7 @@ template <typename T, bool WIDE>
 int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitch, int8_t* codes, float* scales, hipStream_t st) {
   const T* p = (const T*)x;
   // a wave a row where there are many of up to 4096 values: no barrier (4096 rows of 4096: fp32 21.5 -> 19.0 us)
-  const dim3 by_wave((unsigned)((rows + 3) / 4)), by_group((unsigned)rows), block(256);
+  const dim3 by_wave((unsigned)std::min<int64_t>((rows + 3) / 4, MOST_BLOCKS)), by_group((unsigned)std::min<int64_t>(rows, MOST_BLOCKS)), block(256);
   if (pitch <= 2048 && rows > 512) PIPE_KLAUNCH((token_quantize_kernel<T, 64, 4, WIDE>), by_wave, block, 0, st, p, rows, in, stride, pitch, codes, scales);
   else if (pitch <= 4096 && rows > 512) PIPE_KLAUNCH((token_quantize_kernel<T, 64, 8, WIDE>), by_wave, block, 0, st, p, rows, in, stride, pitch, codes, scales);
   else if (pitch <= 4096) PIPE_KLAUNCH((token_quantize_kernel<T, 256, 2, WIDE>), by_group, block, 0, st, p, rows, in, stride, pitch, codes, scales);
@@ -180,7 +182,7 @@ __device__ __forceinline__ int pairs_of(const SortArgs& a, int b) {
 }
 __device__ __forceinline__ int key_of(int expert, int E) { return (unsigned)expert < (unsigned)E ? expert : E; }
 extern __shared__ int sort_lds[];
-static size_t sort_lds_bytes(int E) { return (size_t)(E + 1) * (2 * sizeof(int) + PAIRS / 64 * sizeof(uint16_t)); }   // (41 KiB at most)
+static size_t sort_lds_bytes(int E) { return (size_t)(E + 1) * (2 * sizeof(int) + PAIRS / 64 * sizeof(uint16_t)); }   // (24 KiB at most)
 
 __global__ __launch_bounds__(PAIRS) void expert_place_kernel(const int32_t* __restrict__ experts, const SortArgs a) {
   const int b = blockIdx.x, n = pairs_of(a, b);
@@ -288,39 +290,39 @@ template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void expert_combine_kernel(const T* __restrict__ y, int64_t n, int H, int64_t stride, const int32_t* __restrict__ places,
                                                              const float* __restrict__ weights, int64_t items, int top_k, T* __restrict__ out) {
   const int chunks = (H + 7) >> 3;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= items) return;
-  const int64_t t = id / chunks;
-  const int c = (int)(id - t * chunks) * 8, have = min(8, H - c);
-  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  for (int j = 0; j < top_k; ++j) {
-    const int64_t p = places[t * top_k + j];
-    if (p < 0 || p >= n) continue;
-    const float w = weights[t * top_k + j];
-    const T* src = y + p * stride + c;
-    float v[8];
-    if (have == 8) {
-      load8<T, WIDE>(src, v);
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < items; id += (int64_t)gridDim.x * 256) {
+    const int64_t t = id / chunks;
+    const int c = (int)(id - t * chunks) * 8, have = min(8, H - c);
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < top_k; ++j) {
+      const int64_t p = places[t * top_k + j];
+      if (p < 0 || p >= n) continue;
+      const float w = weights[t * top_k + j];
+      const T* src = y + p * stride + c;
+      float v[8];
+      if (have == 8) {
+        load8<T, WIDE>(src, v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < have ? to_f(src[i]) : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+    }
+    T* dst = out + t * H + c;
+    if (WIDE && have == 8) {
+      Vec8<T> r;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r.v[i] = from_f<T>(sum[i]);
+      uint4 w[sizeof(T) / 2];
+      __builtin_memcpy(w, &r, sizeof r);
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(dst)[i] = w[i];
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < have ? to_f(src[i]) : 0.f;
+      for (int i = 0; i < 8; ++i)
+        if (i < have) dst[i] = from_f<T>(sum[i]);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
-  }
-  T* dst = out + t * H + c;
-  if (WIDE && have == 8) {
-    Vec8<T> r;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = from_f<T>(sum[i]);
-    uint4 w[sizeof(T) / 2];
-    __builtin_memcpy(w, &r, sizeof r);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(dst)[i] = w[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < have) dst[i] = from_f<T>(sum[i]);
   }
 }
 
@@ -343,7 +345,7 @@ template <typename T>
 int combine_typed(const void* y, int64_t n, int H, int64_t stride, const int32_t* places, const float* weights, int T_, int top_k, void* out,
                   hipStream_t st) {
   const int64_t items = (int64_t)T_ * ((H + 7) / 8);
-  const dim3 grid((unsigned)((items + 255) / 256));
+  const dim3 grid((unsigned)std::min<int64_t>((items + 255) / 256, MOST_BLOCKS));
   constexpr int V = 16 / (int)sizeof(T);
   const bool wide = ((reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(out)) & 15) == 0 && stride % V == 0 && H % V == 0;
   if (wide)

@@ -228,11 +228,13 @@ __device__ __forceinline__ const int8_t* uniform(const int8_t* p) {
   return reinterpret_cast<const int8_t*>((uint64_t)hi << 32 | lo);
 }
 // Where a wave's loads of 8 rows x 128 codes come from: row `first` + 8 p + (lane >> 3) of the tile's B rows of weights (first < B) or of its tokens.
-// Addresses are a resource's base and 32 bits; of a gated layer 16 rows of the gate and of the other half in turn.
-template <bool GATED, int B, int P>
+// Addresses are a resource's base and 32 bits, FAR: of tokens 64 bits; of a gated layer 16 rows of the gate and of the other half in turn.
+template <bool GATED, int B, int P, bool FAR = false>
 struct Source {
   const int8_t *b0, *b1;
   unsigned off[P];
+  const int8_t* far[FAR ? P : 1];
+  bool by_far;
   __device__ __forceinline__ Source(const TokenProductArgs& a, const Rows& r, int o0, int first) {
     const int lane = threadIdx.x & 63;
     const bool weights = first < B;
@@ -251,10 +253,13 @@ struct Source {
       if (weights) at = min(o0 + (GATED ? (row >> 5) * 16 + (row & 15) : row), a.out - 1) - o0;
       else at = max(input_of(a, r, row - B), (int64_t)0) - (a.order ? 0 : r.row);
       off[p] = (unsigned)(at * a.pitch) + (lane & 7) * 16;
+      if (FAR) far[p] = b0 + at * a.pitch + (lane & 7) * 16;
     }
+    by_far = FAR && !weights;
   }
   // load p of the codes from k on; zeros, without an access, where there are none
   __device__ __forceinline__ v4i load(int p, int k, int pitch) const {
+    if (FAR && by_far) return (v4i)gload16(far[p] + min(k, pitch - 128));      // (behind the end the last codes again, for a slot that nobody reads)
     const __amdgpu_buffer_rsrc_t from =
         __builtin_amdgcn_make_buffer_rsrc((void*)uniform(((p >> 1) & 1) ? b1 : b0), 0, __builtin_amdgcn_readfirstlane(k < pitch ? 0xffffffffu : 0u), 0x00020000);
     return (v4i)__builtin_amdgcn_raw_buffer_load_b128(from, off[p], k, 0);
@@ -531,7 +536,7 @@ __global__ __launch_bounds__(512, 4) void token_stream_fused_kernel(const TokenP
 // B rows of weights x B tokens a workgroup of four waves, a quarter each.  A stage is 128 codes of every row; the eight pieces of 16 of a row lie in
 // LDS in an order that differs by pairs of rows, so that the reads of 16 rows' same piece meet all banks.  One stage is in LDS ahead, D more are in
 // registers or on their way there.
-template <bool GATED, int B, int D>
+template <bool GATED, int B, int D, bool FAR>
 __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void token_tile_kernel(const TokenProductArgs a, int o_tiles) {
   constexpr int KB = 128, P = B / 16, F = B / 32, WIDTH = GATED ? B / 2 : B, SLOT = 2 * B * KB / 16;
   __shared__ alignas(1024) v4i slots[2 * SLOT];
@@ -541,7 +546,7 @@ __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void token_tile_kernel(const
   if (!place_of(o_tiles, live_tiles<B>(a), &ot, &id)) return;
   const Rows r = find_rows<B>(a, id);
   const int o0 = ot * WIDTH;
-  const Source<GATED, B, P> src(a, r, o0, wave * (B / 2));
+  const Source<GATED, B, P, FAR> src(a, r, o0, wave * (B / 2));
   v4i st[D][P];
   auto ask = [&](v4i (&q)[P], int k) __attribute__((always_inline)) {
 #pragma unroll
@@ -717,7 +722,7 @@ __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArg
 }
 
 // ------------------------------------------------------------------ launches
-enum { AUTOMATIC = 0, STREAM = 1, TILES_64 = 2, TILES_128 = 3, TILES_256 = 4 };   // see pipe_set_token_kernel
+enum { AUTOMATIC = 0, STREAM = 1, TILES_64 = 2, TILES_128 = 3, TILES_256 = 4, TILES_FAR = 5 };   // see pipe_set_token_kernel
 
 template <int TB, int S>
 int launch_stream_split(const TokenProductArgs& a, bool gated, int o_tiles, int tiles, hipStream_t st) {
@@ -731,7 +736,7 @@ template <int TB>
 int launch_stream(const TokenProductArgs& a, bool gated, hipStream_t st) {
   const int o_tiles = (a.out + 15) / 16;
   const int64_t tiles = (int64_t)o_tiles * row_tiles<16 * TB>(a);
-  if (tiles > 0x7fffffff - 8) return PIPE_ESHAPE;
+  if (tiles >= (int64_t)1 << 23) return PIPE_ESHAPE;      // (a launch holds fewer than 2^32 threads)
   // as many waves a tile as keep about four to eight a SIMD (32 tokens, six of 64 experts: one wave 80 us, four 100, eight 106; 16 tokens of
   // 4096-11008, gated: eight 27, four 30, one 48)
   if (tiles <= 1024) return launch_stream_split<TB, 8>(a, gated, o_tiles, (int)tiles, st);
@@ -739,18 +744,18 @@ int launch_stream(const TokenProductArgs& a, bool gated, hipStream_t st) {
   return launch_stream_split<TB, 1>(a, gated, o_tiles, (int)tiles, st);
 }
 
-template <int B>
+template <int B, bool FAR = false>
 int launch_tiles(const TokenProductArgs& a, bool gated, hipStream_t st) {
   const int width = gated ? B / 2 : B;
   const int64_t o_tiles = (a.out + width - 1) / width, t_tiles = row_tiles<B>(a);
-  if (o_tiles * t_tiles > 0x7ffffff0) return PIPE_ESHAPE;
+  if (o_tiles * t_tiles > ((int64_t)1 << 23) - 8) return PIPE_ESHAPE;
   const dim3 grid((unsigned)((o_tiles * t_tiles + 7) / 8 * 8));
   if constexpr (B == 256) {
     if (gated) PIPE_KLAUNCH((token_big_kernel<true>), grid, dim3(512), 0, st, a, (int)o_tiles);
     else PIPE_KLAUNCH((token_big_kernel<false>), grid, dim3(512), 0, st, a, (int)o_tiles);
   } else {
-    if (gated) PIPE_KLAUNCH((token_tile_kernel<true, B, B == 128 ? 2 : 3>), grid, dim3(256), 0, st, a, (int)o_tiles);
-    else PIPE_KLAUNCH((token_tile_kernel<false, B, B == 128 ? 2 : 3>), grid, dim3(256), 0, st, a, (int)o_tiles);
+    if (gated) PIPE_KLAUNCH((token_tile_kernel<true, B, B == 128 ? 2 : 3, FAR>), grid, dim3(256), 0, st, a, (int)o_tiles);
+    else PIPE_KLAUNCH((token_tile_kernel<false, B, B == 128 ? 2 : 3, FAR>), grid, dim3(256), 0, st, a, (int)o_tiles);
   }
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
@@ -780,7 +785,7 @@ static int kernel_of(const TokenProductArgs& a) {
       which = t64 <= t128 && t64 <= t256 ? TILES_64 : t128 <= t256 ? TILES_128 : TILES_256;
     }
   }
-  return near(a) ? which : STREAM;
+  return near(a) || which == STREAM ? which : TILES_FAR;
 }
 
 template <bool GATED>
@@ -797,7 +802,11 @@ int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStr
   const bool gated = a.act == PIPE_ACT_SILU_GATED;
   const int which = kernel_of(a);
   const int n_wide = 16 / type_size(a.type), o_tiles = (a.out + 15) / 16;
-  if (which == STREAM && a.n * a.pitch <= FUSED_CODES && o_tiles * row_tiles<16>(a) <= FUSED_TILES) {
+  // (every workgroup reads x while others write y: not where these overlap)
+  const char *x0 = (const char*)a.x, *y0 = (const char*)a.y;
+  const int64_t size = type_size(a.type);
+  const bool apart = x0 + ((a.n_x - 1) * a.x_stride + a.in) * size <= y0 || y0 + a.n * a.out * size <= x0;
+  if (which == STREAM && apart && a.n * a.pitch <= FUSED_CODES && o_tiles * row_tiles<16>(a) <= FUSED_TILES) {
     a.x_wide = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride % n_wide == 0;
     return gated ? launch_fused<true>(a, o_tiles, st) : launch_fused<false>(a, o_tiles, st);
   }
@@ -810,5 +819,6 @@ int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStr
   if (which == TILES_256) return launch_tiles<256>(a, gated, st);
   if (which == TILES_128) return launch_tiles<128>(a, gated, st);
   if (which == TILES_64) return launch_tiles<64>(a, gated, st);
+  if (which == TILES_FAR) return launch_tiles<128, true>(a, gated, st);
   return each <= 16 ? launch_stream<1>(a, gated, st) : launch_stream<2>(a, gated, st);
 }

@@ -242,6 +242,28 @@ def test_forward_of_slices_into_an_output(pipe):
         close(y, *ref.linear(v[:, a:a + 300], w, s, None, "none", "bf16"))
 
 
+@pytest.mark.parametrize("T,kind", [(1, "f32"), (1, "bf16"), (5, "f16"), (40, "f32"), (700, "bf16")])
+def test_forward_over_its_own_input(pipe, T, kind):
+    """An output that is the input, or shares some of its memory."""
+    rng = np.random.default_rng(T)
+    cw, sw, w, s = weights(rng, (), 1024, 1024)
+    for shift in (0, 64):
+        room = torch.zeros(T * 1024 + 64, dtype=DT[kind], device="cuda")
+        x, v = typed(rng, (T, 1024), kind)
+        room[:T * 1024] = x.flatten()
+        y = pipe.pipe_token_forward(room[:T * 1024].view(T, 1024), cw, sw, out=room[shift:shift + T * 1024].view(T, 1024))
+        close(y, *ref.linear(v, w, s, None, "none", kind))
+
+
+def test_quantize_of_more_rows_than_a_launch_has_waves(pipe):
+    rows = (1 << 25) + 5
+    x = torch.ones(rows, 1, dtype=torch.bfloat16, device="cuda")
+    x[::2] = -2
+    c, s = pipe.pipe_token_quantize(x)
+    assert bool((c[::2, 0] == -127).all()) and bool((c[1::2, 0] == 127).all())
+    assert bool((s[::2] == s[0]).all()) and bool((s[1::2] == s[1]).all()) and float(s[0]) == 2 * float(s[1])
+
+
 # ------------------------------------------------------------------ the router
 
 ROUTES = [
@@ -396,7 +418,7 @@ def test_experts_beyond_4_gib(pipe, kernel):
     pick = rng.integers(0, out, 200)
     pick[-1] = out - 1
     at = torch.from_numpy(pick).cuda()
-    some = torch.randint(-127, 128, (E, 200, n), dtype=torch.int8, device="cuda")
+    some = torch.from_numpy(rng.integers(-127, 128, (E, 200, n)).astype(np.int8)).cuda()
     codes[:, at] = some
     some = codes[:, at]                               # (a row picked twice holds one of them)
     x, v = typed(rng, (6, n), "f32")
@@ -404,6 +426,36 @@ def test_experts_beyond_4_gib(pipe, kernel):
     y = pipe.pipe_expert_forward(x, codes, sw, ints([0, 2, 3, 6]))
     want, far = ref.experts_layer(v, some.cpu().numpy(), np.ones((E, 200), np.float32), None, [0, 2, 3, 6], None, 1, 6, "none", "f32")
     close(y[:, at], want, far)
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_gathered_inputs_beyond_4_gib(pipe, which):
+    """Tokens whose codes lie past 32-bit offsets, in tiles and streamed past."""
+    T, n, E, out, k = 33000, 130944, 2, 40, 2                # 4.3e9 bytes of codes
+    rng = np.random.default_rng(1)
+    x = torch.zeros(T, n, dtype=torch.bfloat16, device="cuda")
+    rows = 300
+    order = rng.integers(0, T * k, rows)
+    order[-1], order[0], order[7] = T * k - 1, T * k - 2, -1
+    tokens = torch.from_numpy(np.unique(order[order >= 0] // k)).cuda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x[tokens] = torch.randn(tokens.numel(), n, generator=g, dtype=torch.bfloat16, device="cuda")
+    cw, sw, w, s = weights(rng, (E,), out, n)
+    starts = [0, 170, rows]
+    pipe.pipe_set_token_kernel(which)
+    try:
+        y = pipe.pipe_expert_forward(x, cw, sw, ints(starts), order=ints(order), top_k=k)
+    finally:
+        pipe.pipe_set_token_kernel(0)
+    few = np.unique(order[order >= 0] // k)                  # the same with the tokens that are named, next to each other
+    near = np.where(order >= 0, np.searchsorted(few, order // k) * k, -1)
+    assert torch.equal(y, pipe.pipe_expert_forward(x[tokens], cw, sw, ints(starts), order=ints(near), top_k=k))
+    want, far = ref.experts_layer(x[tokens[:20]].double().cpu().numpy(), w, s, None, [0, 20, 20], None, 1, 20, "none", "bf16")
+    at = [int(np.nonzero((order >= 0) & (order // k == t))[0][0]) for t in few[:20]]
+    here = [i for i, r in enumerate(at) if r < 170]
+    assert len(here) >= 3
+    close(y[[at[i] for i in here]], want[here], far[here])
 
 
 # ------------------------------------------------------------------ back to the tokens
