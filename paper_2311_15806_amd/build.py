@@ -31,7 +31,7 @@ SOURCES = [
     ("pipe_cache_attn.hip", []),
     ("pipe_prompt_attn.hip", []),
     ("pipe_token.hip", PRELOAD),
-    ("pipe_token_gemm.hip", []),
+    ("pipe_token_gemm.hip", ["-ffp-contract=off"]),
 ]
 
 COMMON = [
