@@ -1002,7 +1002,7 @@ def _starts(T: int, k: int, E: int, like: torch.Tensor):
     extra = 0 if T * k <= 481 else pipe_expert_scratch(T, k, E) // 4      # (481 pairs need none, whatever k)
     if extra == 0:
         return like.new_empty(E + 1, dtype=torch.int32), None
-    at = (E + 2) // 2 * 2
+    at = (E + 4) // 4 * 4
     room = like.new_empty(at + extra, dtype=torch.int32)
     return room[:E + 1], room.data_ptr() + 4 * at
 

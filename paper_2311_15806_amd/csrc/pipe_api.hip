@@ -2574,7 +2574,7 @@ extern "C" int pipe_expert_sort(const int32_t* experts_dev, int T, int top_k, in
                                 int32_t* places_dev, void* scratch_dev, void* stream) {
   if (!router_ok(T, E, top_k)) return PIPE_ESHAPE;
   if (!starts_dev || (T > 0 && (!experts_dev || !order_dev || !places_dev))) return PIPE_EINVAL;
-  if (expert_sort_scratch(T, top_k, E) > 0 && (!scratch_dev || (reinterpret_cast<uintptr_t>(scratch_dev) & 7) != 0)) return PIPE_EINVAL;
+  if (expert_sort_scratch(T, top_k, E) > 0 && (!scratch_dev || !aligned16(scratch_dev))) return PIPE_EINVAL;
   return launch_expert_sort(experts_dev, T, top_k, E, starts_dev, order_dev, places_dev, scratch_dev, (hipStream_t)stream);
 }
 
@@ -2584,7 +2584,7 @@ extern "C" int pipe_expert_route(const void* logits_dev, int type, int T, int E,
   if (!known_type(type) || (renormalize != 0 && renormalize != 1)) return PIPE_EINVAL;
   if (!router_ok(T, E, top_k) || top_k > E || row_stride < 0) return PIPE_ESHAPE;
   if (!starts_dev || (T > 0 && (!logits_dev || !experts_dev || !weights_dev || !order_dev || !places_dev))) return PIPE_EINVAL;
-  if (expert_sort_scratch(T, top_k, E) > 0 && (!scratch_dev || (reinterpret_cast<uintptr_t>(scratch_dev) & 7) != 0)) return PIPE_EINVAL;
+  if (expert_sort_scratch(T, top_k, E) > 0 && (!scratch_dev || !aligned16(scratch_dev))) return PIPE_EINVAL;
   if (T == 0) return launch_expert_sort(nullptr, 0, top_k, E, starts_dev, order_dev, places_dev, nullptr, (hipStream_t)stream);
   ExpertRouteArgs a{};
   a.logits = logits_dev; a.type = type; a.T = T; a.E = E; a.top_k = top_k; a.renormalize = renormalize; a.row_stride = row_stride;

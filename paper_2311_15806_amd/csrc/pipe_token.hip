@@ -10,6 +10,7 @@ namespace {
 constexpr int64_t MOST_BLOCKS = 1 << 23;      // workgroups of 256 threads a launch
 
 // ------------------------------------------------------------------ rows to codes
+// Bound by the bytes: 4096 rows of 4096 in fp32 17.8 us, 4.7 TB/s; in 16 bits beside them by the instructions (16 us for 50 MB); few rows by latency, 3.4 us.
 // s = max|x| / 127, c = rint(x / s): NT threads a row, 8 values a thread and step, the first CH steps kept in registers between the maximum
 // and the codes, the rest (rows of more than 8 NT CH values) read again.  A row with a NaN or an infinity has the maximum +infinity here.
 template <typename T, int NT, int CH, bool WIDE>
@@ -77,6 +78,7 @@ int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitc
 // Pairs (token, choice) go by blocks of up to 512, whole tokens each, a pair a thread.  Where there is one block a single workgroup does all.  Otherwise a
 // launch counts each block's pairs by expert (the router's beside its choice), and another has every workgroup sum the counts of the blocks
 // before its own and of all, which gives its pairs' rows.  Nothing passes between the workgroups of a launch; no order of theirs is in the result.
+// Bound by latency: 16384 tokens, eight of 128 experts, bf16, take 10 us for the choice (6 MB in and out), 4 for the sums and 4.5 for the rows; 48 tokens, six of 64, 5.5.
 constexpr int PAIRS = 512;
 __host__ __device__ constexpr int block_tokens(int top_k) { return PAIRS / top_k; }
 static int block_count(int T, int top_k) { return (T + block_tokens(top_k) - 1) / block_tokens(top_k); }
@@ -85,8 +87,12 @@ struct SortArgs {
   int T, E, top_k, blocks;
   int32_t *starts, *order, *places;
   uint16_t* counts;     // [blocks][E + 1, rounded up to four], the last: pairs without an expert
+  int32_t* before;      // their sums over the blocks before, and over all, [blocks + 1][likewise], or nullptr
 };
 __host__ __device__ constexpr int count_pitch(int E) { return (E + 4) / 4 * 4; }
+// From more than this many blocks on a launch in between sums the counts, which every workgroup would sum for itself (256 blocks of 128 experts: 8.4 us,
+// two launches 8.1; the work of the one grows with the square of the blocks).
+constexpr int SUM_BLOCKS = 128;
 
 // lanes of the wave with the same key (of `bits` bits)
 __device__ __forceinline__ unsigned long long same_key(int key, int bits) {
@@ -111,7 +117,14 @@ __device__ __forceinline__ void place(const SortArgs& a, int b, int n, int key, 
   const unsigned long long same = same_key(mine ? key : q, 32 - __clz(q));
   const int before = __popcll(same & ((1ull << lane) - 1));
   if (mine && before == 0) cnt[wave * q + key] = (uint16_t)__popcll(same);
-  if (a.blocks > 1) {
+  if (a.before != nullptr) {
+    const int pitch = count_pitch(a.E);
+    __syncthreads();
+    for (int e = threadIdx.x; e < q; e += PAIRS) {
+      base[e] = a.before[(int64_t)b * pitch + e];
+      total[e] = a.before[(int64_t)a.blocks * pitch + e];
+    }
+  } else if (a.blocks > 1) {
     const int quads = count_pitch(a.E) / 4, groups = max(1, PAIRS / quads);      // four experts a thread, the blocks dealt to groups of threads
     for (int x = threadIdx.x; x < groups * quads; x += PAIRS) {
       const int g = x / quads, e = (x - g * quads) * 4;
@@ -176,6 +189,49 @@ __device__ __forceinline__ void place(const SortArgs& a, int b, int n, int key, 
   a.places[pair] = key < a.E ? row : -1;
 }
 
+// A workgroup four experts: the counts of all blocks summed up, a thread a share of the blocks.
+constexpr int SUM_NT = 256;
+__global__ __launch_bounds__(SUM_NT) void expert_sum_kernel(const SortArgs a) {
+  __shared__ int wave_total[SUM_NT / 64][4];
+  const int pitch = count_pitch(a.E), e = blockIdx.x * 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int share = (a.blocks + SUM_NT - 1) / SUM_NT, lo = min((int)threadIdx.x * share, a.blocks), hi = min(lo + share, a.blocks);
+  auto counts_of = [&](int r, int* v) __attribute__((always_inline)) {
+    const uint2 c = *reinterpret_cast<const uint2*>(a.counts + (int64_t)r * pitch + e);
+    v[0] = (int)(c.x & 0xffff); v[1] = (int)(c.x >> 16); v[2] = (int)(c.y & 0xffff); v[3] = (int)(c.y >> 16);
+  };
+  int sum[4] = {0, 0, 0, 0}, v[4];
+#pragma unroll 4
+  for (int r = lo; r < hi; ++r) {
+    counts_of(r, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += v[i];
+  }
+  int at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    int upto = sum[i];
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    at[i] = upto - sum[i];
+    if (lane == 63) wave_total[wave][i] = upto;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    for (int w = 0; w < wave; ++w) at[i] += wave_total[w][i];
+#pragma unroll 4
+  for (int r = lo; r < hi; ++r) {
+    counts_of(r, v);
+    *reinterpret_cast<int4*>(a.before + (int64_t)r * pitch + e) = make_int4(at[0], at[1], at[2], at[3]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at[i] += v[i];
+  }
+  if (threadIdx.x == SUM_NT - 1) *reinterpret_cast<int4*>(a.before + (int64_t)a.blocks * pitch + e) = make_int4(at[0], at[1], at[2], at[3]);
+}
+
 // pairs of block b
 __device__ __forceinline__ int pairs_of(const SortArgs& a, int b) {
   return min(block_tokens(a.top_k), a.T - b * block_tokens(a.top_k)) * a.top_k;
@@ -222,7 +278,7 @@ __device__ __forceinline__ int row_min(int x) {
 }
 
 // 16 lanes a token, lane l its logits l, l + 16, ...; each of the top_k steps is a maximum and then the lowest index that holds it.  A NaN equals
-// nothing and is never chosen.  16384 tokens, eight of 128, bf16: 4.6 us (a wave a token: 12.7).
+// nothing and is never chosen.  16384 tokens, eight of 128, bf16: 9.9 us with the counts of the blocks (a wave a token, without: 12.7).
 template <typename T, int EL>
 __global__ __launch_bounds__(PAIRS) void expert_route_kernel(const ExpertRouteArgs a, const SortArgs s) {
   __shared__ int keys[PAIRS];
@@ -285,7 +341,8 @@ __global__ __launch_bounds__(PAIRS) void expert_route_kernel(const ExpertRouteAr
 }
 
 // ------------------------------------------------------------------ back to the tokens
-// 8 values of a token a thread, the rows of its experts summed in fp32 in the order of its choices.
+// 8 values of a token a thread, the rows of its experts summed in fp32 in the order of its choices.  Bound by the bytes: 8192 tokens, eight rows of 4096 each (a
+// quarter of them left out), fp16, 100 us for 470 MB; 32 tokens of six rows of 2048 3.7 us.
 template <typename T, bool WIDE>
 __global__ __launch_bounds__(256) void expert_combine_kernel(const T* __restrict__ y, int64_t n, int H, int64_t stride, const int32_t* __restrict__ places,
                                                              const float* __restrict__ weights, int64_t items, int top_k, T* __restrict__ out) {
@@ -367,24 +424,35 @@ int launch_token_quantize(const void* x, int type, int64_t rows, int in, int64_t
 }
 
 int64_t expert_sort_scratch(int T, int top_k, int E) {
-  const int blocks = block_count(T, top_k);
-  return blocks > 1 ? (int64_t)blocks * count_pitch(E) * sizeof(uint16_t) : 0;
+  const int64_t blocks = block_count(T, top_k), pitch = count_pitch(E);
+  if (blocks <= 1) return 0;
+  return round_up64(blocks * pitch * sizeof(uint16_t), 16) + (blocks > SUM_BLOCKS ? (blocks + 1) * pitch * (int64_t)sizeof(int32_t) : 0);
+}
+static SortArgs sort_args(int T, int E, int top_k, int32_t* starts, int32_t* order, int32_t* places, void* scratch) {
+  const int blocks = std::max(1, block_count(T, top_k));
+  SortArgs s{T, E, top_k, blocks, starts, order, places, (uint16_t*)scratch, nullptr};
+  if (blocks > SUM_BLOCKS) s.before = (int32_t*)((char*)scratch + round_up64((int64_t)blocks * count_pitch(E) * sizeof(uint16_t), 16));
+  return s;
 }
 
 static int launch_place(const int32_t* experts, const SortArgs& s, hipStream_t st) {
+  if (s.before != nullptr) {
+    PIPE_KLAUNCH(expert_sum_kernel, dim3(count_pitch(s.E) / 4), dim3(SUM_NT), 0, st, s);
+    PIPE_HIP(hipGetLastError());
+  }
   PIPE_KLAUNCH(expert_place_kernel, dim3(s.blocks), dim3(PAIRS), sort_lds_bytes(s.E), st, experts, s);
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
 }
 
 int launch_expert_route(const ExpertRouteArgs& a, int32_t* starts, int32_t* order, int32_t* places, void* scratch, hipStream_t st) {
-  const SortArgs s{a.T, a.E, a.top_k, block_count(a.T, a.top_k), starts, order, places, (uint16_t*)scratch};
+  const SortArgs s = sort_args(a.T, a.E, a.top_k, starts, order, places, scratch);
   const int rc = a.type == PIPE_F32 ? route_typed<float>(a, s, st) : a.type == PIPE_F16 ? route_typed<f16>(a, s, st) : route_typed<bf16>(a, s, st);
   return rc || s.blocks == 1 ? rc : launch_place(a.experts, s, st);
 }
 
 int launch_expert_sort(const int32_t* experts, int T, int top_k, int E, int32_t* starts, int32_t* order, int32_t* places, void* scratch, hipStream_t st) {
-  const SortArgs s{T, E, top_k, std::max(1, block_count(T, top_k)), starts, order, places, (uint16_t*)scratch};
+  const SortArgs s = sort_args(T, E, top_k, starts, order, places, scratch);
   if (s.blocks > 1) {
     PIPE_KLAUNCH(expert_count_kernel, dim3(s.blocks), dim3(PAIRS), (E + 1) * sizeof(int), st, experts, s);
     PIPE_HIP(hipGetLastError());

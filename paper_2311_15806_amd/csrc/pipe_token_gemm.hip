@@ -1,6 +1,11 @@
 // Products of 8-bit codes with a scale for each token and each channel, y = act(s_t s_o sum_i c_ti w_oi + b_o), of one layer or of a router's
 // experts, whose rows lie one after the other in y.
 //
+// What bounds them: few tokens, the weights' bytes (32 tokens, six of 64 gated experts of 2048-1408, 370 MB: 69 us, 5.4 TB/s; 16 tokens of gated
+// 4096-11008, 90 MB: 20 us); many, the matrix units at the clock that power leaves: 8192 tokens of 8192-8192 take 455 us, 2420 TOP/s, where the largest
+// library product of that size reaches 2134 and multiplies alone, on random bytes, 3764.  Between them latency: a stage of 128 codes takes a tile of 64
+// tokens that is alone on its unit 0.45 us, of 128 0.95, of 256 1.3.
+//
 // Sums are exact in 32 bits.  Both scales' exponents are kept apart from their mantissas until the end, so that no product of a sum and one of
 // the scales leaves fp32's range where the whole does not.  Every kernel here computes an output by the same operations: which one serves a call
 // changes no bit.
@@ -117,7 +122,8 @@ __device__ __forceinline__ void act4(float* z, int act) {
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504f)); }
 
 // Four channels' scales and biases: z = (sum s_t) s_o + b.  The product is made of the scales' mantissas and scaled by both exponents at once -- or, where
-// these are so small (`plain`) that nothing on the way leaves fp32's normal range, of the scales as they are, which gives the same bits (4096 tokens of 4096-11008, fp32: 204 us, 199 so).
+// these are so small (`plain`) that nothing on the way leaves fp32's normal range, of the scales as they are, which gives the
+// same bits (4096 tokens of 4096-11008, fp32: 204 us, 199 so).
 constexpr int PLAIN_EXPONENT = 50;
 __device__ __forceinline__ bool plain_scale(float s) {
   const int e = __builtin_amdgcn_frexp_expf(s);
@@ -325,7 +331,7 @@ __device__ __forceinline__ void outputs(const TokenProductArgs& a, const Rows& r
   const int o = o0 + 4 * ((threadIdx.x & 63) >> 4);
   put4(a.y, a.type, (r.row + t) * a.out + o, z[0], a.out - o, a.out % 4 == 0);
 }
-// Bound by the bytes of the weights, which go straight from memory to operands.  A tile is 16 rows of weights (of the gate and of the other half as well) x
+// The weights go straight from memory to operands.  A tile is 16 rows of weights (of the gate and of the other half as well) x
 // 16 TB tokens; S of a workgroup's eight waves take its steps of 64 codes in turn and join their sums in LDS.
 template <bool GATED, int TB, int S>
 __global__ __launch_bounds__(512, 4) void token_stream_kernel(const TokenProductArgs a, int o_tiles, int tiles) {
@@ -634,11 +640,14 @@ __global__ __launch_bounds__(256, B == 128 ? 2 : 4) void token_tile_kernel(const
   side.template load<GATED, 256>(a, r, o0);
   __syncthreads();
   static_assert(SLOT >= 4 * 16 * 4 * F && SLOT * sizeof(v4i) >= sizeof(side), "turn");
-  finish<GATED>(a, r, o0, wo, wt, acc, slots + wave * (16 * 4 * F), side);
+  if (wt < r.n) finish<GATED>(a, r, o0, wo, wt, acc, slots + wave * (16 * 4 * F), side);
 }
 
 // ------------------------------------------------------------------ large tiles
-// 256 rows of weights x 256 tokens a workgroup of eight waves, 128 x 64 a wave.
+// 256 rows of weights x 256 tokens a workgroup of eight waves, 128 x 64 a wave: 128 sums a lane, two waves a SIMD (four waves of 128 x 128 leave no register for
+// what is on its way).  At 4096 tokens of 4096-11008 the matrix units are busy 46 % of the time: a stage takes 3100 cycles for 2048 of multiplies, the rest of a tile
+// (first loads, outputs, whose stores all units send at once) 12 to 15 us beside 47, and 688 tiles make 2.7 rounds.  Loads straight to LDS, 64 codes a
+// stage: 250 us for 200; lines of the stage after next requested ahead: 226 for 220.
 template <bool GATED>
 __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArgs a, int o_tiles) {
   constexpr int N = 256, KB = 128, P = 8, WIDTH = GATED ? N / 2 : N;
@@ -750,7 +759,7 @@ __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArg
   auto& side = *reinterpret_cast<Side<N, N>*>(slots + SLOT);
   side.template load<GATED, 512>(a, r, o0);
   __syncthreads();
-  finish<GATED>(a, r, o0, wo, wt, acc, slots + wave * (16 * 32), side);
+  if (wt < r.n) finish<GATED>(a, r, o0, wo, wt, acc, slots + wave * (16 * 32), side);
 }
 
 // ------------------------------------------------------------------ launches

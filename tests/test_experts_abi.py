@@ -104,12 +104,13 @@ def test_router_refusals(lib):
     for f in (route, sort):
         for bad in (dict(E=0), dict(E=1025)):
             assert f(lib, **bad) == ESHAPE, bad
-        assert f(lib, T=600, scratch=None) == EINVAL and f(lib, T=600, scratch=C.c_void_p(4100)) == EINVAL
+        assert f(lib, T=600, scratch=None) == EINVAL and f(lib, T=600, scratch=ODD) == EINVAL
     lib.pipe_expert_scratch.restype = I
     for k in range(1, 33):                       # whole tokens of up to 512 pairs a block
         assert lib.pipe_expert_scratch(481 // k, k, 8) == 0 and lib.pipe_expert_scratch(512 // k, k, 8) == 0
         assert lib.pipe_expert_scratch(512 // k + 1, k, 8) == 2 * 12 * 2
     assert lib.pipe_expert_scratch(0, 3, 5) == 0
+    assert lib.pipe_expert_scratch(128 * 256, 2, 8) == 128 * 12 * 2 and lib.pipe_expert_scratch(128 * 256 + 1, 2, 8) == 3104 + 130 * 12 * 4
     for bad in ((-1, 2, 8), (4, 0, 8), (4, 33, 8), (4, 2, 0), (4, 2, 1025), (1 << 29, 2, 8)):
         assert lib.pipe_expert_scratch(*bad) == -1
     for bad in (dict(type=3), dict(renormalize=2)):

@@ -271,7 +271,7 @@ ROUTES = [
     (1, 1, 1, True, "f32", False), (1, 8, 2, True, "f32", False), (3, 8, 8, False, "f32", True), (48, 64, 6, True, "f32", False),
     (7, 63, 4, False, "bf16", True), (130, 65, 3, True, "f16", True), (33, 128, 8, False, "bf16", True), (20, 200, 1, True, "f32", False),
     (70, 256, 8, True, "bf16", True), (9, 300, 32, False, "f32", True), (1000, 16, 2, True, "bf16", True), (5, 1000, 32, True, "f16", True),
-    (17, 1024, 7, False, "f32", True), (4100, 6, 3, True, "f32", True), (2, 33, 32, False, "f32", False),
+    (17, 1024, 7, False, "f32", True), (4100, 6, 3, True, "f32", True), (6000, 24, 8, True, "bf16", True), (2, 33, 32, False, "f32", False),
 ]
 
 
@@ -316,7 +316,7 @@ def test_route_of_no_tokens(pipe):
 
 
 @pytest.mark.parametrize("T,k,E", [(0, 2, 4), (1, 1, 1), (1, 32, 3), (5, 3, 7), (64, 6, 64), (341, 3, 100), (1024, 1, 5), (1025, 1, 1024), (3000, 8, 128),
-                                   (20000, 4, 16), (100, 2, 1)])
+                                   (20000, 4, 16), (100, 2, 1), (32768, 2, 8), (32769, 2, 8), (40000, 3, 1000), (200000, 8, 33)])
 def test_sort(pipe, T, k, E):
     rng = np.random.default_rng(T + k + E)
     for lo, hi in ((0, E), (-2, E + 2), (0, max(1, E // 8)), (E - 1, E), (-1, 0), (-2 ** 31, 2 ** 31)):
