@@ -778,10 +778,11 @@ int launch_stream(const TokenProductArgs& a, bool gated, hipStream_t st) {
   const int o_tiles = (a.out + 15) / 16;
   const int64_t tiles = (int64_t)o_tiles * row_tiles<16 * TB>(a);
   if (tiles >= (int64_t)1 << 23) return PIPE_ESHAPE;      // (a launch holds fewer than 2^32 threads)
-  // as many waves a tile as keep about four to eight a SIMD (32 tokens, six of 64 experts: one wave 80 us, four 100, eight 106; 16 tokens of
-  // 4096-11008, gated: eight 27, four 30, one 48)
+  // as many waves a tile as keep about four a SIMD busy (us with one, two, four, eight waves: 8 tokens of 4096-11008 29, 18, 18, 16; nine, one of 16 experts of
+  // 4096-4096, 42, 34, 34, 42; 32, six of 64 gated ones of 2048-1408, 72, 76, 77, 97)
   if (tiles <= 1024) return launch_stream_split<TB, 8>(a, gated, o_tiles, (int)tiles, st);
   if (tiles <= 2048) return launch_stream_split<TB, 4>(a, gated, o_tiles, (int)tiles, st);
+  if (tiles <= 4096) return launch_stream_split<TB, 2>(a, gated, o_tiles, (int)tiles, st);
   return launch_stream_split<TB, 1>(a, gated, o_tiles, (int)tiles, st);
 }
 
@@ -804,25 +805,36 @@ int launch_tiles(const TokenProductArgs& a, bool gated, hipStream_t st) {
 
 }  // namespace
 
+// whether a workgroup can make the codes of its tokens itself
+static bool one_launch(const TokenProductArgs& a) {
+  return a.n * a.pitch <= FUSED_CODES && (int64_t)((a.out + 15) / 16) * row_tiles<16>(a) <= FUSED_TILES;
+}
 static int kernel_of(const TokenProductArgs& a) {
   const bool gated = a.act == PIPE_ACT_SILU_GATED;
   int which = g_token_kernel;
   const int64_t each = a.n / a.E;       // tokens of an expert, about
   if (which == AUTOMATIC) {
-    // Few tokens are streamed past: the weights' bytes are all that counts up to 32 tokens (4096-4096: 13 us, tiles 17; 48 tokens 17 both), longer where the
-    // outputs make few tiles (33 tokens of 8192-64: 19 us, tiles 27).  Experts' tokens are not spread evenly, a second tile reads the weights again: four each
-    // (16 tokens, two of eight experts of 4096-4096: 29 us, tiles 30; 64 tokens: 60 and 30).
+    // Few tokens are streamed past: the weights' bytes are all that counts up to 32 tokens (4096-4096: 13 us, tiles 17; 48 tokens 17 both), longer where
+    // that makes few tiles (136 tokens of 4096-704: 13 us, 17; 875 of 3136-128 16 and 19), not where they are many (16 of gated 4096-11008: 24 us, tiles
+    // 23; 20 of 4096-32000 42 and 27; 8 of 4096-11008 16 and 17).  Experts' tokens are not spread evenly, a second tile reads the weights again: four each
+    // (16 tokens, two of eight experts of 4096-4096: 28 us, tiles 29; 64 tokens: 60 and 30).
     const double w_rows = gated ? 2.0 * a.out : a.out;
-    if (a.starts ? each <= 4 : a.n <= (w_rows <= 1024 ? 64 : 32)) {
+    const int64_t streamed = (a.out + 15) / 16 * (each <= 16 ? row_tiles<16>(a) : row_tiles<32>(a));
+    if (one_launch(a) || streamed <= 384 || (a.starts ? each <= 4 : a.n <= 32 && w_rows < 16384)) {
       which = STREAM;
     } else {
-      // Microseconds of a launch, from what a stage of 128 codes takes each kernel with few tiles and with many (half a tile more for each expert), and its
-      // ends, in stages.  Calls of 64, 128 and 256 tokens a tile: 512 tokens of 4096-4096 27, 37 and 60 us; 1000 42, 40 and 62; 2048 73, 57 and 68; 4096 of
-      // 4096-11008 312, 239 and 198; 512 tokens, six of 64 gated experts of 2048-1408 93, 100 and 114; 8192, two of 128 of 1024-1024 138, 122 and 152.
-      const double more = a.starts ? 0.5 * a.E : 0.0, stages = a.pitch / 128;
-      auto tiles = [&](int B) { return std::ceil(w_rows / B) * std::ceil((double)a.n / B + more); };
-      const double t64 = std::max(0.45, 0.0010 * tiles(64)) * (stages + 3), t128 = std::max(0.95, 0.0032 * tiles(128)) * (stages + 3),
-                   t256 = std::max(1.85, 0.0084 * tiles(256)) * (stages + 5);
+      // Microseconds of a launch: of a stage of 128 codes with few tiles and for each round of them that the chip holds (1024, 512 and 256; half a tile more
+      // for each expert, one at least), and its ends, in stages.  Calls of 64, 128 and 256 tokens a tile: 512 tokens of 4096-4096 27, 37 and 60 us; 1000 42,
+      // 40 and 62; 2048 73, 57 and 68; 4096 of 4096-11008 312, 239 and 198; 5227 of 3648-1730 87, 91 and 79; 512 tokens, six of 64 gated experts of
+      // 2048-1408 93, 100 and 114; 1024, two of eight of 4096-4096 81, 80 and 69; 8192, two of 128 of 1024-1024 138, 122 and 152; 2069, two of 110 of
+      // 3200-640 56, 81 and 100.
+      const double stages = a.pitch / 128, n = (double)a.n;
+      auto rounds = [&](int B, double held) {
+        return std::ceil(w_rows / B) * (a.starts ? a.E * std::max(1.0, n / a.E / B + 0.5) : std::ceil(n / B)) / held;
+      };
+      const double r64 = rounds(64, 1024), r128 = rounds(128, 512), r256 = rounds(256, 256);
+      const double t64 = (r64 <= 1 ? std::max(0.45, r64) : r64 + 0.3) * (stages + 4),
+                   t128 = (r128 <= 1 ? std::max(0.95, 1.5 * r128) : 1.5 * r128 + 0.3) * (stages + 4), t256 = std::max(1.55, 1.6 * r256 + 0.1) * (stages + 10);
       which = t64 <= t128 && t64 <= t256 ? TILES_64 : t128 <= t256 ? TILES_128 : TILES_256;
     }
   }
@@ -847,7 +859,7 @@ int launch_token_layer(TokenProductArgs& a, int8_t* codes, float* scales, hipStr
   const char *x0 = (const char*)a.x, *y0 = (const char*)a.y;
   const int64_t size = type_size(a.type);
   const bool apart = x0 + ((a.n_x - 1) * a.x_stride + a.in) * size <= y0 || y0 + a.n * a.out * size <= x0;
-  if (which == STREAM && apart && a.n * a.pitch <= FUSED_CODES && o_tiles * row_tiles<16>(a) <= FUSED_TILES) {
+  if (which == STREAM && apart && one_launch(a)) {
     a.x_wide = (reinterpret_cast<uintptr_t>(a.x) & 15) == 0 && a.x_stride % n_wide == 0;
     return gated ? launch_fused<true>(a, o_tiles, st) : launch_fused<false>(a, o_tiles, st);
   }
