@@ -78,7 +78,7 @@ int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitc
 // Pairs (token, choice) go by blocks of up to 512, whole tokens each, a pair a thread.  Where there is one block a single workgroup does all.  Otherwise a
 // launch counts each block's pairs by expert (the router's beside its choice), and another has every workgroup sum the counts of the blocks
 // before its own and of all, which gives its pairs' rows.  Nothing passes between the workgroups of a launch; no order of theirs is in the result.
-// Bound by latency: 16384 tokens, eight of 128 experts, bf16, take 10 us for the choice (6 MB in and out), 4 for the sums and 4.5 for the rows; 48 tokens, six of 64, 5.5.
+// Bound by latency: 16384 tokens, eight of 128 experts, bf16, take 7 us for the choice (6 MB in and out), 4 for the sums and 4.5 for the rows; 48 tokens, six of 64, 5.5.
 constexpr int PAIRS = 512;
 __host__ __device__ constexpr int block_tokens(int top_k) { return PAIRS / top_k; }
 static int block_count(int T, int top_k) { return (T + block_tokens(top_k) - 1) / block_tokens(top_k); }
@@ -104,14 +104,15 @@ __device__ __forceinline__ unsigned long long same_key(int key, int bits) {
   return m;
 }
 
-// The rows of block `b`'s pairs, `n` of them, a pair a thread: `key` is its expert (E: none; E + 1: behind the end).
+// The rows of block `b`'s pairs, `n` of them, a pair each of the first of NT threads: `key` is its expert (E: none; E + 1: behind the end).
+template <int NT>
 __device__ __forceinline__ void place(const SortArgs& a, int b, int n, int key, int* lds) {
   const int q = a.E + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int *base = lds, *total = lds + q;                                // of each expert
   uint16_t* cnt = reinterpret_cast<uint16_t*>(lds + 2 * q);         // ... and of each wave's pairs
-  __shared__ int wave_total[PAIRS / 64];
-  for (int i = threadIdx.x; i < PAIRS / 64 * q; i += PAIRS) cnt[i] = 0;
-  for (int e = threadIdx.x; e < q; e += PAIRS) base[e] = total[e] = 0;
+  __shared__ int wave_total[NT / 64];
+  for (int i = threadIdx.x; i < PAIRS / 64 * q; i += NT) cnt[i] = 0;
+  for (int e = threadIdx.x; e < q; e += NT) base[e] = total[e] = 0;
   __syncthreads();
   const bool mine = (int)threadIdx.x < n;
   const unsigned long long same = same_key(mine ? key : q, 32 - __clz(q));
@@ -120,13 +121,13 @@ __device__ __forceinline__ void place(const SortArgs& a, int b, int n, int key, 
   if (a.before != nullptr) {
     const int pitch = count_pitch(a.E);
     __syncthreads();
-    for (int e = threadIdx.x; e < q; e += PAIRS) {
+    for (int e = threadIdx.x; e < q; e += NT) {
       base[e] = a.before[(int64_t)b * pitch + e];
       total[e] = a.before[(int64_t)a.blocks * pitch + e];
     }
   } else if (a.blocks > 1) {
-    const int quads = count_pitch(a.E) / 4, groups = max(1, PAIRS / quads);      // four experts a thread, the blocks dealt to groups of threads
-    for (int x = threadIdx.x; x < groups * quads; x += PAIRS) {
+    const int quads = count_pitch(a.E) / 4, groups = max(1, NT / quads);      // four experts a thread, the blocks dealt to groups of threads
+    for (int x = threadIdx.x; x < groups * quads; x += NT) {
       const int g = x / quads, e = (x - g * quads) * 4;
       int pre[4] = {0, 0, 0, 0}, all[4] = {0, 0, 0, 0};
 #pragma unroll 8
@@ -148,7 +149,7 @@ __device__ __forceinline__ void place(const SortArgs& a, int b, int n, int key, 
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < q; e += PAIRS) {      // counts of the waves before
+  for (int e = threadIdx.x; e < q; e += NT) {      // counts of the waves before
     int sum = 0;
 #pragma unroll
     for (int w = 0; w < PAIRS / 64; ++w) {
@@ -160,7 +161,7 @@ __device__ __forceinline__ void place(const SortArgs& a, int b, int n, int key, 
   }
   __syncthreads();
   // first rows: all pairs of the experts before, `per` experts a thread
-  const int per = (a.E + PAIRS - 1) / PAIRS, e0 = min((int)threadIdx.x * per, a.E), e1 = min(e0 + per, a.E);
+  const int per = (a.E + NT - 1) / NT, e0 = min((int)threadIdx.x * per, a.E), e1 = min(e0 + per, a.E);
   int own = 0;
   for (int e = e0; e < e1; ++e) own += total[e];
   int upto = own;
@@ -243,22 +244,23 @@ static size_t sort_lds_bytes(int E) { return (size_t)(E + 1) * (2 * sizeof(int) 
 __global__ __launch_bounds__(PAIRS) void expert_place_kernel(const int32_t* __restrict__ experts, const SortArgs a) {
   const int b = blockIdx.x, n = pairs_of(a, b);
   const int key = (int)threadIdx.x < n ? key_of(experts[(int64_t)b * (block_tokens(a.top_k) * a.top_k) + threadIdx.x], a.E) : 0;
-  place(a, b, n, key, sort_lds);
+  place<PAIRS>(a, b, n, key, sort_lds);
 }
 
 // counts of a block by expert
+template <int NT>
 __device__ __forceinline__ void count_block(const SortArgs& a, int b, int n, int key, int* hist /* [E + 1] */) {
   const int q = a.E + 1;
-  for (int e = threadIdx.x; e < q; e += PAIRS) hist[e] = 0;
+  for (int e = threadIdx.x; e < q; e += NT) hist[e] = 0;
   __syncthreads();
   if ((int)threadIdx.x < n) atomicAdd(&hist[key], 1);
   __syncthreads();
-  for (int e = threadIdx.x; e < q; e += PAIRS) a.counts[(int64_t)b * count_pitch(a.E) + e] = (uint16_t)hist[e];
+  for (int e = threadIdx.x; e < q; e += NT) a.counts[(int64_t)b * count_pitch(a.E) + e] = (uint16_t)hist[e];
 }
 __global__ __launch_bounds__(PAIRS) void expert_count_kernel(const int32_t* __restrict__ experts, const SortArgs a) {
   const int b = blockIdx.x, n = pairs_of(a, b);
   const int key = (int)threadIdx.x < n ? key_of(experts[(int64_t)b * (block_tokens(a.top_k) * a.top_k) + threadIdx.x], a.E) : 0;
-  count_block(a, b, n, key, sort_lds);
+  count_block<PAIRS>(a, b, n, key, sort_lds);
 }
 
 // over the 16 lanes of a token
@@ -277,45 +279,103 @@ __device__ __forceinline__ int row_min(int x) {
   return min(x, dpp_i<0x140>(x));
 }
 
-// 16 lanes a token, lane l its logits l, l + 16, ...; each of the top_k steps is a maximum and then the lowest index that holds it.  A NaN equals
-// nothing and is never chosen.  16384 tokens, eight of 128, bf16: 9.9 us with the counts of the blocks (a wave a token, without: 12.7).
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+  x = max(x, (uint32_t)dpp_i<0xB1>((int)x));
+  x = max(x, (uint32_t)dpp_i<0x4E>((int)x));
+  x = max(x, (uint32_t)dpp_i<0x141>((int)x));
+  return max(x, (uint32_t)dpp_i<0x140>((int)x));
+}
+// A 16-bit logit and its expert in one number: above others if the logit is larger, or the same (-0 as 0) and the expert lower.  0: not to be chosen.
+template <typename T>
+__device__ __forceinline__ uint32_t logit_key(T x, float v, int e) {
+  const int u = v == 0.f ? 0 : __builtin_bit_cast(int16_t, x);      // in the upper half: a negative number's bits turned around, of another the sign
+  const uint32_t key = (uint32_t)(u ^ (u >> 15 | 0x8000)) << 16 | (0xffffu - (uint32_t)e);
+  return v > -INFINITY ? key : 0u;
+}
+template <typename T>
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  const uint32_t u = key >> 16;
+  return to_f(__builtin_bit_cast(T, (uint16_t)(u & 0x8000u ? u ^ 0x8000u : u ^ 0xffffu)));
+}
+
+// 16 lanes a token, lane l its logits l, l + 16, ...  In fp32 each of the top_k steps is a maximum and then the lowest index that holds it; a NaN equals
+// nothing and is never chosen.  In 16 bits a logit and its index are one number k, no two alike, and a step is one maximum: with the last choice m the
+// differences k - m, modulo 2^32, put all k below m over the others, in their order.  Bound by the instructions of a step (a wave a token: 12.7 us; 16 lanes
+// by maximum and index 9.9, 1024 threads instead of 512 8.7; one number 6.8: 16384 tokens, eight of 128, bf16, with the counts of the blocks).
+constexpr int route_threads(int EL) { return EL < 32 ? 1024 : 512; }      // (of 32 logits a lane the registers hold 512)
 template <typename T, int EL>
-__global__ __launch_bounds__(PAIRS) void expert_route_kernel(const ExpertRouteArgs a, const SortArgs s) {
+__global__ __launch_bounds__(route_threads(EL)) void expert_route_kernel(const ExpertRouteArgs a, const SortArgs s) {
+  constexpr int NT = route_threads(EL);
   __shared__ int keys[PAIRS];
   const int lane = threadIdx.x & 63, l = lane & 15, b = blockIdx.x;
   const int t0 = b * block_tokens(a.top_k), tokens = min(block_tokens(a.top_k), a.T - t0);
-  for (int i0 = (threadIdx.x >> 6) * 4; i0 < tokens; i0 += PAIRS / 16) {
+  for (int i0 = (threadIdx.x >> 6) * 4; i0 < tokens; i0 += NT / 16) {
     const int i = i0 + (lane >> 4), t = t0 + min(i, tokens - 1);
     const T* row = (const T*)a.logits + (int64_t)t * a.row_stride;
     float v[EL];
+    uint32_t k[EL], last = 0;      // (16 bits)
 #pragma unroll
-    for (int e = 0; e < EL; ++e) v[e] = e * 16 + l < a.E ? to_f(row[e * 16 + l]) : -INFINITY;
+    for (int c = 0; c < EL; c += 16) {      // (up to 16 loads at once, none behind a branch)
+      constexpr int N = EL < 16 ? EL : 16;
+      T x[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = 2 * (c + i) < EL && EL > 1 ? row[(c + i) * 16 + l] : row[min((c + i) * 16 + l, a.E - 1)];      // (E > 8 EL there)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v[c + i] = (c + i) * 16 + l < a.E ? to_f(x[i]) : -INFINITY;
+        if constexpr (sizeof(T) == 2) k[c + i] = logit_key(x[i], v[c + i], (c + i) * 16 + l);
+      }
+      if (EL > 16) __builtin_amdgcn_sched_barrier(0);
+    }
     float chosen[2] = {-INFINITY, -INFINITY};      // lane l: the l-th and the 16 + l-th largest
     int expert[2] = {-1, -1};
+    uint32_t picked[2] = {0, 0};                   // (16 bits: both)
     float first = 0.f, total = 0.f;
-    for (int j = 0; j < a.top_k; ++j) {
-      float m = v[0];
 #pragma unroll
-      for (int e = 1; e < EL; ++e) m = fmaxf(m, v[e]);
-      m = row_reduce<16, true>(m);
-      int at = 0x7fffffff;
+    for (int h = 0; h < 2; ++h) {
+      for (int j = 0, steps = min(16, a.top_k - 16 * h); j < steps; ++j) {
+        float m;
+        int at = 0x7fffffff;
+        if constexpr (sizeof(T) == 2) {
+          uint32_t up = 0;
 #pragma unroll
-      for (int e = EL - 1; e >= 0; --e) at = v[e] == m ? e * 16 + l : at;
-      at = row_min(at);
-      const bool there = m > -INFINITY;      // (no logit left: the maximum of NaNs is one, or -infinity)
-      if (j == 0) {
-        first = there ? m : 0.f;
-        if (!a.renormalize) {
+          for (int e = 0; e < EL; ++e) up = max(up, k[e] - last);
+          const uint32_t next = row_max(up) + last;
+          const bool there = next - 1u < last - 1u;      // 0 < next < last, or any but 0 at first; else no logit is left
+          last = there ? next : last;
+          picked[h] = l == j && there ? next : picked[h];
+          m = there ? logit_of<T>(next) : -INFINITY;
+        } else {
+          m = v[0];
 #pragma unroll
-          for (int e = 0; e < EL; ++e) total += expf(v[e] - first);
+          for (int e = 1; e < EL; ++e) m = fmaxf(m, v[e]);
+          m = row_reduce<16, true>(m);
+#pragma unroll
+          for (int e = EL - 1; e >= 0; --e) at = v[e] == m ? e * 16 + l : at;
+          at = row_min(at);
+          if (l == j && m > -INFINITY) {                 // (a maximum of NaNs is one, or -infinity)
+            chosen[h] = m;
+            expert[h] = at;
+          }
+        }
+        if (h == 0 && j == 0) {
+          first = m > -INFINITY ? m : 0.f;
+          if (!a.renormalize) {
+#pragma unroll
+            for (int e = 0; e < EL; ++e) total += expf(v[e] - first);
+          }
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int e = 0; e < EL; ++e) v[e] = e * 16 + l == at ? -INFINITY : v[e];
         }
       }
-      if (l == (j & 15) && there) {
-        chosen[j >> 4] = m;
-        expert[j >> 4] = at;
+      if constexpr (sizeof(T) == 2) {
+        if (picked[h] != 0) {
+          chosen[h] = logit_of<T>(picked[h]);
+          expert[h] = 0xffff - (int)(picked[h] & 0xffffu);
+        }
       }
-#pragma unroll
-      for (int e = 0; e < EL; ++e) v[e] = e * 16 + l == at ? -INFINITY : v[e];
     }
     float w[2];
 #pragma unroll
@@ -336,8 +396,8 @@ __global__ __launch_bounds__(PAIRS) void expert_route_kernel(const ExpertRouteAr
   }
   __syncthreads();
   const int n = tokens * a.top_k, key = (int)threadIdx.x < n ? keys[threadIdx.x] : 0;
-  if (s.blocks == 1) place(s, b, n, key, sort_lds);
-  else count_block(s, b, n, key, sort_lds);
+  if (s.blocks == 1) place<NT>(s, b, n, key, sort_lds);
+  else count_block<NT>(s, b, n, key, sort_lds);
 }
 
 // ------------------------------------------------------------------ back to the tokens
@@ -385,15 +445,15 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(const T* __restrict
 
 template <typename T>
 int route_typed(const ExpertRouteArgs& a, const SortArgs& s, hipStream_t st) {
-  const dim3 grid(s.blocks), block(PAIRS);
+  const dim3 grid(s.blocks);
   const size_t lds = sort_lds_bytes(a.E);
-  if (a.E <= 16) PIPE_KLAUNCH((expert_route_kernel<T, 1>), grid, block, lds, st, a, s);
-  else if (a.E <= 32) PIPE_KLAUNCH((expert_route_kernel<T, 2>), grid, block, lds, st, a, s);
-  else if (a.E <= 64) PIPE_KLAUNCH((expert_route_kernel<T, 4>), grid, block, lds, st, a, s);
-  else if (a.E <= 128) PIPE_KLAUNCH((expert_route_kernel<T, 8>), grid, block, lds, st, a, s);
-  else if (a.E <= 256) PIPE_KLAUNCH((expert_route_kernel<T, 16>), grid, block, lds, st, a, s);
-  else if (a.E <= 512) PIPE_KLAUNCH((expert_route_kernel<T, 32>), grid, block, lds, st, a, s);
-  else PIPE_KLAUNCH((expert_route_kernel<T, 64>), grid, block, lds, st, a, s);
+  if (a.E <= 16) PIPE_KLAUNCH((expert_route_kernel<T, 1>), grid, dim3(route_threads(1)), lds, st, a, s);
+  else if (a.E <= 32) PIPE_KLAUNCH((expert_route_kernel<T, 2>), grid, dim3(route_threads(2)), lds, st, a, s);
+  else if (a.E <= 64) PIPE_KLAUNCH((expert_route_kernel<T, 4>), grid, dim3(route_threads(4)), lds, st, a, s);
+  else if (a.E <= 128) PIPE_KLAUNCH((expert_route_kernel<T, 8>), grid, dim3(route_threads(8)), lds, st, a, s);
+  else if (a.E <= 256) PIPE_KLAUNCH((expert_route_kernel<T, 16>), grid, dim3(route_threads(16)), lds, st, a, s);
+  else if (a.E <= 512) PIPE_KLAUNCH((expert_route_kernel<T, 32>), grid, dim3(route_threads(32)), lds, st, a, s);
+  else PIPE_KLAUNCH((expert_route_kernel<T, 64>), grid, dim3(route_threads(64)), lds, st, a, s);
   PIPE_HIP(hipGetLastError());
   return PIPE_OK;
 }

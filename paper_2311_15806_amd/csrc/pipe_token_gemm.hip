@@ -2,7 +2,7 @@
 // experts, whose rows lie one after the other in y.
 //
 // What bounds them: few tokens, the weights' bytes (32 tokens, six of 64 gated experts of 2048-1408, 370 MB: 69 us, 5.4 TB/s; 16 tokens of gated
-// 4096-11008, 90 MB: 20 us); many, the matrix units at the clock that power leaves: 8192 tokens of 8192-8192 take 455 us, 2420 TOP/s, where the largest
+// 4096-11008, 90 MB: 19 us); many, the matrix units at the clock that power leaves: 8192 tokens of 8192-8192 take 455 us, 2420 TOP/s, where the largest
 // library product of that size reaches 2134 and multiplies alone, on random bytes, 3764.  Between them latency: a stage of 128 codes takes a tile of 64
 // tokens that is alone on its unit 0.45 us, of 128 0.95, of 256 1.3.
 //

@@ -300,6 +300,30 @@ def test_route(pipe, case):
             assert np.array_equal(g.cpu().numpy(), v)
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("E", [1, 7, 16, 17, 64, 100, 128, 129, 256, 400, 512, 513, 1024])
+def test_route_of_all_bits(pipe, kind, E):
+    """16-bit logits of any bits: zeros of both signs are one value, NaN of both signs never chosen, subnormals and infinities in their order."""
+    rng = np.random.default_rng(E)
+    T, k = 301, min(E, 32)
+    bits = rng.integers(-2 ** 15, 2 ** 15, (T, E)).astype(np.int16)
+    few = np.array([0, -2 ** 15, 1, -2 ** 15 + 1, 2 ** 15 - 1, -1], dtype=np.int16)      # +-0, the least of both signs, NaN of both signs
+    bits[::3] = few[rng.integers(0, few.size, bits[::3].shape)]
+    l = torch.from_numpy(bits).view(DT[kind])
+    want_e, _ = ref.route(l.double().numpy(), k, True)
+    experts, _, starts, order, places = pipe.pipe_expert_route(l.cuda(), k)
+    assert np.array_equal(experts.cpu().numpy(), want_e)
+    for g, v in zip((starts, order, places), ref.sort(want_e, E)):
+        assert np.array_equal(g.cpu().numpy(), v)
+    l = torch.where(l.isfinite(), l, torch.zeros_like(l))
+    for renormalize in (True, False):
+        want_e, want_w = ref.route(l.double().numpy(), k, renormalize)
+        experts, w, *_ = pipe.pipe_expert_route(l.cuda(), k, renormalize=renormalize)
+        assert np.array_equal(experts.cpu().numpy(), want_e)
+        # as above with an argument of at most 104 (beyond it exp is 0 in fp32); an exp below fp32's normal numbers is off by 2^-126 at most
+        close(w, want_w, (124 + E) * ref.U32 * want_w + 2.0 ** -126)
+
+
 def test_route_of_infinities(pipe):
     inf = float("inf")
     l = torch.tensor([[1.0, inf, 2.0, -inf], [inf, inf, 0.0, 1.0], [float("nan")] * 4], device="cuda")
