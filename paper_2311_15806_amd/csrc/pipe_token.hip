@@ -77,8 +77,9 @@ int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitc
 // ------------------------------------------------------------------ the choice of experts, and the order by expert
 // Pairs (token, choice) go by blocks of up to 512, whole tokens each, a pair a thread.  Where there is one block a single workgroup does all.  Otherwise a
 // launch counts each block's pairs by expert (the router's beside its choice), and another has every workgroup sum the counts of the blocks
-// before its own and of all, which gives its pairs' rows.  Nothing passes between the workgroups of a launch; no order of theirs is in the result.
-// Bound by latency: 16384 tokens, eight of 128 experts, bf16, take 7 us for the choice (6 MB in and out), 4 for the sums and 4.5 for the rows; 48 tokens, six of 64, 5.5.
+// before its own and of all (of many blocks and experts a third launch does), which gives its pairs' rows.  Nothing passes between the workgroups of a
+// launch; no order of theirs is in the result.
+// Bound by latency: 16384 tokens, eight of 128 experts, bf16, take 7 us for the choice (6 MB in and out), 8 for sums and rows; 48 tokens, six of 64, 5.5.
 constexpr int PAIRS = 512;
 __host__ __device__ constexpr int block_tokens(int top_k) { return PAIRS / top_k; }
 static int block_count(int T, int top_k) { return (T + block_tokens(top_k) - 1) / block_tokens(top_k); }
@@ -90,9 +91,10 @@ struct SortArgs {
   int32_t* before;      // their sums over the blocks before, and over all, [blocks + 1][likewise], or nullptr
 };
 __host__ __device__ constexpr int count_pitch(int E) { return (E + 4) / 4 * 4; }
-// From more than this many blocks on a launch in between sums the counts, which every workgroup would sum for itself (256 blocks of 128 experts: 8.4 us,
-// two launches 8.1; the work of the one grows with the square of the blocks).
-constexpr int SUM_BLOCKS = 128;
+// Whether a launch in between sums the counts, which every workgroup would else sum for itself.  One launch less is worth more than 2 us to a call, the
+// work of the workgroups grows with the counts that each reads (a call, and one of a graph of calls, without and with: 136 blocks of 64 experts 18.3, 10.0
+// and 21.9, 11.9 us; 256 of 128 18.3, 14.5 and 20.9, 14.0; 512 of 64 19.2, 17.9 and 21.1, 17.7; 384 of 128 21.6, 20.6 and 21.4, 18.1; 256 of 512 38 and 22).
+static bool sums_apart(int64_t blocks, int E) { return blocks > 512 || blocks * count_pitch(E) > 36864; }
 
 // lanes of the wave with the same key (of `bits` bits)
 __device__ __forceinline__ unsigned long long same_key(int key, int bits) {
@@ -486,12 +488,12 @@ int launch_token_quantize(const void* x, int type, int64_t rows, int in, int64_t
 int64_t expert_sort_scratch(int T, int top_k, int E) {
   const int64_t blocks = block_count(T, top_k), pitch = count_pitch(E);
   if (blocks <= 1) return 0;
-  return round_up64(blocks * pitch * sizeof(uint16_t), 16) + (blocks > SUM_BLOCKS ? (blocks + 1) * pitch * (int64_t)sizeof(int32_t) : 0);
+  return round_up64(blocks * pitch * sizeof(uint16_t), 16) + (sums_apart(blocks, E) ? (blocks + 1) * pitch * (int64_t)sizeof(int32_t) : 0);
 }
 static SortArgs sort_args(int T, int E, int top_k, int32_t* starts, int32_t* order, int32_t* places, void* scratch) {
   const int blocks = std::max(1, block_count(T, top_k));
   SortArgs s{T, E, top_k, blocks, starts, order, places, (uint16_t*)scratch, nullptr};
-  if (blocks > SUM_BLOCKS) s.before = (int32_t*)((char*)scratch + round_up64((int64_t)blocks * count_pitch(E) * sizeof(uint16_t), 16));
+  if (sums_apart(blocks, E)) s.before = (int32_t*)((char*)scratch + round_up64((int64_t)blocks * count_pitch(E) * sizeof(uint16_t), 16));
   return s;
 }
 

@@ -110,7 +110,10 @@ def test_router_refusals(lib):
         assert lib.pipe_expert_scratch(481 // k, k, 8) == 0 and lib.pipe_expert_scratch(512 // k, k, 8) == 0
         assert lib.pipe_expert_scratch(512 // k + 1, k, 8) == 2 * 12 * 2
     assert lib.pipe_expert_scratch(0, 3, 5) == 0
-    assert lib.pipe_expert_scratch(128 * 256, 2, 8) == 128 * 12 * 2 and lib.pipe_expert_scratch(128 * 256 + 1, 2, 8) == 3104 + 130 * 12 * 4
+    assert lib.pipe_expert_scratch(128 * 256, 2, 8) == 128 * 12 * 2 and lib.pipe_expert_scratch(128 * 256 + 1, 2, 8) == 3104
+    # sums by a launch of their own: of more than 512 blocks, and of more than 36864 counts
+    assert lib.pipe_expert_scratch(512 * 256, 2, 8) == 512 * 12 * 2 and lib.pipe_expert_scratch(512 * 256 + 1, 2, 8) == 12320 + 514 * 12 * 4
+    assert lib.pipe_expert_scratch(354 * 64, 8, 100) == 73632 and lib.pipe_expert_scratch(354 * 64 + 1, 8, 100) == 73840 + 356 * 104 * 4
     for bad in ((-1, 2, 8), (4, 0, 8), (4, 33, 8), (4, 2, 0), (4, 2, 1025), (1 << 29, 2, 8)):
         assert lib.pipe_expert_scratch(*bad) == -1
     for bad in (dict(type=3), dict(renormalize=2)):

@@ -340,7 +340,8 @@ def test_route_of_no_tokens(pipe):
 
 
 @pytest.mark.parametrize("T,k,E", [(0, 2, 4), (1, 1, 1), (1, 32, 3), (5, 3, 7), (64, 6, 64), (341, 3, 100), (1024, 1, 5), (1025, 1, 1024), (3000, 8, 128),
-                                   (20000, 4, 16), (100, 2, 1), (32768, 2, 8), (32769, 2, 8), (40000, 3, 1000), (200000, 8, 33)])
+                                   (20000, 4, 16), (100, 2, 1), (32768, 2, 8), (32769, 2, 8), (40000, 3, 1000), (200000, 8, 33),
+                                   (131072, 2, 8), (131073, 2, 8), (22656, 8, 100), (22657, 8, 100), (2304, 8, 1000), (2368, 8, 1000)])
 def test_sort(pipe, T, k, E):
     rng = np.random.default_rng(T + k + E)
     for lo, hi in ((0, E), (-2, E + 2), (0, max(1, E // 8)), (E - 1, E), (-1, 0), (-2 ** 31, 2 ** 31)):
