@@ -231,6 +231,27 @@ def test_tokens_with_nan_or_infinity(pipe, kernel, T, act):
     close(y[torch.from_numpy(keep).cuda()], *ref.linear(x.double().cpu().numpy()[keep], w, s, b, act, "f32"))
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [3, 70])
+def test_gates_far_below_zero(pipe, kernel, T, kind):
+    """SiLU(g) is a number of fp32 down to g = -103: where 1 + exp(-g) or its reciprocal leave fp32's normal numbers as well."""
+    g = np.concatenate([np.linspace(-112, -80, 257), np.linspace(-80, 20, 101), [-1e4, -3e38, 3e38, 0]]).astype(np.float32)
+    u = np.where(np.abs(g) < 1e3, np.float32(2.0 ** 100), np.float32(1)) * np.where(np.arange(g.size) % 2, -1, 1).astype(np.float32)
+    out = g.size
+    # the sums are zeros: what the activation takes is the bias, exactly
+    x = torch.ones(T, 5, dtype=DT[kind], device="cuda")
+    codes = torch.zeros(2 * out, 128, dtype=torch.int8, device="cuda")
+    y = pipe.pipe_token_forward(x, codes, torch.ones(2 * out, device="cuda"), bias=torch.from_numpy(np.concatenate([g, u])).cuda(), act=pipe.PIPE_ACT_SILU_GATED)
+    g, u = g.astype(np.float64), u.astype(np.float64)
+    with np.errstate(over="ignore"):
+        want = g / (1 + np.exp(-g)) * u
+    # the exponent g / ln 2: 1.23 half steps (the constant's 0.23 and the product's rounding), times |g| in the value where g < 0; the exponential and the reciprocal
+    # two each, the sum and the products with g and u one each: 7; fp32's smallest step under SiLU, and the output's rounding
+    far = (7.1 + 1.24 * np.where((g < 0) & (g > -200), -g, 0)) * ref.U32 * np.abs(want) + np.abs(u) * 2.0 ** -149
+    far = far + ref.HALF[kind] * (np.abs(want) + far) + ref.LEAST[kind]
+    close(y, np.tile(want, (T, 1)), np.tile(far, (T, 1)))
+
+
 def test_forward_of_slices_into_an_output(pipe):
     rng = np.random.default_rng(8)
     base, v = typed(rng, (40, 901), "bf16")
