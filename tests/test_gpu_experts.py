@@ -504,6 +504,45 @@ def test_gathered_inputs_beyond_4_gib(pipe, which):
     close(y[[at[i] for i in here]], want[here], far[here])
 
 
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+@pytest.mark.parametrize("which", [0, 3])
+def test_gathered_inputs_beyond_4_gib_in_tiles(pipe, which, gated):
+    """Tokens whose codes lie past 32-bit offsets, in the tiles that have 64-bit addresses: so many streamed tiles that none is streamed."""
+    T, n, E, out, k, rows = 33000, 130944, 2, 570, 2, 300
+    assert T * n > 2 ** 32 and -(-out // 16) * (rows // 32 + E) > 384 and rows // E > 4
+    rng = np.random.default_rng(2)
+    order = rng.integers(0, T * k, rows)
+    order[::3] = rng.integers(32810 * k, T * k, order[::3].size)          # past 2^32 bytes
+    order[-1], order[0], order[7] = T * k - 1, T * k - 2, -1
+    few = np.unique(order[order >= 0] // k)
+    tokens = torch.from_numpy(few).cuda()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    x = torch.zeros(T, n, dtype=torch.bfloat16, device="cuda")
+    x[tokens] = torch.randn(tokens.numel(), n, generator=g, dtype=torch.bfloat16, device="cuda")
+    lines = out * (2 if gated else 1)
+    cw = torch.randint(-127, 128, (E, lines, n), generator=g, dtype=torch.int8, device="cuda")
+    sw = torch.rand(E, lines, generator=g, device="cuda") * 1e-4
+    b = torch.randn(E, lines, generator=g, device="cuda")
+    act = ref.ACTS["gated" if gated else "none"]
+    starts = [0, 170, rows - 2]
+    near = np.where(order >= 0, np.searchsorted(few, order // k) * k, -1)  # the same with the tokens that are named, next to each other
+    try:
+        pipe.pipe_set_token_kernel(which)
+        y = pipe.pipe_expert_forward(x, cw, sw, ints(starts), order=ints(order), top_k=k, bias=b, act=act)
+        pipe.pipe_set_token_kernel(1)
+        want = pipe.pipe_expert_forward(x[tokens], cw, sw, ints(starts), order=ints(near), top_k=k, bias=b, act=act)
+    finally:
+        pipe.pipe_set_token_kernel(0)
+    assert torch.equal(y, want) and not y[rows - 2:].any() and not y[7].any()
+    at = [0, 3, 6, 168]                                                    # some rows of the first expert by the definition
+    cols = np.concatenate([[0, 17, 255, out - 1]] + ([[out, out + 17, out + 255, lines - 1]] if gated else []))
+    c0 = cw[0][torch.from_numpy(cols).cuda()].cpu().numpy()
+    want, far = ref.linear(x[torch.from_numpy(order[at] // k).cuda()].double().cpu().numpy(), c0, sw[0].cpu().numpy()[cols], b[0].cpu().numpy()[cols],
+                           "gated" if gated else "none", "bf16")
+    close(y[at][:, cols[:4]], want, far)
+
+
 # ------------------------------------------------------------------ back to the tokens
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
