@@ -107,6 +107,61 @@ def test_quantize_of_special_rows(pipe, n):
     assert np.array_equal(c[:, :n].cpu().numpy(), want_c)
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 100, 1000, 2047, 2048, 2049, 3001, 4095, 4096])
+def test_quantize_of_many_rows(pipe, kind, n):
+    """More than 512 rows: a wave a row up to 4096 codes."""
+    rng = np.random.default_rng(n + 1)
+    for rows in (513, 702):
+        x, v = typed(rng, (rows, n), kind, 3.0)
+        c, s = pipe.pipe_token_quantize(x)
+        want_c, want_s = ref.quantize(v)
+        assert np.array_equal(s.cpu().numpy(), want_s) and c.shape == (rows, -(-n // 128) * 128)
+        assert np.array_equal(c[:, :n].cpu().numpy(), want_c) and not c[:, n:].any()
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,first,stride", [(300, 0, 512), (300, 8, 512), (300, 1, 512), (296, 4, 301), (2040, 8, 2051), (2500, 3, 2503), (2500, 8, 2504),
+                                            (4096, 0, 4104), (4090, 2, 4093), (1, 5, 9), (17, 0, 17), (200, 0, 0), (3001, 1, 0)])
+def test_quantize_of_many_slices(pipe, kind, n, first, stride):
+    """The same of rows that are 16-byte aligned or not, with strides of their own, one row for all."""
+    rng = np.random.default_rng(n)
+    base, _ = typed(rng, (600 * stride + n + first,), kind)
+    x = base.as_strided((600, n), (stride, 1), first)
+    c, s = pipe.pipe_token_quantize(x)
+    want_c, want_s = ref.quantize(x.double().cpu().numpy())
+    assert np.array_equal(s.cpu().numpy(), want_s)
+    assert np.array_equal(c[:, :n].cpu().numpy(), want_c) and not c[:, n:].any()
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [130, 2048, 2500, 4096])
+def test_quantize_of_special_rows_among_many(pipe, kind, n):
+    rng = np.random.default_rng(3)
+    x = rng.standard_normal((601, n)).astype(np.float32)
+    x[0::16] = 0
+    x[1::16, n - 1] = np.nan
+    x[2::16, n // 2] = np.inf
+    x[3::16, 0] = -np.inf
+    x[4::16] *= np.float32(1e-30)
+    x[5::16] *= np.float32(1e-38)
+    x[6::16] *= np.float32(1e-42)
+    x[7::16] = np.float32(3.2e38) * np.sign(x[7::16])
+    x[8::16] *= np.float32(1e30)
+    x[9::16] = 0
+    x[9::16, n - 1] = -5
+    x[10::16] = np.round(x[10::16] * 2) / 2            # quotients half way between codes
+    x[10::16, 0] = 63.5
+    x[11::16] *= np.float32(2e-28)
+    x[12::16, 1:] *= np.float32(1e-20)
+    x[13::16, :3] = (np.inf, np.nan, -np.inf)
+    t = torch.from_numpy(x).to(DT[kind])               # (of fp16 some are infinities and zeros then)
+    c, s = pipe.pipe_token_quantize(t.cuda())
+    want_c, want_s = ref.quantize(t.float().numpy())
+    assert np.array_equal(s.cpu().numpy(), want_s, equal_nan=True)
+    assert np.array_equal(c[:, :n].cpu().numpy(), want_c) and not c[:, n:].any()
+
+
 # ------------------------------------------------------------------ layers
 
 LINEAR = [
