@@ -598,6 +598,39 @@ def test_gathered_inputs_beyond_4_gib_in_tiles(pipe, which, gated):
     close(y[at][:, cols[:4]], want, far)
 
 
+# rows, experts, out and what the streaming kernel makes of them: 16 or 32 rows a tile, eight, four, two waves a tile or one
+STREAMED = [(120, 40, 300, 16, 8), (120, 40, 650, 16, 4), (120, 40, 1299, 16, 2), (120, 40, 1501, 16, 1),
+            (150, 6, 1601, 32, 8), (150, 6, 3196, 32, 4), (150, 6, 6500, 32, 2), (150, 6, 7001, 32, 1)]
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["plain", "gated"])
+@pytest.mark.parametrize("case", STREAMED, ids=["-".join(str(v) for v in c) for c in STREAMED])
+def test_streamed_tiles_of_every_kind(pipe, case, gated):
+    """Several tiles a workgroup, those behind the last row and partial ones among them, against the definition and against tiles of 128 tokens."""
+    rows, E, out, tile, waves = case
+    tiles = -(-out // 16) * (rows // tile + min(E, rows))
+    assert (16 if rows // E <= 16 else 32) == tile and next(w for w, most in ((8, 1024), (4, 2048), (2, 4096), (1, 1 << 23)) if tiles <= most) == waves
+    rng = np.random.default_rng(rows + out)
+    n, act = 1100 if E > 6 else 300, "gated" if gated else "none"
+    kind = "bf16" if out % 2 else "f32"
+    cuts = np.sort(rng.integers(0, rows - 6, E - 3))                    # some experts without a row
+    starts = np.concatenate([[0, 0], cuts, [cuts[-1], rows - 7]])
+    order = rng.integers(0, 40, rows)
+    order[3], order[rows // 2] = -1, 40
+    x, v = typed(rng, (20, n), kind, 1.5)
+    cw, sw, w, s = weights(rng, (E,), out * (2 if gated else 1), n)
+    b = rng.standard_normal(s.shape).astype(np.float32)
+    got = []
+    for which in (1, 3):
+        pipe.pipe_set_token_kernel(which)
+        try:
+            got.append(pipe.pipe_expert_forward(x, cw, sw, ints(starts), order=ints(order), top_k=2, bias=torch.from_numpy(b).cuda(), act=ref.ACTS[act]))
+        finally:
+            pipe.pipe_set_token_kernel(0)
+    assert torch.equal(*got)
+    close(got[0], *ref.experts_layer(v, w, s, b, starts, order, 2, rows, act, kind))
+
+
 # ------------------------------------------------------------------ back to the tokens
 
 @pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
