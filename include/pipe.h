@@ -680,7 +680,9 @@ int pipe_prompt_attention(const void* q_dev, const void* k_dev, const void* v_de
  * x has a row stride in elements (>= 0), its rows are dense; 16-byte aligned addresses and strides are read with wider loads.  y is dense, 16-byte aligned, and may
  * overlap x, but nothing else that the call reads.  1 <= in <= 130944.  All calls are asynchronous on `stream`, allocate nothing, use no library scratch and may be captured
  * into a graph at any time.  scratch_dev: pipe_token_scratch(T, in) bytes, 16-byte aligned, of the caller's, in use until the call has run on the stream.
- * NULL is PIPE_EINVAL unless the call makes its codes in the one launch that also multiplies, which calls of few rows do (rows of y * pitch <= 8192).
+ * NULL is served where the call makes its codes in the one launch that also multiplies, and PIPE_EINVAL elsewhere, before anything is launched.  That one launch is
+ * taken where rows of y * pitch <= 8192, ceil(out / 16) * R <= 1024 (R = ceil(T / 16) of pipe_token_forward, rows / 16 + min(E, rows) of pipe_expert_forward), no
+ * byte of y lies between x's first and last, and pipe_set_token_kernel's setting is 0 or 1.
  * Launches of 2^23 tiles or more (16 outputs x 16 tokens of few tokens, 64 x 64 and more of many) are refused, PIPE_ESHAPE.                          */
 int pipe_token_pitch(int in);                                  /* 0: no such row */
 int64_t pipe_token_scratch(int64_t rows, int in);              /* -1: no such rows */

@@ -76,6 +76,25 @@ def test_layer_refusals(lib):
         assert experts(lib, **bad) == ESHAPE, bad
 
 
+def test_layers_without_scratch(lib):
+    """NULL for the scratch is refused wherever the codes have a launch of their own: of few codes too, where outputs are many, lie over the input, or the kernel is set."""
+    apart = dict(x=C.c_void_p(1 << 20), y=C.c_void_p(1 << 30), scratch=None)
+    for f, one in ((forward, {}), (experts, dict(E=3, rows=I(1), order=BUF, k=1))):
+        for out in (16385, 40000, 1 << 28):
+            assert f(lib, **apart, T=I(1), n=4096, out=out, **one) == EINVAL
+        assert f(lib, **apart, T=I(3), n=4096, out=8, **(dict(one, rows=I(3)) if one else {})) == EINVAL
+        for shift, out in ((0, 8), (16, 8), (192, 8), (-16, 16)):                # a row of 100 fp16 values, 200 bytes
+            assert f(lib, **dict(apart, y=C.c_void_p((1 << 20) + shift)), T=I(1), out=out, type=1, **one) == EINVAL
+        try:
+            for which in (2, 3, 4):
+                assert lib.pipe_set_token_kernel(which) == 0
+                assert f(lib, **apart, T=I(1), out=8, **one) == EINVAL
+        finally:
+            assert lib.pipe_set_token_kernel(0) == 0
+    # experts: a tile for each that may have a row
+    assert experts(lib, **apart, T=I(30), n=100, E=1024, rows=I(60), order=BUF, k=2, out=257) == EINVAL
+
+
 def route(lib, **o):
     a = dict(logits=BUF, type=0, T=4, E=8, stride=I(8), k=2, renormalize=1, experts=BUF, weights=BUF, starts=BUF, order=BUF, places=BUF, scratch=BUF)
     a.update(o)
