@@ -709,7 +709,7 @@ int pipe_set_token_kernel(int which);
  *   order_dev  [T*top_k]  row -> pair token * top_k + choice; -1 from the total on
  *   places_dev [T][top_k] pair -> row, or -1
  *   scratch_dev           pipe_expert_scratch(T, top_k, E) bytes of the caller's, 16-byte aligned, in use until the call has run; NULL where that is 0
- *                         (up to 481 pairs; -1: no such router)
+ *                         (T * top_k <= 512; -1: no such router)
  * Errors: PIPE_EINVAL (NULL, type, renormalize), PIPE_ESHAPE (T < 0, T * top_k >= 2^30, E outside 1..1024, top_k outside 1..32 or over E, stride).
  * (pipe_expert_sort: top_k may exceed E.)                                                                           */
 int pipe_expert_route(const void* logits_dev, int type, int T, int E, int64_t row_stride, int top_k, int renormalize,

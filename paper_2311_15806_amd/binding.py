@@ -999,7 +999,7 @@ def pipe_expert_scratch(tokens: int, top_k: int, num_experts: int) -> int:
 
 def _starts(T: int, k: int, E: int, like: torch.Tensor):
     """(starts [E + 1], address of the calls' scratch)"""
-    extra = 0 if T * k <= 481 else pipe_expert_scratch(T, k, E) // 4      # (481 pairs need none, whatever k)
+    extra = 0 if T * k <= 512 else pipe_expert_scratch(T, k, E) // 4      # (512 pairs need none, whatever k)
     if extra == 0:
         return like.new_empty(E + 1, dtype=torch.int32), None
     at = (E + 4) // 4 * 4

@@ -1,12 +1,13 @@
 """Argument checks of the calls with a scale for each token and of the experts' calls, which end before anything touches a device, and the definitions that the
 GPU tests compare with (no GPU)."""
 import ctypes as C
+import os
 
 import numpy as np
 import pytest
 
 import _experts as ref
-from test_abi import LIB
+from test_abi import LIB, ROOT
 
 EINVAL, ESHAPE = -1, -2
 I = C.c_int64
@@ -143,6 +144,14 @@ def test_router_refusals(lib):
     for bad in (dict(rows=I(-1)), dict(rows=I(1 << 30)), dict(out=0), dict(stride=I(-1))):
         assert combine(lib, **bad) == ESHAPE, bad
     assert combine(lib, T=0, places=None, weights=None, dst=None) == 0
+
+
+def test_512_pairs_need_no_scratch(lib):
+    lib.pipe_expert_scratch.restype = I
+    for k in range(1, 33):
+        assert all(lib.pipe_expert_scratch(T, k, 1024) == 0 for T in range(512 // k + 1))
+    header = open(os.path.join(ROOT, "include", "pipe.h")).read()
+    assert "T * top_k <= 512; -1: no such router" in header
 
 
 def test_quantize_definition():
