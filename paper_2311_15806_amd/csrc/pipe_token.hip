@@ -241,7 +241,7 @@ __device__ __forceinline__ int pairs_of(const SortArgs& a, int b) {
 }
 __device__ __forceinline__ int key_of(int expert, int E) { return (unsigned)expert < (unsigned)E ? expert : E; }
 extern __shared__ int sort_lds[];
-static size_t sort_lds_bytes(int E) { return (size_t)(E + 1) * (2 * sizeof(int) + PAIRS / 64 * sizeof(uint16_t)); }   // (24 KiB at most)
+static size_t sort_lds_bytes(int E) { return (size_t)(E + 1) * (2 * sizeof(int) + PAIRS / 64 * sizeof(uint16_t)); }   // (24600 at most)
 
 __global__ __launch_bounds__(PAIRS) void expert_place_kernel(const int32_t* __restrict__ experts, const SortArgs a) {
   const int b = blockIdx.x, n = pairs_of(a, b);

@@ -141,9 +141,9 @@ __device__ __forceinline__ void gate4(float* g, const float* u) {
 }
 
 // Four channels' scales and biases: z = (sum s_t) s_o + b.  The product is made of the scales' mantissas and scaled by both exponents at once -- or, where
-// these are so small (`plain`) that nothing on the way leaves fp32's normal range, of the scales as they are, which gives the
-// same bits (4096 tokens of 4096-11008, fp32: 204 us, 199 so).
-constexpr int PLAIN_EXPONENT = 50;
+// these are so small (`plain`) that nothing on the way leaves fp32's normal range (a sum is below 2^31, each scale from 2^-49 up to below 2^48), of the
+// scales as they are, which gives the same bits (4096 tokens of 4096-11008, fp32: 204 us, 199 so).
+constexpr int PLAIN_EXPONENT = 48;
 __device__ __forceinline__ bool plain_scale(float s) {
   const int e = __builtin_amdgcn_frexp_expf(s);
   return e <= PLAIN_EXPONENT && e >= -PLAIN_EXPONENT;

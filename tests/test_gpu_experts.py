@@ -270,6 +270,32 @@ def test_scales_of_any_size(pipe, kernel, T):
         assert np.all(np.abs(g[np.abs(want) > 3.5e38]) == np.inf)
 
 
+@pytest.mark.parametrize("n", [100, 130944])
+def test_scales_at_the_border_of_the_plain_product(pipe, n):
+    """Tokens' and channels' scales next to 2^48 and 2^-49, sums up to 2^31: the two ways of the product give the same bits."""
+    rng = np.random.default_rng(n)
+    T, out = 45, 24
+    c = torch.from_numpy(rng.integers(-127, 128, (out, -(-n // 128) * 128)).astype(np.int8)).cuda()
+    c[::3] = 127
+    c[1::3] = -128
+    for ex in (-51, -49, 0, 46, 48):
+        x = np.abs(rng.standard_normal((T, n))) + 20
+        x = (x * (127.0 * 2.0 ** (ex + rng.integers(0, 4, T)) / x.max(1))[:, None]).astype(np.float32)
+        for ew in (-51, 0, 46):
+            sw = torch.from_numpy((rng.uniform(1, 2, out) * 2.0 ** (ew + rng.integers(0, 4, out))).astype(np.float32)).cuda()
+            got = []
+            for which in (1, 2, 3, 4):
+                pipe.pipe_set_token_kernel(which)
+                try:
+                    got.append(pipe.pipe_token_forward(torch.from_numpy(x).cuda(), c, sw))
+                finally:
+                    pipe.pipe_set_token_kernel(0)
+            assert all(torch.equal(g, got[0]) for g in got[1:]), (ex, ew)
+            want, far = ref.linear(x, c[:, :n].cpu().numpy(), sw.cpu().numpy(), None, "none", "f32")
+            inside = np.abs(want) < 3.4e38
+            assert np.all(np.abs(got[0].double().cpu().numpy() - want)[inside] <= far[inside]), (ex, ew)
+
+
 @pytest.mark.parametrize("act", ["none", "gelu", "gated", "relu"])
 @pytest.mark.parametrize("T", [6, 50, 300])
 def test_tokens_with_nan_or_infinity(pipe, kernel, T, act):
