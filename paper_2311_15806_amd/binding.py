@@ -937,7 +937,8 @@ def pipe_token_scratch(rows: int, in_features: int) -> int:
 
 
 def pipe_token_quantize(x: torch.Tensor):
-    """(codes [rows, pitch] int8, scales [rows] fp32) of the rows x [rows, n]: activations, or weights [out, in] for the calls below."""
+    """(codes [rows, pitch] int8, scales [rows] fp32) of the rows x [rows, n]: activations, or weights [out, in] for the calls below.  The output has no
+    gradient."""
     dev = _device()
     xp, stride = _rows(x, "x", dev)
     rows, n = x.shape
@@ -1009,7 +1010,8 @@ def _starts(T: int, k: int, E: int, like: torch.Tensor):
 
 def pipe_expert_route(logits: torch.Tensor, top_k: int, renormalize: bool = True):
     """Of each token's logits [T, E] the top_k largest: (experts [T, top_k], weights [T, top_k], starts [E + 1], order [T * top_k], places
-    [T, top_k]), the tables as pipe_expert_sort gives them.  weights: softmax over the chosen (renormalize) or over all."""
+    [T, top_k]), the tables as pipe_expert_sort gives them.  weights: softmax over the chosen (renormalize) or over all; they have no gradient, also where
+    the logits require one."""
     dev = _device()
     lp, stride = _rows(logits, "logits", dev)
     T, E = logits.shape
@@ -1042,7 +1044,8 @@ def pipe_expert_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tens
                         top_k: int = 1, bias: Optional[torch.Tensor] = None, act: int = PIPE_ACT_NONE,
                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """pipe_token_forward of every expert on its rows, starts[e] .. starts[e+1]-1 of the result [rows, out].  codes [E, out, pitch], scales and bias
-    [E, out] (gated: 2 * out).  order [rows]: row r is token order[r] // top_k of x; None: row r of x.  Rows behind starts[E] are zeros."""
+    [E, out] (gated: 2 * out).  order [rows]: row r is token order[r] // top_k of x; None: row r of x.  Rows behind starts[E] are zeros.  The output has no
+    gradient, also where x requires one."""
     dev = _device()
     xp, stride = _rows(x, "x", dev)
     T, n = x.shape
@@ -1063,7 +1066,8 @@ def pipe_expert_forward(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tens
 
 
 def pipe_expert_combine(y: torch.Tensor, places: torch.Tensor, weights: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """out[t] = sum_j weights[t, j] * y[places[t, j]] [T, width] of y's type (places [T, top_k] int32, weights fp32; a place outside y's rows is left out)."""
+    """out[t] = sum_j weights[t, j] * y[places[t, j]] [T, width] of y's type (places [T, top_k] int32, weights fp32; a place outside y's rows is left out).  The output
+    has no gradient, also where an input requires one."""
     dev = _device()
     yp, stride = _rows(y, "y", dev)
     if places.dim() != 2:

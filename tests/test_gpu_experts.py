@@ -761,6 +761,21 @@ def test_two_streams_at_once(pipe):
         assert all(torch.equal(g, want[i]) for g in got[i])
 
 
+def test_no_call_has_a_gradient(pipe):
+    """Inputs that require one are served the same, and every call says that its outputs do not."""
+    rng = np.random.default_rng(12)
+    x = typed(rng, (9, 128), "f32")[0].requires_grad_()
+    router, up, down = weights(rng, (), 4, 128)[:2], weights(rng, (4,), 64, 128)[:2], weights(rng, (4,), 128, 32)[:2]
+    got = _path(pipe, x, router, *up, *down, 2)
+    for a, b in zip(got, _path(pipe, x.detach(), router, *up, *down, 2)):
+        assert torch.equal(a, b) and not a.requires_grad and a.grad_fn is None
+    assert not pipe.pipe_token_quantize(x)[1].requires_grad
+    w = torch.rand(9, 2, device="cuda", requires_grad=True)
+    assert not pipe.pipe_expert_combine(x, ints(np.zeros((9, 2))), w).requires_grad
+    for call in (pipe.pipe_token_quantize, pipe.pipe_token_forward, pipe.pipe_expert_route, pipe.pipe_expert_forward, pipe.pipe_expert_combine):
+        assert "no gradient" in " ".join(call.__doc__.split()), call.__name__
+
+
 def test_weights_by_the_quantizer_and_a_dense_layer(pipe):
     """W through pipe_token_quantize: the layer's error is that of 8 bits on both sides."""
     rng = np.random.default_rng(11)
