@@ -296,6 +296,21 @@ def test_scales_at_the_border_of_the_plain_product(pipe, n):
             assert np.all(np.abs(got[0].double().cpu().numpy() - want)[inside] <= far[inside]), (ex, ew)
 
 
+@pytest.mark.parametrize("act", ["none", "gated"])
+@pytest.mark.parametrize("T", [3, 90])
+def test_subnormal_scales_of_channels(pipe, kernel, T, act):
+    """Channels' scales under fp32's normal numbers, and the largest, beside tokens that make up for them."""
+    rng = np.random.default_rng(T)
+    n, out = 200, 40
+    lines = 2 * out if act == "gated" else out
+    full = rng.integers(-127, 128, (lines, 256)).astype(np.int8)
+    for ex, exponents in ((110, (-149, -148, -140, -130, -127, -126)), (-110, (100, 110, 120, 126))):
+        x = (rng.standard_normal((T, n)) * 2.0 ** ex).astype(np.float32)
+        sw = (rng.uniform(1, 2, lines) * 2.0 ** rng.choice(exponents, lines)).astype(np.float32)
+        y = pipe.pipe_token_forward(torch.from_numpy(x).cuda(), torch.from_numpy(full).cuda(), torch.from_numpy(sw).cuda(), act=ref.ACTS[act])
+        close(y, *ref.linear(x, full[:, :n], sw, None, act, "f32"), ex)
+
+
 @pytest.mark.parametrize("act", ["none", "gelu", "gated", "relu"])
 @pytest.mark.parametrize("T", [6, 50, 300])
 def test_tokens_with_nan_or_infinity(pipe, kernel, T, act):
