@@ -10,7 +10,8 @@ namespace {
 constexpr int64_t MOST_BLOCKS = 1 << 23;      // workgroups of 256 threads a launch
 
 // ------------------------------------------------------------------ rows to codes
-// Bound by the bytes: 4096 rows of 4096 in fp32 17.8 us, 4.7 TB/s; in 16 bits beside them by the instructions (16 us for 50 MB); few rows by latency, 3.4 us.
+// Bound by the bytes: 4096 rows of 4096 in fp32 17.7 us, 4.7 TB/s.  In 16 bits (14.2 us for 50 MB) by neither: 17 vector instructions a value are 7.4 us of a
+// SIMD's four waves, and a wave, whose loads, maximum and codes follow one another, waits 56 % of its time.  Few rows by latency, 2.3 to 3.4 us.
 // s = max|x| / 127, c = rint(x / s): NT threads a row, 8 values a thread and step, the first CH steps kept in registers between the maximum
 // and the codes, the rest (rows of more than 8 NT CH values) read again.  A row with a NaN or an infinity has the maximum +infinity here.
 template <typename T, int NT, int CH, bool WIDE>
@@ -79,7 +80,8 @@ int quantize_typed(const void* x, int64_t rows, int in, int64_t stride, int pitc
 // launch counts each block's pairs by expert (the router's beside its choice), and another has every workgroup sum the counts of the blocks
 // before its own and of all (of many blocks and experts a third launch does), which gives its pairs' rows.  Nothing passes between the workgroups of a
 // launch; no order of theirs is in the result.
-// Bound by latency: 16384 tokens, eight of 128 experts, bf16, take 7 us for the choice (6 MB in and out), 8 for sums and rows; 48 tokens, six of 64, 5.5.
+// Bound by latency: 16384 tokens, eight of 128 experts, bf16, take 7 us for the choice (6 MB in and out), 8 to 10 for sums and rows (every workgroup
+// reads the counts of all blocks); 48 tokens, six of 64, 5.4.
 constexpr int PAIRS = 512;
 __host__ __device__ constexpr int block_tokens(int top_k) { return PAIRS / top_k; }
 static int block_count(int T, int top_k) { return (T + block_tokens(top_k) - 1) / block_tokens(top_k); }

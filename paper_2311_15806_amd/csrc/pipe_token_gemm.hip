@@ -2,8 +2,8 @@
 // experts, whose rows lie one after the other in y.
 //
 // What bounds them: few tokens, the weights' bytes (32 tokens, six of 64 gated experts of 2048-1408, 370 MB: 69 us, 5.4 TB/s; 16 tokens of gated
-// 4096-11008, 90 MB: 19 us); many, the matrix units at the clock that power leaves: 8192 tokens of 8192-8192 take 455 us, 2420 TOP/s, where the largest
-// library product of that size reaches 2134 and multiplies alone, on random bytes, 3764.  Between them latency: a stage of 128 codes takes a tile of 64
+// 4096-11008, 90 MB: 19 us); many, the matrix units at the clock that power leaves: 8192 tokens of 8192-8192 take 477 us, 39 of them the
+// codes: 2510 TOP/s of the product, where the library's largest of that size reaches 2134 and multiplies alone, on random bytes, 3764.  Between them latency: a stage of 128 codes takes a tile of 64
 // tokens that is alone on its unit 0.45 us, of 128 0.95, of 256 1.3.
 //
 // Sums are exact in 32 bits.  Both scales' exponents are kept apart from their mantissas until the end, so that no product of a sum and one of
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(512, 4) void token_stream_kernel(const TokenProduct
 }
 
 // The same for a call of up to FUSED_CODES codes in one launch: every workgroup makes the codes of its tile's tokens itself, while its first weights are on
-// their way.  (One token of 4096-4096 in bf16: 8.2 us a call, two launches 10.5.)
+// their way.  (One token of 4096-4096 in bf16: 7.3 us a call, 5.4 on the device; two launches 13.0 and 7.2.)
 constexpr int FUSED_CODES = 8192, FUSED_TILES = 1024;
 template <bool GATED, typename T>
 __global__ __launch_bounds__(512, 4) void token_stream_fused_kernel(const TokenProductArgs a, int o_tiles) {
@@ -692,8 +692,8 @@ __global__ __launch_bounds__(512, 2) void token_big_kernel(const TokenProductArg
   // A stage in 16 steps, each of which multiplies one of the weights' operands with the four of the tokens': the first three of the weights' are in w, the
   // tokens' in x, a step reads what one three further on takes.  Beside them the next stage's codes go from registers to its slot, which nobody reads any
   // more, and the one's after it are requested.  The only barrier lies before step 14: behind it nobody reads this stage any more, the next one is there, and
-  // its first operands are read (8192 tokens of 8192-8192 with its quantizer: 476 us, 2309 TOP/s; with one barrier near the
-  // begin and one in the middle 504).
+  // its first operands are read (8192 tokens of 8192-8192 with their codes: 477 us; with one barrier near the begin and one
+  // in the middle 504).
   constexpr int MFMA = 0x008, LOAD = 0x020, READ = 0x100, WRITE = 0x200;
   auto stage = [&](int now, int next, int k) __attribute__((always_inline)) {
     constexpr int move[16] = {0, 1, -1, 2, -1, 3, -1, 4, -1, 5, -1, 6, 7, -1, -1, -1};
@@ -841,10 +841,10 @@ static int kernel_of(const TokenProductArgs& a) {
       which = STREAM;
     } else {
       // Microseconds of a launch: of a stage of 128 codes with few tiles and for each round of them that the chip holds (1024, 512 and 256; half a tile more
-      // for each expert, one at least), and its ends, in stages.  Calls of 64, 128 and 256 tokens a tile: 512 tokens of 4096-4096 27, 37 and 60 us; 1000 42,
-      // 40 and 62; 2048 73, 57 and 68; 4096 of 4096-11008 312, 239 and 198; 5227 of 3648-1730 87, 91 and 79; 512 tokens, six of 64 gated experts of
-      // 2048-1408 93, 100 and 114; 1024, two of eight of 4096-4096 81, 80 and 69; 8192, two of 128 of 1024-1024 138, 122 and 152; 2069, two of 110 of
-      // 3200-640 56, 81 and 100.
+      // for each expert, one at least), and its ends, in stages.  Calls of 64, 128 and 256 tokens a tile: 512 tokens of 4096-4096 26, 35 and 53 us; 1000 42,
+      // 40 and 56; 2048 75, 56 and 59; 4096 of 4096-11008 303, 223 and 173; 5227 of 3648-1730 84, 78 and 66; 512 tokens, six of 64 gated experts of
+      // 2048-1408 96, 102 and 109; 1024, two of eight of 4096-4096 84, 77 and 60; 8192, two of 128 gated ones of 1024-1024 149, 127 and 146; 2069, two of
+      // 110 of 3200-640 54, 80 and 99.  Off where rows are short: 2236 rows of five experts of 192-4096 25, 31 and 29, the rule's are of 128.
       const double stages = a.pitch / 128, n = (double)a.n;
       auto rounds = [&](int B, double held) {
         return std::ceil(w_rows / B) * (a.starts ? a.E * std::max(1.0, n / a.E / B + 0.5) : std::ceil(n / B)) / held;
